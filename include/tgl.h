@@ -569,6 +569,193 @@ tgl_status tgl_time_encode(const float *dt, int64_t n, const int64_t *count, int
                            void *out, void *stream);
 
 /* ------------------------------------------------------------------------ */
+/* Rows and histories in 8 bits: serving a temporal attention layer         */
+/* (Section 2.2; node memory and mailboxes, Section 2.1)                    */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Values in 8 bits.  A set of numbers x is held as signed bytes q in
+ * [-127, 127] and one float32 step s, standing for q * s:
+ *   a = max |x|;  s = a * (1 / 127);  q = x * (1 / s) rounded to the nearest
+ *   whole number, ties to even (every operation a float32 one rounded to
+ *   nearest, 1 / 127 a float32 constant);
+ *   a < 2^-100:     s = 0 and q = 0;
+ *   a not finite (an infinity or NaN among x):  s = NaN and q = 0, so that
+ *   what is computed from the set is NaN, not a number that looks right.
+ * Nothing here has a gradient: these are the operators of serving.
+ *
+ * Element types of x, k, v, queries and outputs: TGL_OUT_F32 (4-byte aligned)
+ * or TGL_OUT_BF16 (2-byte aligned).  Strides are in elements.
+ */
+#define TGL_MAX_ROW_DIM    (1 << 20)  /* elements of a row of tgl_norm_quant    */
+#define TGL_MAX_LINEAR_K   131072     /* its int32 sums cannot overflow         */
+#define TGL_MAX_LINEAR_OUT (1 << 20)
+#define TGL_MAX_HEAD_DIM   256
+#define TGL_MAX_HEADS      1024
+#define TGL_MAX_PAGE       128
+
+/*
+ * Residual addition, root-mean-square norm and rounding of rows to 8 bits.
+ * For every row i < n, with x = x[i], r = residual[i] (0 without it):
+ *   h = x + r;  sum[i] = h in x's type
+ *   t = h * weight;  (q[i], s) = t in 8 bits
+ *   scale[i] = s / sqrt(mean(h^2) + eps)
+ * so that q * scale = h / rms(h) * weight.  h, t and the mean are float32
+ * (the mean is of h before its rounding to x's type).  Without the norm
+ * (normalize = 0): scale[i] = s, eps is not read; with weight NULL too, this
+ * is the plain rounding of rows, for weights and for rows that need no norm.
+ *   x, residual  [device] n rows of dim elements of type dtype; residual may
+ *                be NULL (then sum may be NULL)
+ *   weight       [device] float[dim], or NULL for ones
+ *   dim          in [1, TGL_MAX_ROW_DIM]
+ *   q            [device] int8, n rows q_stride apart: 16-byte aligned, q_stride
+ *                a multiple of 16 and at least dim.  Columns from dim to the
+ *                next multiple of 16 are written 0.
+ *   scale        [device] float[n]
+ *   sum          [device] n rows of dim elements of type dtype (may be x or
+ *                residual itself, with its stride), or NULL
+ * Never synchronises.  Errors: TGL_EINVAL, TGL_EDEVICE.
+ */
+tgl_status tgl_norm_quant(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride,
+                          const float *weight, int64_t n, int32_t dim, int32_t dtype, int32_t normalize,
+                          float eps, int8_t *q, int64_t q_stride, float *scale, void *sum,
+                          int64_t sum_stride, void *stream);
+
+/*
+ * Product of rows in 8 bits with a weight matrix in 8 bits:
+ *   out[i][j] = x_scale[i] * w_scale[j] * sum_k x[i][k] * w[j][k]  (+ bias[j])
+ * The sum is exact (int32); scales, bias and the one rounding to out_type are
+ * float32 operations, the product of the sum with x_scale first.
+ *   x         [device] int8, m rows x_stride apart, 16-byte aligned, x_stride
+ *             a multiple of 16; each row is readable up to the next multiple
+ *             of 16 of k (what tgl_norm_quant leaves), whatever is there
+ *   w         [device] int8, n rows (one per output column), same rules
+ *   x_scale   [device] float[m];  w_scale [device] float[n]
+ *   bias      [device] float[n], or NULL
+ *   m         >= 0;  n in [1, TGL_MAX_LINEAR_OUT];  k in [1, TGL_MAX_LINEAR_K]
+ *   out       [device] m rows of n elements of out_type, out_stride apart
+ *   workspace [device] at least tgl_linear_i8_workspace(m, n, k) bytes, 256-byte
+ *             aligned (NULL where that is 0)
+ * Never synchronises.  Errors: TGL_EINVAL, TGL_ENOSPACE, TGL_EDEVICE.
+ */
+size_t tgl_linear_i8_workspace(int64_t m, int32_t n, int32_t k);
+tgl_status tgl_linear_i8(const int8_t *x, int64_t x_stride, const float *x_scale, int64_t m, const int8_t *w,
+                         int64_t w_stride, const float *w_scale, const float *bias, int32_t n, int32_t k,
+                         void *out, int64_t out_stride, int32_t out_type, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+/*
+ * A cache of keys and values in 8 bits, in pages of page_tokens tokens.  The
+ * tokens of one page and head share one step for their keys and one for
+ * their values.
+ *   data    [device] int8[num_pages][heads][2][page_tokens][Dp], 16-byte
+ *           aligned: keys ([..][0]) and values ([..][1]) of a page and head
+ *           beside each other; Dp = dim rounded up to a multiple of 16
+ *   scales  [device] float[num_pages][heads][2], 8-byte aligned
+ *   num_pages    >= 0 and below 2^31
+ *   page_tokens  a power of two in [1, TGL_MAX_PAGE]; 1: one token per page, as
+ *                for a node's memory, so that sampled neighbour ids are pages
+ *   heads        in [1, TGL_MAX_HEADS];  dim in [1, TGL_MAX_HEAD_DIM]
+ */
+typedef struct tgl_cache {
+    int8_t *data;
+    float *scales;
+    int64_t num_pages;
+    int32_t page_tokens;
+    int32_t heads;
+    int32_t dim;
+    int32_t reserved;       /* 0 */
+} tgl_cache;
+
+/*
+ * The sequences (histories) that a call works on.  Position p of sequence b
+ * is row p % page_tokens of page table[b * table_stride + p / page_tokens];
+ * a page id outside [0, num_pages) is padding (PAD slots carry -1), and so is
+ * every position at or beyond pages_per_seq * page_tokens.
+ *   table          [device] int32, rows of pages_per_seq ids
+ *   start          [device] int64[num_seqs] first position, or NULL for 0
+ *   offsets        [device] int64[num_seqs + 1], non-decreasing: sequence b has the
+ *                  call's tokens [offsets[b], offsets[b+1]) at positions start[b],
+ *                  start[b] + 1, ...; or NULL: as many for every sequence
+ */
+typedef struct tgl_seqs {
+    const int32_t *table;
+    int64_t table_stride;
+    int64_t num_seqs;
+    int32_t pages_per_seq;
+    int32_t reserved;       /* 0 */
+    const int64_t *start;
+    const int64_t *offsets;
+} tgl_seqs;
+
+/* Rows of heads: element (token, head, d) at token * token_stride + head *
+ * head_stride + d. */
+typedef struct tgl_heads {
+    void *ptr;
+    int64_t token_stride;
+    int64_t head_stride;
+} tgl_heads;
+
+/*
+ * Appends the keys and values of num_tokens tokens to histories.  For every
+ * page that receives tokens and every head, keys and values apart:
+ *   kept rows: those below start[b] % page_tokens of the page that start[b]
+ *     lies in (what the history holds before the call); none in other pages;
+ *   the new step is that of the new rows or, with kept rows, the larger of it
+ *     and the page's old step (NaN if either is);
+ *   new rows are rounded with the new step s (x * (1 / s)); if s is not the old
+ *     step, kept rows q become q * (s_old * (1 / s)) rounded to whole numbers;
+ *   rows past the new ones keep whatever they hold.
+ * Tokens whose place is padding are dropped; sequences without tokens change
+ * nothing.  start[b] must not be negative.  A page must belong to one sequence
+ * of the call only (two that share one race).
+ *   k, v        [device] num_tokens x heads x dim elements of type dtype
+ * Without offsets, num_tokens must be a multiple of num_seqs.  Tokens at or
+ * beyond num_tokens are not read whatever offsets says.
+ * Never synchronises.  Errors: TGL_EINVAL, TGL_EDEVICE.
+ */
+tgl_status tgl_cache_write(const tgl_cache *cache, const tgl_heads *k, const tgl_heads *v, int32_t dtype,
+                           int64_t num_tokens, const tgl_seqs *seqs, void *stream);
+
+/*
+ * Reads tokens back: k and v of token i are its bytes times their page's step,
+ * or zeros where its place is padding.  Arguments as tgl_cache_write, k and v
+ * being outputs of type out_type.  Tokens that no sequence owns are not
+ * written.  Never synchronises.  Errors: TGL_EINVAL, TGL_EDEVICE.
+ */
+tgl_status tgl_cache_read(const tgl_cache *cache, const tgl_heads *k, const tgl_heads *v, int32_t out_type,
+                          int64_t num_tokens, const tgl_seqs *seqs, void *stream);
+
+/*
+ * Attention of queries over the cache.  Query t of sequence b (row b *
+ * queries + t of q) sees the positions [begin[b], end[b] - (queries - 1 - t))
+ * that are not padding: the last query sees up to end[b], those before it one
+ * position less each, as the newest events of a history see their past.  With
+ *   score_j = scale * <q, k_j>
+ *   out = sum_j exp(score_j) v_j / sum_j exp(score_j)
+ *   lse = log(sum_j exp(score_j))
+ * over what it sees; where that is nothing, out = 0 and lse = -inf.  Query
+ * head h reads the cache's head h / (q_heads / heads).  Sampled slots are a
+ * cache of one-token pages with the slots' neighbour ids as the table.
+ *   q          [device] num_seqs * queries x q_heads x dim elements of type dtype
+ *   q_heads    a multiple of the cache's heads, at most TGL_MAX_HEADS
+ *   queries    >= 1
+ *   seqs       start is begin (NULL: 0); end is `end`; offsets must be NULL
+ *   end        [device] int64[num_seqs], or NULL: pages_per_seq * page_tokens
+ *   out        [device] like q, of the same type
+ *   lse        [device] float[num_seqs * queries][q_heads], or NULL
+ *   workspace  [device] at least tgl_cache_attend_workspace(...) bytes, 256-byte
+ *              aligned (NULL where that is 0)
+ * Scores, maxima, sums and the output are accumulated in float32 or exactly.
+ * Never synchronises.  Errors: TGL_EINVAL, TGL_ENOSPACE, TGL_EDEVICE.
+ */
+size_t tgl_cache_attend_workspace(const tgl_cache *cache, const tgl_seqs *seqs, int32_t q_heads, int64_t queries);
+tgl_status tgl_cache_attend(const tgl_cache *cache, const tgl_heads *q, int32_t q_heads, int64_t queries,
+                            int32_t dtype, const tgl_seqs *seqs, const int64_t *end, float scale,
+                            const tgl_heads *out, float *lse, void *workspace, size_t workspace_bytes,
+                            void *stream);
+
+/* ------------------------------------------------------------------------ */
 /* Kernel timers (instrumentation for benchmarks)                           */
 /* ------------------------------------------------------------------------ */
 

@@ -42,7 +42,9 @@ MODES = {"recent": MOST_RECENT, "most_recent": MOST_RECENT, "uniform": UNIFORM,
 EXPORTS = ("tgl_version", "tgl_status_str", "tgl_tcsr_build_workspace", "tgl_tcsr_build",
            "tgl_index_len", "tgl_tcsr_nodes", "tgl_tcsr_pack", "tgl_tcsr_unpack", "tgl_sample_capacity", "tgl_sample_workspace", "tgl_sample",
            "tgl_sample_ex", "tgl_sample_noalloc", "tgl_pointers_reset", "tgl_mfg_workspace", "tgl_mfg_export",
-           "tgl_gather", "tgl_time_encode", "tgl_timer_enable",
+           "tgl_gather", "tgl_time_encode",
+           "tgl_norm_quant", "tgl_linear_i8_workspace", "tgl_linear_i8", "tgl_cache_write", "tgl_cache_read",
+           "tgl_cache_attend_workspace", "tgl_cache_attend", "tgl_timer_enable",
            "tgl_timer_disable", "tgl_timer_read", "tgl_timer_reset", "tgl_timer_select")
 
 
@@ -80,6 +82,21 @@ class c_mfg(C.Structure):
 class c_hop_out(C.Structure):
     _fields_ = [("nbr", C.c_void_p), ("eid", C.c_void_p), ("ts", C.c_void_p),
                 ("dt", C.c_void_p), ("parent", C.c_void_p)]
+
+
+class c_cache(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scales", C.c_void_p), ("num_pages", C.c_int64),
+                ("page_tokens", C.c_int32), ("heads", C.c_int32), ("dim", C.c_int32), ("reserved", C.c_int32)]
+
+
+class c_seqs(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("table_stride", C.c_int64), ("num_seqs", C.c_int64),
+                ("pages_per_seq", C.c_int32), ("reserved", C.c_int32), ("start", C.c_void_p),
+                ("offsets", C.c_void_p)]
+
+
+class c_heads(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
 _lib: Optional[C.CDLL] = None
@@ -135,6 +152,20 @@ def lib() -> C.CDLL:
     L.tgl_gather.argtypes = [P, P, i64, P, i64, C.POINTER(c_table), i32, P]
     L.tgl_time_encode.restype = i32
     L.tgl_time_encode.argtypes = [P, i64, P, i64, P, P, i32, i32, P, P]
+    L.tgl_norm_quant.restype = i32
+    L.tgl_norm_quant.argtypes = [P, i64, P, i64, P, i64, i32, i32, i32, f32, P, i64, P, P, i64, P]
+    L.tgl_linear_i8_workspace.restype = C.c_size_t
+    L.tgl_linear_i8_workspace.argtypes = [i64, i32, i32]
+    L.tgl_linear_i8.restype = i32
+    L.tgl_linear_i8.argtypes = [P, i64, P, i64, P, i64, P, P, i32, i32, P, i64, i32, P, C.c_size_t, P]
+    for f in (L.tgl_cache_write, L.tgl_cache_read):
+        f.restype = i32
+        f.argtypes = [C.POINTER(c_cache), C.POINTER(c_heads), C.POINTER(c_heads), i32, i64, C.POINTER(c_seqs), P]
+    L.tgl_cache_attend_workspace.restype = C.c_size_t
+    L.tgl_cache_attend_workspace.argtypes = [C.POINTER(c_cache), C.POINTER(c_seqs), i32, i64]
+    L.tgl_cache_attend.restype = i32
+    L.tgl_cache_attend.argtypes = [C.POINTER(c_cache), C.POINTER(c_heads), i32, i64, i32, C.POINTER(c_seqs), P, f32,
+                                   C.POINTER(c_heads), P, P, C.c_size_t, P]
     L.tgl_timer_enable.restype = i32
     L.tgl_timer_enable.argtypes = [i32]
     L.tgl_timer_disable.restype = i32

@@ -1,0 +1,89 @@
+// tgl_int8.hpp -- what the 8-bit operators share: element types, the rounding
+// of a set of numbers to bytes and a step, wave reductions, argument checks.
+#pragma once
+
+#include "tgl_internal.hpp"
+
+namespace tgl {
+
+using i32x4 = int __attribute__((ext_vector_type(4)));
+using i32x2 = int __attribute__((ext_vector_type(2)));
+using f32x4 = float __attribute__((ext_vector_type(4)));
+
+struct bf16_t {
+    uint16_t bits;
+};
+
+__device__ __forceinline__ float as_float(float v) { return v; }
+__device__ __forceinline__ float as_float(bf16_t v) { return __builtin_bit_cast(float, static_cast<uint32_t>(v.bits) << 16); }
+
+template <class T>
+__device__ __forceinline__ T from_float(float v);
+template <>
+__device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ bf16_t from_float<bf16_t>(float v) {
+    return bf16_t{__builtin_bit_cast(uint16_t, static_cast<__bf16>(v))};
+}
+
+// ---- a set of numbers in 8 bits ----
+
+constexpr float kTiny = 0x1p-100f;      // sets whose largest magnitude is below have step 0
+
+// The larger of two magnitudes, NaN if either is (fmaxf drops a NaN).
+__device__ __forceinline__ float max_nan(float a, float b) { return a > b || a != a ? a : b; }
+
+// The step of a set whose largest magnitude is a (NaN if there was one).
+__device__ __forceinline__ float step_of(float a) {
+    if (!(a <= 3.4028235e38f)) return __builtin_nanf("");
+    return a < kTiny ? 0.0f : a * (1.0f / 127.0f);
+}
+
+// 1 / s, or 0 where every byte is to be 0 (a step of 0 or NaN).
+__device__ __forceinline__ float inverse_step(float s) { return s > 0.0f ? 1.0f / s : 0.0f; }
+
+// x in units of the step, as a byte; v_rndne.  inv = 0 gives 0 whatever x is.
+__device__ __forceinline__ int to_byte(float x, float inv) {
+    return inv == 0.0f ? 0 : static_cast<int>(rintf(x * inv));
+}
+
+template <int W>
+__device__ __forceinline__ float group_max_nan(float v) {
+#pragma unroll
+    for (int d = W / 2; d >= 1; d >>= 1) v = max_nan(v, __shfl_xor(v, d, kWave));
+    return v;
+}
+
+template <int W>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+    for (int d = W / 2; d >= 1; d >>= 1) v += __shfl_xor(v, d, kWave);
+    return v;
+}
+
+// ---- host side ----
+
+inline bool is_elem_type(int32_t t) { return t == TGL_OUT_F32 || t == TGL_OUT_BF16; }
+inline size_t elem_size(int32_t t) { return t == TGL_OUT_F32 ? 4 : 2; }
+inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+__host__ __device__ inline int32_t round16(int32_t d) { return (d + 15) & ~15; }
+
+inline bool valid_cache(const tgl_cache *c) {
+    return c && c->num_pages >= 0 && c->num_pages < (int64_t(1) << 31) && c->page_tokens >= 1 &&
+           c->page_tokens <= TGL_MAX_PAGE && (c->page_tokens & (c->page_tokens - 1)) == 0 && c->heads >= 1 &&
+           c->heads <= TGL_MAX_HEADS && c->dim >= 1 && c->dim <= TGL_MAX_HEAD_DIM && c->reserved == 0 &&
+           (c->num_pages == 0 || (c->data && c->scales)) && aligned(c->data, 16) && aligned(c->scales, 8);
+}
+
+inline bool valid_seqs(const tgl_seqs *s) {
+    return s && s->num_seqs >= 0 && s->num_seqs < (int64_t(1) << 31) && s->pages_per_seq >= 0 && s->reserved == 0 &&
+           s->table_stride >= 0 && (s->num_seqs == 0 || s->pages_per_seq == 0 || s->table) && aligned(s->table, 4) &&
+           aligned(s->start, 8) && aligned(s->offsets, 8);
+}
+
+// Rows of heads whose elements have that type; strides may be 0 or negative for inputs.
+inline bool valid_heads(const tgl_heads *h, int64_t rows, int32_t dtype) {
+    return h && (rows == 0 || h->ptr) && aligned(h->ptr, elem_size(dtype));
+}
+
+}  // namespace tgl

@@ -1,0 +1,634 @@
+"""The 8-bit operators against their plain definitions (oracle/layer8.py)."""
+import math
+
+import numpy as np
+import pytest
+
+import paper_2203_14883_amd as P
+from gpu_util import announce, require_gpu
+from oracle import layer8 as O
+
+pytestmark = pytest.mark.gpu
+TYPES = ["f32", "bf16"]
+HALF = 2.0 ** -24       # half a unit in the last place of a float32 near 1
+
+
+def _torch_type(torch, t):
+    return torch.float32 if t == "f32" else torch.bfloat16
+
+
+def _up(torch, a, t="f32"):
+    """Device tensor of type t, and its values as the host sees them."""
+    x = torch.from_numpy(np.ascontiguousarray(a, np.float32)).to(_torch_type(torch, t))
+    return x.cuda(), x.float().numpy()
+
+
+def _host(t):
+    return t.detach().float().cpu().numpy()
+
+
+# ---- rows -------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,dim,residual,weight", [
+    (1, 1, True, True), (1, 768, True, True), (3, 50, False, True), (5, 100, True, False), (65, 172, True, True),
+    (2, 513, False, False), (7, 1024, True, True), (4, 2049, True, True), (3, 5000, True, True), (2, 20011, True, True),
+    (1001, 64, True, True), (0, 64, True, True),
+])
+def test_norm_quant(n, dim, residual, weight, dtype):
+    torch = require_gpu()
+    announce("norm_quant %d x %d %s" % (n, dim, dtype))
+    rng = np.random.default_rng(n * 7919 + dim)
+    x, xh = _up(torch, 3 * rng.standard_normal((n, dim)), dtype)
+    r, rh = _up(torch, rng.standard_normal((n, dim)), dtype) if residual else (None, None)
+    w, wh = _up(torch, 1 + 0.2 * rng.standard_normal(dim)) if weight else (None, None)
+    q, scale, h = P.norm_quant(x, w, residual=r, eps=1e-5)
+    oq, oscale, oh = O.norm_quant(xh, rh, wh, 1e-5)
+    assert np.array_equal(q.cpu().numpy(), oq)
+    # the mean's sum: dim / 64 terms in turn at the least parallel, then a tree; a division, a root
+    np.testing.assert_allclose(scale.cpu().numpy(), oscale, rtol=(dim / 64 + 24) * HALF)
+    if residual:
+        assert np.array_equal(_host(h), oh if dtype == "f32" else O.to_bf16(oh))
+    else:
+        assert h is None
+    if n:
+        store = torch.as_strided(q, (n, O.round16(dim)), (q.stride(0), 1))
+        assert q.stride(0) % 16 == 0 and not store[:, dim:].any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm_quant_strided_rows_and_sum_in_place(dtype):
+    torch = require_gpu()
+    announce("norm_quant strides")
+    rng = np.random.default_rng(5)
+    wide, _ = _up(torch, rng.standard_normal((37, 3 * 131 + 1)), dtype)
+    x, r = wide[:, 1:132], wide[:, 132:263]
+    xh, rh = _host(x), _host(r)
+    w, wh = _up(torch, rng.standard_normal(131))
+    q, scale, h = P.norm_quant(x, w, residual=r, eps=0.0, out=r)
+    oq, oscale, oh = O.norm_quant(xh, rh, wh, 0.0)
+    assert h is r and np.array_equal(q.cpu().numpy(), oq)
+    assert np.array_equal(_host(r), oh if dtype == "f32" else O.to_bf16(oh))
+    assert np.array_equal(_host(x), xh)
+    np.testing.assert_allclose(scale.cpu().numpy(), oscale, rtol=(131 / 64 + 24) * HALF)
+
+
+def test_rows_of_extremes():
+    torch = require_gpu()
+    announce("rows of extremes")
+    x = np.zeros((7, 33), np.float32)
+    x[1, 5] = 1e-35                     # below 2^-100: all zeros
+    x[2, :] = np.linspace(-3e38, 3e38, 33)
+    x[3, 7] = np.inf
+    x[4, 32] = np.nan
+    x[5, :] = 2.0 ** -90
+    x[6, :] = np.arange(33) - 16.5
+    t, xh = _up(torch, x)
+    q, scale = P.quant_rows(t)
+    oq, oscale, _ = O.norm_quant(xh, None, None, 0.0, normalize=False)
+    assert np.array_equal(q.cpu().numpy(), oq)
+    np.testing.assert_array_equal(scale.cpu().numpy(), oscale.astype(np.float32))
+    assert scale[0] == 0 and scale[1] == 0 and math.isnan(scale[3]) and math.isnan(scale[4])
+    q, scale, _ = P.norm_quant(t[[0, 1, 5]].contiguous(), eps=1e-6)
+    assert torch.isfinite(scale).all()
+
+
+# ---- product ----------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k,bias", [
+    (1, 1, 1, True), (1, 100, 272, True), (2, 65, 15, False), (1, 2304, 768, False), (15, 33, 64, True), (17, 16, 63, True),
+    (16, 1000, 1041, False), (33, 31, 129, True), (64, 256, 4096, False), (100, 100, 100, True), (257, 129, 500, True),
+    (300, 513, 1000, False), (1801, 100, 272, True), (515, 770, 257, True), (0, 16, 64, True), (128, 128, 8208, False),
+])
+def test_linear_i8(m, n, k, bias, dtype):
+    torch = require_gpu()
+    announce("linear_i8 %d x %d x %d %s" % (m, n, k, dtype))
+    rng = np.random.default_rng(m * 31 + n * 7 + k)
+    kp = O.round16(k)
+    # padding bytes hold rubbish: they must not count
+    xb = rng.integers(-128, 128, (m, kp)).astype(np.int8)
+    wb = rng.integers(-128, 128, (n, kp)).astype(np.int8)
+    xs, ws = rng.uniform(0.5, 2, m).astype(np.float32), rng.uniform(0.01, 0.02, n).astype(np.float32)
+    b = (100 * rng.standard_normal(n)).astype(np.float32) if bias else None
+    x, w = torch.from_numpy(xb).cuda()[:, :k], torch.from_numpy(wb).cuda()[:, :k]
+    y = P.linear_i8(x, torch.from_numpy(xs).cuda(), w, torch.from_numpy(ws).cuda(),
+                    None if b is None else torch.from_numpy(b).cuda(), out_dtype=_torch_type(torch, dtype))
+    want = O.linear_i8(xb[:, :k], xs, wb[:, :k], ws, b)
+    prod = want if b is None else want - b
+    # the exact sum to float32, two products, the bias: a rounding each
+    tol = 4 * HALF * (np.abs(prod) + (0 if b is None else np.abs(b)))
+    if dtype == "bf16":
+        tol = tol + 2.0 ** -8 * np.abs(want)    # half a unit in the last of 8 bits
+    assert y.shape == (m, n)
+    assert np.all(np.abs(_host(y) - want) <= tol + 1e-30)
+
+
+def test_linear_i8_strides_and_far_rows():
+    torch = require_gpu()
+    announce("linear_i8 strides")
+    rng = np.random.default_rng(3)
+    m, n, k = 70, 90, 200
+    xb = rng.integers(-127, 128, (m, 512)).astype(np.int8)
+    wb = rng.integers(-127, 128, (n, 256)).astype(np.int8)
+    x, w = torch.from_numpy(xb).cuda()[:, 32:32 + k], torch.from_numpy(wb).cuda()[:, 16:16 + k]
+    one = torch.ones(m).cuda(), torch.ones(n).cuda()
+    wide = torch.full((m, 200), 7.0).cuda()
+    out = P.linear_i8(x, one[0], w, one[1], out=wide[:, 50:50 + n])
+    want = O.linear_i8(xb[:, 32:32 + k], np.ones(m), wb[:, 16:16 + k], np.ones(n), None)
+    assert np.array_equal(_host(out), want)             # whole numbers below 2^24
+    assert (wide[:, :50] == 7).all() and (wide[:, 50 + n:] == 7).all()
+
+
+def test_linear_i8_extreme_bytes_and_scales():
+    torch = require_gpu()
+    announce("linear_i8 extremes")
+    k = 131072
+    x = torch.full((3, k), 127, dtype=torch.int8).cuda()
+    w = torch.full((2, k), -127, dtype=torch.int8).cuda()
+    y = P.linear_i8(x, torch.tensor([1.0, math.nan, 0.0]).cuda(), w, torch.ones(2).cuda(), out_dtype=torch.float32)
+    assert (y[0] == -127.0 * 127 * k).all() and torch.isnan(y[1]).all() and (y[2] == 0).all()
+
+
+# ---- cache ------------------------------------------------------------------
+
+def _cache(rng, torch, pages, heads, page, dim, bad=()):
+    data = rng.integers(-127, 128, (pages, heads, 2, page, O.round16(dim))).astype(np.int8)
+    data[..., dim:] = 0
+    scales = np.exp(0.7 * rng.standard_normal((pages, heads, 2))).astype(np.float32) / 64
+    for p in bad:                       # pages that nothing may look at
+        scales[p] = np.nan
+    c = P.HistoryCache(torch.from_numpy(data).cuda(), torch.from_numpy(scales).cuda(), dim)
+    return c, O.Cache(data, scales, dim)
+
+
+def _tables(rng, need, width, pages):
+    """A page table of sequences that need that many pages each, every page once."""
+    order = rng.permutation(pages)[:int(np.sum(need))]
+    table = np.full((len(need), width), -1, np.int32)
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = order[at:at + n]
+        at += n
+    return table
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("page,heads,dim", [(1, 2, 50), (2, 1, 1), (4, 3, 16), (16, 2, 50), (16, 8, 128), (64, 1, 256), (128, 2, 100)])
+def test_cache_write_and_read(page, heads, dim, dtype):
+    torch = require_gpu()
+    announce("cache write page %d heads %d dim %d %s" % (page, heads, dim, dtype))
+    rng = np.random.default_rng(page * 100 + heads * 10 + dim)
+    B = 9
+    kept = np.array([0, 1, page - 1, page, page + 1, 0, 3 * page + 2, 5, 0])
+    new = np.array([1, 0, 1, 2 * page, page, 0, 3, 2 * page + 1, 7 * page])
+    need = -(-(kept + new) // page)
+    width, pages = int(need.max()) + 1, int(need.sum()) + 4
+    table = _tables(rng, need, width, pages)
+    table[3, 1] = -1                    # a page that is padding: its tokens are dropped
+    table[8, 2] = pages + 5             # an id that is no page
+    unused = sorted(set(range(pages)) - set(table[table >= 0].tolist()))
+    c, oc = _cache(rng, torch, pages, heads, page, dim, bad=unused)
+    n = int(new.sum())
+    size = np.exp(rng.uniform(-3, 3, n))[:, None, None, None]
+    kv, kvh = _up(torch, size * rng.standard_normal((n, 2, heads, dim)), dtype)
+    offsets = np.concatenate([[0], np.cumsum(new)])
+    dev = dict(start=torch.from_numpy(kept).cuda(), offsets=torch.from_numpy(offsets).cuda())
+    tab = torch.from_numpy(table).cuda()
+    P.cache_write(c, kv[:, 0], kv[:, 1], tab, **dev)
+    oc.write(kvh[:, 0], kvh[:, 1], table, kept, offsets)
+    np.testing.assert_array_equal(c.scales.cpu().numpy(), oc.scales)
+    np.testing.assert_array_equal(c.data.cpu().numpy(), oc.data)
+    # again, as it was: nothing changes
+    P.cache_write(c, kv[:, 0], kv[:, 1], tab, **dev)
+    np.testing.assert_array_equal(c.data.cpu().numpy(), oc.data)
+    # read everything back, from odd places too
+    first = np.minimum(kept, 1)
+    count = kept + new - first
+    offs = np.concatenate([[0], np.cumsum(count)])
+    k, v = P.cache_read(c, tab, start=torch.from_numpy(first).cuda(), offsets=torch.from_numpy(offs).cuda(),
+                        n=int(offs[-1]), out_dtype=_torch_type(torch, dtype))
+    for b in range(B):
+        ok, ov, _ = oc.tokens(table, b, range(first[b], first[b] + count[b]))
+        for got, want in ((k, ok), (v, ov)):
+            want = want.astype(np.float32)
+            np.testing.assert_array_equal(_host(got[offs[b]:offs[b + 1]]), want if dtype == "f32" else O.to_bf16(want))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("page", [1, 8, 32])
+def test_cache_appended_token_by_token(page, dtype):
+    torch = require_gpu()
+    announce("append one by one, page %d %s" % (page, dtype))
+    rng = np.random.default_rng(page)
+    B, L, heads, dim = 5, 41, 2, 50
+    width = -(-L // page)
+    table = _tables(rng, np.full(B, width), width, B * width)
+    c, oc = _cache(rng, torch, B * width, heads, page, dim)
+    tab = torch.from_numpy(table).cuda()
+    for t in range(L):
+        size = np.exp(rng.uniform(-2, 2))
+        k, kh = _up(torch, size * rng.standard_normal((B, heads, dim)), dtype)
+        v, vh = _up(torch, rng.standard_normal((B, heads, dim)), dtype)
+        if t == 7:
+            k.zero_()
+            kh = kh * 0
+        P.cache_write(c, k, v, tab, start=torch.full((B,), t, dtype=torch.int64).cuda())
+        oc.write(kh, vh, table, np.full(B, t), np.arange(B + 1))
+    np.testing.assert_array_equal(c.data.cpu().numpy(), oc.data)
+    np.testing.assert_array_equal(c.scales.cpu().numpy(), oc.scales)
+
+
+def test_cache_write_of_infinities_and_nan():
+    torch = require_gpu()
+    announce("write of infinities and NaN")
+    c = P.HistoryCache.empty(4, 1, 16, 4)
+    x = torch.ones(8, 1, 16).cuda()
+    x[1, 0, 3] = math.inf
+    x[6, 0, 0] = math.nan
+    tab = torch.arange(4, dtype=torch.int32).cuda()[None]
+    P.cache_write(c, x, torch.ones_like(x), tab)
+    k, v = P.cache_read(c, tab, n=8)
+    assert torch.isnan(k).all() and (v == 1).all()
+    # a page is given up with its history: written from its first row on, it is new
+    P.cache_write(c, torch.ones_like(x), torch.ones_like(x), tab)
+    k, v = P.cache_read(c, tab, n=8)
+    assert (k == 1).all()
+
+
+def test_cache_read_of_a_whole_table():
+    torch = require_gpu()
+    announce("read of a table of slots")
+    rng = np.random.default_rng(8)
+    c, oc = _cache(rng, torch, 50, 2, 1, 50, bad=[49])
+    table = rng.integers(-1, 49, (301, 7)).astype(np.int32)
+    k, v = P.cache_read(c, torch.from_numpy(table).cuda())
+    assert k.shape == (301 * 7, 2, 50)
+    want = [oc.tokens(table, b, range(7)) for b in range(301)]
+    np.testing.assert_array_equal(_host(k), np.concatenate([w[0] for w in want]).astype(np.float32))
+    np.testing.assert_array_equal(_host(v), np.concatenate([w[1] for w in want]).astype(np.float32))
+
+
+# ---- attention --------------------------------------------------------------
+
+def _tolerance(dtype, oc, qh, scale, length, want):
+    """Bound of the output's error.
+
+    A query row is held to 2^-17 (bfloat16) or 2^-24 (float32) of its largest
+    element and the exponentials to 2^-11 or 2^-20 of themselves; scores are
+    rounded to float32 and the sums taken in it, length / 16 terms in turn
+    at the least parallel.  An error e of every score moves a mean of values
+    by at most 2 e max|v|."""
+    dim = qh.shape[-1]
+    fine = np.where(np.isfinite(oc.scales), oc.scales, 0)
+    ks, vs = 127 * float(fine[..., 0].max()), 127 * float(fine[..., 1].max())
+    top = dim * ks * float(np.abs(qh).max()) * abs(scale)
+    held, exps = (2.0 ** -17, 2.0 ** -11) if dtype == "bf16" else (2.0 ** -24, 2.0 ** -20)
+    tol = vs * (2 * top * (held + 4 * HALF) + exps + (16 + length / 16) * HALF)
+    return tol + (2.0 ** -8 * np.abs(want) if dtype == "bf16" else 0)
+
+
+def _attend(torch, rng, dtype, page, heads, group, dim, T, lengths, begin=None, holes=0, extra=1, scale=None, spread=1.0):
+    lengths = np.asarray(lengths, np.int64)
+    B = len(lengths)
+    need = -(-lengths // page)
+    width = max(1, int(need.max()) + extra)
+    pages = int(need.sum()) + 3
+    table = _tables(rng, need, width, pages)
+    if holes:
+        some = rng.random(table.shape) < holes
+        table[some] = np.where(rng.random(int(some.sum())) < 0.5, -1, pages + 7)
+    unused = sorted(set(range(pages)) - set(table[table >= 0].tolist()))
+    c, oc = _cache(rng, torch, pages, heads, page, dim, bad=unused)
+    q, qh = _up(torch, spread * rng.standard_normal((B, T, heads * group, dim)), dtype)
+    kw = dict(end=torch.from_numpy(lengths).cuda())
+    if begin is not None:
+        begin = np.asarray(begin, np.int64)
+        kw["begin"] = torch.from_numpy(begin).cuda()
+    tab = torch.from_numpy(table).cuda()
+    out, lse = P.cache_attend(c, q, tab, scale=scale, return_lse=True, **kw)
+    sc = 1 / math.sqrt(dim) if scale is None else scale
+    want, wlse = oc.attend(qh, table, begin, lengths, sc)
+    tol = _tolerance(dtype, oc, qh, sc, int(lengths.max(initial=1)), want)
+    err = np.abs(_host(out) - want)
+    assert np.all(err <= tol), "largest error %.3g of a bound of %.3g" % (err.max(), np.max(tol))
+    none = np.isneginf(wlse)
+    assert np.array_equal(np.isneginf(lse.cpu().numpy()), none)
+    assert (_host(out)[none] == 0).all()
+    dim_top = dim * 127 * float(np.where(np.isfinite(oc.scales), oc.scales, 0)[..., 0].max()) * np.abs(qh).max() * abs(sc)
+    held = 2.0 ** -17 if dtype == "bf16" else 2.0 ** -24
+    ltol = dim_top * (held + 4 * HALF) + 2.0 ** -20 + (16 + lengths.max(initial=1) / 16) * HALF
+    assert np.all(np.abs(lse.cpu().numpy()[~none] - wlse[~none]) <= ltol)
+    return c, q, tab, kw, out
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("page", [1, 2, 4, 8, 16, 32, 64, 128])
+def test_attend_pages(page, dtype):
+    torch = require_gpu()
+    announce("attend page %d %s" % (page, dtype))
+    rng = np.random.default_rng(page)
+    _attend(torch, rng, dtype, page, 2, 3, 64, 1, [0, 1, 2, 15, 16, 17, 31, 33, 63, 64, 65, 127, 129, 200, 257], holes=0.1)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [1, 7, 16, 31, 32, 33, 50, 64, 80, 96, 100, 112, 128, 129, 192, 200, 255, 256])
+def test_attend_dims(dim, dtype):
+    torch = require_gpu()
+    announce("attend dim %d %s" % (dim, dtype))
+    rng = np.random.default_rng(dim)
+    _attend(torch, rng, dtype, 16, 2, 2, dim, 1, [70, 1, 40, 0, 129])
+    _attend(torch, rng, dtype, 1, 1, 5, dim, 1, [10, 3, 0, 1, 40], holes=0.3)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads,group", [(1, 1), (1, 8), (8, 1), (2, 16), (1, 17), (3, 5), (1, 40)])
+def test_attend_head_layouts(heads, group, dtype):
+    torch = require_gpu()
+    announce("attend heads %d group %d %s" % (heads, group, dtype))
+    rng = np.random.default_rng(heads * 50 + group)
+    _attend(torch, rng, dtype, 8, heads, group, 48, 1, [77, 200, 5, 0])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,group", [(2, 1), (3, 4), (16, 1), (17, 2), (70, 1), (9, 8)])
+def test_attend_several_queries(T, group, dtype):
+    torch = require_gpu()
+    announce("attend %d queries group %d %s" % (T, group, dtype))
+    rng = np.random.default_rng(T * 9 + group)
+    _attend(torch, rng, dtype, 16, 2, group, 64, T, [100, T, T - 1, 1, 0, 203], holes=0.05)
+    _attend(torch, rng, dtype, 4, 1, group, 50, T, [90, 150, 33], begin=[20, 149, 50])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attend_windows(dtype):
+    torch = require_gpu()
+    announce("attend windows %s" % dtype)
+    rng = np.random.default_rng(17)
+    lengths = [300, 300, 300, 300, 300, 300, 5, 64]
+    begin = [299, 300, 301, 0, 37, 64, -3, 63]
+    for page in (1, 4, 16, 64):
+        _attend(torch, rng, dtype, page, 2, 2, 50, 1, lengths, begin=begin)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,length,page,heads,group", [(1, 40_000, 64, 2, 4), (1, 30_011, 4, 1, 1), (3, 5000, 1, 1, 2), (2, 20_003, 16, 1, 16)])
+def test_attend_long(B, length, page, heads, group, dtype):
+    torch = require_gpu()
+    announce("attend long %d x %d page %d %s" % (B, length, page, dtype))
+    rng = np.random.default_rng(length)
+    lengths = [length] + [length // 3 + 1, 1][:B - 1]
+    _attend(torch, rng, dtype, page, heads, group, 64, 1, lengths, holes=0.02)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attend_sharp_and_flat_scores(dtype):
+    torch = require_gpu()
+    announce("attend sharp and flat %s" % dtype)
+    rng = np.random.default_rng(23)
+    _attend(torch, rng, dtype, 16, 1, 2, 32, 1, [500, 3, 64], scale=0.0)        # every token the same weight
+    _attend(torch, rng, dtype, 16, 1, 2, 32, 1, [500, 3, 64], spread=1e-6)
+    _attend(torch, rng, dtype, 1, 1, 2, 32, 1, [500, 3, 64], scale=-0.5)
+    # scores of thousands: one token has all the weight and nothing overflows
+    data = np.zeros((64, 1, 2, 1, 16), np.int8)
+    data[:, 0, 0, 0, 0] = np.arange(64)
+    data[:, 0, 1, 0, :] = np.arange(64)[:, None]
+    c = P.HistoryCache(torch.from_numpy(data).cuda(), torch.ones(64, 1, 2).cuda(), 16)
+    q = torch.zeros(1, 1, 16).cuda().to(_torch_type(torch, dtype))
+    q[0, 0, 0] = 2048.0
+    out, lse = P.cache_attend(c, q, torch.arange(64, dtype=torch.int32).cuda()[None], scale=1.0, return_lse=True)
+    assert (out == 63).all() and abs(lse.item() - 63 * 2048.0) <= 63 * 2048.0 * 2.0 ** -21      # a few roundings of the scale
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attend_one_outlier_over_many_small_weights(dtype):
+    """One token far above the rest, which still add up: what is summed is not lost below a fixed step."""
+    torch = require_gpu()
+    announce("attend outlier %s" % dtype)
+    L = 32768
+    data = np.zeros((L, 1, 2, 1, 16), np.int8)
+    data[7, 0, 0, 0, 0] = 127
+    data[:, 0, 1, 0, :] = 100
+    data[7, 0, 1, 0, :] = -100
+    c = P.HistoryCache(torch.from_numpy(data).cuda(), torch.ones(L, 1, 2).cuda(), 16)
+    q = torch.zeros(1, 1, 16).cuda().to(_torch_type(torch, dtype))
+    q[0, 0, 0] = 1.0
+    for scale in (10.0 / 127, 12.0 / 127):
+        out = P.cache_attend(c, q, torch.arange(L, dtype=torch.int32).cuda()[None], scale=scale)
+        w = math.exp(float(np.float32(scale)) * 127)
+        want = (100.0 * (L - 1) - 100.0 * w) / (L - 1 + w)
+        assert abs(out.float() - want).max().item() <= 100 * (2.0 ** -10 if dtype == "bf16" else 2.0 ** -18) + (2.0 ** -8 * abs(want) if dtype == "bf16" else 0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attend_steps_of_very_different_size(dtype):
+    """Pages whose steps differ by many orders of magnitude, zero among them, in one tile."""
+    torch = require_gpu()
+    announce("attend steps %s" % dtype)
+    rng = np.random.default_rng(31)
+    L, D = 96, 32
+    data = rng.integers(-127, 128, (L, 1, 2, 1, D)).astype(np.int8)
+    scales = np.ones((L, 1, 2), np.float32) / 64
+    scales[:, 0, 1] = 10.0 ** rng.uniform(-20, 12, L)
+    scales[::5, 0, 1] = 0
+    scales[::7, 0, 0] = 0
+    oc = O.Cache(data, scales, D)
+    c = P.HistoryCache(torch.from_numpy(data).cuda(), torch.from_numpy(scales).cuda(), D)
+    q, qh = _up(torch, rng.standard_normal((1, 1, 2, D)), dtype)
+    table = np.arange(L, dtype=np.int32)[None]
+    out = P.cache_attend(c, q, torch.from_numpy(table).cuda())
+    want, _ = oc.attend(qh, table, None, None, 1 / math.sqrt(D))
+    assert np.all(np.abs(_host(out) - want) <= _tolerance(dtype, oc, qh, 1 / math.sqrt(D), L, want))
+    # all steps 0: zeros, not NaN
+    c.scales.zero_()
+    assert (P.cache_attend(c, q, torch.from_numpy(table).cuda()) == 0).all()
+
+
+def test_attend_nan_only_where_it_is_seen():
+    torch = require_gpu()
+    announce("attend NaN")
+    rng = np.random.default_rng(41)
+    c, _ = _cache(rng, torch, 40, 2, 4, 50)
+    c.scales[17, 1, 1] = math.nan
+    table = torch.arange(40, dtype=torch.int32).cuda().view(2, 20)
+    q = torch.randn(2, 4, 50).cuda()
+    out = P.cache_attend(c, q, table)
+    assert torch.isnan(out[0, 2:]).all() and torch.isfinite(out[0, :2]).all() and torch.isfinite(out[1]).all()
+    end = torch.tensor([17 * 4, 80]).cuda()             # the page is masked
+    assert torch.isfinite(P.cache_attend(c, q, table, end=end)).all()
+    table[0, 17] = -1
+    assert torch.isfinite(P.cache_attend(c, q, table)).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attend_strided_queries_and_outputs(dtype):
+    torch = require_gpu()
+    announce("attend strides %s" % dtype)
+    rng = np.random.default_rng(43)
+    c, oc = _cache(rng, torch, 60, 2, 4, 50)
+    wide, _ = _up(torch, rng.standard_normal((3, 5, 8 * 50 + 3)), dtype)
+    q = wide[:, :, 3:203].unflatten(2, (4, 50))
+    table = torch.arange(60, dtype=torch.int32).cuda().view(3, 20)[:, :13]
+    room = torch.full((3, 5, 4, 61), 9.0).cuda().to(q.dtype)
+    out = P.cache_attend(c, q, table, out=room[..., 4:54])
+    assert torch.equal(out, P.cache_attend(c, q.contiguous(), table.contiguous()))
+    assert (room[..., :4] == 9).all() and (room[..., 54:] == 9).all()
+
+
+def test_attend_and_io_beyond_32_bit_offsets():
+    torch = require_gpu()
+    announce("a cache of 6 GiB")
+    heads, dim, page = 16, 128, 64                       # 256 KiB a page
+    rng = np.random.default_rng(47)
+    c = P.HistoryCache.empty(24_576, heads, dim, page)
+    far = np.array([[24_575, 3, 20_000, 16_385, 8_191, 16_384]], np.int32)
+    L = 6 * page - 5
+    k, kh = _up(torch, rng.standard_normal((L, heads, dim)))
+    v, vh = _up(torch, rng.standard_normal((L, heads, dim)))
+    tab = torch.from_numpy(far).cuda()
+    P.cache_write(c, k, v, tab)
+    got, _ = P.cache_read(c, tab, n=L)
+    small = O.Cache(np.zeros((6, heads, 2, page, dim), np.int8), np.zeros((6, heads, 2), np.float32), dim)
+    near = np.arange(6, dtype=np.int32)[None]
+    small.write(kh, vh, near, [0], [0, L])
+    want, _, _ = small.tokens(near, 0, range(L))
+    np.testing.assert_array_equal(_host(got), want.astype(np.float32))
+    q, qh = _up(torch, rng.standard_normal((1, 1, heads, dim)))
+    out = P.cache_attend(c, q, tab, end=torch.tensor([L]).cuda())
+    o, _ = small.attend(qh, near, None, [L], 1 / math.sqrt(dim))
+    assert np.all(np.abs(_host(out) - o) <= _tolerance("f32", small, qh, 1 / math.sqrt(dim), L, o))
+
+
+def test_empty_calls():
+    torch = require_gpu()
+    announce("empty calls")
+    c = P.HistoryCache.empty(0, 2, 50, 4)
+    q = torch.randn(3, 2, 50).cuda()
+    table = torch.full((3, 5), -1, dtype=torch.int32).cuda()
+    out, lse = P.cache_attend(c, q, table, return_lse=True)
+    assert (out == 0).all() and torch.isneginf(lse).all()
+    out = P.cache_attend(c, q, table[:, :0])
+    assert (out == 0).all()
+    assert P.cache_attend(c, q[:0], table[:0]).shape == (0, 2, 50)
+    k, v = P.cache_read(c, table)
+    assert (k == 0).all() and (v == 0).all() and k.shape == (60, 2, 50)
+    P.cache_write(c, torch.randn(3, 2, 50).cuda(), torch.randn(3, 2, 50).cuda(), table)
+    P.cache_write(c, q[:0], q[:0], table, offsets=torch.zeros(4, dtype=torch.int64).cuda())
+
+
+# ---- streams, repeats, graphs ----------------------------------------------
+
+def _chain(torch, c, x, r, w, wq, ws, table, start, kv, stream=None):
+    """A layer's step: norm, projection, append, attend."""
+    heads, dim = c.heads, c.dim
+    q8, s8, h = P.norm_quant(x, w, residual=r, stream=stream)
+    y = P.linear_i8(q8, s8, wq, ws, out_dtype=x.dtype, stream=stream).view(len(x), -1, dim)
+    P.cache_write(c, y[:, -2 * heads:-heads], y[:, -heads:], table, start=start, stream=stream)
+    return P.cache_attend(c, y[:, :-2 * heads], table, end=start + 1, stream=stream), h
+
+
+def _chain_inputs(torch):
+    g = torch.Generator(device="cuda").manual_seed(3)
+    B, D, heads, dim, page = 33, 172, 2, 50, 4
+    rand = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    x, r, w = rand(B, D), rand(B, D), rand(D)
+    wq, ws = P.quant_rows(rand(8 * dim, D) / math.sqrt(D))
+    table = torch.randperm(B * 6, device="cuda", generator=g).to(torch.int32).view(B, 6)
+    start = torch.randint(0, 23, (B,), device="cuda", generator=g)
+    c = P.HistoryCache.empty(B * 6, heads, dim, page)
+    old = rand(B * 24, heads, dim)
+    P.cache_write(c, old, old, table)
+    return c, x, r, w, wq, ws, table, start
+
+
+def test_same_results_again_and_on_another_stream():
+    torch = require_gpu()
+    announce("streams")
+    a = _chain_inputs(torch)
+    first = _chain(torch, *a, None)
+    again = _chain(torch, *a, None)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    side = torch.cuda.Stream()
+    b = _chain_inputs(torch)
+    end = b[-1] + 1
+    torch.cuda.synchronize()
+    q8, s8, h = P.norm_quant(b[1], b[3], residual=b[2], stream=side)
+    y = P.linear_i8(q8, s8, b[4], b[5], out_dtype=torch.float32, stream=side).view(33, 8, 50)
+    P.cache_write(b[0], y[:, 4:6], y[:, 6:], b[6], start=b[7], stream=side)
+    out = P.cache_attend(b[0], y[:, :4], b[6], end=end, stream=side)
+    side.synchronize()
+    assert torch.equal(out, first[0]) and torch.equal(h, first[1])
+
+
+def test_replayed_in_a_graph():
+    torch = require_gpu()
+    announce("graph")
+    a = _chain_inputs(torch)
+    c, x, r = a[0], a[1], a[2]
+    _chain(torch, *a, None)
+    torch.cuda.synchronize()
+    data, scales = c.data.clone(), c.scales.clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out, h = _chain(torch, *a, None)
+    for i in range(4):
+        x.copy_(torch.randn(x.shape, generator=torch.Generator().manual_seed(i)))
+        c.data.copy_(data)
+        c.scales.copy_(scales)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        got, got_h = out.clone(), h.clone()
+        c.data.copy_(data)
+        c.scales.copy_(scales)
+        want, want_h = _chain(torch, *a, None)
+        assert torch.equal(got, want) and torch.equal(got_h, want_h)
+
+
+# ---- refusals ---------------------------------------------------------------
+
+def test_refusals():
+    torch = require_gpu()
+    announce("refusals")
+    x = torch.randn(4, 32).cuda()
+    w = torch.ones(32).cuda()
+    bad = [
+        lambda: P.norm_quant(x.half()), lambda: P.norm_quant(x.cpu()), lambda: P.norm_quant(x.t()),
+        lambda: P.norm_quant(x, w[:31]), lambda: P.norm_quant(x, w.double()), lambda: P.norm_quant(x, residual=x[:3]),
+        lambda: P.norm_quant(x, residual=x.bfloat16()), lambda: P.norm_quant(x.clone().requires_grad_()),
+        lambda: P.norm_quant(x[0]), lambda: P.norm_quant(x, w.cpu()),
+    ]
+    q, s = P.quant_rows(x)
+    odd = torch.zeros(4, 33, dtype=torch.int8).cuda()
+    bad += [
+        lambda: P.linear_i8(q, s, q[:, :16], s), lambda: P.linear_i8(q, s[:3], q, s), lambda: P.linear_i8(q, s, q, s, bias=s[:1]),
+        lambda: P.linear_i8(odd, s, odd, s), lambda: P.linear_i8(q[:, 1:17], s, q[:, 1:17], s),
+        lambda: P.linear_i8(q, s, q, s, out_dtype=torch.float16), lambda: P.linear_i8(x, s, q, s),
+        lambda: P.linear_i8(q, s, q, s.clone().requires_grad_()),
+    ]
+    c = P.HistoryCache.empty(8, 2, 16, 4)
+    table = torch.zeros(3, 2, dtype=torch.int32).cuda()
+    k = torch.randn(3, 2, 16).cuda()
+    three = torch.zeros(3, dtype=torch.int64).cuda()
+    bad += [
+        lambda: P.HistoryCache.empty(8, 2, 16, 3), lambda: P.HistoryCache.empty(8, 2, 257, 4), lambda: P.HistoryCache.empty(8, 2, 16, 256),
+        lambda: P.HistoryCache(c.data, c.scales, 17), lambda: P.HistoryCache(c.data, c.scales[:7], 16),
+        lambda: P.HistoryCache(c.data.float(), c.scales, 16),
+        lambda: P.cache_write(c, k[:2], k[:2], table), lambda: P.cache_write(c, k, k.bfloat16(), table),
+        lambda: P.cache_write(c, k, k, table.long()), lambda: P.cache_write(c, k, k, table, start=three.int()),
+        lambda: P.cache_write(c, k, k, table, start=three[:2]), lambda: P.cache_write(c, k, k, table, offsets=three),
+        lambda: P.cache_write(c, k[:, :1], k[:, :1], table), lambda: P.cache_write(c, k.clone().requires_grad_(), k, table),
+        lambda: P.cache_read(c, table, n=4), lambda: P.cache_read(c, table, out_dtype=torch.float64), lambda: P.cache_read(c, table, k=k),
+        lambda: P.cache_attend(c, k[:, :1], table), lambda: P.cache_attend(c, k[:2], table), lambda: P.cache_attend(c, k.half(), table),
+        lambda: P.cache_attend(c, k[..., :8], table), lambda: P.cache_attend(c, k, table, end=three[:1]),
+        lambda: P.cache_attend(c, k, table, begin=three.float()), lambda: P.cache_attend(c, k, table.cpu()),
+        lambda: P.cache_attend(c, k, table, out=k.bfloat16()), lambda: P.cache_attend(c, k.clone().requires_grad_(), table),
+        lambda: P.cache_attend(c, torch.randn(3, 4, 5, 16).cuda(), table),
+    ]
+    for i, f in enumerate(bad):
+        with pytest.raises((ValueError, P.TglError)):
+            f()
+            print("refusal %d was accepted" % i)
+    with torch.no_grad():
+        P.cache_write(c, k.clone().requires_grad_(), k, torch.arange(6, dtype=torch.int32).cuda().view(3, 2))
+    torch.cuda.synchronize()
