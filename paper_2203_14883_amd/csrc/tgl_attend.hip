@@ -37,6 +37,22 @@ constexpr int kRows = 16;           // rows of a tile
 constexpr int kTile = 32;           // tokens of a wavefront's step
 constexpr float kLog2E = 1.44269504088896340736f;
 
+// Division of whole numbers below 2^31 by a fixed one: with 2^l >= d and
+// mul = ceil(2^(31+l) / d) the quotient is n mul >> (31 + l), exactly.
+struct Div {
+    uint32_t mul = 0, shift = 0, d = 1;
+    Div() = default;
+    explicit Div(uint32_t by) : d(by) {
+        int l = 0;
+        while ((uint64_t(1) << l) < by) l++;
+        shift = 31 + l;
+        mul = static_cast<uint32_t>(((uint64_t(1) << shift) + by - 1) / by);
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const {
+        return static_cast<uint32_t>((static_cast<uint64_t>(n) * mul) >> shift);
+    }
+};
+
 struct AttendArgs {
     CacheView c;
     SeqsView s;
@@ -47,25 +63,29 @@ struct AttendArgs {
     float *part_o;          // [rows of all heads][chunks][dim], or null
     float *part_ml;         // [rows of all heads][chunks][2]
     int64_t qt, qh, ot, oh;
-    int64_t queries;
-    int64_t row_tiles;      // of one sequence and head
-    int64_t chunk;          // tokens of a workgroup
-    int64_t work;           // workgroups
-    int32_t chunks;
-    int32_t group;          // query heads of one head of the cache
+    int64_t chunk;          // tokens of a workgroup, below 2^31
+    uint32_t queries;
+    uint32_t rows;          // of one sequence and head: queries * group
+    uint32_t work;          // workgroups
+    uint32_t all_rows;      // rows of all sequences and heads
+    Div tiles;              // row tiles of one sequence and head
+    Div chunks;
+    Div heads;
+    Div group;              // query heads of one head of the cache
+    Div row_of;             // rows of one sequence and head
+    int32_t spread;         // how workgroups go to the dies: see die_order
     float scale;
 };
 
-// What a lane knows of its row: the query, the head, whether it exists.
-struct Row {
-    int64_t q;              // row of q and out
-    int32_t head;           // query head
-    bool there;
-};
-
-__device__ __forceinline__ Row row_of(const AttendArgs &a, int64_t b, int head, int64_t r) {
-    const int64_t t = r / a.group;
-    return Row{b * a.queries + t, static_cast<int32_t>(head * a.group + (r - t * a.group)), r < a.queries * a.group};
+// The unit of work of a workgroup.  Workgroups go to the 8 dies in turn.  Row
+// tiles of one head read the same tokens, so with several of them each die
+// gets a contiguous stretch of the work and its L2 serves them; without, the
+// order as it is spreads long and short sequences evenly.
+__device__ __forceinline__ uint32_t die_order(const AttendArgs &a) {
+    if (!a.spread) return blockIdx.x;
+    const uint32_t per = (a.work + 7) / 8;
+    const uint32_t at = blockIdx.x >> 3;
+    return at >= per ? a.work : (blockIdx.x & 7) * per + at;
 }
 
 template <class T>
@@ -83,46 +103,72 @@ constexpr float kSlack<float> = 1.0f;
 template <class T>
 constexpr float kOffset = 14.0f - kSlack<T>;
 
-// The row's query as signed bytes, kk-th piece of 64 columns, part p; returns
-// the size of one unit.
-template <class T, int KK>
-__device__ __forceinline__ float load_query(const AttendArgs &a, const Row &row, int lane, i32x4 (&parts)[kParts<T>][KK]) {
-    constexpr int N = kParts<T>;
-    const T *q = static_cast<const T *>(a.q) + row.q * a.qt + row.head * a.qh;
-    float x[KK][16];
-    float top = 0.0f;
+// n consecutive elements that need not lie at a multiple of their size: one
+// wide access wherever they start.
+template <class T, int N>
+struct __attribute__((packed, aligned(alignof(T)))) Run {
+    T t[N];
+};
+
+// N elements of a row from column d on, zeros from column dim on.
+template <class T, int N>
+__device__ __forceinline__ void load_columns(const T *q, int d, int dim, float (&x)[N]) {
+    if (d + N <= dim) {
+        const Run<T, N> w = *reinterpret_cast<const Run<T, N> *>(q + d);
 #pragma unroll
-    for (int kk = 0; kk < KK; kk++) {
+        for (int i = 0; i < N; i++) x[i] = as_float(w.t[i]);
+    } else {
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-            const int d = 64 * kk + 16 * (lane >> 4) + i;
-            x[kk][i] = row.there && d < a.c.dim ? as_float(q[d]) : 0.0f;
-            top = max_nan(top, fabsf(x[kk][i]));
+        for (int i = 0; i < N; i++) {
+            const float v = as_float(q[d + i < dim ? d + i : dim - 1]);
+            x[i] = d + i < dim ? v : 0.0f;
         }
     }
-    top = max_nan(top, __shfl_xor(top, 16, kWave));
-    top = max_nan(top, __shfl_xor(top, 32, kWave));
+}
+
+// The row's query as signed bytes, kk-th piece of 64 columns, part p (the
+// highest first); returns the size of one unit.  v + 0x808080 has, byte by
+// byte, the digits of v in base 256 between -128 and 127, each plus 128.
+template <class T, int KK>
+__device__ __forceinline__ float load_query(const AttendArgs &a, const T *q, bool there, int lane, i32x4 (&parts)[kParts<T>][KK]) {
+    constexpr int N = kParts<T>;
+    float x[KK][16];
+    uint32_t bits = 0;              // of the largest magnitude: NaN above infinity above numbers
+#pragma unroll
+    for (int kk = 0; kk < KK; kk++) {
+        load_columns<T, 16>(q, 64 * kk + 16 * (lane >> 4), a.c.dim, x[kk]);
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            const uint32_t v = __builtin_bit_cast(uint32_t, x[kk][i]) & 0x7fffffffu;
+            bits = v > bits ? v : bits;
+        }
+    }
+    uint32_t other = __shfl_xor(bits, 16, kWave);
+    bits = other > bits ? other : bits;
+    other = __shfl_xor(bits, 32, kWave);
+    bits = other > bits ? other : bits;
+    const float top = __builtin_bit_cast(float, bits);
     constexpr float kUnits = N == 2 ? 127.0f * 256.0f : 127.0f * 65536.0f;
     // not finite: a NaN unit makes the row NaN; tiny: zeros
-    const float unit = !(top <= 3.4028235e38f) ? __builtin_nanf("") : top < kTiny ? 0.0f : top / kUnits;
-    const float inv = inverse_step(unit);
+    const float unit = bits >= 0x7f800000u ? __builtin_nanf("") : top < kTiny ? 0.0f : top * (1.0f / kUnits);
+    const float inv = there ? inverse_step(unit) : 0.0f;
 #pragma unroll
     for (int kk = 0; kk < KK; kk++) {
 #pragma unroll
         for (int w = 0; w < 4; w++) {
-            int word[N] = {};
+            int v[4];
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                int v = to_byte(x[kk][4 * w + i], inv);
-#pragma unroll
-                for (int p = N - 1; p >= 0; p--) {
-                    const int low = static_cast<int8_t>(v);
-                    word[p] |= (low & 255) << (8 * i);
-                    v = (v - low) >> 8;
-                }
+                const float y = inv == 0.0f ? 0.0f : x[kk][4 * w + i] * inv;
+                v[i] = static_cast<int>(rintf(y)) + (N == 2 ? 0x8080 : 0x808080);
             }
 #pragma unroll
-            for (int p = 0; p < N; p++) parts[p][kk][w] = word[p];
+            for (int p = 0; p < N; p++) {
+                const unsigned byte = N - 1 - p;
+                const unsigned two = 0x0c0c0000u | ((4 + byte) << 8) | byte;
+                const int ab = __builtin_amdgcn_perm(v[1], v[0], two), cd = __builtin_amdgcn_perm(v[3], v[2], two);
+                parts[p][kk][w] = (ab | (cd << 16)) ^ 0x80808080;
+            }
         }
     }
     return unit;
@@ -161,49 +207,76 @@ __device__ __forceinline__ int pack_f16(float a, float b) {
     return __builtin_bit_cast(int, f16x2{static_cast<_Float16>(a), static_cast<_Float16>(b)});
 }
 
+// N consecutive elements from column d on, as far as there are columns.
+template <class T, int N>
+__device__ __forceinline__ void store_columns(T *out, int d, int dim, const float (&x)[N]) {
+    if (d + N <= dim) {
+        Run<T, N> w;
+#pragma unroll
+        for (int i = 0; i < N; i++) w.t[i] = from_float<T>(x[i]);
+        *reinterpret_cast<Run<T, N> *>(out + d) = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i++)
+            if (d + i < dim) out[d + i] = from_float<T>(x[i]);
+    }
+}
+
+__device__ __forceinline__ int clamp_to(int64_t v, int most) {
+    return v < 0 ? 0 : v > most ? most : static_cast<int>(v);
+}
+
+// Wavefronts of a SIMD that the registers are cut for (the most that spill
+// nothing).
+template <class T, int JV, bool kWhole>
+constexpr int kWavesPerSimd = JV == 16 ? 2 : JV == 8 ? (kWhole ? (kParts<T> == 2 ? 4 : 3) : (kParts<T> == 2 ? 3 : 2)) : kWhole ? 4 : 3;
+
 // JV: columns of a lane, so heads of up to 16 JV.  kWhole: pages of at least
 // 16 tokens, one page to each half of a step.  NW: wavefronts that share a
 // workgroup's tokens.
 template <class T, int JV, bool kWhole, int NW>
-__global__ __launch_bounds__(NW * kWave) void attend_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole>)) void attend_kernel(const AttendArgs a) {
     constexpr int N = kParts<T>;
     constexpr int KK = JV >= 4 ? JV / 4 : 1;
     const CacheView &c = a.c;
     const int lane = lane_id();
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int g = lane >> 4, i16 = lane & 15;
-    // a contiguous stretch of the work for each of the 8 dies, whose L2 then
-    // serves the row tiles of one head
-    const int64_t per = (a.work + 7) / 8;
-    const int64_t id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((blockIdx.x >> 3) >= per || id >= a.work) return;
-    const int64_t tile = id % a.row_tiles;
-    const int64_t rest = id / a.row_tiles;
-    const int chunk = static_cast<int>(rest % a.chunks);
-    const int head = static_cast<int>(rest / a.chunks % c.heads);
-    const int64_t b = rest / a.chunks / c.heads;
+    const uint32_t id = die_order(a);
+    if (id >= a.work) return;
+    uint32_t rest = a.tiles(id);
+    const uint32_t tile = id - rest * a.tiles.d;
+    const uint32_t bh = a.chunks(rest);                                 // sequence and head
+    const uint32_t chunk = rest - bh * a.chunks.d;
+    const uint32_t b = a.heads(bh);
+    const int head = static_cast<int>(bh - b * a.heads.d);
 
-    const int64_t rows = a.queries * a.group;
-    const int64_t r0 = tile * kRows;
-    const int64_t rl = r0 + kRows - 1 < rows - 1 ? r0 + kRows - 1 : rows - 1;      // last row
-    const Row row = row_of(a, b, head, r0 + i16);
-    // what the tile's rows see: from begin to at most stop, the row up to last
+    const uint32_t r0 = tile * kRows;
+    const uint32_t rl = r0 + kRows < a.rows ? r0 + kRows - 1 : a.rows - 1;      // last row
+    const bool there = r0 + i16 < a.rows;
+    const uint32_t r = there ? r0 + i16 : rl;
+    const uint32_t t = a.group(r);                                      // the lane's query
+    const int64_t q_row = static_cast<int64_t>(b) * a.queries + t;
+    const int q_head = static_cast<int>(head * a.group.d + (r - t * a.group.d));
+    // what the tile's rows see: from begin to at most stop, this lane's to row_end
     const int64_t all = static_cast<int64_t>(a.s.pages_per_seq) << c.shift;
     int64_t begin = a.s.begin(b);
     begin = begin < 0 ? 0 : begin;
     const int64_t end = a.end ? a.end[b] : all;
-    const int64_t row_end = end - (a.queries - 1 - (r0 + i16) / a.group);
-    int64_t stop = end - (a.queries - 1 - rl / a.group);
-    int64_t safe = end - (a.queries - 1 - r0 / a.group);        // every row sees up to here
+    int64_t row_end = end - (a.queries - 1 - t);
+    row_end = row_end > all ? all : row_end;
+    int64_t stop = end - (a.queries - 1 - a.group(rl));
+    int64_t safe = end - (a.queries - 1 - a.group(r0));                 // every row sees up to here
     stop = stop > all ? all : stop;
     safe = safe > all ? all : safe;
-    const int64_t base = begin & ~static_cast<int64_t>(kTile - 1);
-    const int64_t c0 = base + chunk * a.chunk;
-    const int64_t c1 = c0 + a.chunk < stop ? c0 + a.chunk : stop;
+    const int64_t c0 = (begin & ~static_cast<int64_t>(kTile - 1)) + chunk * a.chunk;
     if (a.part_o && c0 >= stop && chunk > 0) return;            // nothing there, and the join knows
+    // positions from here on count from c0
+    const int n = clamp_to(stop - c0, static_cast<int>(a.chunk));
+    const int first = clamp_to(begin - c0, n), last = clamp_to(row_end - c0, n), full = clamp_to(safe - c0, n);
 
     i32x4 qp[N][KK];
-    const float unit = load_query<T, KK>(a, row, lane, qp);
+    const float unit = load_query<T, KK>(a, static_cast<const T *>(a.q) + q_row * a.qt + q_head * a.qh, there, lane, qp);
     const float to_log2 = unit * a.scale * kLog2E;
 
     f32x4 o[JV];
@@ -213,13 +286,14 @@ __global__ __launch_bounds__(NW * kWave) void attend_kernel(const AttendArgs a) 
     float step = 0x1p-126f, inv = 0x1p126f;                     // the running step of values
 
     const int block = static_cast<int>(c.block_bytes());
-    const int64_t pitch = static_cast<int64_t>(c.heads) * 2 * block;
+    const uint32_t pitch = static_cast<uint32_t>(c.heads) * 2 * block;
     const int8_t *data = c.data + static_cast<int64_t>(head) * 2 * block;
-    const int32_t *table = a.s.table + b * a.s.table_stride;
     const int pmask = c.tokens() - 1;
+    const int32_t *table = a.s.table + b * a.s.table_stride + (c0 >> c.shift);
+    const int c0r = static_cast<int>(c0) & pmask;               // c0's row in its page
     const int vcol = JV * i16 < c.width - JV ? JV * i16 : c.width - JV;
 
-    for (int64_t t0 = c0 + wave * kTile; t0 < c1; t0 += NW * kTile) {
+    for (int t0 = wave * kTile; t0 < n; t0 += NW * kTile) {
         // ---- where the tokens are ----
         int bad = 0;                                            // bit of a lane's 8 tokens: padding
         float ks[2][4], vs[2][4];
@@ -228,21 +302,21 @@ __global__ __launch_bounds__(NW * kWave) void attend_kernel(const AttendArgs a) 
         if constexpr (kWhole) {
 #pragma unroll
             for (int u = 0; u < 2; u++) {
-                const int64_t t = t0 + 16 * u;
+                const int p = t0 + 16 * u;
                 int64_t page = -1;
-                if (t < c1 && t + 16 > begin) page = table[t >> c.shift];
+                if (p < n && p + 16 > first) page = table[(c0r + p) >> c.shift];
                 const bool ok = page >= 0 && page < c.pages;
                 const int64_t at = ok ? page : 0;
                 const int8_t *kb = data + at * pitch;
-                const int r = static_cast<int>(t) & pmask;
+                const int row = (c0r + p) & pmask;
                 const float2 sc = *reinterpret_cast<const float2 *>(c.scales + (at * c.heads + head) * 2);
 #pragma unroll
                 for (int kk = 0; kk < KK; kk++) {
                     const int col = 64 * kk + 16 * g < c.width - 16 ? 64 * kk + 16 * g : c.width - 16;
-                    kv[u][kk] = *reinterpret_cast<const i32x4 *>(kb + (r + i16) * c.width + col);
+                    kv[u][kk] = *reinterpret_cast<const i32x4 *>(kb + (row + i16) * c.width + col);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; i++) vv[4 * u + i].load(kb + block + (r + 4 * g + i) * c.width + vcol);
+                for (int i = 0; i < 4; i++) vv[4 * u + i].load(kb + block + (row + 4 * g + i) * c.width + vcol);
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     ks[u][i] = sc.x;
@@ -251,17 +325,18 @@ __global__ __launch_bounds__(NW * kWave) void attend_kernel(const AttendArgs a) 
                 if (!ok) bad |= 0xf << (4 * u);
             }
         } else {
-            const int64_t t = t0 + (lane & 31);
+            const int p = t0 + (lane & 31);
             int page = -1;
-            if (t < c1 && t >= begin) page = table[t >> c.shift];
-            const bool ok = page >= 0 && page < c.pages;
-            page = ok ? page : 0;
-            float2 sc = *reinterpret_cast<const float2 *>(c.scales + (static_cast<int64_t>(page) * c.heads + head) * 2);
-            sc.y = ok ? sc.y : 0.0f;
+            if (p < n && p >= first) page = table[(c0r + p) >> c.shift];
+            page = page < c.pages ? page : -1;
+            const uint32_t own = page < 0 ? 0 : page;
+            float2 sc = *reinterpret_cast<const float2 *>(c.scales + (static_cast<int64_t>(own) * c.heads + head) * 2);
+            sc.y = page < 0 ? 0.0f : sc.y;
 #pragma unroll
             for (int u = 0; u < 2; u++) {
-                const int64_t at = __shfl(page, 16 * u + i16, kWave);
-                const int8_t *kb = data + at * pitch + (static_cast<int>(t0 + 16 * u + i16) & pmask) * c.width;
+                const int got = __builtin_amdgcn_ds_bpermute(4 * (16 * u + i16), page);
+                const uint32_t at = got < 0 ? 0 : got;
+                const int8_t *kb = data + static_cast<uint64_t>(at) * pitch + ((c0r + t0 + 16 * u + i16) & pmask) * c.width;
 #pragma unroll
                 for (int kk = 0; kk < KK; kk++) {
                     const int col = 64 * kk + 16 * g < c.width - 16 ? 64 * kk + 16 * g : c.width - 16;
@@ -271,11 +346,12 @@ __global__ __launch_bounds__(NW * kWave) void attend_kernel(const AttendArgs a) 
 #pragma unroll
             for (int x = 0; x < 8; x++) {
                 const int from = 16 * (x >> 2) + 4 * g + (x & 3);
-                const int64_t at = __shfl(page, from, kWave);
-                vv[x].load(data + at * pitch + block + (static_cast<int>(t0 + from) & pmask) * c.width + vcol);
-                ks[x >> 2][x & 3] = __shfl(sc.x, from, kWave);
-                vs[x >> 2][x & 3] = __shfl(sc.y, from, kWave);
-                bad |= (__shfl(static_cast<int>(ok), from, kWave) ^ 1) << x;
+                const int got = __builtin_amdgcn_ds_bpermute(4 * from, page);
+                const uint32_t at = got < 0 ? 0 : got;
+                vv[x].load(data + static_cast<uint64_t>(at) * pitch + block + ((c0r + t0 + from) & pmask) * c.width + vcol);
+                ks[x >> 2][x & 3] = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * from, __builtin_bit_cast(int, sc.x)));
+                vs[x >> 2][x & 3] = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * from, __builtin_bit_cast(int, sc.y)));
+                bad |= (got < 0 ? 1 : 0) << x;
             }
         }
 
@@ -298,12 +374,13 @@ __global__ __launch_bounds__(NW * kWave) void attend_kernel(const AttendArgs a) 
                 s[u][i] = dot * (ks[u][i] * to_log2);
             }
         }
-        const bool inside = t0 >= begin && t0 + kTile <= safe;
-        if (!inside || __ballot(bad) != 0) {
+        const bool inside = t0 >= first && t0 + kTile <= full;
+        const bool masked = !inside || __ballot(bad) != 0;
+        if (masked) {
 #pragma unroll
             for (int x = 0; x < 8; x++) {
-                const int64_t t = t0 + 16 * (x >> 2) + 4 * g + (x & 3);
-                if (t < begin || t >= row_end || t >= all) bad |= 1 << x;
+                const int p = t0 + 16 * (x >> 2) + 4 * g + (x & 3);
+                if (p < first || p >= last) bad |= 1 << x;
                 if ((bad >> x) & 1) s[x >> 2][x & 3] = -INFINITY;
             }
         }
@@ -323,8 +400,10 @@ __global__ __launch_bounds__(NW * kWave) void attend_kernel(const AttendArgs a) 
         float big = fmaxf(fmaxf(fmaxf(vs[0][0], vs[0][1]), fmaxf(vs[0][2], vs[0][3])),
                           fmaxf(fmaxf(vs[1][0], vs[1][1]), fmaxf(vs[1][2], vs[1][3])));
         if (__ballot(big > 2.0f * step)) {
-#pragma unroll
-            for (int x = 1; x < kWave; x <<= 1) big = fmaxf(big, __shfl_xor(big, x, kWave));
+            if constexpr (!kWhole) {                            // else the same in every lane
+                big = fmaxf(big, __shfl_xor(big, 16, kWave));
+                big = fmaxf(big, __shfl_xor(big, 32, kWave));
+            }
             const float f = step / big;
 #pragma unroll
             for (int j = 0; j < JV; j++) o[j] *= f;
@@ -338,7 +417,11 @@ __global__ __launch_bounds__(NW * kWave) void attend_kernel(const AttendArgs a) 
         for (int x = 0; x < 8; x++) {
             const float p = __builtin_amdgcn_exp2f(s[x >> 2][x & 3] - from);
             l += p;
-            w[x] = (bad >> x) & 1 ? 0.0f : p * (vs[x >> 2][x & 3] * inv);
+            w[x] = p * (vs[x >> 2][x & 3] * inv);
+        }
+        if (masked) {
+#pragma unroll
+            for (int x = 0; x < 8; x++) w[x] = (bad >> x) & 1 ? 0.0f : w[x];    // a step that is not seen may be NaN
         }
         i32x4 hi, lo;
 #pragma unroll
@@ -369,9 +452,7 @@ __global__ __launch_bounds__(NW * kWave) void attend_kernel(const AttendArgs a) 
     // ---- join the lanes of a row, then the wavefronts ----
     l += __shfl_xor(l, 16, kWave);
     l += __shfl_xor(l, 32, kWave);
-    const float back = step * 512.0f;
-#pragma unroll
-    for (int j = 0; j < JV; j++) o[j] *= back;
+    float back = step * 512.0f;
     if constexpr (NW > 1) {
         constexpr int kPad = 16 * JV + 4;
         __shared__ float so[NW - 1][kRows][kPad];
@@ -382,9 +463,9 @@ __global__ __launch_bounds__(NW * kWave) void attend_kernel(const AttendArgs a) 
         }
         if (wave > 0) {
 #pragma unroll
-            for (int j = 0; j < JV; j++)
+            for (int i = 0; i < 4; i++)
 #pragma unroll
-                for (int i = 0; i < 4; i++) so[wave - 1][i16][JV * (4 * g + i) + j] = o[j][i];
+                for (int j = 0; j < JV; j++) so[wave - 1][i16][JV * (4 * g + i) + j] = o[j][i] * back;
         }
         __syncthreads();
         if (wave > 0) return;
@@ -394,112 +475,291 @@ __global__ __launch_bounds__(NW * kWave) void attend_kernel(const AttendArgs a) 
         const float f0 = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - all_m);
         l *= f0;
 #pragma unroll
-        for (int j = 0; j < JV; j++) o[j] *= f0;
+        for (int j = 0; j < JV; j++) o[j] *= back * f0;
+        back = 1.0f;
 #pragma unroll
         for (int x = 1; x < NW; x++) {
             const float f = sm[x][i16] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[x][i16] - all_m);
             l += sl[x][i16] * f;
 #pragma unroll
-            for (int j = 0; j < JV; j++)
+            for (int i = 0; i < 4; i++)
 #pragma unroll
-                for (int i = 0; i < 4; i++) o[j][i] += so[x - 1][i16][JV * (4 * g + i) + j] * f;
+                for (int j = 0; j < JV; j++) o[j][i] += so[x - 1][i16][JV * (4 * g + i) + j] * f;
         }
         m = all_m;
     }
-    if (!row.there) return;
+    if (!there) return;
+    const bool none = l == 0.0f;             // a NaN among what is seen stays one
     if (a.part_o) {
-        const int64_t r = ((b * c.heads + head) * rows + r0 + i16) * a.chunks + chunk;
-        float *po = a.part_o + r * c.dim;
+        const int64_t at = (static_cast<int64_t>(bh) * a.rows + r) * a.chunks.d + chunk;
 #pragma unroll
-        for (int i = 0; i < 4; i++)
+        for (int i = 0; i < 4; i++) {
+            float x[JV];
 #pragma unroll
-            for (int j = 0; j < JV; j++) {
-                const int d = JV * (4 * g + i) + j;
-                if (d < c.dim) po[d] = o[j][i];
-            }
+            for (int j = 0; j < JV; j++) x[j] = o[j][i] * back;
+            store_columns<float, JV>(a.part_o + at * c.dim, JV * (4 * g + i), c.dim, x);
+        }
         if (g == 0) {
-            a.part_ml[2 * r] = m;
-            a.part_ml[2 * r + 1] = l;
+            a.part_ml[2 * at] = m;
+            a.part_ml[2 * at + 1] = l;
         }
         return;
     }
-    const bool none = m == -INFINITY;
-    T *out = static_cast<T *>(a.out) + row.q * a.ot + row.head * a.oh;
+    T *out = static_cast<T *>(a.out) + q_row * a.ot + q_head * a.oh;
+    const float norm = none ? 0.0f : back / l;
 #pragma unroll
-    for (int i = 0; i < 4; i++)
+    for (int i = 0; i < 4; i++) {
+        float x[JV];
 #pragma unroll
-        for (int j = 0; j < JV; j++) {
-            const int d = JV * (4 * g + i) + j;
-            if (d < c.dim) out[d] = from_float<T>(none ? 0.0f : o[j][i] / l);
-        }
+        for (int j = 0; j < JV; j++) x[j] = none ? 0.0f : o[j][i] * norm;
+        store_columns<T, JV>(out, JV * (4 * g + i), c.dim, x);
+    }
     if (a.lse && g == 0)
-        a.lse[row.q * (c.heads * a.group) + row.head] = none ? -INFINITY : (m - kOffset<T> + __builtin_amdgcn_logf(l)) / kLog2E;
+        a.lse[q_row * (c.heads * a.group.d) + q_head] = none ? -INFINITY : (m - kOffset<T> + __builtin_amdgcn_logf(l)) / kLog2E;
 }
 
-// Joins the chunks of a row: a wavefront per row of a head.
-template <class T>
-__global__ __launch_bounds__(kBlock) void attend_join_kernel(const AttendArgs a) {
+// Joins the chunks of a row with NW wavefronts, which take 8 chunks at a time
+// in turn; a lane takes the columns lane, lane + 64, ...  With NW = 1 a
+// workgroup has a row for each of its wavefronts.
+template <class T, int NW>
+__global__ __launch_bounds__((NW == 1 ? kBlock : NW * kWave)) void attend_join_kernel(const AttendArgs a) {
+    constexpr int kCols = TGL_MAX_HEAD_DIM / kWave, kStep = 8;
+    __shared__ float so[NW][TGL_MAX_HEAD_DIM];
+    __shared__ float sl[NW];
     const CacheView &c = a.c;
     const int lane = lane_id();
-    const int64_t rows = a.queries * a.group;
-    const int64_t all_rows = a.s.seqs * c.heads * rows;
-    const int64_t x = static_cast<int64_t>(blockIdx.x) * (kBlock / kWave) + threadIdx.x / kWave;
-    if (x >= all_rows) return;
-    const int64_t bh = x / rows, r = x - bh * rows;
-    const int64_t b = bh / c.heads;
-    const Row row = row_of(a, b, static_cast<int>(bh - b * c.heads), r);
+    const int at_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wave = NW == 1 ? 0 : at_wave;
+    const uint32_t x = NW == 1 ? blockIdx.x * (kBlock / kWave) + at_wave : blockIdx.x;
+    if (NW == 1 && x >= a.all_rows) return;
+    const uint32_t bh = a.row_of(x), r = x - bh * a.rows;
+    const uint32_t b = a.heads(bh), t = a.group(r);
+    const int64_t q_row = static_cast<int64_t>(b) * a.queries + t;
+    const int q_head = static_cast<int>((bh - b * a.heads.d) * a.group.d + (r - t * a.group.d));
     // the chunks that the row's tile has, as the tile counts them
-    const int64_t rl = (r | (kRows - 1)) < rows - 1 ? (r | (kRows - 1)) : rows - 1;
+    const uint32_t rl = (r | (kRows - 1)) < a.rows ? (r | (kRows - 1)) : a.rows - 1;
     const int64_t all = static_cast<int64_t>(a.s.pages_per_seq) << c.shift;
     int64_t begin = a.s.begin(b);
     begin = begin < 0 ? 0 : begin;
-    int64_t stop = (a.end ? a.end[b] : all) - (a.queries - 1 - rl / a.group);
+    int64_t stop = (a.end ? a.end[b] : all) - (a.queries - 1 - a.group(rl));
     stop = stop > all ? all : stop;
     const int64_t span = stop - (begin & ~static_cast<int64_t>(kTile - 1));
-    int64_t n = span <= 0 ? 1 : (span + a.chunk - 1) / a.chunk;
-    n = n < a.chunks ? n : a.chunks;
-    const float *ml = a.part_ml + 2 * x * a.chunks;
-    const float *po = a.part_o + x * a.chunks * c.dim;
+    const int64_t want = span <= 0 ? 1 : (span + a.chunk - 1) / a.chunk;
+    const int n = static_cast<int>(want < a.chunks.d ? want : a.chunks.d);
+    const int64_t at = (static_cast<int64_t>(bh) * a.rows + r) * a.chunks.d;
+    const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + at;
+    const float *po = a.part_o + at * c.dim;
     float m = -INFINITY;
-    for (int64_t i = lane; i < n; i += kWave) m = fmaxf(m, ml[2 * i]);
+    for (int i = lane; i < n; i += kWave) m = fmaxf(m, ml[i].x);
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, kWave));
     float l = 0.0f;
-    float o[TGL_MAX_HEAD_DIM / kWave] = {};
-    for (int64_t i0 = 0; i0 < n; i0 += kWave) {
-        const int64_t i = i0 + lane;
-        float f = 0.0f;
-        if (i < n && ml[2 * i] != -INFINITY) f = __builtin_amdgcn_exp2f(ml[2 * i] - m);
-        l += i < n ? ml[2 * i + 1] * f : 0.0f;
-        const int count = n - i0 < kWave ? static_cast<int>(n - i0) : kWave;
-        for (int y = 0; y < count; y++) {
-            const float fy = __shfl(f, y, kWave);
+    float o[kCols] = {};
+    for (int i0 = wave * kStep; i0 < n; i0 += NW * kStep) {
+        float v[kStep][kCols], f[kStep];
 #pragma unroll
-            for (int k = 0; k < TGL_MAX_HEAD_DIM / kWave; k++)
-                if (k * kWave + lane < c.dim) o[k] += po[(i0 + y) * c.dim + k * kWave + lane] * fy;
+        for (int y = 0; y < kStep; y++) {
+            const int i = i0 + y < n ? i0 + y : n - 1;
+            const float2 w = ml[i];
+            f[y] = w.x == -INFINITY || i0 + y >= n ? 0.0f : __builtin_amdgcn_exp2f(w.x - m);
+            l += i0 + y < n ? w.y * f[y] : 0.0f;
+#pragma unroll
+            for (int k = 0; k < kCols; k++) {
+                const int d = k * kWave + lane < c.dim ? k * kWave + lane : c.dim - 1;
+                v[y][k] = k * kWave < c.dim ? po[static_cast<int64_t>(i) * c.dim + d] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int y = 0; y < kStep; y++)
+#pragma unroll
+            for (int k = 0; k < kCols; k++) o[k] += i0 + y < n ? v[y][k] * f[y] : 0.0f;
+    }
+    if constexpr (NW > 1) {
+#pragma unroll
+        for (int k = 0; k < kCols; k++) so[wave][k * kWave + lane] = o[k];
+        if (lane == 0) sl[wave] = l;
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int y = 1; y < NW; y++) {
+            l += sl[y];
+#pragma unroll
+            for (int k = 0; k < kCols; k++) o[k] += so[y][k * kWave + lane];
         }
     }
-    l = group_sum<kWave>(l);
-    const bool none = m == -INFINITY;
-    T *out = static_cast<T *>(a.out) + row.q * a.ot + row.head * a.oh;
+    const bool none = l == 0.0f;
+    T *out = static_cast<T *>(a.out) + q_row * a.ot + q_head * a.oh;
+    const float norm = 1.0f / l;
 #pragma unroll
-    for (int k = 0; k < TGL_MAX_HEAD_DIM / kWave; k++) {
+    for (int k = 0; k < kCols; k++) {
         const int d = k * kWave + lane;
-        if (d < c.dim) out[d] = from_float<T>(none ? 0.0f : o[k] / l);
+        if (d < c.dim) out[d] = from_float<T>(none ? 0.0f : o[k] * norm);
     }
     if (a.lse && lane == 0)
-        a.lse[row.q * (c.heads * a.group) + row.head] = none ? -INFINITY : (m - kOffset<T> + __builtin_amdgcn_logf(l)) / kLog2E;
+        a.lse[q_row * (c.heads * a.group.d) + q_head] = none ? -INFINITY : (m - kOffset<T> + __builtin_amdgcn_logf(l)) / kLog2E;
+}
+
+// ---- few tokens -------------------------------------------------------------
+//
+// A sequence with a few tokens (sampled slots) leaves the matrix instructions
+// mostly idle and pays for their set-up.  Here 16 lanes serve a sequence and
+// head, JV columns each, and a wavefront four of them; everything is float32.
+// 16 tokens at a time: lane i looks token i up; every lane multiplies its
+// columns of all 16; the products are summed over the lanes so that token i's
+// sum arrives in lane i (four exchanges, halving the tokens each time); the
+// weights come back from lane i by a swizzle.
+
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xf, 0xf, true));
+}
+// Lane i's partner among 16: i ^ 8, i ^ 7, i ^ 2, i ^ 1, which together reach all.
+constexpr int kXor8 = 0x128, kXor7 = 0x141, kXor2 = 0x4e, kXor1 = 0xb1;
+
+template <int kBit, int kCtrl, int N>
+__device__ __forceinline__ void scatter_sum(float (&p)[16], int i) {
+#pragma unroll
+    for (int k = 0; k < N; k++) {
+        const float keep = i & kBit ? p[k + N] : p[k], send = i & kBit ? p[k] : p[k + N];
+        p[k] = keep + dpp<kCtrl>(send);
+    }
+}
+
+// Lane j of each 16.
+template <int J>
+__device__ __forceinline__ int from_lane(int v) {
+    return __builtin_amdgcn_ds_swizzle(v, (J << 5) | 0x10);
+}
+
+// f(0), f(1), ... f(N - 1) with constant arguments.
+template <int K>
+struct Const {
+    static constexpr int value = K;
+};
+template <int N, int K = 0, class F>
+__device__ __forceinline__ void unrolled(const F &f) {
+    if constexpr (K < N) {
+        f(Const<K>());
+        unrolled<N, K + 1>(f);
+    }
+}
+
+template <class T, int JV>
+__global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(const AttendArgs a) {
+    constexpr int kWords = JV / 4;
+    const CacheView &c = a.c;
+    const int i = threadIdx.x & 15;
+    const uint32_t items = a.s.seqs * a.heads.d;
+    const uint32_t item = (blockIdx.x * kBlock + threadIdx.x) / 16;
+    const bool there = item < items;
+    const uint32_t it = there ? item : items - 1;
+    const uint32_t b = a.heads(it);
+    const int head = static_cast<int>(it - b * a.heads.d);
+    const int64_t all = static_cast<int64_t>(a.s.pages_per_seq) << c.shift;
+    int64_t begin = a.s.begin(b);
+    begin = begin < 0 ? 0 : begin;
+    const int64_t end = a.end ? a.end[b] : all;
+    const int block = static_cast<int>(c.block_bytes());
+    const uint32_t pitch = static_cast<uint32_t>(c.heads) * 2 * block;
+    const int col = JV * i < c.width - JV ? JV * i : c.width - JV;
+    const int8_t *data = c.data + static_cast<int64_t>(head) * 2 * block + col;
+    const int pmask = c.tokens() - 1;
+    const int32_t *table = a.s.table + b * a.s.table_stride;
+
+    for (uint32_t r = 0; r < a.rows; r++) {
+        const uint32_t t = a.group(r);
+        const int64_t q_row = static_cast<int64_t>(b) * a.queries + t;
+        const int q_head = static_cast<int>(head * a.group.d + (r - t * a.group.d));
+        int64_t stop = end - (a.queries - 1 - t);
+        stop = stop > all ? all : stop;
+        const int n = there ? clamp_to(stop - begin, 1 << 30) : 0;
+        float q[JV];
+        load_columns<T, JV>(static_cast<const T *>(a.q) + q_row * a.qt + q_head * a.qh, JV * i, c.dim, q);
+#pragma unroll
+        for (int k = 0; k < JV; k++) q[k] *= a.scale * kLog2E;
+        float m = -INFINITY, l = 0.0f, o[JV] = {};
+        for (int j0 = 0; __any(j0 < n); j0 += 16) {
+            int page = -1;
+            if (j0 + i < n) page = table[(begin + j0 + i) >> c.shift];
+            page = page < c.pages ? page : -1;
+            const int own = page < 0 ? 0 : page;
+            const float2 sc = *reinterpret_cast<const float2 *>(c.scales + (static_cast<int64_t>(own) * c.heads + head) * 2);
+            const int r0 = static_cast<int>(begin + j0);
+            int kw[16][kWords], vw[16][kWords];
+            unrolled<16>([&](auto J) {
+                constexpr int j = decltype(J)::value;
+                    const uint32_t at = from_lane<j>(own);
+                    const int8_t *k = data + static_cast<uint64_t>(at) * pitch + ((r0 + j) & pmask) * c.width;
+                    Columns<JV> x;
+                    x.load(k);
+#pragma unroll
+                    for (int w = 0; w < kWords; w++) kw[j][w] = x.w[w];
+                    x.load(k + block);
+#pragma unroll
+                    for (int w = 0; w < kWords; w++) vw[j][w] = x.w[w];
+            });
+            float p[16];
+#pragma unroll
+            for (int j = 0; j < 16; j++) {
+                p[j] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < JV; k++)
+                    p[j] = __builtin_fmaf(static_cast<float>(static_cast<int8_t>(kw[j][k / 4] >> (8 * (k % 4)))), q[k], p[j]);
+            }
+            scatter_sum<8, kXor8, 8>(p, i);
+            scatter_sum<4, kXor7, 4>(p, i);
+            scatter_sum<2, kXor2, 2>(p, i);
+            scatter_sum<1, kXor1, 1>(p, i);
+            const float s = page < 0 ? -INFINITY : p[0] * sc.x;
+            float top = fmaxf(s, dpp<kXor8>(s));
+            top = fmaxf(top, dpp<kXor7>(top));
+            top = fmaxf(top, dpp<kXor2>(top));
+            top = fmaxf(top, dpp<kXor1>(top));
+            const float next = fmaxf(m, top);
+            const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - next);
+            m = next;
+            const float e = __builtin_amdgcn_exp2f(s - (m == -INFINITY ? 0.0f : m));
+            l = l * f + e;
+            const int w = __builtin_bit_cast(int, page < 0 ? 0.0f : e * sc.y);
+#pragma unroll
+            for (int k = 0; k < JV; k++) o[k] *= f;
+            unrolled<16>([&](auto J) {
+                constexpr int j = decltype(J)::value;
+                const float wj = __builtin_bit_cast(float, from_lane<j>(w));
+#pragma unroll
+                for (int k = 0; k < JV; k++)
+                    o[k] = __builtin_fmaf(static_cast<float>(static_cast<int8_t>(vw[j][k / 4] >> (8 * (k % 4)))), wj, o[k]);
+            });
+        }
+        l += dpp<kXor8>(l);
+        l += dpp<kXor7>(l);
+        l += dpp<kXor2>(l);
+        l += dpp<kXor1>(l);
+        const bool none = l == 0.0f;
+        const float norm = 1.0f / l;
+#pragma unroll
+        for (int k = 0; k < JV; k++) o[k] = none ? 0.0f : o[k] * norm;
+        if (there) {
+            store_columns<T, JV>(static_cast<T *>(a.out) + q_row * a.ot + q_head * a.oh, JV * i, c.dim, o);
+            if (a.lse && i == 0)
+                a.lse[q_row * (c.heads * a.group.d) + q_head] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) / kLog2E;
+        }
+    }
 }
 
 // Workgroups that fill the card a few times over; a long axis is cut until
-// there are that many, into chunks of at least kMinChunk tokens.
-constexpr int64_t kFill = 2048;
+// there are that many, into chunks of at least kMinChunk tokens, and 64 for
+// each row of a tile (whose partial sums then are at most 1/16 of the bytes).
+constexpr int64_t kFill = 4096;
 constexpr int64_t kMinChunk = 256;
+
+constexpr uint32_t kFewRows = 4;
+constexpr int64_t kFewTokens = 64;
 
 struct Plan {
     int64_t row_tiles;
     int64_t chunk;
-    int32_t chunks;
+    int64_t chunks;
     size_t part_o;          // bytes of each part of the workspace, 0 without chunks
     size_t part_ml;
 };
@@ -510,14 +770,15 @@ Plan plan_of(const CacheView &c, int64_t num_seqs, int32_t pages_per_seq, int32_
     p.row_tiles = (rows + kRows - 1) / kRows;
     const int64_t most = (static_cast<int64_t>(pages_per_seq) << c.shift) + kTile;      // begin need not be at a step's start
     const int64_t items = num_seqs * c.heads * p.row_tiles;
-    int64_t chunks = items > 0 ? kFill / items : 1;
-    const int64_t cap = most / kMinChunk;
+    int64_t chunks = items > 0 && items < kFill / 2 ? kFill / items : 1;
+    const int64_t tile_rows = rows < kRows ? rows : kRows;
+    const int64_t cap = most / (64 * tile_rows > kMinChunk ? 64 * tile_rows : kMinChunk);
     chunks = chunks > cap ? cap : chunks;
-    chunks = chunks < 1 ? 1 : chunks;
+    const int64_t least = (most >> 30) + 1;             // positions in a chunk are 32-bit
+    chunks = chunks < least ? least : chunks;
     p.chunk = (most + chunks - 1) / chunks;
     p.chunk = (p.chunk + 4 * kTile - 1) / (4 * kTile) * (4 * kTile);
-    p.chunks = static_cast<int32_t>((most + p.chunk - 1) / p.chunk);
-    if (p.chunks < 1) p.chunks = 1;
+    p.chunks = (most + p.chunk - 1) / p.chunk;
     if (p.chunks > 1) {
         const size_t n = static_cast<size_t>(num_seqs) * c.heads * rows * p.chunks;
         p.part_o = align_up(n * c.dim * 4, 256);
@@ -528,7 +789,7 @@ Plan plan_of(const CacheView &c, int64_t num_seqs, int32_t pages_per_seq, int32_
 
 template <class T, int JV, bool kWhole>
 void launch(const AttendArgs &a, int nw, hipStream_t st) {
-    const unsigned grid = static_cast<unsigned>((a.work + 7) / 8 * 8);
+    const unsigned grid = (a.work + 7) / 8 * 8;
     if (nw == 1) attend_kernel<T, JV, kWhole, 1><<<grid, kWave, 0, st>>>(a);
     else attend_kernel<T, JV, kWhole, 4><<<grid, 4 * kWave, 0, st>>>(a);
 }
@@ -540,18 +801,28 @@ void launch(const AttendArgs &a, int nw, hipStream_t st) {
     else if (a.c.width <= 64) whole ? launch<T, 4, true>(a, nw, st) : launch<T, 4, false>(a, nw, st);
     else if (a.c.width <= 128) whole ? launch<T, 8, true>(a, nw, st) : launch<T, 8, false>(a, nw, st);
     else whole ? launch<T, 16, true>(a, nw, st) : launch<T, 16, false>(a, nw, st);
-    if (a.chunks > 1) {
-        const int64_t rows = a.s.seqs * a.c.heads * a.queries * a.group;
-        attend_join_kernel<T><<<static_cast<unsigned>((rows + 3) / 4), kBlock, 0, st>>>(a);
+    if (a.part_o) {
+        // wavefronts of a row: enough that each has a few chunks
+        if (a.chunks.d <= 16) attend_join_kernel<T, 1><<<(a.all_rows + 3) / 4, kBlock, 0, st>>>(a);
+        else attend_join_kernel<T, 16><<<a.all_rows, 16 * kWave, 0, st>>>(a);
     }
+}
+
+// Whether the kernel for few tokens is the faster one.
+bool few(const AttendArgs &a) { return a.rows <= kFewRows && (static_cast<int64_t>(a.s.pages_per_seq) << a.c.shift) <= kFewTokens; }
+
+template <class T>
+void launch_few(const AttendArgs &a, unsigned grid, hipStream_t st) {
+    if (a.c.width <= 64) attend_few_kernel<T, 4><<<grid, kBlock, 0, st>>>(a);
+    else if (a.c.width <= 128) attend_few_kernel<T, 8><<<grid, kBlock, 0, st>>>(a);
+    else attend_few_kernel<T, 16><<<grid, kBlock, 0, st>>>(a);
 }
 
 // Rows without anything to see: zeros.
 template <class T>
 __global__ __launch_bounds__(kBlock) void attend_none_kernel(const AttendArgs a) {
-    const int64_t rows = a.s.seqs * a.queries;
-    const int heads = a.c.heads * a.group;
-    const int64_t n = rows * heads * a.c.dim;
+    const int heads = a.c.heads * a.group.d;
+    const int64_t n = static_cast<int64_t>(a.s.seqs) * a.queries * heads * a.c.dim;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * kBlock) {
         const int64_t rh = i / a.c.dim;
         static_cast<T *>(a.out)[rh / heads * a.ot + rh % heads * a.oh + i % a.c.dim] = from_float<T>(0.0f);
@@ -584,8 +855,21 @@ tgl_status tgl_cache_attend(const tgl_cache *cache, const tgl_heads *q, int32_t 
     const int64_t rows = seqs->num_seqs * queries;
     if (rows >= (int64_t(1) << 31) / q_heads) return TGL_EINVAL;
     if (!valid_heads(q, rows, dtype) || !valid_heads(out, rows, dtype)) return TGL_EINVAL;
-    AttendArgs a{view_of(*cache), view_of(*seqs, rows), end, q->ptr, out->ptr, lse, nullptr, nullptr, q->token_stride,
-                 q->head_stride, out->token_stride, out->head_stride, queries, 1, 0, 0, 1, q_heads / cache->heads, scale};
+    AttendArgs a{};
+    a.c = view_of(*cache);
+    a.s = view_of(*seqs, rows);
+    a.end = end;
+    a.q = q->ptr;
+    a.out = out->ptr;
+    a.lse = lse;
+    a.qt = q->token_stride;
+    a.qh = q->head_stride;
+    a.ot = out->token_stride;
+    a.oh = out->head_stride;
+    a.queries = static_cast<uint32_t>(queries);
+    a.scale = scale;
+    const uint32_t group = q_heads / cache->heads;
+    a.group = Div(group);
     const Plan p = plan_of(a.c, seqs->num_seqs, seqs->pages_per_seq, q_heads, queries);
     if (p.part_o + p.part_ml > 0) {
         if (!workspace || workspace_bytes < p.part_o + p.part_ml) return TGL_ENOSPACE;
@@ -601,14 +885,26 @@ tgl_status tgl_cache_attend(const tgl_cache *cache, const tgl_heads *q, int32_t 
         else attend_none_kernel<bf16_t><<<grid, kBlock, 0, st>>>(a);
         return launch_status();
     }
-    a.row_tiles = p.row_tiles;
+    const int64_t work = seqs->num_seqs * a.c.heads * p.row_tiles * p.chunks;
+    if (work > 0x7ffffff0) return TGL_EINVAL;
+    a.rows = static_cast<uint32_t>(queries * group);
+    a.row_of = Div(a.rows);
+    a.all_rows = a.rows * a.s.seqs * a.c.heads;
     a.chunk = p.chunk;
-    a.chunks = p.chunks;
-    a.work = seqs->num_seqs * a.c.heads * p.row_tiles * p.chunks;
-    if (a.work > 0x7ffffff0) return TGL_EINVAL;
+    a.work = static_cast<uint32_t>(work);
+    a.tiles = Div(static_cast<uint32_t>(p.row_tiles));
+    a.chunks = Div(static_cast<uint32_t>(p.chunks));
+    a.heads = Div(a.c.heads);
+    a.spread = p.row_tiles > 1;
     if (p.part_o) {
         a.part_o = static_cast<float *>(workspace);
         a.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + p.part_o);
+    }
+    if (few(a)) {
+        const unsigned grid = static_cast<unsigned>((a.s.seqs * int64_t(a.c.heads) + 15) / 16);
+        if (dtype == TGL_OUT_F32) launch_few<float>(a, grid, st);
+        else launch_few<bf16_t>(a, grid, st);
+        return launch_status();
     }
     // a wavefront alone where a sequence has at most two steps for it
     const int nw = (static_cast<int64_t>(a.s.pages_per_seq) << a.c.shift) <= 2 * kTile ? 1 : 4;

@@ -382,6 +382,41 @@ def test_attend_long(B, length, page, heads, group, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [1, 3, 16, 50, 64, 65, 100, 128, 130, 256])
+@pytest.mark.parametrize("page,heads,group,T", [(1, 2, 1, 1), (1, 1, 2, 2), (8, 3, 4, 1), (16, 1, 1, 3)])
+def test_attend_few_tokens(page, heads, group, T, dim, dtype):
+    """Sampled slots: tables of at most 64 places."""
+    torch = require_gpu()
+    announce("attend few page %d heads %d group %d T %d dim %d %s" % (page, heads, group, T, dim, dtype))
+    rng = np.random.default_rng(dim + page)
+    for lengths in ([10, 0, 1, 7, 10, 3, 10], [15, 16, 17, 0, 31, 32, 33, 47, 48], [1], [48, 2]):
+        _attend(torch, rng, dtype, page, heads, group, dim, T, lengths, holes=0.2, extra=0)
+    _attend(torch, rng, dtype, page, heads, group, dim, T, [20, 33, 9], begin=[3, 32, 9], extra=0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("L", [40, 200, 5000])
+def test_attend_nan_queries_and_keys(L, dtype):
+    """A row that sees a NaN or an infinite score is NaN, never 0; a row that sees nothing stays 0."""
+    torch = require_gpu()
+    announce("attend NaN rows %d %s" % (L, dtype))
+    rng = np.random.default_rng(L)
+    c, _ = _cache(rng, torch, 3 * L, 1, 1, 32)
+    table = torch.arange(3 * L, dtype=torch.int32).cuda().view(3, L)
+    q = torch.randn(3, 2, 32).cuda().to(_torch_type(torch, dtype))
+    q[0, 1, 5] = math.nan
+    q[2, 0, 31] = math.inf
+    end = torch.tensor([L, 0, L]).cuda()
+    out, lse = P.cache_attend(c, q, table, end=end, return_lse=True)
+    assert torch.isfinite(out[0, 0]).all() and torch.isnan(out[0, 1]).all()
+    assert (out[1] == 0).all() and torch.isneginf(lse[1]).all()
+    assert torch.isnan(out[2, 0]).all() and torch.isfinite(out[2, 1]).all()
+    c.scales[L // 2, 0, 0] = math.nan
+    out = P.cache_attend(c, q, table, end=end)
+    assert torch.isnan(out[0]).all() and torch.isfinite(out[2, 1]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_attend_sharp_and_flat_scores(dtype):
     torch = require_gpu()
     announce("attend sharp and flat %s" % dtype)
