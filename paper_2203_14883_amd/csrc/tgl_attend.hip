@@ -60,16 +60,18 @@ struct AttendArgs {
     const void *q;
     void *out;
     float *lse;
-    float *part_o;          // [rows of all heads][chunks][dim], or null
+    float *part_o;          // [rows of all heads][chunks][width], or null
     float *part_ml;         // [rows of all heads][chunks][2]
     int64_t qt, qh, ot, oh;
     int64_t chunk;          // tokens of a workgroup, below 2^31
     uint32_t queries;
     uint32_t rows;          // of one sequence and head: queries * group
     uint32_t work;          // workgroups
+    uint32_t chunks;
+    uint32_t tile_rows;     // rows of a workgroup: 16, or 32
     uint32_t all_rows;      // rows of all sequences and heads
     Div tiles;              // row tiles of one sequence and head
-    Div chunks;
+    Div items;              // sequences times heads
     Div heads;
     Div group;              // query heads of one head of the cache
     Div row_of;             // rows of one sequence and head
@@ -228,14 +230,25 @@ __device__ __forceinline__ int clamp_to(int64_t v, int most) {
 
 // Wavefronts of a SIMD that the registers are cut for (the most that spill
 // nothing).
-template <class T, int JV, bool kWhole>
-constexpr int kWavesPerSimd = JV == 16 ? 2 : JV == 8 ? (kWhole ? (kParts<T> == 2 ? 4 : 3) : (kParts<T> == 2 ? 3 : 2)) : kWhole ? 4 : 3;
+template <class T, int JV, bool kWhole, int R>
+constexpr int kWavesPerSimd = JV == 16 ? 2 : R == 2 ? 2 : JV == 8 ? (kParts<T> == 2 && kWhole ? 3 : 2) : 3;
+
+// A wavefront's 32 tokens: where they are, then what they hold.
+template <int JV, bool kWhole>
+struct Step {
+    static constexpr int KK = JV >= 4 ? JV / 4 : 1;
+    int page[kWhole ? 2 : 1];       // kWhole: of the two halves, uniform; else of token lane & 31; -1: nothing to see
+    float2 sc[kWhole ? 2 : 1];      // the steps of keys and values
+    i32x4 kv[2][KK];
+    Columns<JV> vv[8];
+};
 
 // JV: columns of a lane, so heads of up to 16 JV.  kWhole: pages of at least
 // 16 tokens, one page to each half of a step.  NW: wavefronts that share a
-// workgroup's tokens.
-template <class T, int JV, bool kWhole, int NW>
-__global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole>)) void attend_kernel(const AttendArgs a) {
+// workgroup's tokens.  R: row tiles of a wavefront, which share the keys'
+// loads and the values' conversion.
+template <class T, int JV, bool kWhole, int NW, int R>
+__global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void attend_kernel(const AttendArgs a) {
     constexpr int N = kParts<T>;
     constexpr int KK = JV >= 4 ? JV / 4 : 1;
     const CacheView &c = a.c;
@@ -244,27 +257,22 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole>)) void at
     const int g = lane >> 4, i16 = lane & 15;
     const uint32_t id = die_order(a);
     if (id >= a.work) return;
-    uint32_t rest = a.tiles(id);
+    // row tiles first, then heads and sequences, chunks last: the chunks that
+    // only long sequences have are then spread over the dies
+    const uint32_t rest = a.tiles(id);
     const uint32_t tile = id - rest * a.tiles.d;
-    const uint32_t bh = a.chunks(rest);                                 // sequence and head
-    const uint32_t chunk = rest - bh * a.chunks.d;
+    const uint32_t chunk = a.items(rest);
+    const uint32_t bh = rest - chunk * a.items.d;                       // sequence and head
     const uint32_t b = a.heads(bh);
     const int head = static_cast<int>(bh - b * a.heads.d);
 
-    const uint32_t r0 = tile * kRows;
-    const uint32_t rl = r0 + kRows < a.rows ? r0 + kRows - 1 : a.rows - 1;      // last row
-    const bool there = r0 + i16 < a.rows;
-    const uint32_t r = there ? r0 + i16 : rl;
-    const uint32_t t = a.group(r);                                      // the lane's query
-    const int64_t q_row = static_cast<int64_t>(b) * a.queries + t;
-    const int q_head = static_cast<int>(head * a.group.d + (r - t * a.group.d));
-    // what the tile's rows see: from begin to at most stop, this lane's to row_end
+    const uint32_t r0 = tile * (kRows * R);
+    const uint32_t rl = r0 + kRows * R < a.rows ? r0 + kRows * R - 1 : a.rows - 1;      // last row
+    // what the tile's rows see: from begin to at most stop, a row up to row_end
     const int64_t all = static_cast<int64_t>(a.s.pages_per_seq) << c.shift;
     int64_t begin = a.s.begin(b);
     begin = begin < 0 ? 0 : begin;
     const int64_t end = a.end ? a.end[b] : all;
-    int64_t row_end = end - (a.queries - 1 - t);
-    row_end = row_end > all ? all : row_end;
     int64_t stop = end - (a.queries - 1 - a.group(rl));
     int64_t safe = end - (a.queries - 1 - a.group(r0));                 // every row sees up to here
     stop = stop > all ? all : stop;
@@ -273,132 +281,133 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole>)) void at
     if (a.part_o && c0 >= stop && chunk > 0) return;            // nothing there, and the join knows
     // positions from here on count from c0
     const int n = clamp_to(stop - c0, static_cast<int>(a.chunk));
-    const int first = clamp_to(begin - c0, n), last = clamp_to(row_end - c0, n), full = clamp_to(safe - c0, n);
+    const int first = clamp_to(begin - c0, n), full = clamp_to(safe - c0, n);
 
-    i32x4 qp[N][KK];
-    const float unit = load_query<T, KK>(a, static_cast<const T *>(a.q) + q_row * a.qt + q_head * a.qh, there, lane, qp);
-    const float to_log2 = unit * a.scale * kLog2E;
-
-    f32x4 o[JV];
+    bool there[R];
+    int64_t q_row[R];
+    int q_head[R], last[R];
+    i32x4 qp[R][N][KK];
+    float to_log2[R];
 #pragma unroll
-    for (int j = 0; j < JV; j++) o[j] = f32x4{0, 0, 0, 0};
-    float m = -INFINITY, l = 0.0f;
+    for (int y = 0; y < R; y++) {
+        const uint32_t at = r0 + kRows * y + i16;
+        there[y] = at < a.rows;
+        const uint32_t r = there[y] ? at : rl;
+        const uint32_t t = a.group(r);                                  // the lane's query
+        q_row[y] = static_cast<int64_t>(b) * a.queries + t;
+        q_head[y] = static_cast<int>(head * a.group.d + (r - t * a.group.d));
+        int64_t row_end = end - (a.queries - 1 - t);
+        row_end = row_end > all ? all : row_end;
+        last[y] = clamp_to(row_end - c0, n);
+        const float unit = load_query<T, KK>(a, static_cast<const T *>(a.q) + q_row[y] * a.qt + q_head[y] * a.qh, there[y], lane, qp[y]);
+        to_log2[y] = unit * a.scale * kLog2E;
+    }
+
+    f32x4 o[R][JV];
+    float m[R], l[R];
+#pragma unroll
+    for (int y = 0; y < R; y++) {
+        m[y] = -INFINITY;
+        l[y] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < JV; j++) o[y][j] = f32x4{0, 0, 0, 0};
+    }
     float step = 0x1p-126f, inv = 0x1p126f;                     // the running step of values
 
-    const int block = static_cast<int>(c.block_bytes());
-    const uint32_t pitch = static_cast<uint32_t>(c.heads) * 2 * block;
+    const uint32_t width = c.width;
+    const uint32_t block = width << c.shift;
+    const uint32_t pitch = a.heads.d * 2 * block;
     const int8_t *data = c.data + static_cast<int64_t>(head) * 2 * block;
-    const int pmask = c.tokens() - 1;
+    const float2 *steps = reinterpret_cast<const float2 *>(c.scales) + head;
+    const uint32_t pages = static_cast<uint32_t>(c.pages);
+    const uint32_t pmask = c.tokens() - 1;
     const int32_t *table = a.s.table + b * a.s.table_stride + (c0 >> c.shift);
-    const int c0r = static_cast<int>(c0) & pmask;               // c0's row in its page
-    const int vcol = JV * i16 < c.width - JV ? JV * i16 : c.width - JV;
+    const uint32_t c0r = static_cast<uint32_t>(c0) & pmask;     // c0's row in its page
+    // a lane's columns: those of a row that lie beyond its width are read from its end and not used
+    uint32_t kcol[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; kk++) kcol[kk] = 64 * kk + 16 * g < static_cast<int>(width) - 16 ? 64 * kk + 16 * g : width - 16;
+    const uint32_t vcol = JV * i16 < static_cast<int>(width) - JV ? JV * i16 : width - JV;
 
-    for (int t0 = wave * kTile; t0 < n; t0 += NW * kTile) {
-        // ---- where the tokens are ----
-        int bad = 0;                                            // bit of a lane's 8 tokens: padding
-        float ks[2][4], vs[2][4];
-        i32x4 kv[2][KK];
-        Columns<JV> vv[8];
+    // the pages of the step at t0 (whose table entries exist up to token n - 1)
+    auto look_up = [&](int t0, int (&page)[kWhole ? 2 : 1]) {
         if constexpr (kWhole) {
 #pragma unroll
             for (int u = 0; u < 2; u++) {
                 const int p = t0 + 16 * u;
-                int64_t page = -1;
-                if (p < n && p + 16 > first) page = table[(c0r + p) >> c.shift];
-                const bool ok = page >= 0 && page < c.pages;
-                const int64_t at = ok ? page : 0;
-                const int8_t *kb = data + at * pitch;
-                const int row = (c0r + p) & pmask;
-                const float2 sc = *reinterpret_cast<const float2 *>(c.scales + (at * c.heads + head) * 2);
-#pragma unroll
-                for (int kk = 0; kk < KK; kk++) {
-                    const int col = 64 * kk + 16 * g < c.width - 16 ? 64 * kk + 16 * g : c.width - 16;
-                    kv[u][kk] = *reinterpret_cast<const i32x4 *>(kb + (row + i16) * c.width + col);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; i++) vv[4 * u + i].load(kb + block + (row + 4 * g + i) * c.width + vcol);
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    ks[u][i] = sc.x;
-                    vs[u][i] = ok ? sc.y : 0.0f;
-                }
-                if (!ok) bad |= 0xf << (4 * u);
+                const int got = table[(c0r + (p < n ? p : n - 1)) >> c.shift];
+                page[u] = p < n && p + 16 > first && static_cast<uint32_t>(got) < pages ? got : -1;
             }
         } else {
             const int p = t0 + (lane & 31);
-            int page = -1;
-            if (p < n && p >= first) page = table[(c0r + p) >> c.shift];
-            page = page < c.pages ? page : -1;
-            const uint32_t own = page < 0 ? 0 : page;
-            float2 sc = *reinterpret_cast<const float2 *>(c.scales + (static_cast<int64_t>(own) * c.heads + head) * 2);
-            sc.y = page < 0 ? 0.0f : sc.y;
+            const int got = table[(c0r + (p < n ? p : n - 1)) >> c.shift];
+            page[0] = p < n && p >= first && static_cast<uint32_t>(got) < pages ? got : -1;
+        }
+    };
+
+    Step<JV, kWhole> x;
+    int t0 = wave * kTile;
+    if (t0 < n) look_up(t0, x.page);
+    for (; t0 < n; t0 += NW * kTile) {
+        // ---- loads: this step's rows and steps, the next one's pages ----
+        if constexpr (kWhole) {
 #pragma unroll
             for (int u = 0; u < 2; u++) {
-                const int got = __builtin_amdgcn_ds_bpermute(4 * (16 * u + i16), page);
-                const uint32_t at = got < 0 ? 0 : got;
-                const int8_t *kb = data + static_cast<uint64_t>(at) * pitch + ((c0r + t0 + 16 * u + i16) & pmask) * c.width;
+                const uint32_t at = x.page[u] < 0 ? 0 : x.page[u];
+                x.sc[u] = steps[static_cast<uint64_t>(at) * a.heads.d];
+                const int8_t *kb = data + static_cast<uint64_t>(at) * pitch + ((c0r + t0 + 16 * u) & pmask) * width;
 #pragma unroll
-                for (int kk = 0; kk < KK; kk++) {
-                    const int col = 64 * kk + 16 * g < c.width - 16 ? 64 * kk + 16 * g : c.width - 16;
-                    kv[u][kk] = *reinterpret_cast<const i32x4 *>(kb + col);
-                }
+                for (int kk = 0; kk < KK; kk++) x.kv[u][kk] = *reinterpret_cast<const i32x4 *>(kb + (i16 * width + kcol[kk]));
+                const int8_t *vb = kb + block;
+#pragma unroll
+                for (int i = 0; i < 4; i++) x.vv[4 * u + i].load(vb + ((4 * g + i) * width + vcol));
+            }
+        } else {
+            const uint32_t own = x.page[0] < 0 ? 0 : x.page[0];
+            x.sc[0] = steps[static_cast<uint64_t>(own) * a.heads.d];
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                const uint32_t at = __builtin_amdgcn_ds_bpermute(4 * (16 * u + i16), own);
+                const int8_t *kb = data + static_cast<uint64_t>(at) * pitch + ((c0r + t0 + 16 * u + i16) & pmask) * width;
+#pragma unroll
+                for (int kk = 0; kk < KK; kk++) x.kv[u][kk] = *reinterpret_cast<const i32x4 *>(kb + kcol[kk]);
             }
 #pragma unroll
-            for (int x = 0; x < 8; x++) {
-                const int from = 16 * (x >> 2) + 4 * g + (x & 3);
-                const int got = __builtin_amdgcn_ds_bpermute(4 * from, page);
-                const uint32_t at = got < 0 ? 0 : got;
-                vv[x].load(data + static_cast<uint64_t>(at) * pitch + block + ((c0r + t0 + from) & pmask) * c.width + vcol);
-                ks[x >> 2][x & 3] = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * from, __builtin_bit_cast(int, sc.x)));
-                vs[x >> 2][x & 3] = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * from, __builtin_bit_cast(int, sc.y)));
-                bad |= (got < 0 ? 1 : 0) << x;
+            for (int k = 0; k < 8; k++) {
+                const int from = 16 * (k >> 2) + 4 * g + (k & 3);
+                const uint32_t at = __builtin_amdgcn_ds_bpermute(4 * from, own);
+                x.vv[k].load(data + static_cast<uint64_t>(at) * pitch + block + ((c0r + t0 + from) & pmask) * width + vcol);
             }
         }
+        int next_page[kWhole ? 2 : 1];
+        look_up(t0 + NW * kTile, next_page);
+        __builtin_amdgcn_sched_barrier(0);
 
-        // ---- scores, in powers of two ----
-        float s[2][4];
+        // ---- steps of the lane's 8 tokens, which of them nobody sees ----
+        int bad = 0;
+        float ks[8], vs[8];
 #pragma unroll
-        for (int u = 0; u < 2; u++) {
-            i32x4 acc[N];
-#pragma unroll
-            for (int p = 0; p < N; p++) {
-                acc[p] = i32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int kk = 0; kk < KK; kk++)
-                    acc[p] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kv[u][kk], qp[p][kk], acc[p], 0, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                float dot = static_cast<float>(acc[0][i] * 256 + acc[1][i]);
-                if constexpr (N == 3) dot = __builtin_fmaf(dot, 256.0f, static_cast<float>(acc[2][i]));
-                s[u][i] = dot * (ks[u][i] * to_log2);
+        for (int k = 0; k < 8; k++) {
+            if constexpr (kWhole) {
+                const bool ok = x.page[k >> 2] >= 0;
+                ks[k] = x.sc[k >> 2].x;
+                vs[k] = ok ? x.sc[k >> 2].y : 0.0f;
+                if (!ok) bad |= 1 << k;
+            } else {
+                const int from = 4 * (16 * (k >> 2) + 4 * g + (k & 3));
+                const float y = x.page[0] < 0 ? 0.0f : x.sc[0].y;
+                ks[k] = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(from, __builtin_bit_cast(int, x.sc[0].x)));
+                vs[k] = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(from, __builtin_bit_cast(int, y)));
+                bad |= (__builtin_amdgcn_ds_bpermute(from, x.page[0]) < 0 ? 1 : 0) << k;
             }
         }
         const bool inside = t0 >= first && t0 + kTile <= full;
-        const bool masked = !inside || __ballot(bad) != 0;
-        if (masked) {
-#pragma unroll
-            for (int x = 0; x < 8; x++) {
-                const int p = t0 + 16 * (x >> 2) + 4 * g + (x & 3);
-                if (p < first || p >= last) bad |= 1 << x;
-                if ((bad >> x) & 1) s[x >> 2][x & 3] = -INFINITY;
-            }
-        }
-        // ---- the running maximum and step ----
-        float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                          fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-        if (__ballot(top > m + kSlack<T>)) {
-            top = fmaxf(top, __shfl_xor(top, 16, kWave));
-            top = fmaxf(top, __shfl_xor(top, 32, kWave));
-            const float next = fmaxf(m, top);
-            const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - next);
-            l *= f;
-#pragma unroll
-            for (int j = 0; j < JV; j++) o[j] *= f;
-            m = next;
-        }
-        float big = fmaxf(fmaxf(fmaxf(vs[0][0], vs[0][1]), fmaxf(vs[0][2], vs[0][3])),
-                          fmaxf(fmaxf(vs[1][0], vs[1][1]), fmaxf(vs[1][2], vs[1][3])));
+        bool masked = !inside;
+        if constexpr (kWhole) masked = masked || x.page[0] < 0 || x.page[1] < 0;
+        else masked = masked || __ballot(x.page[0] < 0) != 0;
+
+        // ---- the running step of values ----
+        float big = fmaxf(fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3])), fmaxf(fmaxf(vs[4], vs[5]), fmaxf(vs[6], vs[7])));
         if (__ballot(big > 2.0f * step)) {
             if constexpr (!kWhole) {                            // else the same in every lane
                 big = fmaxf(big, __shfl_xor(big, 16, kWave));
@@ -406,126 +415,183 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole>)) void at
             }
             const float f = step / big;
 #pragma unroll
-            for (int j = 0; j < JV; j++) o[j] *= f;
+            for (int y = 0; y < R; y++)
+#pragma unroll
+                for (int j = 0; j < JV; j++) o[y][j] *= f;
             step = big;
             inv = 1.0f / big;
         }
-        // ---- weights ----
-        const float from = m == -INFINITY ? 0.0f : m - kOffset<T>;
-        float w[8];
+
+        i32x4 hi[R], lo[R];
 #pragma unroll
-        for (int x = 0; x < 8; x++) {
-            const float p = __builtin_amdgcn_exp2f(s[x >> 2][x & 3] - from);
-            l += p;
-            w[x] = p * (vs[x >> 2][x & 3] * inv);
-        }
-        if (masked) {
+        for (int y = 0; y < R; y++) {
+            // ---- scores, in powers of two ----
+            float s[8];
 #pragma unroll
-            for (int x = 0; x < 8; x++) w[x] = (bad >> x) & 1 ? 0.0f : w[x];    // a step that is not seen may be NaN
-        }
-        i32x4 hi, lo;
+            for (int u = 0; u < 2; u++) {
+                i32x4 acc[N];
 #pragma unroll
-        for (int x = 0; x < 4; x++) {
-            const int pair = pack_f16(w[2 * x], w[2 * x + 1]);
-            hi[x] = pair;
-            if constexpr (N == 3) {
-                const f16x2 h = __builtin_bit_cast(f16x2, pair);    // of a scalar: hi[x] would be read as hi[0]
-                lo[x] = pack_f16(w[2 * x] - static_cast<float>(h[0]), w[2 * x + 1] - static_cast<float>(h[1]));
+                for (int p = 0; p < N; p++) {
+                    acc[p] = i32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (int kk = 0; kk < KK; kk++)
+                        acc[p] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x.kv[u][kk], qp[y][p][kk], acc[p], 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    float dot = static_cast<float>(acc[0][i] * 256 + acc[1][i]);
+                    if constexpr (N == 3) dot = __builtin_fmaf(dot, 256.0f, static_cast<float>(acc[2][i]));
+                    s[4 * u + i] = dot * (ks[4 * u + i] * to_log2[y]);
+                }
+            }
+            int hide = bad;
+            if (masked) {
+#pragma unroll
+                for (int k = 0; k < 8; k++) {
+                    const int p = t0 + 16 * (k >> 2) + 4 * g + (k & 3);
+                    if (p < first || p >= last[y]) hide |= 1 << k;
+                    if ((hide >> k) & 1) s[k] = -INFINITY;
+                }
+            }
+            // ---- the running maximum ----
+            float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+            if (__ballot(top > m[y] + kSlack<T>)) {
+                top = fmaxf(top, __shfl_xor(top, 16, kWave));
+                top = fmaxf(top, __shfl_xor(top, 32, kWave));
+                const float next = fmaxf(m[y], top);
+                const float f = m[y] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[y] - next);
+                l[y] *= f;
+#pragma unroll
+                for (int j = 0; j < JV; j++) o[y][j] *= f;
+                m[y] = next;
+            }
+            // ---- weights ----
+            const float from = m[y] == -INFINITY ? 0.0f : m[y] - kOffset<T>;
+            float w[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                const float p = __builtin_amdgcn_exp2f(s[k] - from);
+                l[y] += p;
+                w[k] = p * (vs[k] * inv);
+            }
+            if (masked) {
+#pragma unroll
+                for (int k = 0; k < 8; k++) w[k] = (hide >> k) & 1 ? 0.0f : w[k];    // a step that is not seen may be NaN
+            }
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const int pair = pack_f16(w[2 * k], w[2 * k + 1]);
+                hi[y][k] = pair;
+                if constexpr (N == 3) {
+                    const f16x2 h = __builtin_bit_cast(f16x2, pair);    // of a scalar: hi[y][k] would be read as hi[y][0]
+                    lo[y][k] = pack_f16(w[2 * k] - static_cast<float>(h[0]), w[2 * k + 1] - static_cast<float>(h[1]));
+                }
             }
         }
         // ---- output ----
 #pragma unroll
-        for (int x = 0; x < 8; x++)
+        for (int k = 0; k < 8; k++)
 #pragma unroll
-            for (int k = 0; k < Columns<JV>::kWords; k++) vv[x].w[k] ^= 0x80808080;
+            for (int w = 0; w < Columns<JV>::kWords; w++) x.vv[k].w[w] ^= 0x80808080;
 #pragma unroll
         for (int j = 0; j < JV; j++) {
             i32x4 v;
 #pragma unroll
-            for (int x = 0; x < 4; x++) v[x] = column_pair(vv[2 * x].w[j / 4], vv[2 * x + 1].w[j / 4], j % 4);
-            o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, hi), o[j], 0, 0, 0);
-            if constexpr (N == 3)
-                o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, lo), o[j], 0, 0, 0);
+            for (int k = 0; k < 4; k++) v[k] = column_pair(x.vv[2 * k].w[j / 4], x.vv[2 * k + 1].w[j / 4], j % 4);
+#pragma unroll
+            for (int y = 0; y < R; y++) {
+                o[y][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, hi[y]), o[y][j], 0, 0, 0);
+                if constexpr (N == 3)
+                    o[y][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, lo[y]), o[y][j], 0, 0, 0);
+            }
         }
+#pragma unroll
+        for (int u = 0; u < (kWhole ? 2 : 1); u++) x.page[u] = next_page[u];
     }
 
     // ---- join the lanes of a row, then the wavefronts ----
-    l += __shfl_xor(l, 16, kWave);
-    l += __shfl_xor(l, 32, kWave);
-    float back = step * 512.0f;
-    if constexpr (NW > 1) {
-        constexpr int kPad = 16 * JV + 4;
-        __shared__ float so[NW - 1][kRows][kPad];
-        __shared__ float sm[NW][kRows], sl[NW][kRows];
-        if (lane < 16) {
-            sm[wave][i16] = m;
-            sl[wave][i16] = l;
+    constexpr int kPad = 16 * JV + 4;
+    __shared__ float so[NW > 1 ? NW - 1 : 1][kRows][kPad];
+    __shared__ float sm[NW][kRows], sl[NW][kRows];
+#pragma unroll
+    for (int y = 0; y < R; y++) {
+        l[y] += __shfl_xor(l[y], 16, kWave);
+        l[y] += __shfl_xor(l[y], 32, kWave);
+        float back = step * 512.0f;
+        if constexpr (NW > 1) {
+            if (y > 0) __syncthreads();
+            if (lane < 16) {
+                sm[wave][i16] = m[y];
+                sl[wave][i16] = l[y];
+            }
+            if (wave > 0) {
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+#pragma unroll
+                    for (int j = 0; j < JV; j++) so[wave - 1][i16][JV * (4 * g + i) + j] = o[y][j][i] * back;
+            }
+            __syncthreads();
+            if (wave == 0) {
+                float all_m = m[y];
+#pragma unroll
+                for (int w = 1; w < NW; w++) all_m = fmaxf(all_m, sm[w][i16]);
+                const float f0 = m[y] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[y] - all_m);
+                l[y] *= f0;
+#pragma unroll
+                for (int j = 0; j < JV; j++) o[y][j] *= back * f0;
+                back = 1.0f;
+#pragma unroll
+                for (int w = 1; w < NW; w++) {
+                    const float f = sm[w][i16] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][i16] - all_m);
+                    l[y] += sl[w][i16] * f;
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+#pragma unroll
+                        for (int j = 0; j < JV; j++) o[y][j][i] += so[w - 1][i16][JV * (4 * g + i) + j] * f;
+                }
+                m[y] = all_m;
+            }
         }
-        if (wave > 0) {
+        const bool none = l[y] == 0.0f;             // a NaN among what is seen stays one
+        if (wave == 0 && there[y] && a.part_o) {
+            const int64_t at = (static_cast<int64_t>(bh) * a.rows + r0 + kRows * y + i16) * a.chunks + chunk;
 #pragma unroll
-            for (int i = 0; i < 4; i++)
+            for (int i = 0; i < 4; i++) {
+                float v[JV];
 #pragma unroll
-                for (int j = 0; j < JV; j++) so[wave - 1][i16][JV * (4 * g + i) + j] = o[j][i] * back;
+                for (int j = 0; j < JV; j++) v[j] = o[y][j][i] * back;
+                store_columns<float, JV>(a.part_o + at * width, JV * (4 * g + i), width, v);
+            }
+            if (g == 0) {
+                a.part_ml[2 * at] = m[y];
+                a.part_ml[2 * at + 1] = l[y];
+            }
         }
-        __syncthreads();
-        if (wave > 0) return;
-        float all_m = m;
+        if (wave == 0 && there[y] && !a.part_o) {
+            T *out = static_cast<T *>(a.out) + q_row[y] * a.ot + q_head[y] * a.oh;
+            const float norm = none ? 0.0f : back / l[y];
 #pragma unroll
-        for (int x = 1; x < NW; x++) all_m = fmaxf(all_m, sm[x][i16]);
-        const float f0 = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - all_m);
-        l *= f0;
+            for (int i = 0; i < 4; i++) {
+                float v[JV];
 #pragma unroll
-        for (int j = 0; j < JV; j++) o[j] *= back * f0;
-        back = 1.0f;
-#pragma unroll
-        for (int x = 1; x < NW; x++) {
-            const float f = sm[x][i16] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[x][i16] - all_m);
-            l += sl[x][i16] * f;
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-#pragma unroll
-                for (int j = 0; j < JV; j++) o[j][i] += so[x - 1][i16][JV * (4 * g + i) + j] * f;
+                for (int j = 0; j < JV; j++) v[j] = none ? 0.0f : o[y][j][i] * norm;
+                store_columns<T, JV>(out, JV * (4 * g + i), c.dim, v);
+            }
+            if (a.lse && g == 0)
+                a.lse[q_row[y] * (a.heads.d * a.group.d) + q_head[y]] = none ? -INFINITY : (m[y] - kOffset<T> + __builtin_amdgcn_logf(l[y])) / kLog2E;
         }
-        m = all_m;
     }
-    if (!there) return;
-    const bool none = l == 0.0f;             // a NaN among what is seen stays one
-    if (a.part_o) {
-        const int64_t at = (static_cast<int64_t>(bh) * a.rows + r) * a.chunks.d + chunk;
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            float x[JV];
-#pragma unroll
-            for (int j = 0; j < JV; j++) x[j] = o[j][i] * back;
-            store_columns<float, JV>(a.part_o + at * c.dim, JV * (4 * g + i), c.dim, x);
-        }
-        if (g == 0) {
-            a.part_ml[2 * at] = m;
-            a.part_ml[2 * at + 1] = l;
-        }
-        return;
-    }
-    T *out = static_cast<T *>(a.out) + q_row * a.ot + q_head * a.oh;
-    const float norm = none ? 0.0f : back / l;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        float x[JV];
-#pragma unroll
-        for (int j = 0; j < JV; j++) x[j] = none ? 0.0f : o[j][i] * norm;
-        store_columns<T, JV>(out, JV * (4 * g + i), c.dim, x);
-    }
-    if (a.lse && g == 0)
-        a.lse[q_row * (c.heads * a.group.d) + q_head] = none ? -INFINITY : (m - kOffset<T> + __builtin_amdgcn_logf(l)) / kLog2E;
 }
 
-// Joins the chunks of a row with NW wavefronts, which take 8 chunks at a time
-// in turn; a lane takes the columns lane, lane + 64, ...  With NW = 1 a
-// workgroup has a row for each of its wavefronts.
-template <class T, int NW>
+// Joins the chunks of a row with NW wavefronts.  A lane takes four columns of
+// every (NW kWave / kLanes)-th chunk, kLanes the lanes of a row's columns, eight
+// chunks in flight.  With NW = 1 a workgroup has a row for each of its
+// wavefronts.
+template <class T, int NW, int kLanes>
 __global__ __launch_bounds__((NW == 1 ? kBlock : NW * kWave)) void attend_join_kernel(const AttendArgs a) {
-    constexpr int kCols = TGL_MAX_HEAD_DIM / kWave, kStep = 8;
-    __shared__ float so[NW][TGL_MAX_HEAD_DIM];
-    __shared__ float sl[NW];
+    constexpr int kStep = 8, kStride = NW * kWave / kLanes;
+    __shared__ float so[NW][4 * kLanes];
+    __shared__ float sl[NW], sm[NW];
     const CacheView &c = a.c;
     const int lane = lane_id();
     const int at_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -537,7 +603,8 @@ __global__ __launch_bounds__((NW == 1 ? kBlock : NW * kWave)) void attend_join_k
     const int64_t q_row = static_cast<int64_t>(b) * a.queries + t;
     const int q_head = static_cast<int>((bh - b * a.heads.d) * a.group.d + (r - t * a.group.d));
     // the chunks that the row's tile has, as the tile counts them
-    const uint32_t rl = (r | (kRows - 1)) < a.rows ? (r | (kRows - 1)) : a.rows - 1;
+    const uint32_t tile_end = r / a.tile_rows * a.tile_rows + a.tile_rows;
+    const uint32_t rl = tile_end < a.rows ? tile_end - 1 : a.rows - 1;
     const int64_t all = static_cast<int64_t>(a.s.pages_per_seq) << c.shift;
     int64_t begin = a.s.begin(b);
     begin = begin < 0 ? 0 : begin;
@@ -545,56 +612,65 @@ __global__ __launch_bounds__((NW == 1 ? kBlock : NW * kWave)) void attend_join_k
     stop = stop > all ? all : stop;
     const int64_t span = stop - (begin & ~static_cast<int64_t>(kTile - 1));
     const int64_t want = span <= 0 ? 1 : (span + a.chunk - 1) / a.chunk;
-    const int n = static_cast<int>(want < a.chunks.d ? want : a.chunks.d);
-    const int64_t at = (static_cast<int64_t>(bh) * a.rows + r) * a.chunks.d;
+    const int n = static_cast<int>(want < a.chunks ? want : a.chunks);
+    const int64_t at = (static_cast<int64_t>(bh) * a.rows + r) * a.chunks;
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + at;
-    const float *po = a.part_o + at * c.dim;
+    const int col = 4 * (lane % kLanes) < c.width ? 4 * (lane % kLanes) : 0;
+    const float *po = a.part_o + at * c.width + col;
     float m = -INFINITY;
-    for (int i = lane; i < n; i += kWave) m = fmaxf(m, ml[i].x);
+    for (int i = wave * kWave + lane; i < n; i += NW * kWave) m = fmaxf(m, ml[i].x);
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, kWave));
+    if constexpr (NW > 1) {
+        if (lane == 0) sm[wave] = m;
+        __syncthreads();
+#pragma unroll
+        for (int y = 0; y < NW; y++) m = fmaxf(m, sm[y]);
+    }
     float l = 0.0f;
-    float o[kCols] = {};
-    for (int i0 = wave * kStep; i0 < n; i0 += NW * kStep) {
-        float v[kStep][kCols], f[kStep];
+    f32x4 o = {0, 0, 0, 0};
+    for (int i0 = (wave * kWave + lane) / kLanes; i0 < n; i0 += kStep * kStride) {
+        f32x4 v[kStep];
+        float2 w[kStep];
 #pragma unroll
         for (int y = 0; y < kStep; y++) {
-            const int i = i0 + y < n ? i0 + y : n - 1;
-            const float2 w = ml[i];
-            f[y] = w.x == -INFINITY || i0 + y >= n ? 0.0f : __builtin_amdgcn_exp2f(w.x - m);
-            l += i0 + y < n ? w.y * f[y] : 0.0f;
-#pragma unroll
-            for (int k = 0; k < kCols; k++) {
-                const int d = k * kWave + lane < c.dim ? k * kWave + lane : c.dim - 1;
-                v[y][k] = k * kWave < c.dim ? po[static_cast<int64_t>(i) * c.dim + d] : 0.0f;
-            }
+            const int i = i0 + y * kStride < n ? i0 + y * kStride : n - 1;
+            w[y] = ml[i];
+            v[y] = *reinterpret_cast<const f32x4 *>(po + static_cast<int64_t>(i) * c.width);
         }
 #pragma unroll
-        for (int y = 0; y < kStep; y++)
+        for (int y = 0; y < kStep; y++) {
+            if (i0 + y * kStride >= n) continue;
+            const float f = w[y].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(w[y].x - m);
+            l += w[y].y * f;
+            o += v[y] * f;
+        }
+    }
+    // the wavefront's other chunks, then the other wavefronts
 #pragma unroll
-            for (int k = 0; k < kCols; k++) o[k] += i0 + y < n ? v[y][k] * f[y] : 0.0f;
+    for (int d = kLanes; d < kWave; d <<= 1) {
+        l += __shfl_xor(l, d, kWave);
+#pragma unroll
+        for (int k = 0; k < 4; k++) o[k] += __shfl_xor(o[k], d, kWave);
     }
     if constexpr (NW > 1) {
-#pragma unroll
-        for (int k = 0; k < kCols; k++) so[wave][k * kWave + lane] = o[k];
+        if (lane < kLanes) *reinterpret_cast<f32x4 *>(&so[wave][4 * lane]) = o;
         if (lane == 0) sl[wave] = l;
         __syncthreads();
         if (wave > 0) return;
 #pragma unroll
         for (int y = 1; y < NW; y++) {
             l += sl[y];
-#pragma unroll
-            for (int k = 0; k < kCols; k++) o[k] += so[y][k * kWave + lane];
+            o += *reinterpret_cast<const f32x4 *>(&so[y][4 * (lane % kLanes)]);
         }
     }
     const bool none = l == 0.0f;
     T *out = static_cast<T *>(a.out) + q_row * a.ot + q_head * a.oh;
     const float norm = 1.0f / l;
+    float v[4];
 #pragma unroll
-    for (int k = 0; k < kCols; k++) {
-        const int d = k * kWave + lane;
-        if (d < c.dim) out[d] = from_float<T>(none ? 0.0f : o[k] * norm);
-    }
+    for (int k = 0; k < 4; k++) v[k] = none ? 0.0f : o[k] * norm;
+    if (lane < kLanes && 4 * lane < c.width) store_columns<T, 4>(out, 4 * lane, c.dim, v);
     if (a.lse && lane == 0)
         a.lse[q_row * (c.heads * a.group.d) + q_head] = none ? -INFINITY : (m - kOffset<T> + __builtin_amdgcn_logf(l)) / kLog2E;
 }
@@ -750,13 +826,14 @@ __global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(
 // Workgroups that fill the card a few times over; a long axis is cut until
 // there are that many, into chunks of at least kMinChunk tokens, and 64 for
 // each row of a tile (whose partial sums then are at most 1/16 of the bytes).
-constexpr int64_t kFill = 4096;
+constexpr int64_t kFill = 2048;
 constexpr int64_t kMinChunk = 256;
 
 constexpr uint32_t kFewRows = 4;
 constexpr int64_t kFewTokens = 64;
 
 struct Plan {
+    int64_t tile_rows;
     int64_t row_tiles;
     int64_t chunk;
     int64_t chunks;
@@ -767,11 +844,12 @@ struct Plan {
 Plan plan_of(const CacheView &c, int64_t num_seqs, int32_t pages_per_seq, int32_t q_heads, int64_t queries) {
     Plan p{};
     const int64_t rows = queries * (q_heads / c.heads);
-    p.row_tiles = (rows + kRows - 1) / kRows;
+    p.tile_rows = rows > kRows && c.width <= 128 ? 2 * kRows : kRows;
+    p.row_tiles = (rows + p.tile_rows - 1) / p.tile_rows;
     const int64_t most = (static_cast<int64_t>(pages_per_seq) << c.shift) + kTile;      // begin need not be at a step's start
     const int64_t items = num_seqs * c.heads * p.row_tiles;
-    int64_t chunks = items > 0 && items < kFill / 2 ? kFill / items : 1;
-    const int64_t tile_rows = rows < kRows ? rows : kRows;
+    int64_t chunks = items > 0 && items < kFill ? kFill / items : 1;
+    const int64_t tile_rows = rows < p.tile_rows ? rows : p.tile_rows;
     const int64_t cap = most / (64 * tile_rows > kMinChunk ? 64 * tile_rows : kMinChunk);
     chunks = chunks > cap ? cap : chunks;
     const int64_t least = (most >> 30) + 1;             // positions in a chunk are 32-bit
@@ -781,7 +859,7 @@ Plan plan_of(const CacheView &c, int64_t num_seqs, int32_t pages_per_seq, int32_
     p.chunks = (most + p.chunk - 1) / p.chunk;
     if (p.chunks > 1) {
         const size_t n = static_cast<size_t>(num_seqs) * c.heads * rows * p.chunks;
-        p.part_o = align_up(n * c.dim * 4, 256);
+        p.part_o = align_up(n * c.width * 4, 256);
         p.part_ml = align_up(n * 8, 256);
     }
     return p;
@@ -790,8 +868,21 @@ Plan plan_of(const CacheView &c, int64_t num_seqs, int32_t pages_per_seq, int32_
 template <class T, int JV, bool kWhole>
 void launch(const AttendArgs &a, int nw, hipStream_t st) {
     const unsigned grid = (a.work + 7) / 8 * 8;
-    if (nw == 1) attend_kernel<T, JV, kWhole, 1><<<grid, kWave, 0, st>>>(a);
-    else attend_kernel<T, JV, kWhole, 4><<<grid, 4 * kWave, 0, st>>>(a);
+    if constexpr (JV < 16) {
+        if (a.tile_rows > kRows) {
+            attend_kernel<T, JV, kWhole, 4, 2><<<grid, 4 * kWave, 0, st>>>(a);
+            return;
+        }
+    }
+    if (nw == 1) attend_kernel<T, JV, kWhole, 1, 1><<<grid, kWave, 0, st>>>(a);
+    else attend_kernel<T, JV, kWhole, 4, 1><<<grid, 4 * kWave, 0, st>>>(a);
+}
+
+template <class T, int kLanes>
+void launch_join(const AttendArgs &a, hipStream_t st) {
+    // wavefronts of a row: enough that each has a few chunks
+    if (a.chunks <= 16) attend_join_kernel<T, 1, kLanes><<<(a.all_rows + 3) / 4, kBlock, 0, st>>>(a);
+    else attend_join_kernel<T, 16, kLanes><<<a.all_rows, 16 * kWave, 0, st>>>(a);
 }
 
 template <class T>
@@ -801,11 +892,10 @@ void launch(const AttendArgs &a, int nw, hipStream_t st) {
     else if (a.c.width <= 64) whole ? launch<T, 4, true>(a, nw, st) : launch<T, 4, false>(a, nw, st);
     else if (a.c.width <= 128) whole ? launch<T, 8, true>(a, nw, st) : launch<T, 8, false>(a, nw, st);
     else whole ? launch<T, 16, true>(a, nw, st) : launch<T, 16, false>(a, nw, st);
-    if (a.part_o) {
-        // wavefronts of a row: enough that each has a few chunks
-        if (a.chunks.d <= 16) attend_join_kernel<T, 1><<<(a.all_rows + 3) / 4, kBlock, 0, st>>>(a);
-        else attend_join_kernel<T, 16><<<a.all_rows, 16 * kWave, 0, st>>>(a);
-    }
+    if (!a.part_o) return;
+    if (a.c.width <= 64) launch_join<T, 16>(a, st);
+    else if (a.c.width <= 128) launch_join<T, 32>(a, st);
+    else launch_join<T, 64>(a, st);
 }
 
 // Whether the kernel for few tokens is the faster one.
@@ -892,8 +982,10 @@ tgl_status tgl_cache_attend(const tgl_cache *cache, const tgl_heads *q, int32_t 
     a.all_rows = a.rows * a.s.seqs * a.c.heads;
     a.chunk = p.chunk;
     a.work = static_cast<uint32_t>(work);
+    a.tile_rows = static_cast<uint32_t>(p.tile_rows);
     a.tiles = Div(static_cast<uint32_t>(p.row_tiles));
-    a.chunks = Div(static_cast<uint32_t>(p.chunks));
+    a.chunks = static_cast<uint32_t>(p.chunks);
+    a.items = Div(static_cast<uint32_t>(seqs->num_seqs * a.c.heads));
     a.heads = Div(a.c.heads);
     a.spread = p.row_tiles > 1;
     if (p.part_o) {
