@@ -37,22 +37,6 @@ constexpr int kRows = 16;           // rows of a tile
 constexpr int kTile = 32;           // tokens of a wavefront's step
 constexpr float kLog2E = 1.44269504088896340736f;
 
-// Division of whole numbers below 2^31 by a fixed one: with 2^l >= d and
-// mul = ceil(2^(31+l) / d) the quotient is n mul >> (31 + l), exactly.
-struct Div {
-    uint32_t mul = 0, shift = 0, d = 1;
-    Div() = default;
-    explicit Div(uint32_t by) : d(by) {
-        int l = 0;
-        while ((uint64_t(1) << l) < by) l++;
-        shift = 31 + l;
-        mul = static_cast<uint32_t>(((uint64_t(1) << shift) + by - 1) / by);
-    }
-    __device__ __forceinline__ uint32_t operator()(uint32_t n) const {
-        return static_cast<uint32_t>((static_cast<uint64_t>(n) * mul) >> shift);
-    }
-};
-
 struct AttendArgs {
     CacheView c;
     SeqsView s;
@@ -104,29 +88,6 @@ template <>
 constexpr float kSlack<float> = 1.0f;
 template <class T>
 constexpr float kOffset = 14.0f - kSlack<T>;
-
-// n consecutive elements that need not lie at a multiple of their size: one
-// wide access wherever they start.
-template <class T, int N>
-struct __attribute__((packed, aligned(alignof(T)))) Run {
-    T t[N];
-};
-
-// N elements of a row from column d on, zeros from column dim on.
-template <class T, int N>
-__device__ __forceinline__ void load_columns(const T *q, int d, int dim, float (&x)[N]) {
-    if (d + N <= dim) {
-        const Run<T, N> w = *reinterpret_cast<const Run<T, N> *>(q + d);
-#pragma unroll
-        for (int i = 0; i < N; i++) x[i] = as_float(w.t[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; i++) {
-            const float v = as_float(q[d + i < dim ? d + i : dim - 1]);
-            x[i] = d + i < dim ? v : 0.0f;
-        }
-    }
-}
 
 // The row's query as signed bytes, kk-th piece of 64 columns, part p (the
 // highest first); returns the size of one unit.  v + 0x808080 has, byte by
@@ -207,21 +168,6 @@ __device__ __forceinline__ int column_pair(int a, int b, int jj) {
 
 __device__ __forceinline__ int pack_f16(float a, float b) {
     return __builtin_bit_cast(int, f16x2{static_cast<_Float16>(a), static_cast<_Float16>(b)});
-}
-
-// N consecutive elements from column d on, as far as there are columns.
-template <class T, int N>
-__device__ __forceinline__ void store_columns(T *out, int d, int dim, const float (&x)[N]) {
-    if (d + N <= dim) {
-        Run<T, N> w;
-#pragma unroll
-        for (int i = 0; i < N; i++) w.t[i] = from_float<T>(x[i]);
-        *reinterpret_cast<Run<T, N> *>(out + d) = w;
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; i++)
-            if (d + i < dim) out[d + i] = from_float<T>(x[i]);
-    }
 }
 
 __device__ __forceinline__ int clamp_to(int64_t v, int most) {

@@ -3,20 +3,29 @@
 // A page's head holds its keys (and its values) with one step, the largest
 // magnitude among them over 127.  A page that is written in parts keeps one
 // step: when new rows need a larger one, the rows that are there are rounded
-// again.  One wavefront owns a page and head, so nothing is shared and no
-// order matters.
+// again.  One group of lanes owns the keys, or the values, of a page and head,
+// so nothing is shared and no order matters.  Both directions only move bytes:
+// new rows are read once, into registers, and written as soon as their
+// largest magnitude is known.
 #include "tgl_cache.hpp"
 
 namespace tgl {
 namespace {
+
+constexpr int kRun = 8;             // elements of a lane's access
 
 struct IoArgs {
     CacheView c;
     SeqsView s;
     void *k;
     void *v;
-    int64_t kt, kh, vt, vh;     // token and head strides
-    int64_t items;              // write: page slots to look at
+    int64_t kt, kh, vt, vh;         // token and head strides
+    int64_t units;                  // write: page slots to look at, times heads, times 2
+    Div heads2;                     // 2 heads
+    Div runs;                       // write: whole runs of a row (1 for none); read: runs of a row's elements
+    int32_t whole;                  // write: whole runs of a row
+    Div row_runs;                   // read: runs of a token, all heads
+    int32_t block_tokens;           // read: tokens of a workgroup
 };
 
 // Sequence b may touch the page slots (items) from base(b) on: cnt >= 1 tokens
@@ -27,82 +36,216 @@ __device__ __forceinline__ int64_t item_base(const SeqsView &s, int64_t b, int s
     return (s.first_token(b) + b * (2 * P - 2)) >> shift;
 }
 
-// A wavefront per page slot and head, values in two passes over the new rows.
-template <class T>
-__global__ __launch_bounds__(kBlock) void write_kernel(const IoArgs a) {
-    const int lane = lane_id();
+// The last sequence whose items start at or before this one; the G lanes of a
+// group look at G places at a time.
+template <int G>
+__device__ __forceinline__ int64_t find_sequence(const SeqsView &s, int64_t item, int shift, int i) {
+    int64_t lo = 0, hi = s.seqs;
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + G - 1) / G;
+        const int64_t at = lo + i * step;
+        const bool before = at < hi && item_base(s, at, shift) <= item;
+        const uint64_t found = group_ballot<G>(before);
+        const int n = __popcll(found);
+        lo += (n > 0 ? n - 1 : 0) * step;
+        hi = lo + step < hi ? lo + step : hi;
+    }
+    return lo;
+}
+
+// L lanes own a unit: the keys, or the values, of a page slot and head.  Up to
+// kHold runs of 8 elements a lane stay in registers between the two looks at
+// them; what does not fit (pages that fill up beyond the call's average) is
+// read again.
+template <class T, int L>
+__global__ __launch_bounds__((L > kBlock ? L : kBlock)) void write_kernel(const IoArgs a) {
+    constexpr int kHold = sizeof(T) == 2 ? 8 : 4;
+    constexpr int kGroup = L > kWave ? kWave : L;
+    constexpr int kUnits = L > kBlock ? 1 : kBlock / L;                 // of a workgroup
+    __shared__ float tops[L / kWave + 1];
     const CacheView &c = a.c;
     const int P = c.tokens(), D = c.dim, W = c.width;
-    const int64_t waves = static_cast<int64_t>(gridDim.x) * (kBlock / kWave);
-    for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kBlock / kWave) + threadIdx.x / kWave; u < a.items * c.heads; u += waves) {
-        const int64_t item = u / c.heads;
-        const int head = static_cast<int>(u % c.heads);
-        int64_t lo = 0, hi = a.s.seqs;          // the last sequence whose items start at or before this one
-        while (hi - lo > 1) {
-            const int64_t mid = (lo + hi) / 2;
-            if (item_base(a.s, mid, c.shift) <= item) lo = mid;
-            else hi = mid;
-        }
-        const int64_t t0 = a.s.first_token(lo), t1 = a.s.first_token(lo + 1);
-        const int64_t start = a.s.begin(lo);
-        if (start < 0 || t1 <= t0) continue;
-        const int64_t slot = (start >> c.shift) + (item - item_base(a.s, lo, c.shift));
+    const int i = threadIdx.x % L;
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * kUnits;
+    for (int64_t u = static_cast<int64_t>(blockIdx.x) * kUnits + threadIdx.x / L; u - threadIdx.x / L < a.units; u += stride) {
+        // every lane stays for the exchanges below: without work, it has no rows
+        const int64_t unit = u < a.units ? u : a.units - 1;
+        const int64_t item = unit / a.heads2.d;
+        const int rest = static_cast<int>(unit - item * a.heads2.d);
+        const int head = rest >> 1, kind = rest & 1;
+        const int64_t b = find_sequence<kGroup>(a.s, item, c.shift, threadIdx.x % kGroup);
+        const int64_t t0 = a.s.first_token(b), t1 = a.s.first_token(b + 1);
+        const int64_t start = a.s.begin(b);
+        const int64_t slot = (start >> c.shift) + (item - item_base(a.s, b, c.shift));
         const int64_t p0 = slot << c.shift;                             // first position of the page
         const int64_t end = start + (t1 - t0);
-        if (p0 >= end) continue;
-        const int64_t page = a.s.page(lo, slot, c.pages);
-        if (page < 0) continue;
-        const int first = p0 < start ? static_cast<int>(start - p0) : 0;       // rows below are kept
-        const int last = end - p0 < P ? static_cast<int>(end - p0) : P;
+        int64_t page = -1;
+        if (u < a.units && start >= 0 && t1 > t0 && p0 < end) page = a.s.page(b, slot, c.pages);
+        const int first = page >= 0 && p0 < start ? static_cast<int>(start - p0) : 0;      // rows below are kept
+        const int rows = page < 0 ? 0 : static_cast<int>((end - p0 < P ? end - p0 : P) - first);
         const int64_t token = t0 + (p0 + first - start);
-        for (int kind = 0; kind < 2; kind++) {
-            const T *x = (kind ? static_cast<const T *>(a.v) + head * a.vh : static_cast<const T *>(a.k) + head * a.kh);
-            const int64_t stride = kind ? a.vt : a.kt;
-            int8_t *rows = c.rows(page, head, kind);
-            float top = 0.0f;
-            for (int r = first; r < last; r++)
-                for (int d = lane; d < D; d += kWave) top = max_nan(top, fabsf(as_float(x[(token + r - first) * stride + d])));
-            top = group_max_nan<kWave>(top);
-            float s = step_of(top);
-            const float old = *c.scale(page, head, kind);
-            if (first > 0) s = max_nan(s, old);
-            const float inv = inverse_step(s);
-            for (int r = first; r < last; r++)
-                for (int d = lane; d < W; d += kWave)
-                    rows[r * W + d] = static_cast<int8_t>(d < D ? to_byte(as_float(x[(token + r - first) * stride + d]), inv) : 0);
-            if (first > 0 && s != old) {
-                const float f = old * inv;
-                for (int d = lane; d < first * W; d += kWave) rows[d] = static_cast<int8_t>(to_byte(static_cast<float>(rows[d]), f));
-            }
-            if (lane == 0) *c.scale(page, head, kind) = s;
+        const T *x = kind ? static_cast<const T *>(a.v) + head * a.vh + token * a.vt
+                          : static_cast<const T *>(a.k) + head * a.kh + token * a.kt;
+        const int64_t pitch = kind ? a.vt : a.kt;
+        int8_t *out = page < 0 ? nullptr : c.rows(page, head, kind);
+        float *step = page < 0 ? nullptr : c.scale(page, head, kind);
+        const float old = first > 0 ? *step : 0.0f;
+        const int runs = rows * a.runs.d;           // whole runs; what is left of a row comes by itself
+        const int tail = a.whole * kRun;
+
+        Run<T, kRun> held[kHold];
+        uint32_t bits = 0;              // of the largest magnitude: NaN above infinity above numbers
+        auto look = [&](float v) {
+            const uint32_t w = __builtin_bit_cast(uint32_t, v) & 0x7fffffffu;
+            bits = w > bits ? w : bits;
+        };
+        auto run_at = [&](int n) {
+            const int r = a.runs(n);
+            return reinterpret_cast<const Run<T, kRun> *>(x + r * pitch + (n - r * a.runs.d) * kRun);
+        };
+        if (a.whole > 0) {
+#pragma unroll
+            for (int h = 0; h < kHold; h++)
+                if (i + h * L < runs) held[h] = *run_at(i + h * L);
         }
+        for (int r = i; r < rows; r += L)
+            for (int d = tail; d < D; d++) look(as_float(x[r * pitch + d]));
+        if (a.whole > 0) {
+#pragma unroll
+            for (int h = 0; h < kHold; h++)
+                if (i + h * L < runs)
+                    for (int k = 0; k < kRun; k++) look(as_float(held[h].t[k]));
+            for (int n = i + kHold * L; n < runs; n += L) {
+                const Run<T, kRun> w = *run_at(n);
+#pragma unroll
+                for (int k = 0; k < kRun; k++) look(as_float(w.t[k]));
+            }
+        }
+#pragma unroll
+        for (int d = kGroup / 2; d >= 1; d >>= 1) {
+            const uint32_t v = __shfl_xor(bits, d, kWave);
+            bits = v > bits ? v : bits;
+        }
+        if constexpr (L > kWave) {
+            __syncthreads();            // the last unit's readers are done
+            if (lane_id() == 0) tops[threadIdx.x / kWave] = __builtin_bit_cast(float, bits);
+            __syncthreads();
+            for (int w = 0; w < L / kWave; w++) {
+                const uint32_t v = __builtin_bit_cast(uint32_t, tops[threadIdx.x / L * (L / kWave) + w]);
+                bits = v > bits ? v : bits;
+            }
+        }
+        float s = step_of(__builtin_bit_cast(float, bits));
+        if (first > 0) s = max_nan(s, old);
+        const float inv = inverse_step(s);
+        auto put = [&](int8_t *at, const Run<T, kRun> &w) {
+            i32x2 v = {0, 0};
+            if (inv != 0.0f)
+                v = i32x2{to_bytes4(as_float(w.t[0]), as_float(w.t[1]), as_float(w.t[2]), as_float(w.t[3]), inv),
+                          to_bytes4(as_float(w.t[4]), as_float(w.t[5]), as_float(w.t[6]), as_float(w.t[7]), inv)};
+            *reinterpret_cast<i32x2 *>(at) = v;
+        };
+        auto place = [&](int n) {
+            const int r = a.runs(n);
+            return out + (first + r) * W + (n - r * a.runs.d) * kRun;
+        };
+        if (a.whole > 0) {
+#pragma unroll
+            for (int h = 0; h < kHold; h++)
+                if (i + h * L < runs) put(place(i + h * L), held[h]);
+            for (int n = i + kHold * L; n < runs; n += L) put(place(n), *run_at(n));
+        }
+        for (int r = i; r < rows; r += L) {
+            for (int d = tail; d < W; d += kRun) {
+                Run<T, kRun> w;
+#pragma unroll
+                for (int k = 0; k < kRun; k++) w.t[k] = d + k < D ? x[r * pitch + d + k] : from_float<T>(0.0f);
+                put(out + (first + r) * W + d, w);
+            }
+        }
+        if (rows > 0 && first > 0 && s != old) {
+            const float f = old * inv;
+            for (int n = i; n < first * (W / kRun); n += L) {
+                i32x2 *at = reinterpret_cast<i32x2 *>(out + n * kRun);
+                i32x2 v = *at;
+#pragma unroll
+                for (int k = 0; k < 2; k++) {
+                    const int word = v[k];
+                    v[k] = !(fabsf(f) > 0.0f) ? 0
+                                              : to_bytes4(static_cast<float>(static_cast<int8_t>(word)), static_cast<float>(static_cast<int8_t>(word >> 8)),
+                                                          static_cast<float>(static_cast<int8_t>(word >> 16)), static_cast<float>(word >> 24), f);
+                }
+                *at = v;
+            }
+        }
+        if (rows > 0 && i == 0) *step = s;
     }
 }
 
-// A wavefront per token and head.
+// A workgroup takes block_tokens tokens in turn: a thread each looks one up,
+// then all stream its heads, eight elements of keys and of values a lane.
 template <class T>
 __global__ __launch_bounds__(kBlock) void read_kernel(const IoArgs a) {
-    const int lane = lane_id();
+    __shared__ int at_page[kBlock];
+    __shared__ int at_row[kBlock];
     const CacheView &c = a.c;
-    const int64_t waves = static_cast<int64_t>(gridDim.x) * (kBlock / kWave);
-    for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kBlock / kWave) + threadIdx.x / kWave; u < a.s.tokens * c.heads; u += waves) {
-        const int64_t token = u / c.heads;
-        const int head = static_cast<int>(u % c.heads);
-        int64_t lo = 0, hi = a.s.seqs;
-        while (hi - lo > 1) {
-            const int64_t mid = (lo + hi) / 2;
-            if (a.s.first_token(mid) <= token) lo = mid;
-            else hi = mid;
+    const int B = a.block_tokens;
+    const int64_t blocks = (a.s.tokens + B - 1) / B;
+    for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+        const int64_t base = block * B;
+        const int count = a.s.tokens - base < B ? static_cast<int>(a.s.tokens - base) : B;
+        __syncthreads();
+        if (static_cast<int>(threadIdx.x) < count) {
+            const int64_t token = base + threadIdx.x;
+            int64_t b = 0;
+            if (a.s.offsets) {
+                int64_t lo = 0, hi = a.s.seqs;
+                while (hi - lo > 1) {
+                    const int64_t mid = (lo + hi) / 2;
+                    if (a.s.first_token(mid) <= token) lo = mid;
+                    else hi = mid;
+                }
+                b = lo;
+            } else {
+                b = token / a.s.per;
+            }
+            int page = -2;                                              // no sequence's
+            int row = 0;
+            if (token >= a.s.first_token(b) && token < a.s.first_token(b + 1)) {
+                const int64_t pos = a.s.begin(b) + token - a.s.first_token(b);
+                page = pos < 0 ? -1 : static_cast<int>(a.s.page(b, pos >> c.shift, c.pages));
+                row = static_cast<int>(pos) & (c.tokens() - 1);
+            }
+            at_page[threadIdx.x] = page;
+            at_row[threadIdx.x] = row;
         }
-        if (token < a.s.first_token(lo) || token >= a.s.first_token(lo + 1)) continue;
-        const int64_t pos = a.s.begin(lo) + token - a.s.first_token(lo);
-        const int64_t page = pos < 0 ? -1 : a.s.page(lo, pos >> c.shift, c.pages);
-        const int row = static_cast<int>(pos & (c.tokens() - 1));
-        for (int kind = 0; kind < 2; kind++) {
-            T *x = (kind ? static_cast<T *>(a.v) + head * a.vh + token * a.vt : static_cast<T *>(a.k) + head * a.kh + token * a.kt);
-            const int8_t *q = page < 0 ? nullptr : c.rows(page, head, kind) + row * c.width;
-            const float s = page < 0 ? 0.0f : *c.scale(page, head, kind);
-            for (int d = lane; d < c.dim; d += kWave) x[d] = from_float<T>(q ? static_cast<float>(q[d]) * s : 0.0f);
+        __syncthreads();
+        const int total = count * a.row_runs.d;
+#pragma unroll 4
+        for (int n = threadIdx.x; n < total; n += kBlock) {
+            const int t = a.row_runs(n);
+            const int rest = n - t * a.row_runs.d;
+            const int head = a.runs(rest);
+            const int d = (rest - head * a.runs.d) * kRun;
+            const int page = at_page[t];
+            if (page == -2) continue;
+            const int own = page < 0 ? 0 : page;
+            i32x2 kq = {0, 0}, vq = {0, 0};
+            float2 s = {0.0f, 0.0f};
+            if (c.pages > 0) {
+                const int8_t *q = c.rows(own, head, 0) + at_row[t] * c.width + d;
+                kq = *reinterpret_cast<const i32x2 *>(q);
+                vq = *reinterpret_cast<const i32x2 *>(q + c.block_bytes());
+                s = *reinterpret_cast<const float2 *>(c.scale(own, head, 0));
+            }
+            float k[kRun], v[kRun];
+#pragma unroll
+            for (int e = 0; e < kRun; e++) {
+                k[e] = page < 0 ? 0.0f : static_cast<float>(static_cast<int8_t>(kq[e / 4] >> (8 * (e % 4)))) * s.x;
+                v[e] = page < 0 ? 0.0f : static_cast<float>(static_cast<int8_t>(vq[e / 4] >> (8 * (e % 4)))) * s.y;
+            }
+            store_columns<T, kRun>(static_cast<T *>(a.k) + (base + t) * a.kt + head * a.kh, d, c.dim, k);
+            store_columns<T, kRun>(static_cast<T *>(a.v) + (base + t) * a.vt + head * a.vh, d, c.dim, v);
         }
     }
 }
@@ -112,14 +255,30 @@ bool make_args(const tgl_cache *cache, const tgl_heads *k, const tgl_heads *v, i
     if (!valid_cache(cache) || !is_elem_type(dtype) || num_tokens < 0 || !valid_seqs(seqs)) return false;
     if (!valid_heads(k, num_tokens, dtype) || !valid_heads(v, num_tokens, dtype)) return false;
     if (!seqs->offsets && (seqs->num_seqs ? num_tokens % seqs->num_seqs : num_tokens) != 0) return false;
-    *a = IoArgs{view_of(*cache), view_of(*seqs, num_tokens), k->ptr, v->ptr, k->token_stride, k->head_stride,
-                v->token_stride, v->head_stride, 0};
+    *a = IoArgs{};
+    a->c = view_of(*cache);
+    a->s = view_of(*seqs, num_tokens);
+    a->k = k->ptr;
+    a->v = v->ptr;
+    a->kt = k->token_stride;
+    a->kh = k->head_stride;
+    a->vt = v->token_stride;
+    a->vh = v->head_stride;
+    a->heads2 = Div(2 * cache->heads);
     return true;
 }
 
-unsigned grid_of(int64_t waves) {
-    const int64_t blocks = (waves + kBlock / kWave - 1) / (kBlock / kWave);
-    return static_cast<unsigned>(blocks < (1 << 22) ? blocks : 1 << 22);
+unsigned grid_of(int64_t blocks) { return static_cast<unsigned>(blocks < (1 << 22) ? blocks : 1 << 22); }
+
+template <class T>
+void launch_write(const IoArgs &a, int64_t rows, hipStream_t st) {
+    // lanes of a unit by the runs of the rows that it gets on average: a whole
+    // wavefront once a quarter of it has two
+    const int64_t runs = rows * a.runs.d;
+    if (runs <= 32) write_kernel<T, 16><<<grid_of((a.units + 15) / 16), kBlock, 0, st>>>(a);
+    else if (runs <= 512) write_kernel<T, 64><<<grid_of((a.units + 3) / 4), kBlock, 0, st>>>(a);
+    else if (runs <= 2048) write_kernel<T, 256><<<grid_of(a.units), kBlock, 0, st>>>(a);
+    else write_kernel<T, 512><<<grid_of(a.units), 512, 0, st>>>(a);
 }
 
 }  // namespace
@@ -136,10 +295,14 @@ tgl_status tgl_cache_write(const tgl_cache *cache, const tgl_heads *k, const tgl
     if (num_tokens == 0 || seqs->num_seqs == 0 || cache->num_pages == 0) return TGL_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();
-    a.items = ((num_tokens + seqs->num_seqs * (2 * int64_t(a.c.tokens()) - 2)) >> a.c.shift) + 1;
-    const unsigned grid = grid_of(a.items * a.c.heads);
-    if (dtype == TGL_OUT_F32) write_kernel<float><<<grid, kBlock, 0, st>>>(a);
-    else write_kernel<bf16_t><<<grid, kBlock, 0, st>>>(a);
+    const int64_t P = a.c.tokens();
+    a.units = (((num_tokens + seqs->num_seqs * (2 * P - 2)) >> a.c.shift) + 1) * 2 * a.c.heads;
+    a.whole = a.c.dim / kRun;
+    a.runs = Div(a.whole > 0 ? a.whole : 1);
+    const int64_t each = (num_tokens + seqs->num_seqs - 1) / seqs->num_seqs;
+    const int64_t rows = each < P ? each : P;
+    if (dtype == TGL_OUT_F32) launch_write<float>(a, rows, st);
+    else launch_write<bf16_t>(a, rows, st);
     return launch_status();
 }
 
@@ -150,7 +313,14 @@ tgl_status tgl_cache_read(const tgl_cache *cache, const tgl_heads *k, const tgl_
     if (num_tokens == 0 || seqs->num_seqs == 0) return TGL_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();
-    const unsigned grid = grid_of(num_tokens * a.c.heads);
+    a.runs = Div((a.c.dim + kRun - 1) / kRun);
+    a.row_runs = Div(a.runs.d * a.c.heads);
+    // tokens of a workgroup: about 16 runs a thread, fewer where that would leave compute units idle
+    int64_t tokens = 16 * kBlock / a.row_runs.d;
+    const int64_t most = num_tokens / 2048;
+    tokens = tokens > most ? most : tokens;
+    a.block_tokens = static_cast<int32_t>(tokens < 1 ? 1 : tokens > kBlock ? kBlock : tokens);
+    const unsigned grid = grid_of((num_tokens + a.block_tokens - 1) / a.block_tokens);
     if (out_type == TGL_OUT_F32) read_kernel<float><<<grid, kBlock, 0, st>>>(a);
     else read_kernel<bf16_t><<<grid, kBlock, 0, st>>>(a);
     return launch_status();

@@ -61,6 +61,73 @@ __device__ __forceinline__ float group_sum(float v) {
     return v;
 }
 
+// ---- wide accesses ----
+
+// N consecutive elements that need not lie at a multiple of their size: one
+// wide access wherever they start.
+template <class T, int N>
+struct __attribute__((packed, aligned(alignof(T)))) Run {
+    T t[N];
+};
+
+// N elements of a row from column d on, zeros from column dim on.
+template <class T, int N>
+__device__ __forceinline__ void load_columns(const T *q, int d, int dim, float (&x)[N]) {
+    if (d + N <= dim) {
+        const Run<T, N> w = *reinterpret_cast<const Run<T, N> *>(q + d);
+#pragma unroll
+        for (int i = 0; i < N; i++) x[i] = as_float(w.t[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const float v = as_float(q[d + i < dim ? d + i : dim - 1]);
+            x[i] = d + i < dim ? v : 0.0f;
+        }
+    }
+}
+
+// N consecutive elements from column d on, as far as there are columns.
+template <class T, int N>
+__device__ __forceinline__ void store_columns(T *out, int d, int dim, const float (&x)[N]) {
+    if (d + N <= dim) {
+        Run<T, N> w;
+#pragma unroll
+        for (int i = 0; i < N; i++) w.t[i] = from_float<T>(x[i]);
+        *reinterpret_cast<Run<T, N> *>(out + d) = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i++)
+            if (d + i < dim) out[d + i] = from_float<T>(x[i]);
+    }
+}
+
+// Four numbers in units of a step, as the bytes of a word.  Adding 1.5 * 2^23
+// rounds a number to whole ones (ties to even, as rint does) and leaves it in
+// the low bits.  inv must not be 0: the caller writes zeros there.
+__device__ __forceinline__ int to_bytes4(float a, float b, float c, float d, float inv) {
+    constexpr float kRound = 12582912.0f;
+    const int ia = __builtin_bit_cast(int, a * inv + kRound), ib = __builtin_bit_cast(int, b * inv + kRound);
+    const int ic = __builtin_bit_cast(int, c * inv + kRound), id = __builtin_bit_cast(int, d * inv + kRound);
+    const int ab = __builtin_amdgcn_perm(ib, ia, 0x0c0c0400u), cd = __builtin_amdgcn_perm(id, ic, 0x0c0c0400u);
+    return ab | (cd << 16);
+}
+
+// Division of whole numbers below 2^31 by a fixed one: with 2^l >= d and
+// mul = ceil(2^(31+l) / d) the quotient is n mul >> (31 + l), exactly.
+struct Div {
+    uint32_t mul = 0, shift = 0, d = 1;
+    Div() = default;
+    explicit Div(uint32_t by) : d(by) {
+        int l = 0;
+        while ((uint64_t(1) << l) < by) l++;
+        shift = 31 + l;
+        mul = static_cast<uint32_t>(((uint64_t(1) << shift) + by - 1) / by);
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const {
+        return static_cast<uint32_t>((static_cast<uint64_t>(n) * mul) >> shift);
+    }
+};
+
 // ---- host side ----
 
 inline bool is_elem_type(int32_t t) { return t == TGL_OUT_F32 || t == TGL_OUT_BF16; }
