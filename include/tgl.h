@@ -709,7 +709,8 @@ typedef struct tgl_heads {
  * Tokens whose place is padding are dropped; sequences without tokens change
  * nothing.  start[b] must not be negative.  A page must belong to one sequence
  * of the call only (two that share one race).
- *   k, v        [device] num_tokens x heads x dim elements of type dtype
+ *   k, v        [device] num_tokens x heads x dim elements of type dtype, their
+ *               token strides within 32 bits
  * Without offsets, num_tokens must be a multiple of num_seqs.  Tokens at or
  * beyond num_tokens are not read whatever offsets says.
  * Never synchronises.  Errors: TGL_EINVAL, TGL_EDEVICE.

@@ -13,6 +13,7 @@ namespace tgl {
 namespace {
 
 constexpr int kRun = 8;             // elements of a lane's access
+constexpr int64_t kFill = 16384;    // wavefronts that fill the card four times over
 
 struct IoArgs {
     CacheView c;
@@ -20,8 +21,8 @@ struct IoArgs {
     void *k;
     void *v;
     int64_t kt, kh, vt, vh;         // token and head strides
-    int64_t units;                  // write: page slots to look at, times heads, times 2
-    Div heads2;                     // 2 heads
+    int64_t units;                  // write: page slots to look at, times parts
+    int32_t parts, pairs;           // write: 2 heads = parts * pairs
     Div runs;                       // write: whole runs of a row (1 for none); read: runs of a row's elements
     int32_t whole;                  // write: whole runs of a row
     Div row_runs;                   // read: runs of a token, all heads
@@ -53,13 +54,14 @@ __device__ __forceinline__ int64_t find_sequence(const SeqsView &s, int64_t item
     return lo;
 }
 
-// L lanes own a unit: the keys, or the values, of a page slot and head.  Up to
+// L lanes own a unit: a.pairs of the 2 heads keys and values of a page slot, one
+// after another, so that a place is looked up once for all of them.  Up to
 // kHold runs of 8 elements a lane stay in registers between the two looks at
 // them; what does not fit (pages that fill up beyond the call's average) is
 // read again.
 template <class T, int L>
-__global__ __launch_bounds__((L > kBlock ? L : kBlock)) void write_kernel(const IoArgs a) {
-    constexpr int kHold = sizeof(T) == 2 ? 8 : 4;
+__global__ __launch_bounds__((L > kBlock ? L : kBlock), 4) void write_kernel(const IoArgs a) {
+    constexpr int kHold = sizeof(T) == 2 ? 4 : 2;       // 16 registers
     constexpr int kGroup = L > kWave ? kWave : L;
     constexpr int kUnits = L > kBlock ? 1 : kBlock / L;                 // of a workgroup
     __shared__ float tops[L / kWave + 1];
@@ -70,9 +72,8 @@ __global__ __launch_bounds__((L > kBlock ? L : kBlock)) void write_kernel(const 
     for (int64_t u = static_cast<int64_t>(blockIdx.x) * kUnits + threadIdx.x / L; u - threadIdx.x / L < a.units; u += stride) {
         // every lane stays for the exchanges below: without work, it has no rows
         const int64_t unit = u < a.units ? u : a.units - 1;
-        const int64_t item = unit / a.heads2.d;
-        const int rest = static_cast<int>(unit - item * a.heads2.d);
-        const int head = rest >> 1, kind = rest & 1;
+        const int64_t item = unit / a.parts;
+        const int pair0 = static_cast<int>(unit - item * a.parts) * a.pairs;
         const int64_t b = find_sequence<kGroup>(a.s, item, c.shift, threadIdx.x % kGroup);
         const int64_t t0 = a.s.first_token(b), t1 = a.s.first_token(b + 1);
         const int64_t start = a.s.begin(b);
@@ -84,102 +85,128 @@ __global__ __launch_bounds__((L > kBlock ? L : kBlock)) void write_kernel(const 
         const int first = page >= 0 && p0 < start ? static_cast<int>(start - p0) : 0;      // rows below are kept
         const int rows = page < 0 ? 0 : static_cast<int>((end - p0 < P ? end - p0 : P) - first);
         const int64_t token = t0 + (p0 + first - start);
-        const T *x = kind ? static_cast<const T *>(a.v) + head * a.vh + token * a.vt
-                          : static_cast<const T *>(a.k) + head * a.kh + token * a.kt;
-        const int64_t pitch = kind ? a.vt : a.kt;
-        int8_t *out = page < 0 ? nullptr : c.rows(page, head, kind);
-        float *step = page < 0 ? nullptr : c.scale(page, head, kind);
-        const float old = first > 0 ? *step : 0.0f;
-        const int runs = rows * a.runs.d;           // whole runs; what is left of a row comes by itself
+        const int runs = rows * a.runs.d * (a.whole > 0 ? 1 : 0);      // whole runs; what is left of a row comes by itself
         const int tail = a.whole * kRun;
 
-        Run<T, kRun> held[kHold];
-        uint32_t bits = 0;              // of the largest magnitude: NaN above infinity above numbers
-        auto look = [&](float v) {
-            const uint32_t w = __builtin_bit_cast(uint32_t, v) & 0x7fffffffu;
-            bits = w > bits ? w : bits;
+        auto rows_of = [&](int pair) {
+            return pair & 1 ? static_cast<const T *>(a.v) + (pair >> 1) * a.vh + token * a.vt
+                            : static_cast<const T *>(a.k) + (pair >> 1) * a.kh + token * a.kt;
         };
-        auto run_at = [&](int n) {
+        auto run_at = [&](const T *x, int pitch, int n) {
             const int r = a.runs(n);
-            return reinterpret_cast<const Run<T, kRun> *>(x + r * pitch + (n - r * a.runs.d) * kRun);
+            return reinterpret_cast<const Run<T, kRun> *>(x + (static_cast<int64_t>(r) * pitch + (n - r * a.runs.d) * kRun));
         };
-        if (a.whole > 0) {
+        auto fetch = [&](int pair, Run<T, kRun> (&held)[kHold], float &old) {
+            const T *x = rows_of(pair);
+            const int pitch = static_cast<int>(pair & 1 ? a.vt : a.kt);
 #pragma unroll
             for (int h = 0; h < kHold; h++)
-                if (i + h * L < runs) held[h] = *run_at(i + h * L);
-        }
-        for (int r = i; r < rows; r += L)
-            for (int d = tail; d < D; d++) look(as_float(x[r * pitch + d]));
-        if (a.whole > 0) {
+                if (i + h * L < runs) held[h] = *run_at(x, pitch, i + h * L);
+            old = first > 0 ? *c.scale(page, pair >> 1, pair & 1) : 0.0f;
+        };
+        Run<T, kRun> held[kHold], next[kHold];
+        float old, next_old = 0.0f;
+        fetch(pair0, held, old);
+        for (int pair = pair0; pair < pair0 + a.pairs; pair++) {
+            // the next keys or values are on their way while these are rounded
+            if (pair + 1 < pair0 + a.pairs) fetch(pair + 1, next, next_old);
+            const T *x = rows_of(pair);
+            const int pitch = static_cast<int>(pair & 1 ? a.vt : a.kt);
+            uint32_t bits = 0;          // of the largest magnitude: NaN above infinity above numbers
+            auto look = [&](float v) {
+                const uint32_t w = __builtin_bit_cast(uint32_t, v) & 0x7fffffffu;
+                bits = w > bits ? w : bits;
+            };
 #pragma unroll
             for (int h = 0; h < kHold; h++)
                 if (i + h * L < runs)
                     for (int k = 0; k < kRun; k++) look(as_float(held[h].t[k]));
             for (int n = i + kHold * L; n < runs; n += L) {
-                const Run<T, kRun> w = *run_at(n);
+                const Run<T, kRun> w = *run_at(x, pitch, n);
 #pragma unroll
                 for (int k = 0; k < kRun; k++) look(as_float(w.t[k]));
             }
-        }
+            if (tail < D)
+                for (int r = i; r < rows; r += L)
+                    for (int d = tail; d < D; d++) look(as_float(x[static_cast<int64_t>(r) * pitch + d]));
 #pragma unroll
-        for (int d = kGroup / 2; d >= 1; d >>= 1) {
-            const uint32_t v = __shfl_xor(bits, d, kWave);
-            bits = v > bits ? v : bits;
-        }
-        if constexpr (L > kWave) {
-            __syncthreads();            // the last unit's readers are done
-            if (lane_id() == 0) tops[threadIdx.x / kWave] = __builtin_bit_cast(float, bits);
-            __syncthreads();
-            for (int w = 0; w < L / kWave; w++) {
-                const uint32_t v = __builtin_bit_cast(uint32_t, tops[threadIdx.x / L * (L / kWave) + w]);
+            for (int d = kGroup / 2; d >= 1; d >>= 1) {
+                const uint32_t v = __shfl_xor(bits, d, kWave);
                 bits = v > bits ? v : bits;
             }
-        }
-        float s = step_of(__builtin_bit_cast(float, bits));
-        if (first > 0) s = max_nan(s, old);
-        const float inv = inverse_step(s);
-        auto put = [&](int8_t *at, const Run<T, kRun> &w) {
-            i32x2 v = {0, 0};
-            if (inv != 0.0f)
-                v = i32x2{to_bytes4(as_float(w.t[0]), as_float(w.t[1]), as_float(w.t[2]), as_float(w.t[3]), inv),
-                          to_bytes4(as_float(w.t[4]), as_float(w.t[5]), as_float(w.t[6]), as_float(w.t[7]), inv)};
-            *reinterpret_cast<i32x2 *>(at) = v;
-        };
-        auto place = [&](int n) {
-            const int r = a.runs(n);
-            return out + (first + r) * W + (n - r * a.runs.d) * kRun;
-        };
-        if (a.whole > 0) {
+            if constexpr (L > kWave) {
+                __syncthreads();        // the last ones' readers are done
+                if (lane_id() == 0) tops[threadIdx.x / kWave] = __builtin_bit_cast(float, bits);
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < L / kWave; w++) {
+                    const uint32_t v = __builtin_bit_cast(uint32_t, tops[threadIdx.x / L * (L / kWave) + w]);
+                    bits = v > bits ? v : bits;
+                }
+            }
+            float s = step_of(__builtin_bit_cast(float, bits));
+            if (first > 0) s = max_nan(s, old);
+            const float inv = inverse_step(s);
+            int8_t *out = c.rows(page < 0 ? 0 : page, pair >> 1, pair & 1);
+            auto put = [&](int8_t *at, const Run<T, kRun> &w) {
+                i32x2 v = {0, 0};
+                if (inv != 0.0f)
+                    v = i32x2{to_bytes4(as_float(w.t[0]), as_float(w.t[1]), as_float(w.t[2]), as_float(w.t[3]), inv),
+                              to_bytes4(as_float(w.t[4]), as_float(w.t[5]), as_float(w.t[6]), as_float(w.t[7]), inv)};
+                *reinterpret_cast<i32x2 *>(at) = v;
+            };
+            auto place = [&](int n) {
+                const int r = a.runs(n);
+                return out + ((first + r) * W + (n - r * a.runs.d) * kRun);
+            };
 #pragma unroll
             for (int h = 0; h < kHold; h++)
                 if (i + h * L < runs) put(place(i + h * L), held[h]);
-            for (int n = i + kHold * L; n < runs; n += L) put(place(n), *run_at(n));
-        }
-        for (int r = i; r < rows; r += L) {
-            for (int d = tail; d < W; d += kRun) {
-                Run<T, kRun> w;
+            for (int n = i + kHold * L; n < runs; n += L) put(place(n), *run_at(x, pitch, n));
+            if (tail < W) {
+                for (int r = i; r < rows; r += L) {
+                    for (int d = tail; d < W; d += kRun) {
+                        Run<T, kRun> w;
 #pragma unroll
-                for (int k = 0; k < kRun; k++) w.t[k] = d + k < D ? x[r * pitch + d + k] : from_float<T>(0.0f);
-                put(out + (first + r) * W + d, w);
-            }
-        }
-        if (rows > 0 && first > 0 && s != old) {
-            const float f = old * inv;
-            for (int n = i; n < first * (W / kRun); n += L) {
-                i32x2 *at = reinterpret_cast<i32x2 *>(out + n * kRun);
-                i32x2 v = *at;
-#pragma unroll
-                for (int k = 0; k < 2; k++) {
-                    const int word = v[k];
-                    v[k] = !(fabsf(f) > 0.0f) ? 0
-                                              : to_bytes4(static_cast<float>(static_cast<int8_t>(word)), static_cast<float>(static_cast<int8_t>(word >> 8)),
-                                                          static_cast<float>(static_cast<int8_t>(word >> 16)), static_cast<float>(word >> 24), f);
+                        for (int k = 0; k < kRun; k++) w.t[k] = d + k < D ? x[static_cast<int64_t>(r) * pitch + d + k] : from_float<T>(0.0f);
+                        put(out + ((first + r) * W + d), w);
+                    }
                 }
-                *at = v;
             }
+            if (rows > 0 && first > 0 && s != old) {
+                const float f = old * inv;
+                for (int n = i; n < first * (W / kRun); n += L) {
+                    i32x2 *at = reinterpret_cast<i32x2 *>(out + n * kRun);
+                    i32x2 v = *at;
+#pragma unroll
+                    for (int k = 0; k < 2; k++) {
+                        const int word = v[k];
+                        const float q[4] = {static_cast<float>(static_cast<int8_t>(word)), static_cast<float>(static_cast<int8_t>(word >> 8)),
+                                            static_cast<float>(static_cast<int8_t>(word >> 16)), static_cast<float>(word >> 24)};
+                        v[k] = f > 0.0f ? to_bytes4(q[0], q[1], q[2], q[3], f) : 0;
+                    }
+                    *at = v;
+                }
+            }
+            if (rows > 0 && i == 0) *c.scale(page, pair >> 1, pair & 1) = s;
+#pragma unroll
+            for (int h = 0; h < kHold; h++) held[h] = next[h];
+            old = next_old;
         }
-        if (rows > 0 && i == 0) *step = s;
     }
+}
+
+// The last sequence whose tokens start at or before this one (a wavefront).
+__device__ __forceinline__ int64_t last_at_most(const SeqsView &s, int64_t token) {
+    int64_t lo = 0, hi = s.seqs;
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + kWave - 1) / kWave;
+        const int64_t at = lo + lane_id() * step;
+        const int n = __popcll(__ballot(at < hi && s.first_token(at) <= token));
+        lo += (n > 0 ? n - 1 : 0) * step;
+        hi = lo + step < hi ? lo + step : hi;
+    }
+    return lo;
 }
 
 // A workgroup takes block_tokens tokens in turn: a thread each looks one up,
@@ -188,6 +215,7 @@ template <class T>
 __global__ __launch_bounds__(kBlock) void read_kernel(const IoArgs a) {
     __shared__ int at_page[kBlock];
     __shared__ int at_row[kBlock];
+    __shared__ int64_t ends[2];
     const CacheView &c = a.c;
     const int B = a.block_tokens;
     const int64_t blocks = (a.s.tokens + B - 1) / B;
@@ -195,11 +223,20 @@ __global__ __launch_bounds__(kBlock) void read_kernel(const IoArgs a) {
         const int64_t base = block * B;
         const int count = a.s.tokens - base < B ? static_cast<int>(a.s.tokens - base) : B;
         __syncthreads();
+        // the sequences of the first and of the last token, 64 places at a time
+        if (a.s.offsets) {
+            if (threadIdx.x < 2 * kWave) {
+                const int last = threadIdx.x / kWave;
+                const int64_t b = last_at_most(a.s, last ? base + count - 1 : base);
+                if (lane_id() == 0) ends[last] = b;
+            }
+            __syncthreads();
+        }
         if (static_cast<int>(threadIdx.x) < count) {
             const int64_t token = base + threadIdx.x;
             int64_t b = 0;
             if (a.s.offsets) {
-                int64_t lo = 0, hi = a.s.seqs;
+                int64_t lo = ends[0], hi = ends[1] + 1;
                 while (hi - lo > 1) {
                     const int64_t mid = (lo + hi) / 2;
                     if (a.s.first_token(mid) <= token) lo = mid;
@@ -264,21 +301,33 @@ bool make_args(const tgl_cache *cache, const tgl_heads *k, const tgl_heads *v, i
     a->kh = k->head_stride;
     a->vt = v->token_stride;
     a->vh = v->head_stride;
-    a->heads2 = Div(2 * cache->heads);
     return true;
 }
 
 unsigned grid_of(int64_t blocks) { return static_cast<unsigned>(blocks < (1 << 22) ? blocks : 1 << 22); }
 
+template <class T, int L>
+void launch_write(IoArgs a, int64_t items, hipStream_t st) {
+    // as many keys and values a unit as leave kFill wavefronts, up to 8
+    constexpr int kBlockOf = L > kBlock ? L : kBlock;
+    a.parts = 2 * a.c.heads;
+    a.pairs = 1;
+    while (a.pairs < 8 && a.parts % 2 == 0 && items * (a.parts / 2) * L >= kFill * kWave) {
+        a.parts /= 2;
+        a.pairs *= 2;
+    }
+    a.units = items * a.parts;
+    write_kernel<T, L><<<grid_of((a.units * L + kBlockOf - 1) / kBlockOf), kBlockOf, 0, st>>>(a);
+}
+
+// Lanes of a unit by the runs of the rows that it gets on average.
 template <class T>
-void launch_write(const IoArgs &a, int64_t rows, hipStream_t st) {
-    // lanes of a unit by the runs of the rows that it gets on average: a whole
-    // wavefront once a quarter of it has two
-    const int64_t runs = rows * a.runs.d;
-    if (runs <= 32) write_kernel<T, 16><<<grid_of((a.units + 15) / 16), kBlock, 0, st>>>(a);
-    else if (runs <= 512) write_kernel<T, 64><<<grid_of((a.units + 3) / 4), kBlock, 0, st>>>(a);
-    else if (runs <= 2048) write_kernel<T, 256><<<grid_of(a.units), kBlock, 0, st>>>(a);
-    else write_kernel<T, 512><<<grid_of(a.units), 512, 0, st>>>(a);
+void launch_write(const IoArgs &a, int64_t items, int64_t rows, hipStream_t st) {
+    const int64_t runs = rows * (a.c.width / kRun);
+    if (runs <= 32) launch_write<T, 16>(a, items, st);
+    else if (runs <= 256) launch_write<T, 64>(a, items, st);
+    else if (runs <= 1024) launch_write<T, 256>(a, items, st);
+    else launch_write<T, 512>(a, items, st);
 }
 
 }  // namespace
@@ -292,17 +341,20 @@ tgl_status tgl_cache_write(const tgl_cache *cache, const tgl_heads *k, const tgl
                            int64_t num_tokens, const tgl_seqs *seqs, void *stream) {
     IoArgs a;
     if (!make_args(cache, k, v, dtype, num_tokens, seqs, &a)) return TGL_EINVAL;
+    // a row's place in its page is found with 32 bits
+    if (k->token_stride != static_cast<int32_t>(k->token_stride) || v->token_stride != static_cast<int32_t>(v->token_stride))
+        return TGL_EINVAL;
     if (num_tokens == 0 || seqs->num_seqs == 0 || cache->num_pages == 0) return TGL_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();
     const int64_t P = a.c.tokens();
-    a.units = (((num_tokens + seqs->num_seqs * (2 * P - 2)) >> a.c.shift) + 1) * 2 * a.c.heads;
+    const int64_t items = ((num_tokens + seqs->num_seqs * (2 * P - 2)) >> a.c.shift) + 1;
     a.whole = a.c.dim / kRun;
     a.runs = Div(a.whole > 0 ? a.whole : 1);
     const int64_t each = (num_tokens + seqs->num_seqs - 1) / seqs->num_seqs;
     const int64_t rows = each < P ? each : P;
-    if (dtype == TGL_OUT_F32) launch_write<float>(a, rows, st);
-    else launch_write<bf16_t>(a, rows, st);
+    if (dtype == TGL_OUT_F32) launch_write<float>(a, items, rows, st);
+    else launch_write<bf16_t>(a, items, rows, st);
     return launch_status();
 }
 
