@@ -627,7 +627,7 @@ tgl_status tgl_norm_quant(const void *x, int64_t x_stride, const void *residual,
  * The sum is exact (int32); scales, bias and the one rounding to out_type are
  * float32 operations, the product of the sum with x_scale first.
  *   x         [device] int8, m rows x_stride apart, 16-byte aligned, x_stride
- *             a multiple of 16; each row is readable up to the next multiple
+ *             a multiple of 16 below 2^22; each row is readable up to the next multiple
  *             of 16 of k (what tgl_norm_quant leaves), whatever is there
  *   w         [device] int8, n rows (one per output column), same rules
  *   x_scale   [device] float[m];  w_scale [device] float[n]

@@ -16,6 +16,9 @@ struct LinearArgs {
     int64_t xstride, wstride, ostride;
     int64_t m;
     int32_t n, k;
+    Div tiles_n;            // small products: tiles of 16 columns
+    Div band;               // large ones: tiles of a band of band_rows tiles of rows
+    uint32_t band_rows, tiles_m, work;
 };
 
 // 16 consecutive bytes of a row from column c on, zeros from column k on.
@@ -36,37 +39,240 @@ __device__ __forceinline__ i32x4 mask_piece(i32x4 v, int c, int k) {
     return v;
 }
 
-// A wavefront per 16 x 16 outputs, operands straight from memory.
-template <class T>
-__global__ __launch_bounds__(kBlock) void linear_kernel(const LinearArgs a) {
+// Scales, bias, the one rounding: N outputs of a row from column j on.
+template <class T, int N>
+__device__ __forceinline__ void finish(const LinearArgs &a, int64_t row, int j, const int (&sum)[N], const float (&ws)[N], const float (&bias)[N]) {
+    const float xs = a.xs[row];
+    float y[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        y[i] = static_cast<float>(sum[i]) * xs * ws[i];
+        if (a.bias) y[i] += bias[i];
+    }
+    store_columns<T, N>(static_cast<T *>(a.out) + row * a.ostride, j, a.n, y);
+}
+
+// ---- small products: operands straight from memory --------------------------
+
+// A workgroup per 16 rows and 16 columns, whose wavefronts take 64 of k in turn
+// and add up through LDS.
+template <class T, int NW>
+__global__ __launch_bounds__(NW * kWave) void linear_small_kernel(const LinearArgs a) {
+    __shared__ i32x4 sums[NW > 1 ? NW - 1 : 1][kWave];
     const int lane = lane_id();
-    const int64_t tiles_n = (a.n + 15) / 16;
-    const int64_t tile = static_cast<int64_t>(blockIdx.x) * (kBlock / kWave) + threadIdx.x / kWave;
-    if (tile >= (a.m + 15) / 16 * tiles_n) return;
-    const int64_t m0 = tile / tiles_n * 16;
-    const int n0 = static_cast<int>(tile % tiles_n) * 16;
+    const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const uint32_t tm = a.tiles_n(blockIdx.x), tn = blockIdx.x - tm * a.tiles_n.d;
+    const int64_t m0 = static_cast<int64_t>(tm) * 16;
+    const int n0 = tn * 16;
     const int64_t mr = m0 + (lane & 15) < a.m ? m0 + (lane & 15) : a.m - 1;
     const int nr = n0 + (lane & 15) < a.n ? n0 + (lane & 15) : a.n - 1;
     const int8_t *x = a.x + mr * a.xstride;
     const int8_t *w = a.w + nr * a.wstride;
     i32x4 acc = {0, 0, 0, 0};
-    for (int k = 0; k < a.k; k += 64) {
+    for (int k = wave * 64; k < a.k; k += NW * 64) {
         const int c = k + 16 * (lane >> 4);
-        const i32x4 av = mask_piece(load_piece(x, c, a.k), c, a.k);
-        const i32x4 bv = load_piece(w, c, a.k);
-        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(av, bv, acc, 0, 0, 0);
+        const i32x4 wv = load_piece(w, c, a.k);
+        const i32x4 xv = mask_piece(load_piece(x, c, a.k), c, a.k);
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv, xv, acc, 0, 0, 0);
     }
-    const int col = n0 + (lane & 15);
-    if (col >= a.n) return;
-    const float ws = a.ws[col], b = a.bias ? a.bias[col] : 0.0f;
+    if constexpr (NW > 1) {
+        if (wave > 0) sums[wave - 1][lane] = acc;
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int y = 1; y < NW; y++) acc += sums[y - 1][lane];
+    }
+    const int j = n0 + 4 * (lane >> 4);
+    if (m0 + (lane & 15) >= a.m || j >= a.n) return;
+    int sum[4];
+    float ws[4], bias[4];
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-        const int64_t row = m0 + 4 * (lane >> 4) + i;
-        if (row < a.m) {
-            const float y = static_cast<float>(acc[i]) * a.xs[row] * ws;
-            static_cast<T *>(a.out)[row * a.ostride + col] = from_float<T>(a.bias ? y + b : y);
+        sum[i] = acc[i];
+        const int col = j + i < a.n ? j + i : a.n - 1;
+        ws[i] = a.ws[col];
+        bias[i] = a.bias ? a.bias[col] : 0.0f;
+    }
+    finish<T, 4>(a, mr, j, sum, ws, bias);
+}
+
+// ---- large products: tiles through LDS --------------------------------------
+//
+// A workgroup owns BM x BN outputs and walks k in steps of 128: the step's
+// BM + BN rows of 128 bytes go straight from memory to one of two LDS buffers
+// while the other is multiplied.  A wavefront owns 64 columns and MT x 16 rows;
+// the weights are the first operand, so that a lane ends up with columns of
+// one row, and its four tiles' rows of w are picked so that these are 16
+// consecutive ones: 4 of each (lane / 16) * 16 + 4 tile + 0..3.
+//
+// A 16-byte piece p of row r lies at piece p ^ swizzle(r) of the row's 128
+// bytes, so that the 16 lanes that read one piece of 16 rows touch all banks.
+// What LDS holds past k is 0 (loads beyond the buffer's end give 0); the last
+// bytes of k's own piece are cleared in the x operand.
+
+constexpr int kStepK = 128;
+
+__device__ __forceinline__ int swizzle_x(int r) { return (r >> 1) & 7; }
+__device__ __forceinline__ int swizzle_w(int r) { return ((r >> 1) & 1) | (((r >> 4) & 3) << 1); }
+
+using lds_t = __attribute__((address_space(3))) void;
+
+template <class T, int BM, int BN, int MT, bool kTail>
+__global__ __launch_bounds__(BM / (16 * MT) * (BN / 64) * kWave, (MT == 8 ? 2 : 2)) void linear_tile_kernel(const LinearArgs a) {
+    constexpr int kWaves = BM / (16 * MT) * (BN / 64);
+    constexpr int kRowsPerWave = (BM + BN) / kWaves;        // rows of a step that a wavefront fetches, all of w or all of x
+    constexpr int kFetch = kRowsPerWave / 8;
+    static_assert(BN % kRowsPerWave == 0, "a wavefront fetches rows of one operand");
+    __shared__ __attribute__((aligned(1024))) int8_t buf0[(BM + BN) * kStepK];
+    __shared__ __attribute__((aligned(1024))) int8_t buf1[(BM + BN) * kStepK];
+    const int lane = lane_id();
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int g = lane >> 4, i16 = lane & 15;
+    // the 8 dies take workgroups in turn: each gets a contiguous stretch of
+    // tiles, walked in bands of kBand tiles of rows
+    const uint32_t per = (a.work + 7) / 8;
+    const uint32_t id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= per || id >= a.work) return;
+    const uint32_t band = a.band(id);                       // tiles_n * kBand tiles
+    const uint32_t in_band = id - band * a.band.d;
+    const uint32_t rows_left = a.tiles_m - band * a.band_rows;
+    const uint32_t height = rows_left < a.band_rows ? rows_left : a.band_rows;
+    const uint32_t tn = in_band / height, tm = band * a.band_rows + (in_band - tn * height);
+    const int64_t m0 = static_cast<int64_t>(tm) * BM;
+    const int n0 = tn * BN;
+
+    // ---- what the wavefront fetches ----
+    const bool of_w = wave * kRowsPerWave < BN;
+    const int row0 = of_w ? wave * kRowsPerWave : wave * kRowsPerWave - BN;     // of its operand's tile
+    const int8_t *src = of_w ? a.w + static_cast<int64_t>(n0) * a.wstride : a.x + m0 * a.xstride;
+    const uint32_t stride = static_cast<uint32_t>(of_w ? a.wstride : a.xstride);
+    const int64_t left = of_w ? a.n - n0 : a.m - m0;
+    const int last = static_cast<int>(left < (of_w ? BN : BM) ? left : (of_w ? BN : BM)) - 1;   // its tile's last row
+    const uint32_t k16 = (a.k + 15) & ~15;
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(src), 0, last * stride + k16, 0x00027000);
+    uint32_t at[kFetch];
+    uint32_t piece[kFetch];
+#pragma unroll
+    for (int f = 0; f < kFetch; f++) {
+        const int r = row0 + 8 * f + (lane >> 3);
+        piece[f] = ((lane & 7) ^ (of_w ? swizzle_w(r) : swizzle_x(r))) * 16;
+        at[f] = (r < last ? r : last) * stride + piece[f];
+    }
+    const int steps = (a.k + kStepK - 1) / kStepK;
+    auto fetch = [&](int8_t *buf, int step) {
+#pragma unroll
+        for (int f = 0; f < kFetch; f++) {
+            const uint32_t k = step * kStepK;
+            // beyond the row: past the buffer's end, which reads as 0
+            const uint32_t off = k + piece[f] < k16 ? at[f] + k : 0x7ffffff0u;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_t *)(buf + (wave * kRowsPerWave + 8 * f) * kStepK), 16, off, 0, 0, 0);
+        }
+    };
+
+    // ---- what it multiplies ----
+    const int wm = wave / (BN / 64), wn = wave % (BN / 64);
+    i32x4 acc[MT][4];
+#pragma unroll
+    for (int i = 0; i < MT; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) acc[i][j] = i32x4{0, 0, 0, 0};
+    int w_at[4], x_at[MT];
+#pragma unroll
+    for (int j = 0; j < 4; j++) w_at[j] = wn * 64 + (i16 >> 2) * 16 + 4 * j + (i16 & 3);
+#pragma unroll
+    for (int i = 0; i < MT; i++) x_at[i] = wm * 16 * MT + 16 * i + i16;
+    auto multiply = [&](const int8_t *buf, int step) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const int p = 4 * h + g;
+            i32x4 wv[4], xv[MT];
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                wv[j] = *reinterpret_cast<const i32x4 *>(buf + w_at[j] * kStepK + ((p ^ swizzle_w(w_at[j])) * 16));
+#pragma unroll
+            for (int i = 0; i < MT; i++) {
+                xv[i] = *reinterpret_cast<const i32x4 *>(buf + (BN + x_at[i]) * kStepK + ((p ^ swizzle_x(x_at[i])) * 16));
+                if constexpr (kTail) {
+                    if (step == steps - 1) xv[i] = mask_piece(xv[i], step * kStepK + 16 * p, a.k);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < MT; i++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[j], xv[i], acc[i][j], 0, 0, 0);
+        }
+    };
+    // loads to LDS count as loads from memory: each wavefront waits for its own,
+    // then for the others
+    auto meet = [] {
+        __builtin_amdgcn_s_waitcnt(0x0f70);                 // vmcnt(0)
+        __syncthreads();
+    };
+    fetch(buf0, 0);
+    for (int step = 0; step < steps; step += 2) {
+        meet();                                             // buf0 is there, buf1 free
+        if (step + 1 < steps) fetch(buf1, step + 1);
+        multiply(buf0, step);
+        meet();
+        if (step + 1 < steps) {
+            if (step + 2 < steps) fetch(buf0, step + 2);
+            multiply(buf1, step + 1);
         }
     }
+
+    const int j0 = n0 + wn * 64 + 16 * g;
+    if (j0 >= a.n) return;
+    float ws[16], bias[16];
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+        const int col = j0 + i < a.n ? j0 + i : a.n - 1;
+        ws[i] = a.ws[col];
+        bias[i] = a.bias ? a.bias[col] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < MT; i++) {
+        const int64_t row = m0 + x_at[i];
+        if (row < a.m) {
+            int sum[16];
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) sum[4 * j + e] = acc[i][j][e];
+            finish<T, 16>(a, row, j0, sum, ws, bias);
+        }
+    }
+}
+
+template <class T, int BM, int BN, int MT>
+void launch_tiles(LinearArgs a, hipStream_t st) {
+    constexpr int kThreads = BM / (16 * MT) * (BN / 64) * kWave;
+    const uint32_t tiles_n = (a.n + BN - 1) / BN;
+    a.tiles_m = static_cast<uint32_t>((a.m + BM - 1) / BM);
+    a.work = a.tiles_m * tiles_n;
+    a.band_rows = 8;
+    a.band = Div(tiles_n * a.band_rows);
+    const unsigned grid = (a.work + 7) / 8 * 8;
+    if (a.k % 16) linear_tile_kernel<T, BM, BN, MT, true><<<grid, kThreads, 0, st>>>(a);
+    else linear_tile_kernel<T, BM, BN, MT, false><<<grid, kThreads, 0, st>>>(a);
+}
+
+template <class T>
+bool launch(LinearArgs a, hipStream_t st) {
+    const int64_t tiles = (a.m + 15) / 16 * ((a.n + 15) / 16);
+    if (tiles > 0x7ffffff0) return false;
+    auto count = [&](int bm, int bn) { return ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn); };
+    if (count(256, 256) >= 192) {
+        launch_tiles<T, 256, 256, 8>(a, st);
+    } else if (count(128, 128) >= 128) {
+        launch_tiles<T, 128, 128, 4>(a, st);
+    } else {
+        a.tiles_n = Div((a.n + 15) / 16);
+        // wavefronts that share a tile's k, while tiles alone do not fill the card
+        if (tiles >= 4096 || a.k <= 64) linear_small_kernel<T, 1><<<static_cast<unsigned>(tiles), kWave, 0, st>>>(a);
+        else if (tiles >= 1024 || a.k <= 512) linear_small_kernel<T, 4><<<static_cast<unsigned>(tiles), 4 * kWave, 0, st>>>(a);
+        else linear_small_kernel<T, 8><<<static_cast<unsigned>(tiles), 8 * kWave, 0, st>>>(a);
+    }
+    return true;
 }
 
 }  // namespace
@@ -89,7 +295,8 @@ tgl_status tgl_linear_i8(const int8_t *x, int64_t x_stride, const float *x_scale
                          size_t workspace_bytes, void *stream) {
     if (m < 0 || n < 1 || n > TGL_MAX_LINEAR_OUT || k < 1 || k > TGL_MAX_LINEAR_K || !is_elem_type(out_type))
         return TGL_EINVAL;
-    if (!aligned(x, 16) || !aligned(w, 16) || x_stride % 16 != 0 || w_stride % 16 != 0 || x_stride < 0 || w_stride < 0)
+    if (!aligned(x, 16) || !aligned(w, 16) || x_stride % 16 != 0 || w_stride % 16 != 0 || x_stride < 0 || w_stride < 0 ||
+        x_stride >= (1 << 22) || w_stride >= (1 << 22))
         return TGL_EINVAL;
     if (!aligned(x_scale, 4) || !aligned(w_scale, 4) || !aligned(bias, 4) || !aligned(out, elem_size(out_type)))
         return TGL_EINVAL;
@@ -99,13 +306,20 @@ tgl_status tgl_linear_i8(const int8_t *x, int64_t x_stride, const float *x_scale
     if (m == 0) return TGL_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();
-    const LinearArgs a{x, w, x_scale, w_scale, bias, out, x_stride, w_stride, out_stride, m, n, k};
-    const int64_t tiles = (m + 15) / 16 * ((n + 15) / 16);
-    const int64_t blocks = (tiles + 3) / 4;
-    if (blocks > 0x7fffffff) return TGL_EINVAL;
-    const unsigned grid = static_cast<unsigned>(blocks);
-    if (out_type == TGL_OUT_F32) linear_kernel<float><<<grid, kBlock, 0, st>>>(a);
-    else linear_kernel<bf16_t><<<grid, kBlock, 0, st>>>(a);
+    LinearArgs a{};
+    a.x = x;
+    a.w = w;
+    a.xs = x_scale;
+    a.ws = w_scale;
+    a.bias = bias;
+    a.out = out;
+    a.xstride = x_stride;
+    a.wstride = w_stride;
+    a.ostride = out_stride;
+    a.m = m;
+    a.n = n;
+    a.k = k;
+    if (!(out_type == TGL_OUT_F32 ? launch<float>(a, st) : launch<bf16_t>(a, st))) return TGL_EINVAL;
     return launch_status();
 }
 
