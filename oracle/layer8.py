@@ -54,7 +54,7 @@ def norm_quant(x, residual, weight, eps, normalize=True):
 
 
 def linear_i8(x, xs, w, ws, bias):
-    y = (x.astype(np.int64) @ w.astype(np.int64).T).astype(np.float64)
+    y = x.astype(np.float64) @ w.astype(np.float64).T       # exact: whole numbers below 2^53
     y = y * np.asarray(xs, np.float64)[:, None] * np.asarray(ws, np.float64)[None, :]
     return y if bias is None else y + np.asarray(bias, np.float64)
 

@@ -124,6 +124,33 @@ def test_linear_i8(m, n, k, bias, dtype):
     assert np.all(np.abs(_host(y) - want) <= tol + 1e-30)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k,bias", [
+    (1537, 1409, 200, True), (1600, 1408, 128, False), (2000, 1300, 384, True), (1411, 1537, 1033, False), (1408, 1600, 17, True),
+    (3585, 3500, 100, True), (3584, 3584, 256, False), (3700, 3333, 272, True), (6000, 2100, 395, False), (130000, 130, 48, True),
+])
+def test_linear_i8_tiles(m, n, k, bias, dtype):
+    """Products large enough for tiles of 128 and of 256, cut off in every direction."""
+    torch = require_gpu()
+    announce("linear_i8 tiles %d x %d x %d %s" % (m, n, k, dtype))
+    rng = np.random.default_rng(m + n + k)
+    kp = O.round16(k)
+    xb = rng.integers(-128, 128, (m, kp)).astype(np.int8)
+    wb = rng.integers(-128, 128, (n, kp)).astype(np.int8)
+    xs, ws = rng.uniform(0.5, 2, m).astype(np.float32), rng.uniform(0.01, 0.02, n).astype(np.float32)
+    b = (100 * rng.standard_normal(n)).astype(np.float32) if bias else None
+    room = torch.full((m + 1, n + 3), 5.0).cuda().to(_torch_type(torch, dtype))
+    y = P.linear_i8(torch.from_numpy(xb).cuda()[:, :k], torch.from_numpy(xs).cuda(), torch.from_numpy(wb).cuda()[:, :k],
+                    torch.from_numpy(ws).cuda(), None if b is None else torch.from_numpy(b).cuda(), out=room[:m, 2:n + 2])
+    want = O.linear_i8(xb[:, :k], xs, wb[:, :k], ws, b)
+    prod = want if b is None else want - b
+    tol = 4 * HALF * (np.abs(prod) + (0 if b is None else np.abs(b)))
+    if dtype == "bf16":
+        tol = tol + 2.0 ** -8 * np.abs(want)
+    assert np.all(np.abs(_host(y) - want) <= tol + 1e-30)
+    assert (room[m] == 5).all() and (room[:, :2] == 5).all() and (room[:, n + 2:] == 5).all()
+
+
 def test_linear_i8_strides_and_far_rows():
     torch = require_gpu()
     announce("linear_i8 strides")
