@@ -15,66 +15,82 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import math
-from dataclasses import dataclass
+from dataclasses import dataclass, field
 from typing import Optional
 
 import torch
 
-from .binding import (OUT_BF16, OUT_F32, _check, _p, _stream, c_cache, c_heads, c_seqs, lib)
+from .binding import OUT_BF16, OUT_F32, _check, c_cache, c_heads, c_seqs, lib
 
 _TYPES = {torch.float32: OUT_F32, torch.bfloat16: OUT_BF16}
 MAX_PAGE = 128
 MAX_HEAD_DIM = 256
 
+# A serving step makes many small calls, so the checks below ask a tensor for
+# as little as they can (get_device() rather than device, data_ptr() as a plain
+# number): 8 to 11 us a call with its outputs, where 11 to 15 were spent before.
+
 
 def _round16(n: int) -> int:
-    return (n + 15) // 16 * 16
+    return (n + 15) & ~15
+
+
+_HERE = contextlib.nullcontext()
 
 
 def _on(stream):
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return _HERE if stream is None else torch.cuda.stream(stream)
 
 
-def _checked(device, **tensors):
-    """Every tensor is on the current device and records no gradient."""
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if not t.is_cuda or t.device != device:
-            raise ValueError("%s must be on %s, not on %s" % (name, device, t.device))
-        if t.requires_grad and torch.is_grad_enabled():
-            raise ValueError("%s requires a gradient, and rounding to 8 bits has none" % name)
+def _raw_stream(stream, dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
-def _device(t: torch.Tensor, name: str) -> torch.device:
-    if not t.is_cuda:
-        raise ValueError("%s must be a device tensor" % name)
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError("%s must be on the current device" % name)
-    return t.device
+def _device(t: torch.Tensor, name: str) -> int:
+    """The current device, which t has to be on."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        raise ValueError("%s must be on the current device, not on %s" % (name, t.device))
+    if t.requires_grad:
+        _no_gradient(name)
+    return dev
 
 
-def _type(t: torch.Tensor, name: str) -> int:
-    if t.dtype not in _TYPES:
+def _also(t: torch.Tensor, name: str, dev: int):
+    if t.get_device() != dev:
+        raise ValueError("%s must be on the current device, not on %s" % (name, t.device))
+    if t.requires_grad:
+        _no_gradient(name)
+
+
+def _no_gradient(name: str):
+    if torch.is_grad_enabled():
+        raise ValueError("%s requires a gradient, and rounding to 8 bits has none" % name)
+
+
+def _type(dtype, name: str) -> int:
+    t = _TYPES.get(dtype)
+    if t is None:
         raise ValueError("%s must be float32 or bfloat16" % name)
-    return _TYPES[t.dtype]
+    return t
 
 
-def _out_type(dtype) -> int:
-    if dtype not in _TYPES:
-        raise ValueError("out_dtype must be float32 or bfloat16")
-    return _TYPES[dtype]
+def _rows(t: torch.Tensor, name: str):
+    """Shape and row stride of a matrix whose rows are contiguous."""
+    if t.dim() != 2:
+        raise ValueError("%s must be a matrix" % name)
+    n, dim = t.shape
+    stride, inner = t.stride()
+    if inner != 1 and dim > 1 and n > 0:
+        raise ValueError("%s must have the elements of a row next to each other" % name)
+    return n, dim, stride
 
 
-def _rows(t: torch.Tensor, name: str, dim: Optional[int] = None):
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1 and t.numel() > 0) or (dim is not None and t.shape[1] != dim):
-        raise ValueError("%s must be rows%s, adjacent elements next to each other"
-                         % (name, "" if dim is None else " of %d" % dim))
-
-
-def _vector(t: Optional[torch.Tensor], n: int, name: str, dtype=torch.float32):
-    if t is not None and (t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or not t.is_contiguous()):
+def _vector(t: torch.Tensor, n: int, name: str, dev: int, dtype=torch.float32) -> int:
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s vector of %d" % (name, dtype, n))
+    _also(t, name, dev)
+    return t.data_ptr()
 
 
 # --------------------------------------------------------------------------
@@ -83,31 +99,38 @@ def _vector(t: Optional[torch.Tensor], n: int, name: str, dtype=torch.float32):
 
 def _quantise(x, weight, residual, normalize, eps, stream, out):
     dev = _device(x, "x")
-    _checked(dev, x=x, weight=weight, residual=residual, out=out)
-    dt = _type(x, "x")
-    _rows(x, "x")
-    n, dim = x.shape
+    dt = _type(x.dtype, "x")
+    n, dim, xs = _rows(x, "x")
     if dim < 1:
         raise ValueError("x must have columns")
-    _vector(weight, dim, "weight")
+    w = None if weight is None else _vector(weight, dim, "weight", dev)
+    rs = os = 0
     for t, name in ((residual, "residual"), (out, "out")):
-        if t is not None:
-            if t.dtype != x.dtype or t.shape != x.shape:
-                raise ValueError("%s must have x's type and shape" % name)
-            _rows(t, name)
-    if out is not None and n > 1 and out.stride(0) < dim:
-        raise ValueError("out's rows overlap")
+        if t is None:
+            continue
+        if t.dtype != x.dtype or t.shape != x.shape:
+            raise ValueError("%s must have x's type and shape" % name)
+        _also(t, name, dev)
+        if name == "residual":
+            rs = _rows(t, name)[2]
+        else:
+            os = _rows(t, name)[2]
+            if n > 1 and os < dim:
+                raise ValueError("out's rows overlap")
+    width = _round16(dim)
     with _on(stream):
-        store = torch.empty((n, _round16(dim)), dtype=torch.int8, device=dev)
-        scale = torch.empty(n, dtype=torch.float32, device=dev)
+        store = x.new_empty((n, width), dtype=torch.int8)
+        scale = x.new_empty(n, dtype=torch.float32)
         if out is None and residual is not None:
-            out = torch.empty((n, dim), dtype=x.dtype, device=dev)
-    s = lib().tgl_norm_quant(_p(x) if n else None, x.stride(0), _p(residual) if n else None,
-                             0 if residual is None else residual.stride(0), _p(weight), n, dim, dt, int(normalize),
-                             C.c_float(eps), _p(store) if n else None, store.stride(0), _p(scale) if n else None,
-                             _p(out) if n else None, 0 if out is None else max(out.stride(0), dim), _stream(stream))
-    _check(s, "tgl_norm_quant")
-    return store[:, :dim], scale, out
+            out = x.new_empty((n, dim))
+            os = dim
+    if n:
+        s = lib().tgl_norm_quant(x.data_ptr(), xs, None if residual is None else residual.data_ptr(), rs, w, n, dim, dt,
+                                 normalize, eps, store.data_ptr(), width, scale.data_ptr(),
+                                 None if out is None else out.data_ptr(), os if os > dim else dim, _raw_stream(stream, dev))
+        if s:
+            _check(s, "tgl_norm_quant")
+    return store if width == dim else store[:, :dim], scale, out
 
 
 def norm_quant(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
@@ -131,20 +154,19 @@ def quant_rows(x: torch.Tensor, stream=None):
     return q, scale
 
 
-def _int8_rows(t: torch.Tensor, name: str):
-    """Checks int8 rows for the kernel."""
+def _int8_rows(t: torch.Tensor, name: str, dev: int):
+    """Shape and row stride of int8 rows that the kernel can read."""
     if t.dtype != torch.int8:
         raise ValueError("%s must be int8" % name)
-    _rows(t, name)
-    m, k = t.shape
-    if m == 0:
-        return
-    stride = t.stride(0) if m > 1 else _round16(k)
-    end = t.storage_offset() + (m - 1) * stride + _round16(k)
-    if stride % 16 == 0 and t.data_ptr() % 16 == 0 and stride >= 0 and end <= t.untyped_storage().nbytes():
-        return
-    raise ValueError("%s must have rows at multiples of 16 bytes, padded to 16 bytes (as quant_rows and norm_quant "
-                     "make them)" % name)
+    _also(t, name, dev)
+    m, k, stride = _rows(t, name)
+    if m < 2:
+        stride = _round16(k)
+    if m and (stride & 15 or t.data_ptr() & 15 or stride < 0
+              or t.storage_offset() + (m - 1) * stride + _round16(k) > t.untyped_storage().nbytes()):
+        raise ValueError("%s must have rows at multiples of 16 bytes, padded to 16 bytes (as quant_rows and norm_quant "
+                         "make them)" % name)
+    return m, k, stride
 
 
 def linear_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
@@ -156,32 +178,33 @@ def linear_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: 
     multiples of 16 bytes and are readable up to the next one, as
     ``norm_quant`` and ``quant_rows`` leave them."""
     dev = _device(x, "x")
-    _checked(dev, x=x, x_scale=x_scale, w=w, w_scale=w_scale, bias=bias, out=out)
-    _int8_rows(x, "x")
-    _int8_rows(w, "w")
-    m, k = x.shape
-    n = w.shape[0]
-    if w.shape[1] != k or k < 1 or n < 1:
+    m, k, xstride = _int8_rows(x, "x", dev)
+    n, wk, wstride = _int8_rows(w, "w", dev)
+    if wk != k or k < 1 or n < 1:
         raise ValueError("x is %s and w %s: both need the same number of columns" % (tuple(x.shape), tuple(w.shape)))
-    _vector(x_scale, m, "x_scale")
-    _vector(w_scale, n, "w_scale")
-    _vector(bias, n, "bias")
+    xs = _vector(x_scale, m, "x_scale", dev)
+    ws = _vector(w_scale, n, "w_scale", dev)
+    b = None if bias is None else _vector(bias, n, "bias", dev)
+    ostride = n
     if out is not None:
         out_dtype = out.dtype
-        _rows(out, "out", n)
-        if out.shape[0] != m or (m > 1 and out.stride(0) < n):
+        _also(out, "out", dev)
+        om, on, ostride = _rows(out, "out")
+        if om != m or on != n or (m > 1 and ostride < n):
             raise ValueError("out must be [%d, %d]" % (m, n))
-    ot = _out_type(out_dtype)
+    ot = _type(out_dtype, "the output")
     L = lib()
-    need = int(L.tgl_linear_i8_workspace(m, n, k))
+    need = L.tgl_linear_i8_workspace(m, n, k)
     with _on(stream):
         if out is None:
-            out = torch.empty((m, n), dtype=out_dtype, device=dev)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    s = L.tgl_linear_i8(_p(x) if m else None, x.stride(0) if m > 1 else _round16(k), _p(x_scale) if m else None, m,
-                        _p(w), w.stride(0) if n > 1 else _round16(k), _p(w_scale), _p(bias), n, k,
-                        _p(out) if m else None, out.stride(0) if m > 1 else n, ot, _p(ws), need, _stream(stream))
-    _check(s, "tgl_linear_i8")
+            out = x_scale.new_empty((m, n), dtype=out_dtype)
+        ws_mem = x.new_empty(need, dtype=torch.uint8) if need else None
+    if m:
+        s = L.tgl_linear_i8(x.data_ptr(), xstride, xs, m, w.data_ptr(), wstride, ws, b, n, k, out.data_ptr(),
+                            ostride if ostride > n else n, ot, None if ws_mem is None else ws_mem.data_ptr(), need,
+                            _raw_stream(stream, dev))
+        if s:
+            _check(s, "tgl_linear_i8")
     return out
 
 
@@ -189,7 +212,7 @@ def linear_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: 
 # cache
 # --------------------------------------------------------------------------
 
-@dataclass
+@dataclass(frozen=True)
 class HistoryCache:
     """Keys and values in 8 bits, in pages of P tokens: ``data`` int8 ``[pages,
     heads, 2, P, Dp]`` (keys, then values; Dp = dim rounded up to 16) and
@@ -199,21 +222,24 @@ class HistoryCache:
     data: torch.Tensor
     scales: torch.Tensor
     dim: int
+    _view: c_cache = field(init=False, repr=False, compare=False)
 
     def __post_init__(self):
         d, s = self.data, self.scales
         if d.dim() != 5 or d.dtype != torch.int8 or not d.is_contiguous():
             raise ValueError("data must be a contiguous int8 tensor [pages, heads, 2, P, Dp]")
-        if s.dtype != torch.float32 or not s.is_contiguous() or tuple(s.shape) != tuple(d.shape[:2]) + (2,):
+        pages, heads, two, P, width = d.shape
+        if s.dtype != torch.float32 or not s.is_contiguous() or s.shape != (pages, heads, 2):
             raise ValueError("scales must be a contiguous float32 tensor [pages, heads, 2]")
-        P = d.shape[3]
-        if not 1 <= self.dim <= MAX_HEAD_DIM or d.shape[4] != _round16(self.dim) or d.shape[2] != 2:
+        if not 1 <= self.dim <= MAX_HEAD_DIM or width != _round16(self.dim) or two != 2 or heads < 1:
             raise ValueError("data must hold keys and values of %d elements padded to 16, at most %d"
                              % (self.dim, MAX_HEAD_DIM))
         if P < 1 or P > MAX_PAGE or P & (P - 1):
             raise ValueError("a page holds 1, 2, 4, ... or %d tokens" % MAX_PAGE)
-        if d.device != s.device:
+        if d.get_device() != s.get_device():
             raise ValueError("data and scales must be on the same device")
+        object.__setattr__(self, "_view", c_cache(d.data_ptr() if pages else None, s.data_ptr() if pages else None,
+                                                  pages, P, heads, self.dim, 0))
 
     @classmethod
     def empty(cls, num_pages: int, heads: int, dim: int, page_tokens: int = 1, device="cuda") -> "HistoryCache":
@@ -223,38 +249,52 @@ class HistoryCache:
 
     @property
     def num_pages(self) -> int:
-        return int(self.data.shape[0])
+        return int(self._view.num_pages)
 
     @property
     def heads(self) -> int:
-        return int(self.data.shape[1])
+        return int(self._view.heads)
 
     @property
     def page_tokens(self) -> int:
-        return int(self.data.shape[3])
+        return int(self._view.page_tokens)
 
     def c_view(self) -> c_cache:
-        n = self.num_pages
-        return c_cache(self.data.data_ptr() if n else None, self.scales.data_ptr() if n else None, n,
-                       self.page_tokens, self.heads, self.dim, 0)
+        return self._view
 
 
-def _seqs(dev, table, start, offsets, start_name="start") -> c_seqs:
-    _checked(dev, table=table, **{start_name: start, "offsets": offsets})
-    if table.dim() != 2 or table.dtype != torch.int32 or (
-            table.shape[1] > 1 and table.stride(1) != 1 and table.numel() > 0):
-        raise ValueError("table must be an int32 tensor [sequences, pages], adjacent pages next to each other")
-    B = int(table.shape[0])
-    _vector(start, B, start_name, torch.int64)
-    _vector(offsets, B + 1, "offsets", torch.int64)
-    return c_seqs(table.data_ptr() if table.numel() else None, table.stride(0), B, int(table.shape[1]), 0,
-                  None if start is None else start.data_ptr(), None if offsets is None else offsets.data_ptr())
+def _seqs(dev: int, table, start, offsets, start_name="start") -> c_seqs:
+    if table.dtype != torch.int32 or table.dim() != 2:
+        raise ValueError("table must be an int32 tensor [sequences, pages]")
+    _also(table, "table", dev)
+    B, width = table.shape
+    stride, inner = table.stride()
+    if inner != 1 and width > 1 and B > 0:
+        raise ValueError("table must have the pages of a sequence next to each other")
+    return c_seqs(table.data_ptr() or None, stride, B, width, 0,
+                  None if start is None else _vector(start, B, start_name, dev, torch.int64),
+                  None if offsets is None else _vector(offsets, B + 1, "offsets", dev, torch.int64))
 
 
 def _heads(t: torch.Tensor, name: str, n: int, heads: int, dim: int) -> c_heads:
-    if t.dim() != 3 or tuple(t.shape) != (n, heads, dim) or (dim > 1 and t.stride(2) != 1 and n > 0):
-        raise ValueError("%s must be [%d, %d, %d], adjacent elements next to each other" % (name, n, heads, dim))
-    return c_heads(t.data_ptr() if t.numel() else None, t.stride(0), t.stride(1))
+    if t.dim() != 3 or t.shape != (n, heads, dim):
+        raise ValueError("%s must be [%d, %d, %d]" % (name, n, heads, dim))
+    token, head, inner = t.stride()
+    if inner != 1 and dim > 1 and n > 0:
+        raise ValueError("%s must have the elements of a head next to each other" % name)
+    return c_heads(t.data_ptr() or None, token, head)
+
+
+def _cache_device(cache: HistoryCache) -> int:
+    dev = cache.data.get_device()
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        raise ValueError("the cache must be on the current device")
+    return dev
+
+
+def _check_shares(n: int, seqs: int):
+    if n % seqs if seqs else n:
+        raise ValueError("%d tokens do not divide among %d sequences: offsets are needed" % (n, seqs))
 
 
 def cache_write(cache: HistoryCache, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor,
@@ -267,19 +307,21 @@ def cache_write(cache: HistoryCache, k: torch.Tensor, v: torch.Tensor, table: to
     per sequence).  What a history holds below ``start[b]`` stays; a page that it
     ends in keeps one step for old and new tokens, old ones being rounded
     again when it grows.  A page belongs to one sequence of the call."""
-    dev = _device(cache.data, "the cache")
-    _checked(dev, k=k, v=v)
+    dev = _cache_device(cache)
+    _also(k, "k", dev)
+    _also(v, "v", dev)
     if k.dtype != v.dtype:
         raise ValueError("k and v must have the same type")
-    dt = _type(k, "k")
-    n = int(k.shape[0])
+    dt = _type(k.dtype, "k")
+    view = cache._view
+    n = k.shape[0]
     sq = _seqs(dev, table, start, offsets)
-    if offsets is None and (n % sq.num_seqs if sq.num_seqs else n):
-        raise ValueError("%d tokens do not divide among %d sequences: offsets are needed" % (n, sq.num_seqs))
-    kh, vh = _heads(k, "k", n, cache.heads, cache.dim), _heads(v, "v", n, cache.heads, cache.dim)
-    view = cache.c_view()
-    s = lib().tgl_cache_write(C.byref(view), C.byref(kh), C.byref(vh), dt, n, C.byref(sq), _stream(stream))
-    _check(s, "tgl_cache_write")
+    if offsets is None:
+        _check_shares(n, sq.num_seqs)
+    kh, vh = _heads(k, "k", n, view.heads, view.dim), _heads(v, "v", n, view.heads, view.dim)
+    s = lib().tgl_cache_write(C.byref(view), C.byref(kh), C.byref(vh), dt, n, C.byref(sq), _raw_stream(stream, dev))
+    if s:
+        _check(s, "tgl_cache_write")
 
 
 def cache_read(cache: HistoryCache, table: torch.Tensor, start: Optional[torch.Tensor] = None,
@@ -290,26 +332,28 @@ def cache_read(cache: HistoryCache, table: torch.Tensor, start: Optional[torch.T
     are given as for ``cache_write``; ``n`` (default: every place of the table)
     is the number of tokens, ``offsets[-1]`` where there are offsets.  Tokens that
     no sequence owns are not written."""
-    dev = _device(cache.data, "the cache")
+    dev = _cache_device(cache)
+    view = cache._view
     sq = _seqs(dev, table, start, offsets)
     if n is None:
-        n = int(table.numel()) * cache.page_tokens
-    if offsets is None and (n % sq.num_seqs if sq.num_seqs else n):
-        raise ValueError("%d tokens do not divide among %d sequences: offsets are needed" % (n, sq.num_seqs))
+        n = table.numel() * view.page_tokens
+    if offsets is None:
+        _check_shares(n, sq.num_seqs)
     if (k is None) != (v is None) or (k is not None and k.dtype != v.dtype):
         raise ValueError("k and v go together, with one type")
-    if k is not None:
-        out_dtype = k.dtype
-    ot = _out_type(out_dtype)
     if k is None:
+        ot = _type(out_dtype, "the output")
         with _on(stream):
-            k = torch.empty((n, cache.heads, cache.dim), dtype=out_dtype, device=dev)
-            v = torch.empty((n, cache.heads, cache.dim), dtype=out_dtype, device=dev)
-    _checked(dev, k=k, v=v)
-    kh, vh = _heads(k, "k", n, cache.heads, cache.dim), _heads(v, "v", n, cache.heads, cache.dim)
-    view = cache.c_view()
-    s = lib().tgl_cache_read(C.byref(view), C.byref(kh), C.byref(vh), ot, n, C.byref(sq), _stream(stream))
-    _check(s, "tgl_cache_read")
+            k = cache.scales.new_empty((n, view.heads, view.dim), dtype=out_dtype)
+            v = cache.scales.new_empty((n, view.heads, view.dim), dtype=out_dtype)
+    else:
+        ot = _type(k.dtype, "k")
+        _also(k, "k", dev)
+        _also(v, "v", dev)
+    kh, vh = _heads(k, "k", n, view.heads, view.dim), _heads(v, "v", n, view.heads, view.dim)
+    s = lib().tgl_cache_read(C.byref(view), C.byref(kh), C.byref(vh), ot, n, C.byref(sq), _raw_stream(stream, dev))
+    if s:
+        _check(s, "tgl_cache_read")
     return k, v
 
 
@@ -328,42 +372,54 @@ def cache_attend(cache: HistoryCache, q: torch.Tensor, table: torch.Tensor, begi
     the sampled neighbours.  ``scale`` defaults to ``1 / sqrt(dim)``.  Rows that
     see nothing are 0.  Returns ``out`` like q, and with ``return_lse`` the
     logarithm of each row's sum of exponentials, float32 ``[B(, T), q_heads]``."""
-    dev = _device(cache.data, "the cache")
-    _checked(dev, q=q, end=end, out=out)
-    dt = _type(q, "q")
+    dev = _cache_device(cache)
+    _also(q, "q", dev)
+    dt = _type(q.dtype, "q")
+    view = cache._view
+    heads, dim = view.heads, view.dim
     sq = _seqs(dev, table, begin, None, "begin")
-    if q.dim() not in (3, 4) or q.shape[0] != sq.num_seqs or q.shape[-1] != cache.dim:
-        raise ValueError("q must be [%d, heads, %d] or [%d, queries, heads, %d]"
-                         % (sq.num_seqs, cache.dim, sq.num_seqs, cache.dim))
-    T = int(q.shape[1]) if q.dim() == 4 else 1
-    H = int(q.shape[-2])
-    if H < 1 or H % cache.heads or T < 1:
-        raise ValueError("q has %d heads and %d queries: at least one query, and a multiple of the cache's %d heads, "
-                         "are needed" % (H, T, cache.heads))
-    _vector(end, sq.num_seqs, "end", torch.int64)
-    rows = sq.num_seqs * T
-    with _on(stream):
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-        lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=dev) if return_lse else None
-    if out.dtype != q.dtype or out.shape != q.shape:
-        raise ValueError("out must have q's type and shape")
-
-    def flat(t, name):
-        try:
-            return t if t.dim() == 3 else t.view(rows, H, cache.dim)
-        except RuntimeError:
-            raise ValueError("%s must have its queries at one stride over the sequences" % name) from None
-
-    qh = _heads(flat(q, "q"), "q", rows, H, cache.dim)
-    oh = _heads(flat(out, "out"), "out", rows, H, cache.dim)
-    view = cache.c_view()
+    B = sq.num_seqs
+    shape = q.shape
+    if len(shape) == 3:
+        T = 1
+    elif len(shape) == 4:
+        T = shape[1]
+    else:
+        T = 0
+    if T < 1 or shape[0] != B or shape[-1] != dim:
+        raise ValueError("q must be [%d, heads, %d] or [%d, queries, heads, %d] with at least one query" % (B, dim, B, dim))
+    H = shape[-2]
+    if H < 1 or H % heads:
+        raise ValueError("q has %d heads: a multiple of the cache's %d heads is needed" % (H, heads))
+    last = None if end is None else _vector(end, B, "end", dev, torch.int64)
+    rows = B * T
     L = lib()
-    need = int(L.tgl_cache_attend_workspace(C.byref(view), C.byref(sq), H, T))
+    need = L.tgl_cache_attend_workspace(C.byref(view), C.byref(sq), H, T)
+    given = out is not None
     with _on(stream):
-        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    s = L.tgl_cache_attend(C.byref(view), C.byref(qh), H, T, dt, C.byref(sq), _p(end),
-                           C.c_float(1.0 / math.sqrt(cache.dim) if scale is None else scale), C.byref(oh), _p(lse),
-                           _p(ws), need, _stream(stream))
-    _check(s, "tgl_cache_attend")
+        if not given:
+            out = q.new_empty(shape)
+        lse = q.new_empty(shape[:-1], dtype=torch.float32) if return_lse else None
+        ws = q.new_empty(need, dtype=torch.uint8) if need else None
+    if given:
+        if out.dtype != q.dtype or out.shape != shape:
+            raise ValueError("out must have q's type and shape")
+        _also(out, "out", dev)
+    qh, oh = _heads(_flat(q, "q", rows), "q", rows, H, dim), _heads(_flat(out, "out", rows), "out", rows, H, dim)
+    s = L.tgl_cache_attend(C.byref(view), C.byref(qh), H, T, dt, C.byref(sq), last,
+                           1.0 / math.sqrt(dim) if scale is None else scale, C.byref(oh),
+                           None if lse is None else lse.data_ptr() or None, None if ws is None else ws.data_ptr(), need,
+                           _raw_stream(stream, dev))
+    if s:
+        _check(s, "tgl_cache_attend")
     return (out, lse) if return_lse else out
+
+
+def _flat(t: torch.Tensor, name: str, rows: int) -> torch.Tensor:
+    """[B, T, H, D] as [B T, H, D], without a copy."""
+    if t.dim() == 3:
+        return t
+    try:
+        return t.view(rows, t.shape[2], t.shape[3])
+    except RuntimeError:
+        raise ValueError("%s must have its queries at one stride over the sequences" % name) from None
