@@ -634,15 +634,11 @@ tgl_status tgl_norm_quant(const void *x, int64_t x_stride, const void *residual,
  *   bias      [device] float[n], or NULL
  *   m         >= 0;  n in [1, TGL_MAX_LINEAR_OUT];  k in [1, TGL_MAX_LINEAR_K]
  *   out       [device] m rows of n elements of out_type, out_stride apart
- *   workspace [device] at least tgl_linear_i8_workspace(m, n, k) bytes, 256-byte
- *             aligned (NULL where that is 0)
- * Never synchronises.  Errors: TGL_EINVAL, TGL_ENOSPACE, TGL_EDEVICE.
+ * Never synchronises.  Errors: TGL_EINVAL, TGL_EDEVICE.
  */
-size_t tgl_linear_i8_workspace(int64_t m, int32_t n, int32_t k);
 tgl_status tgl_linear_i8(const int8_t *x, int64_t x_stride, const float *x_scale, int64_t m, const int8_t *w,
                          int64_t w_stride, const float *w_scale, const float *bias, int32_t n, int32_t k,
-                         void *out, int64_t out_stride, int32_t out_type, void *workspace,
-                         size_t workspace_bytes, void *stream);
+                         void *out, int64_t out_stride, int32_t out_type, void *stream);
 
 /*
  * A cache of keys and values in 8 bits, in pages of page_tokens tokens.  The

@@ -43,7 +43,7 @@ EXPORTS = ("tgl_version", "tgl_status_str", "tgl_tcsr_build_workspace", "tgl_tcs
            "tgl_index_len", "tgl_tcsr_nodes", "tgl_tcsr_pack", "tgl_tcsr_unpack", "tgl_sample_capacity", "tgl_sample_workspace", "tgl_sample",
            "tgl_sample_ex", "tgl_sample_noalloc", "tgl_pointers_reset", "tgl_mfg_workspace", "tgl_mfg_export",
            "tgl_gather", "tgl_time_encode",
-           "tgl_norm_quant", "tgl_linear_i8_workspace", "tgl_linear_i8", "tgl_cache_write", "tgl_cache_read",
+           "tgl_norm_quant", "tgl_linear_i8", "tgl_cache_write", "tgl_cache_read",
            "tgl_cache_attend_workspace", "tgl_cache_attend", "tgl_timer_enable",
            "tgl_timer_disable", "tgl_timer_read", "tgl_timer_reset", "tgl_timer_select")
 
@@ -154,10 +154,8 @@ def lib() -> C.CDLL:
     L.tgl_time_encode.argtypes = [P, i64, P, i64, P, P, i32, i32, P, P]
     L.tgl_norm_quant.restype = i32
     L.tgl_norm_quant.argtypes = [P, i64, P, i64, P, i64, i32, i32, i32, f32, P, i64, P, P, i64, P]
-    L.tgl_linear_i8_workspace.restype = C.c_size_t
-    L.tgl_linear_i8_workspace.argtypes = [i64, i32, i32]
     L.tgl_linear_i8.restype = i32
-    L.tgl_linear_i8.argtypes = [P, i64, P, i64, P, i64, P, P, i32, i32, P, i64, i32, P, C.c_size_t, P]
+    L.tgl_linear_i8.argtypes = [P, i64, P, i64, P, i64, P, P, i32, i32, P, i64, i32, P]
     for f in (L.tgl_cache_write, L.tgl_cache_read):
         f.restype = i32
         f.argtypes = [C.POINTER(c_cache), C.POINTER(c_heads), C.POINTER(c_heads), i32, i64, C.POINTER(c_seqs), P]

@@ -137,26 +137,6 @@ __device__ __forceinline__ float load_query(const AttendArgs &a, const T *q, boo
     return unit;
 }
 
-// JV columns of values of a token, as whole dwords.
-template <int JV>
-struct Columns {
-    static constexpr int kWords = JV >= 4 ? JV / 4 : 1;
-    int w[kWords];
-    __device__ __forceinline__ void load(const int8_t *p) {
-        if constexpr (JV == 2) w[0] = *reinterpret_cast<const uint16_t *>(p);
-        if constexpr (JV == 4) w[0] = *reinterpret_cast<const int *>(p);
-        if constexpr (JV == 8) {
-            const i32x2 v = *reinterpret_cast<const i32x2 *>(p);
-            w[0] = v[0];
-            w[1] = v[1];
-        }
-        if constexpr (JV == 16) {
-            const i32x4 v = *reinterpret_cast<const i32x4 *>(p);
-            for (int i = 0; i < 4; i++) w[i] = v[i];
-        }
-    }
-};
-
 // Column jj of a word of two tokens, as f16: (v + 128) 2^-24 -> v 2^-9.
 __device__ __forceinline__ int column_pair(int a, int b, int jj) {
     const unsigned sel = 0x0c000c00u | (static_cast<unsigned>(4 + jj) << 16) | static_cast<unsigned>(jj);
@@ -291,11 +271,8 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
         }
     };
 
-    Step<JV, kWhole> x;
-    int t0 = wave * kTile;
-    if (t0 < n) look_up(t0, x.page);
-    for (; t0 < n; t0 += NW * kTile) {
-        // ---- loads: this step's rows and steps, the next one's pages ----
+    // the rows and steps of the step at t0, whose pages are known
+    auto fetch = [&](int t0, Step<JV, kWhole> &x) {
         if constexpr (kWhole) {
 #pragma unroll
             for (int u = 0; u < 2; u++) {
@@ -325,10 +302,9 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
                 x.vv[k].load(data + static_cast<uint64_t>(at) * pitch + block + ((c0r + t0 + from) & pmask) * width + vcol);
             }
         }
-        int next_page[kWhole ? 2 : 1];
-        look_up(t0 + NW * kTile, next_page);
-        __builtin_amdgcn_sched_barrier(0);
+    };
 
+    auto multiply = [&](int t0, Step<JV, kWhole> &x) {
         // ---- steps of the lane's 8 tokens, which of them nobody sees ----
         int bad = 0;
         float ks[8], vs[8];
@@ -451,8 +427,49 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
                     o[y][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, lo[y]), o[y][j], 0, 0, 0);
             }
         }
+    };
+
+    constexpr int kNext = NW * kTile;
+    constexpr bool kAhead = R == 2 && kWhole && !(JV == 8 && N == 3);      // as far as registers go
+    int t0 = wave * kTile;
+    if (t0 < n) {
+        if constexpr (!kAhead) {
+            // the next step's pages are looked up while this one's rows come;
+            // other wavefronts hide the rows' latency
+            Step<JV, kWhole> x;
+            look_up(t0, x.page);
+            for (; t0 < n; t0 += kNext) {
+                fetch(t0, x);
+                int page[kWhole ? 2 : 1];
+                look_up(t0 + kNext, page);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(t0, x);
 #pragma unroll
-        for (int u = 0; u < (kWhole ? 2 : 1); u++) x.page[u] = next_page[u];
+                for (int u = 0; u < (kWhole ? 2 : 1); u++) x.page[u] = page[u];
+            }
+        } else {
+            // two wavefronts a SIMD hide little: rows come a step ahead, too
+            Step<JV, kWhole> x, y;
+            look_up(t0, x.page);
+            fetch(t0, x);
+            look_up(t0 + kNext, y.page);
+            for (; t0 < n; t0 += 2 * kNext) {
+                fetch(t0 + kNext, y);
+                int page[kWhole ? 2 : 1];
+                look_up(t0 + 2 * kNext, page);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(t0, x);
+#pragma unroll
+                for (int u = 0; u < (kWhole ? 2 : 1); u++) x.page[u] = page[u];
+                if (t0 + kNext >= n) break;
+                fetch(t0 + 2 * kNext, x);
+                look_up(t0 + 3 * kNext, page);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(t0 + kNext, y);
+#pragma unroll
+                for (int u = 0; u < (kWhole ? 2 : 1); u++) y.page[u] = page[u];
+            }
+        }
     }
 
     // ---- join the lanes of a row, then the wavefronts ----

@@ -210,9 +210,10 @@ __device__ __forceinline__ int64_t last_at_most(const SeqsView &s, int64_t token
 }
 
 // A workgroup takes block_tokens tokens in turn: a thread each looks one up,
-// then all stream its heads, eight elements of keys and of values a lane.
+// then all stream its heads, 16 bytes of keys and of values a lane.
 template <class T>
 __global__ __launch_bounds__(kBlock) void read_kernel(const IoArgs a) {
+    constexpr int kRead = 16 / sizeof(T);       // elements of a lane's stores
     __shared__ int at_page[kBlock];
     __shared__ int at_row[kBlock];
     __shared__ int64_t ends[2];
@@ -263,26 +264,26 @@ __global__ __launch_bounds__(kBlock) void read_kernel(const IoArgs a) {
             const int t = a.row_runs(n);
             const int rest = n - t * a.row_runs.d;
             const int head = a.runs(rest);
-            const int d = (rest - head * a.runs.d) * kRun;
+            const int d = (rest - head * a.runs.d) * kRead;
             const int page = at_page[t];
             if (page == -2) continue;
             const int own = page < 0 ? 0 : page;
-            i32x2 kq = {0, 0}, vq = {0, 0};
+            Columns<kRead> kq = {}, vq = {};
             float2 s = {0.0f, 0.0f};
             if (c.pages > 0) {
                 const int8_t *q = c.rows(own, head, 0) + at_row[t] * c.width + d;
-                kq = *reinterpret_cast<const i32x2 *>(q);
-                vq = *reinterpret_cast<const i32x2 *>(q + c.block_bytes());
+                kq.load(q);
+                vq.load(q + c.block_bytes());
                 s = *reinterpret_cast<const float2 *>(c.scale(own, head, 0));
             }
-            float k[kRun], v[kRun];
+            float k[kRead], v[kRead];
 #pragma unroll
-            for (int e = 0; e < kRun; e++) {
-                k[e] = page < 0 ? 0.0f : static_cast<float>(static_cast<int8_t>(kq[e / 4] >> (8 * (e % 4)))) * s.x;
-                v[e] = page < 0 ? 0.0f : static_cast<float>(static_cast<int8_t>(vq[e / 4] >> (8 * (e % 4)))) * s.y;
+            for (int e = 0; e < kRead; e++) {
+                k[e] = page < 0 ? 0.0f : static_cast<float>(static_cast<int8_t>(kq.w[e / 4] >> (8 * (e % 4)))) * s.x;
+                v[e] = page < 0 ? 0.0f : static_cast<float>(static_cast<int8_t>(vq.w[e / 4] >> (8 * (e % 4)))) * s.y;
             }
-            store_columns<T, kRun>(static_cast<T *>(a.k) + (base + t) * a.kt + head * a.kh, d, c.dim, k);
-            store_columns<T, kRun>(static_cast<T *>(a.v) + (base + t) * a.vt + head * a.vh, d, c.dim, v);
+            store_columns<T, kRead, true>(static_cast<T *>(a.k) + (base + t) * a.kt + head * a.kh, d, c.dim, k);
+            store_columns<T, kRead, true>(static_cast<T *>(a.v) + (base + t) * a.vt + head * a.vh, d, c.dim, v);
         }
     }
 }
@@ -365,7 +366,8 @@ tgl_status tgl_cache_read(const tgl_cache *cache, const tgl_heads *k, const tgl_
     if (num_tokens == 0 || seqs->num_seqs == 0) return TGL_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();
-    a.runs = Div((a.c.dim + kRun - 1) / kRun);
+    const int run = 16 / static_cast<int>(elem_size(out_type));
+    a.runs = Div((a.c.dim + run - 1) / run);
     a.row_runs = Div(a.runs.d * a.c.heads);
     // tokens of a workgroup: about 16 runs a thread, fewer where that would leave compute units idle
     int64_t tokens = 16 * kBlock / a.row_runs.d;

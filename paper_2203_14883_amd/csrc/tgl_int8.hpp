@@ -86,20 +86,46 @@ __device__ __forceinline__ void load_columns(const T *q, int d, int dim, float (
     }
 }
 
-// N consecutive elements from column d on, as far as there are columns.
-template <class T, int N>
+// N consecutive elements from column d on, as far as there are columns; kStream:
+// N are 16 bytes that nothing nearby reads again.
+template <class T, int N, bool kStream = false>
 __device__ __forceinline__ void store_columns(T *out, int d, int dim, const float (&x)[N]) {
     if (d + N <= dim) {
         Run<T, N> w;
 #pragma unroll
         for (int i = 0; i < N; i++) w.t[i] = from_float<T>(x[i]);
-        *reinterpret_cast<Run<T, N> *>(out + d) = w;
+        if constexpr (kStream) {
+            using word_t = i32x4 __attribute__((aligned(alignof(T))));
+            __builtin_nontemporal_store(__builtin_bit_cast(i32x4, w), reinterpret_cast<word_t *>(out + d));
+        } else {
+            *reinterpret_cast<Run<T, N> *>(out + d) = w;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < N; i++)
             if (d + i < dim) out[d + i] = from_float<T>(x[i]);
     }
 }
+
+// JV bytes of a row (a multiple of JV from its start), as whole dwords.
+template <int JV>
+struct Columns {
+    static constexpr int kWords = JV >= 4 ? JV / 4 : 1;
+    int w[kWords];
+    __device__ __forceinline__ void load(const int8_t *p) {
+        if constexpr (JV == 2) w[0] = *reinterpret_cast<const uint16_t *>(p);
+        if constexpr (JV == 4) w[0] = *reinterpret_cast<const int *>(p);
+        if constexpr (JV == 8) {
+            const i32x2 v = *reinterpret_cast<const i32x2 *>(p);
+            w[0] = v[0];
+            w[1] = v[1];
+        }
+        if constexpr (JV == 16) {
+            const i32x4 v = *reinterpret_cast<const i32x4 *>(p);
+            for (int i = 0; i < 4; i++) w[i] = v[i];
+        }
+    }
+};
 
 // Four numbers in units of a step, as the bytes of a word.  Adding 1.5 * 2^23
 // rounds a number to whole ones (ties to even, as rint does) and leaves it in

@@ -282,17 +282,9 @@ using namespace tgl;
 
 extern "C" {
 
-size_t tgl_linear_i8_workspace(int64_t m, int32_t n, int32_t k) {
-    (void)m;
-    (void)n;
-    (void)k;
-    return 0;
-}
-
 tgl_status tgl_linear_i8(const int8_t *x, int64_t x_stride, const float *x_scale, int64_t m, const int8_t *w,
                          int64_t w_stride, const float *w_scale, const float *bias, int32_t n, int32_t k,
-                         void *out, int64_t out_stride, int32_t out_type, void *workspace,
-                         size_t workspace_bytes, void *stream) {
+                         void *out, int64_t out_stride, int32_t out_type, void *stream) {
     if (m < 0 || n < 1 || n > TGL_MAX_LINEAR_OUT || k < 1 || k > TGL_MAX_LINEAR_K || !is_elem_type(out_type))
         return TGL_EINVAL;
     if (!aligned(x, 16) || !aligned(w, 16) || x_stride % 16 != 0 || w_stride % 16 != 0 || x_stride < 0 || w_stride < 0 ||
@@ -301,8 +293,6 @@ tgl_status tgl_linear_i8(const int8_t *x, int64_t x_stride, const float *x_scale
     if (!aligned(x_scale, 4) || !aligned(w_scale, 4) || !aligned(bias, 4) || !aligned(out, elem_size(out_type)))
         return TGL_EINVAL;
     if (m > 0 && (!x || !x_scale || !w || !w_scale || !out || out_stride < n)) return TGL_EINVAL;
-    if (workspace_bytes < tgl_linear_i8_workspace(m, n, k)) return TGL_ENOSPACE;
-    (void)workspace;
     if (m == 0) return TGL_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();

@@ -193,16 +193,12 @@ def linear_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: 
         if om != m or on != n or (m > 1 and ostride < n):
             raise ValueError("out must be [%d, %d]" % (m, n))
     ot = _type(out_dtype, "the output")
-    L = lib()
-    need = L.tgl_linear_i8_workspace(m, n, k)
-    with _on(stream):
-        if out is None:
+    if out is None:
+        with _on(stream):
             out = x_scale.new_empty((m, n), dtype=out_dtype)
-        ws_mem = x.new_empty(need, dtype=torch.uint8) if need else None
     if m:
-        s = L.tgl_linear_i8(x.data_ptr(), xstride, xs, m, w.data_ptr(), wstride, ws, b, n, k, out.data_ptr(),
-                            ostride if ostride > n else n, ot, None if ws_mem is None else ws_mem.data_ptr(), need,
-                            _raw_stream(stream, dev))
+        s = lib().tgl_linear_i8(x.data_ptr(), xstride, xs, m, w.data_ptr(), wstride, ws, b, n, k, out.data_ptr(),
+                            ostride if ostride > n else n, ot, _raw_stream(stream, dev))
         if s:
             _check(s, "tgl_linear_i8")
     return out
