@@ -37,6 +37,8 @@ constexpr int kRows = 16;           // rows of a tile
 constexpr int kTile = 32;           // tokens of a wavefront's step
 constexpr float kLog2E = 1.44269504088896340736f;
 
+enum Order { kInTurn, kHeadsInTurn, kStretches };
+
 struct AttendArgs {
     CacheView c;
     SeqsView s;
@@ -59,19 +61,24 @@ struct AttendArgs {
     Div heads;
     Div group;              // query heads of one head of the cache
     Div row_of;             // rows of one sequence and head
-    int32_t spread;         // how workgroups go to the dies: see die_order
+    int32_t order;          // of the workgroups: see die_order
     float scale;
 };
 
-// The unit of work of a workgroup.  Workgroups go to the 8 dies in turn.  Row
-// tiles of one head read the same tokens, so with several of them each die
-// gets a contiguous stretch of the work and its L2 serves them; without, the
-// order as it is spreads long and short sequences evenly.
+// The unit of work of a workgroup: a row tile, fastest, of a sequence's head's
+// chunk.  Workgroups go to the 8 dies in turn.  Row tiles of one head read the
+// same tokens, so all of them go to one die, whose L2 then serves them: heads
+// in turn (the dies get long and short sequences alike), or, where that would
+// leave dies with less, a contiguous stretch of the work each.
 __device__ __forceinline__ uint32_t die_order(const AttendArgs &a) {
-    if (!a.spread) return blockIdx.x;
+    if (a.order == kInTurn) return blockIdx.x;
+    const uint32_t die = blockIdx.x & 7, at = blockIdx.x >> 3;
+    if (a.order == kHeadsInTurn) {
+        const uint32_t head = a.tiles(at);
+        return (head * 8 + die) * a.tiles.d + (at - head * a.tiles.d);      // beyond the work for the last heads
+    }
     const uint32_t per = (a.work + 7) / 8;
-    const uint32_t at = blockIdx.x >> 3;
-    return at >= per ? a.work : (blockIdx.x & 7) * per + at;
+    return at >= per ? a.work : die * per + at;
 }
 
 template <class T>
@@ -114,7 +121,8 @@ __device__ __forceinline__ float load_query(const AttendArgs &a, const T *q, boo
     constexpr float kUnits = N == 2 ? 127.0f * 256.0f : 127.0f * 65536.0f;
     // not finite: a NaN unit makes the row NaN; tiny: zeros
     const float unit = bits >= 0x7f800000u ? __builtin_nanf("") : top < kTiny ? 0.0f : top * (1.0f / kUnits);
-    const float inv = there ? inverse_step(unit) : 0.0f;
+    const float size = there ? inverse_step(unit) : 0.0f;
+    const float inv = a.scale < 0.0f ? -size : size;     // the sign of the scale goes into the bytes
 #pragma unroll
     for (int kk = 0; kk < KK; kk++) {
 #pragma unroll
@@ -148,6 +156,14 @@ __device__ __forceinline__ int column_pair(int a, int b, int jj) {
 
 __device__ __forceinline__ int pack_f16(float a, float b) {
     return __builtin_bit_cast(int, f16x2{static_cast<_Float16>(a), static_cast<_Float16>(b)});
+}
+
+// The value, as if computed here: an address made of a uniform pointer and a
+// 32-bit offset of the lane is one operand each only where the compiler sees
+// that the offset has 32 bits, not where it has moved that out of a loop over t.
+__device__ __forceinline__ uint32_t here(uint32_t v, int t) {
+    asm("" : "+v"(v) : "s"(t));
+    return v;
 }
 
 __device__ __forceinline__ int clamp_to(int64_t v, int most) {
@@ -226,7 +242,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
         row_end = row_end > all ? all : row_end;
         last[y] = clamp_to(row_end - c0, n);
         const float unit = load_query<T, KK>(a, static_cast<const T *>(a.q) + q_row[y] * a.qt + q_head[y] * a.qh, there[y], lane, qp[y]);
-        to_log2[y] = unit * a.scale * kLog2E;
+        to_log2[y] = unit * fabsf(a.scale) * kLog2E;
     }
 
     f32x4 o[R][JV];
@@ -255,6 +271,12 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
     for (int kk = 0; kk < KK; kk++) kcol[kk] = 64 * kk + 16 * g < static_cast<int>(width) - 16 ? 64 * kk + 16 * g : width - 16;
     const uint32_t vcol = JV * i16 < static_cast<int>(width) - JV ? JV * i16 : width - JV;
 
+    uint32_t kat[KK], vat[4];                                   // places in a half step whose rows are one after another
+#pragma unroll
+    for (int kk = 0; kk < KK; kk++) kat[kk] = i16 * width + kcol[kk];
+#pragma unroll
+    for (int i = 0; i < 4; i++) vat[i] = (4 * g + i) * width + vcol;
+
     // the pages of the step at t0 (whose table entries exist up to token n - 1)
     auto look_up = [&](int t0, int (&page)[kWhole ? 2 : 1]) {
         if constexpr (kWhole) {
@@ -280,10 +302,10 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
                 x.sc[u] = steps[static_cast<uint64_t>(at) * a.heads.d];
                 const int8_t *kb = data + static_cast<uint64_t>(at) * pitch + ((c0r + t0 + 16 * u) & pmask) * width;
 #pragma unroll
-                for (int kk = 0; kk < KK; kk++) x.kv[u][kk] = *reinterpret_cast<const i32x4 *>(kb + (i16 * width + kcol[kk]));
+                for (int kk = 0; kk < KK; kk++) x.kv[u][kk] = *reinterpret_cast<const i32x4 *>(kb + here(kat[kk], t0));
                 const int8_t *vb = kb + block;
 #pragma unroll
-                for (int i = 0; i < 4; i++) x.vv[4 * u + i].load(vb + ((4 * g + i) * width + vcol));
+                for (int i = 0; i < 4; i++) x.vv[4 * u + i].load(vb + here(vat[i], t0));
             }
         } else {
             const uint32_t own = x.page[0] < 0 ? 0 : x.page[0];
@@ -344,11 +366,14 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
             inv = 1.0f / big;
         }
 
+        float vw[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++) vw[k] = vs[k] * inv;
         i32x4 hi[R], lo[R];
 #pragma unroll
         for (int y = 0; y < R; y++) {
-            // ---- scores, in powers of two ----
-            float s[8];
+            // ---- dots; a score, in powers of two, is dot * unit, unit >= 0 ----
+            float dot[8], unit[8];
 #pragma unroll
             for (int u = 0; u < 2; u++) {
                 i32x4 acc[N];
@@ -361,9 +386,10 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
                 }
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
-                    float dot = static_cast<float>(acc[0][i] * 256 + acc[1][i]);
-                    if constexpr (N == 3) dot = __builtin_fmaf(dot, 256.0f, static_cast<float>(acc[2][i]));
-                    s[4 * u + i] = dot * (ks[4 * u + i] * to_log2[y]);
+                    float d = static_cast<float>(acc[0][i] * 256 + acc[1][i]);
+                    if constexpr (N == 3) d = __builtin_fmaf(d, 256.0f, static_cast<float>(acc[2][i]));
+                    dot[4 * u + i] = d;
+                    unit[4 * u + i] = ks[4 * u + i] * to_log2[y];
                 }
             }
             int hide = bad;
@@ -372,11 +398,19 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
                 for (int k = 0; k < 8; k++) {
                     const int p = t0 + 16 * (k >> 2) + 4 * g + (k & 3);
                     if (p < first || p >= last[y]) hide |= 1 << k;
-                    if ((hide >> k) & 1) s[k] = -INFINITY;
+                    if ((hide >> k) & 1) dot[k] = -INFINITY;
                 }
             }
-            // ---- the running maximum ----
-            float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+            // ---- the running maximum (of nothing where -inf meets a unit of 0: NaN, which fmaxf drops) ----
+            float top;
+            if constexpr (kWhole) {                             // one unit for each half
+                top = fmaxf(fmaxf(fmaxf(dot[0], dot[1]), fmaxf(dot[2], dot[3])) * unit[0],
+                            fmaxf(fmaxf(dot[4], dot[5]), fmaxf(dot[6], dot[7])) * unit[4]);
+            } else {
+                top = dot[0] * unit[0];
+#pragma unroll
+                for (int k = 1; k < 8; k++) top = fmaxf(top, dot[k] * unit[k]);
+            }
             if (__ballot(top > m[y] + kSlack<T>)) {
                 top = fmaxf(top, __shfl_xor(top, 16, kWave));
                 top = fmaxf(top, __shfl_xor(top, 32, kWave));
@@ -392,9 +426,11 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
             float w[8];
 #pragma unroll
             for (int k = 0; k < 8; k++) {
-                const float p = __builtin_amdgcn_exp2f(s[k] - from);
+                float e = __builtin_fmaf(dot[k], unit[k], -from);
+                if (masked) e = (hide >> k) & 1 ? -INFINITY : e;
+                const float p = __builtin_amdgcn_exp2f(e);
                 l[y] += p;
-                w[k] = p * (vs[k] * inv);
+                w[k] = p * vw[k];
             }
             if (masked) {
 #pragma unroll
@@ -830,7 +866,8 @@ Plan plan_of(const CacheView &c, int64_t num_seqs, int32_t pages_per_seq, int32_
 
 template <class T, int JV, bool kWhole>
 void launch(const AttendArgs &a, int nw, hipStream_t st) {
-    const unsigned grid = (a.work + 7) / 8 * 8;
+    // whole turns of the dies, of heads or of workgroups
+    const unsigned grid = a.order == kHeadsInTurn ? (a.work / a.tiles.d + 7) / 8 * 8 * a.tiles.d : (a.work + 7) / 8 * 8;
     if constexpr (JV < 16) {
         if (a.tile_rows > kRows) {
             attend_kernel<T, JV, kWhole, 4, 2><<<grid, 4 * kWave, 0, st>>>(a);
@@ -939,7 +976,7 @@ tgl_status tgl_cache_attend(const tgl_cache *cache, const tgl_heads *q, int32_t 
         return launch_status();
     }
     const int64_t work = seqs->num_seqs * a.c.heads * p.row_tiles * p.chunks;
-    if (work > 0x7ffffff0) return TGL_EINVAL;
+    if (work > 0x7fffff00 - 8 * p.row_tiles) return TGL_EINVAL;
     a.rows = static_cast<uint32_t>(queries * group);
     a.row_of = Div(a.rows);
     a.all_rows = a.rows * a.s.seqs * a.c.heads;
@@ -950,7 +987,8 @@ tgl_status tgl_cache_attend(const tgl_cache *cache, const tgl_heads *q, int32_t 
     a.chunks = static_cast<uint32_t>(p.chunks);
     a.items = Div(static_cast<uint32_t>(seqs->num_seqs * a.c.heads));
     a.heads = Div(a.c.heads);
-    a.spread = p.row_tiles > 1;
+    const int64_t units = seqs->num_seqs * a.c.heads * p.chunks;
+    a.order = p.row_tiles == 1 ? kInTurn : units >= 32 || units % 8 == 0 ? kHeadsInTurn : kStretches;
     if (p.part_o) {
         a.part_o = static_cast<float *>(workspace);
         a.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + p.part_o);
