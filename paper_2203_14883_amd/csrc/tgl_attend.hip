@@ -466,7 +466,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
     };
 
     constexpr int kNext = NW * kTile;
-    constexpr bool kAhead = R == 2 && kWhole && !(JV == 8 && N == 3);      // as far as registers go
+    constexpr bool kAhead = kWhole && JV < 16 && !(JV == 8 && N == 3);      // as far as registers go
     int t0 = wave * kTile;
     if (t0 < n) {
         if constexpr (!kAhead) {

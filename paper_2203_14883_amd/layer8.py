@@ -12,7 +12,6 @@ made on another stream must be ready, as for every call of the library.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import math
 from dataclasses import dataclass, field
@@ -35,11 +34,12 @@ def _round16(n: int) -> int:
     return (n + 15) & ~15
 
 
-_HERE = contextlib.nullcontext()
-
-
-def _on(stream):
-    return _HERE if stream is None else torch.cuda.stream(stream)
+def _empty(like: torch.Tensor, shape, dtype, stream) -> torch.Tensor:
+    """Memory for a call on that stream (None: the current one)."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _raw_stream(stream, dev: int) -> int:
@@ -118,12 +118,11 @@ def _quantise(x, weight, residual, normalize, eps, stream, out):
             if n > 1 and os < dim:
                 raise ValueError("out's rows overlap")
     width = _round16(dim)
-    with _on(stream):
-        store = x.new_empty((n, width), dtype=torch.int8)
-        scale = x.new_empty(n, dtype=torch.float32)
-        if out is None and residual is not None:
-            out = x.new_empty((n, dim))
-            os = dim
+    store = _empty(x, (n, width), torch.int8, stream)
+    scale = _empty(x, (n,), torch.float32, stream)
+    if out is None and residual is not None:
+        out = _empty(x, (n, dim), x.dtype, stream)
+        os = dim
     if n:
         s = lib().tgl_norm_quant(x.data_ptr(), xs, None if residual is None else residual.data_ptr(), rs, w, n, dim, dt,
                                  normalize, eps, store.data_ptr(), width, scale.data_ptr(),
@@ -163,7 +162,7 @@ def _int8_rows(t: torch.Tensor, name: str, dev: int):
     if m < 2:
         stride = _round16(k)
     if m and (stride & 15 or t.data_ptr() & 15 or stride < 0
-              or t.storage_offset() + (m - 1) * stride + _round16(k) > t.untyped_storage().nbytes()):
+              or (k & 15 and t.storage_offset() + (m - 1) * stride + _round16(k) > t.untyped_storage().nbytes())):
         raise ValueError("%s must have rows at multiples of 16 bytes, padded to 16 bytes (as quant_rows and norm_quant "
                          "make them)" % name)
     return m, k, stride
@@ -194,8 +193,7 @@ def linear_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: 
             raise ValueError("out must be [%d, %d]" % (m, n))
     ot = _type(out_dtype, "the output")
     if out is None:
-        with _on(stream):
-            out = x_scale.new_empty((m, n), dtype=out_dtype)
+        out = _empty(x, (m, n), out_dtype, stream)
     if m:
         s = lib().tgl_linear_i8(x.data_ptr(), xstride, xs, m, w.data_ptr(), wstride, ws, b, n, k, out.data_ptr(),
                             ostride if ostride > n else n, ot, _raw_stream(stream, dev))
@@ -339,9 +337,8 @@ def cache_read(cache: HistoryCache, table: torch.Tensor, start: Optional[torch.T
         raise ValueError("k and v go together, with one type")
     if k is None:
         ot = _type(out_dtype, "the output")
-        with _on(stream):
-            k = cache.scales.new_empty((n, view.heads, view.dim), dtype=out_dtype)
-            v = cache.scales.new_empty((n, view.heads, view.dim), dtype=out_dtype)
+        k = _empty(cache.data, (n, view.heads, view.dim), out_dtype, stream)
+        v = _empty(cache.data, (n, view.heads, view.dim), out_dtype, stream)
     else:
         ot = _type(k.dtype, "k")
         _also(k, "k", dev)
@@ -392,11 +389,10 @@ def cache_attend(cache: HistoryCache, q: torch.Tensor, table: torch.Tensor, begi
     L = lib()
     need = L.tgl_cache_attend_workspace(C.byref(view), C.byref(sq), H, T)
     given = out is not None
-    with _on(stream):
-        if not given:
-            out = q.new_empty(shape)
-        lse = q.new_empty(shape[:-1], dtype=torch.float32) if return_lse else None
-        ws = q.new_empty(need, dtype=torch.uint8) if need else None
+    if not given:
+        out = _empty(q, shape, q.dtype, stream)
+    lse = _empty(q, shape[:-1], torch.float32, stream) if return_lse else None
+    ws = _empty(q, (need,), torch.uint8, stream) if need else None
     if given:
         if out.dtype != q.dtype or out.shape != shape:
             raise ValueError("out must have q's type and shape")
