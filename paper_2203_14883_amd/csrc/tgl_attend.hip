@@ -706,19 +706,6 @@ __device__ __forceinline__ int from_lane(int v) {
     return __builtin_amdgcn_ds_swizzle(v, (J << 5) | 0x10);
 }
 
-// f(0), f(1), ... f(N - 1) with constant arguments.
-template <int K>
-struct Const {
-    static constexpr int value = K;
-};
-template <int N, int K = 0, class F>
-__device__ __forceinline__ void unrolled(const F &f) {
-    if constexpr (K < N) {
-        f(Const<K>());
-        unrolled<N, K + 1>(f);
-    }
-}
-
 template <class T, int JV>
 __global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(const AttendArgs a) {
     constexpr int kWords = JV / 4;

@@ -61,6 +61,21 @@ __device__ __forceinline__ float group_sum(float v) {
     return v;
 }
 
+// ---- loops over constants ----
+
+// f(0), f(1), ... f(N - 1) with constant arguments.
+template <int K>
+struct Const {
+    static constexpr int value = K;
+};
+template <int N, int K = 0, class F>
+__device__ __forceinline__ void unrolled(const F &f) {
+    if constexpr (K < N) {
+        f(Const<K>());
+        unrolled<N, K + 1>(f);
+    }
+}
+
 // ---- wide accesses ----
 
 // N consecutive elements that need not lie at a multiple of their size: one

@@ -54,53 +54,86 @@ __device__ __forceinline__ void finish(const LinearArgs &a, int64_t row, int j, 
 
 // ---- small products: operands straight from memory --------------------------
 
-// A workgroup per 16 rows and 16 columns, whose wavefronts take 64 of k in turn
-// and add up through LDS.
-template <class T, int NW>
+// A workgroup per 16 MT rows and 16 columns, whose wavefronts take 64 of k in
+// turn and add up through LDS: a row of w is read once for 16 MT rows of x.
+template <class T, int NW, int MT>
 __global__ __launch_bounds__(NW * kWave) void linear_small_kernel(const LinearArgs a) {
-    __shared__ i32x4 sums[NW > 1 ? NW - 1 : 1][kWave];
+    __shared__ i32x4 sums[NW > 1 ? NW : 1][MT][kWave];
     const int lane = lane_id();
     const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const uint32_t tm = a.tiles_n(blockIdx.x), tn = blockIdx.x - tm * a.tiles_n.d;
-    const int64_t m0 = static_cast<int64_t>(tm) * 16;
+    const int64_t m0 = static_cast<int64_t>(tm) * (16 * MT);
     const int n0 = tn * 16;
-    const int64_t mr = m0 + (lane & 15) < a.m ? m0 + (lane & 15) : a.m - 1;
     const int nr = n0 + (lane & 15) < a.n ? n0 + (lane & 15) : a.n - 1;
-    const int8_t *x = a.x + mr * a.xstride;
     const int8_t *w = a.w + nr * a.wstride;
-    i32x4 acc = {0, 0, 0, 0};
-    for (int k = wave * 64; k < a.k; k += NW * 64) {
+    const int8_t *x[MT];
+    i32x4 acc[MT];
+#pragma unroll
+    for (int i = 0; i < MT; i++) {
+        const int64_t mr = m0 + 16 * i + (lane & 15);
+        x[i] = a.x + (mr < a.m ? mr : a.m - 1) * a.xstride;
+        acc[i] = i32x4{0, 0, 0, 0};
+    }
+    // whole steps of 64 with nothing to check, then the rest of k
+    const int whole = a.k & ~63;
+    constexpr int kUnroll = MT == 1 ? 4 : 2;
+    int k = wave * 64;
+    for (; k + (kUnroll - 1) * NW * 64 < whole; k += kUnroll * NW * 64) {
+        i32x4 wv[kUnroll], xv[kUnroll][MT];
+#pragma unroll
+        for (int u = 0; u < kUnroll; u++) {
+            const int c = k + u * NW * 64 + 16 * (lane >> 4);
+            wv[u] = *reinterpret_cast<const i32x4 *>(w + c);
+#pragma unroll
+            for (int i = 0; i < MT; i++) xv[u][i] = *reinterpret_cast<const i32x4 *>(x[i] + c);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; u++)
+#pragma unroll
+            for (int i = 0; i < MT; i++) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[u], xv[u][i], acc[i], 0, 0, 0);
+    }
+    for (; k < a.k; k += NW * 64) {
         const int c = k + 16 * (lane >> 4);
         const i32x4 wv = load_piece(w, c, a.k);
-        const i32x4 xv = mask_piece(load_piece(x, c, a.k), c, a.k);
-        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv, xv, acc, 0, 0, 0);
-    }
-    if constexpr (NW > 1) {
-        if (wave > 0) sums[wave - 1][lane] = acc;
-        __syncthreads();
-        if (wave > 0) return;
 #pragma unroll
-        for (int y = 1; y < NW; y++) acc += sums[y - 1][lane];
+        for (int i = 0; i < MT; i++)
+            acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv, mask_piece(load_piece(x[i], c, a.k), c, a.k), acc[i], 0, 0, 0);
     }
     const int j = n0 + 4 * (lane >> 4);
-    if (m0 + (lane & 15) >= a.m || j >= a.n) return;
-    int sum[4];
     float ws[4], bias[4];
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-        sum[i] = acc[i];
         const int col = j + i < a.n ? j + i : a.n - 1;
         ws[i] = a.ws[col];
         bias[i] = a.bias ? a.bias[col] : 0.0f;
     }
-    finish<T, 4>(a, mr, j, sum, ws, bias);
+    auto put = [&](int i, const i32x4 &v) {
+        const int64_t row = m0 + 16 * i + (lane & 15);
+        if (row >= a.m || j >= a.n) return;
+        const int sum[4] = {v[0], v[1], v[2], v[3]};
+        finish<T, 4>(a, row, j, sum, ws, bias);
+    };
+    if constexpr (NW == 1) {
+#pragma unroll
+        for (int i = 0; i < MT; i++) put(i, acc[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < MT; i++) sums[wave][i][lane] = acc[i];
+        __syncthreads();
+        for (int i = wave; i < MT; i += NW) {       // a wavefront finishes a row tile
+            i32x4 v = sums[0][i][lane];
+#pragma unroll
+            for (int y = 1; y < NW; y++) v += sums[y][i][lane];
+            put(i, v);
+        }
+    }
 }
 
 // ---- large products: tiles through LDS --------------------------------------
 //
-// A workgroup owns BM x BN outputs and walks k in steps of 128: the step's
-// BM + BN rows of 128 bytes go straight from memory to one of two LDS buffers
-// while the other is multiplied.  A wavefront owns 64 columns and MT x 16 rows;
+// A workgroup owns BM x BN outputs and walks k in steps of 128: a step's
+// BM + BN rows of 128 bytes go straight from memory to one of S LDS buffers,
+// S - 1 steps ahead of the one that is multiplied.  A wavefront owns 64 columns and MT x 16 rows;
 // the weights are the first operand, so that a lane ends up with columns of
 // one row, and its four tiles' rows of w are picked so that these are 16
 // consecutive ones: 4 of each (lane / 16) * 16 + 4 tile + 0..3.
@@ -117,14 +150,17 @@ __device__ __forceinline__ int swizzle_w(int r) { return ((r >> 1) & 1) | (((r >
 
 using lds_t = __attribute__((address_space(3))) void;
 
-template <class T, int BM, int BN, int MT, bool kTail>
-__global__ __launch_bounds__(BM / (16 * MT) * (BN / 64) * kWave, (MT == 8 ? 2 : 2)) void linear_tile_kernel(const LinearArgs a) {
+template <class T, int BM, int BN, int MT, int S, bool kTail>
+__global__ __launch_bounds__(BM / (16 * MT) * (BN / 64) * kWave, 2) void linear_tile_kernel(const LinearArgs a) {
     constexpr int kWaves = BM / (16 * MT) * (BN / 64);
     constexpr int kRowsPerWave = (BM + BN) / kWaves;        // rows of a step that a wavefront fetches, all of w or all of x
     constexpr int kFetch = kRowsPerWave / 8;
     static_assert(BN % kRowsPerWave == 0, "a wavefront fetches rows of one operand");
+    // one object each: so the compiler sees that a step's reads do not wait for the others' loads
     __shared__ __attribute__((aligned(1024))) int8_t buf0[(BM + BN) * kStepK];
     __shared__ __attribute__((aligned(1024))) int8_t buf1[(BM + BN) * kStepK];
+    __shared__ __attribute__((aligned(1024))) int8_t buf2[S > 2 ? (BM + BN) * kStepK : 16];
+    __shared__ __attribute__((aligned(1024))) int8_t buf3[S > 3 ? (BM + BN) * kStepK : 16];
     const int lane = lane_id();
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int g = lane >> 4, i16 = lane & 15;
@@ -202,23 +238,39 @@ __global__ __launch_bounds__(BM / (16 * MT) * (BN / 64) * kWave, (MT == 8 ? 2 : 
                 for (int j = 0; j < 4; j++) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[j], xv[i], acc[i][j], 0, 0, 0);
         }
     };
-    // loads to LDS count as loads from memory: each wavefront waits for its own,
-    // then for the others
+    // Loads to LDS count as loads from memory: each wavefront waits for its own
+    // of a step, leaving the S - 2 later steps' on their way, then for the
+    // others.  Steps beyond k are fetched too (nothing but zeros, from no
+    // memory), so that there are always as many.
+    constexpr int kLeft = (S - 2) * kFetch;
+    static_assert(kLeft < 64, "the counter has six bits");
     auto meet = [] {
-        __builtin_amdgcn_s_waitcnt(0x0f70);                 // vmcnt(0)
-        __syncthreads();
+        // __syncthreads and fences would wait for every load: the wait and the
+        // barrier by themselves, with nothing moved across them
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070 | (kLeft & 15) | ((kLeft >> 4) << 14));      // vmcnt(kLeft), lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     };
-    fetch(buf0, 0);
-    for (int step = 0; step < steps; step += 2) {
-        meet();                                             // buf0 is there, buf1 free
-        if (step + 1 < steps) fetch(buf1, step + 1);
-        multiply(buf0, step);
-        meet();
-        if (step + 1 < steps) {
-            if (step + 2 < steps) fetch(buf0, step + 2);
-            multiply(buf1, step + 1);
-        }
+    auto buffer = [&](auto I) -> int8_t * {
+        constexpr int i = decltype(I)::value % S;
+        if constexpr (i == 0) return buf0;
+        else if constexpr (i == 1) return buf1;
+        else if constexpr (i == 2) return buf2;
+        else return buf3;
+    };
+    unrolled<S - 1>([&](auto I) { fetch(buffer(I), decltype(I)::value); });
+    for (int step = 0; step < steps; step += S) {
+        unrolled<S>([&](auto I) {
+            constexpr int i = decltype(I)::value;
+            if (step + i < steps) {
+                meet();                                     // this step's buffer is there, the one before free
+                fetch(buffer(Const<i + S - 1>()), step + i + S - 1);
+                multiply(buffer(I), step + i);
+            }
+        });
     }
+    __builtin_amdgcn_s_waitcnt(0x0f70);                     // nothing goes to LDS once it is another workgroup's
 
     const int j0 = n0 + wn * 64 + 16 * g;
     if (j0 >= a.n) return;
@@ -243,7 +295,7 @@ __global__ __launch_bounds__(BM / (16 * MT) * (BN / 64) * kWave, (MT == 8 ? 2 : 
     }
 }
 
-template <class T, int BM, int BN, int MT>
+template <class T, int BM, int BN, int MT, int S>
 void launch_tiles(LinearArgs a, hipStream_t st) {
     constexpr int kThreads = BM / (16 * MT) * (BN / 64) * kWave;
     const uint32_t tiles_n = (a.n + BN - 1) / BN;
@@ -252,26 +304,31 @@ void launch_tiles(LinearArgs a, hipStream_t st) {
     a.band_rows = 8;
     a.band = Div(tiles_n * a.band_rows);
     const unsigned grid = (a.work + 7) / 8 * 8;
-    if (a.k % 16) linear_tile_kernel<T, BM, BN, MT, true><<<grid, kThreads, 0, st>>>(a);
-    else linear_tile_kernel<T, BM, BN, MT, false><<<grid, kThreads, 0, st>>>(a);
+    if (a.k % 16) linear_tile_kernel<T, BM, BN, MT, S, true><<<grid, kThreads, 0, st>>>(a);
+    else linear_tile_kernel<T, BM, BN, MT, S, false><<<grid, kThreads, 0, st>>>(a);
+}
+
+template <class T, int MT>
+void launch_small(LinearArgs a, hipStream_t st) {
+    a.tiles_n = Div((a.n + 15) / 16);
+    const int64_t tiles = (a.m + 16 * MT - 1) / (16 * MT) * a.tiles_n.d;
+    const unsigned grid = static_cast<unsigned>(tiles);
+    // wavefronts that share a tile's k, while tiles alone do not fill the card
+    if (tiles >= 4096 || a.k <= 64) linear_small_kernel<T, 1, MT><<<grid, kWave, 0, st>>>(a);
+    else if (tiles >= 1024 || a.k <= 512) linear_small_kernel<T, 4, MT><<<grid, 4 * kWave, 0, st>>>(a);
+    else linear_small_kernel<T, 8, MT><<<grid, 8 * kWave, 0, st>>>(a);
 }
 
 template <class T>
 bool launch(LinearArgs a, hipStream_t st) {
-    const int64_t tiles = (a.m + 15) / 16 * ((a.n + 15) / 16);
-    if (tiles > 0x7ffffff0) return false;
-    auto count = [&](int bm, int bn) { return ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn); };
-    if (count(256, 256) >= 192) {
-        launch_tiles<T, 256, 256, 8>(a, st);
-    } else if (count(128, 128) >= 128) {
-        launch_tiles<T, 128, 128, 4>(a, st);
-    } else {
-        a.tiles_n = Div((a.n + 15) / 16);
-        // wavefronts that share a tile's k, while tiles alone do not fill the card
-        if (tiles >= 4096 || a.k <= 64) linear_small_kernel<T, 1><<<static_cast<unsigned>(tiles), kWave, 0, st>>>(a);
-        else if (tiles >= 1024 || a.k <= 512) linear_small_kernel<T, 4><<<static_cast<unsigned>(tiles), 4 * kWave, 0, st>>>(a);
-        else linear_small_kernel<T, 8><<<static_cast<unsigned>(tiles), 8 * kWave, 0, st>>>(a);
-    }
+    if ((a.m + 15) / 16 * ((a.n + 15) / 16) > 0x7ffffff0) return false;
+    auto tiles = [&](int b) { return (a.m + b - 1) / b * ((a.n + b - 1) / b); };
+    if (tiles(256) >= 192) launch_tiles<T, 256, 256, 8, 2>(a, st);
+    else if (tiles(128) >= 256) launch_tiles<T, 128, 128, 4, 2>(a, st);
+    else if (a.m > 64 && a.k > 256) launch_tiles<T, 64, 64, 1, 4>(a, st);
+    else if (a.m <= 16 || a.k <= 256) launch_small<T, 1>(a, st);
+    else if (a.m <= 32) launch_small<T, 2>(a, st);
+    else launch_small<T, 4>(a, st);
     return true;
 }
 
