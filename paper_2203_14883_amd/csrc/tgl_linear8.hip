@@ -140,8 +140,8 @@ __global__ __launch_bounds__(NW * kWave) void linear_small_kernel(const LinearAr
 //
 // A 16-byte piece p of row r lies at piece p ^ swizzle(r) of the row's 128
 // bytes, so that the 16 lanes that read one piece of 16 rows touch all banks.
-// What LDS holds past k is 0 (loads beyond the buffer's end give 0); the last
-// bytes of k's own piece are cleared in the x operand.
+// Whole pieces only: past them LDS holds 0, from loads beyond the buffer's end,
+// and a piece that k ends in is multiplied once, after the steps, from memory.
 
 constexpr int kStepK = 128;
 
@@ -150,12 +150,11 @@ __device__ __forceinline__ int swizzle_w(int r) { return ((r >> 1) & 1) | (((r >
 
 using lds_t = __attribute__((address_space(3))) void;
 
-template <class T, int BM, int BN, int MT, int S, bool kTail>
+template <class T, int BM, int BN, int MT, int S>
 __global__ __launch_bounds__(BM / (16 * MT) * (BN / 64) * kWave, 2) void linear_tile_kernel(const LinearArgs a) {
     constexpr int kWaves = BM / (16 * MT) * (BN / 64);
-    constexpr int kRowsPerWave = (BM + BN) / kWaves;        // rows of a step that a wavefront fetches, all of w or all of x
-    constexpr int kFetch = kRowsPerWave / 8;
-    static_assert(BN % kRowsPerWave == 0, "a wavefront fetches rows of one operand");
+    constexpr int kFetchW = BN / 8 / kWaves, kFetch = kFetchW + BM / 8 / kWaves;    // fetches of 8 rows of w, of all
+    static_assert(BN % (8 * kWaves) == 0 && BM % (8 * kWaves) == 0, "the wavefronts fetch as much each");
     // one object each: so the compiler sees that a step's reads do not wait for the others' loads
     __shared__ __attribute__((aligned(1024))) int8_t buf0[(BM + BN) * kStepK];
     __shared__ __attribute__((aligned(1024))) int8_t buf1[(BM + BN) * kStepK];
@@ -178,30 +177,35 @@ __global__ __launch_bounds__(BM / (16 * MT) * (BN / 64) * kWave, 2) void linear_
     const int n0 = tn * BN;
 
     // ---- what the wavefront fetches ----
-    const bool of_w = wave * kRowsPerWave < BN;
-    const int row0 = of_w ? wave * kRowsPerWave : wave * kRowsPerWave - BN;     // of its operand's tile
-    const int8_t *src = of_w ? a.w + static_cast<int64_t>(n0) * a.wstride : a.x + m0 * a.xstride;
-    const uint32_t stride = static_cast<uint32_t>(of_w ? a.wstride : a.xstride);
-    const int64_t left = of_w ? a.n - n0 : a.m - m0;
-    const int last = static_cast<int>(left < (of_w ? BN : BM) ? left : (of_w ? BN : BM)) - 1;   // its tile's last row
-    const uint32_t k16 = (a.k + 15) & ~15;
-    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(src), 0, last * stride + k16, 0x00027000);
+    const int whole = a.k & ~15;                            // what goes through LDS
+    const int last_w = (a.n - n0 < BN ? a.n - n0 : BN) - 1;             // the tile's last rows
+    const int last_x = static_cast<int>(a.m - m0 < BM ? a.m - m0 : BM) - 1;
+    const auto rsrc_w = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(a.w + static_cast<int64_t>(n0) * a.wstride), 0,
+                                                          last_w * static_cast<uint32_t>(a.wstride) + whole, 0x00027000);
+    const auto rsrc_x = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(a.x + m0 * a.xstride), 0,
+                                                          last_x * static_cast<uint32_t>(a.xstride) + whole, 0x00027000);
     uint32_t at[kFetch];
     uint32_t piece[kFetch];
 #pragma unroll
     for (int f = 0; f < kFetch; f++) {
-        const int r = row0 + 8 * f + (lane >> 3);
+        const bool of_w = f < kFetchW;
+        const int r = (of_w ? wave * kFetchW + f : wave * (kFetch - kFetchW) + f - kFetchW) * 8 + (lane >> 3);
+        const int last = of_w ? last_w : last_x;
         piece[f] = ((lane & 7) ^ (of_w ? swizzle_w(r) : swizzle_x(r))) * 16;
-        at[f] = (r < last ? r : last) * stride + piece[f];
+        at[f] = (r < last ? r : last) * static_cast<uint32_t>(of_w ? a.wstride : a.xstride) + piece[f];
     }
-    const int steps = (a.k + kStepK - 1) / kStepK;
+    const int steps = (whole + kStepK - 1) / kStepK;
     auto fetch = [&](int8_t *buf, int step) {
+        const uint32_t k = step * kStepK;
 #pragma unroll
         for (int f = 0; f < kFetch; f++) {
-            const uint32_t k = step * kStepK;
             // beyond the row: past the buffer's end, which reads as 0
-            const uint32_t off = k + piece[f] < k16 ? at[f] + k : 0x7ffffff0u;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_t *)(buf + (wave * kRowsPerWave + 8 * f) * kStepK), 16, off, 0, 0, 0);
+            const uint32_t off = k + piece[f] < static_cast<uint32_t>(whole) ? at[f] + k : 0x7ffffff0u;
+            if (f < kFetchW)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_w, (lds_t *)(buf + (wave * kFetchW + f) * 8 * kStepK), 16, off, 0, 0, 0);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                    rsrc_x, (lds_t *)(buf + (BN + (wave * (kFetch - kFetchW) + f - kFetchW) * 8) * kStepK), 16, off, 0, 0, 0);
         }
     };
 
@@ -217,7 +221,7 @@ __global__ __launch_bounds__(BM / (16 * MT) * (BN / 64) * kWave, 2) void linear_
     for (int j = 0; j < 4; j++) w_at[j] = wn * 64 + (i16 >> 2) * 16 + 4 * j + (i16 & 3);
 #pragma unroll
     for (int i = 0; i < MT; i++) x_at[i] = wm * 16 * MT + 16 * i + i16;
-    auto multiply = [&](const int8_t *buf, int step) {
+    auto multiply = [&](const int8_t *buf) {
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             const int p = 4 * h + g;
@@ -226,12 +230,8 @@ __global__ __launch_bounds__(BM / (16 * MT) * (BN / 64) * kWave, 2) void linear_
             for (int j = 0; j < 4; j++)
                 wv[j] = *reinterpret_cast<const i32x4 *>(buf + w_at[j] * kStepK + ((p ^ swizzle_w(w_at[j])) * 16));
 #pragma unroll
-            for (int i = 0; i < MT; i++) {
+            for (int i = 0; i < MT; i++)
                 xv[i] = *reinterpret_cast<const i32x4 *>(buf + (BN + x_at[i]) * kStepK + ((p ^ swizzle_x(x_at[i])) * 16));
-                if constexpr (kTail) {
-                    if (step == steps - 1) xv[i] = mask_piece(xv[i], step * kStepK + 16 * p, a.k);
-                }
-            }
 #pragma unroll
             for (int i = 0; i < MT; i++)
 #pragma unroll
@@ -266,11 +266,30 @@ __global__ __launch_bounds__(BM / (16 * MT) * (BN / 64) * kWave, 2) void linear_
             if (step + i < steps) {
                 meet();                                     // this step's buffer is there, the one before free
                 fetch(buffer(Const<i + S - 1>()), step + i + S - 1);
-                multiply(buffer(I), step + i);
+                multiply(buffer(I));
             }
         });
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);                     // nothing goes to LDS once it is another workgroup's
+
+    if (a.k % 16 != 0) {                                    // the piece that k ends in, straight from memory
+        i32x4 wv[4], xv[MT];
+        const int c = g == 0 ? whole : a.k;                 // the other lanes' pieces lie past k: zeros
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int r = w_at[j] < last_w ? w_at[j] : last_w;
+            wv[j] = load_piece(a.w + (n0 + r) * a.wstride, c, a.k);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; i++) {
+            const int r = x_at[i] < last_x ? x_at[i] : last_x;
+            xv[i] = mask_piece(load_piece(a.x + (m0 + r) * a.xstride, c, a.k), c, a.k);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[j], xv[i], acc[i][j], 0, 0, 0);
+    }
 
     const int j0 = n0 + wn * 64 + 16 * g;
     if (j0 >= a.n) return;
@@ -304,8 +323,7 @@ void launch_tiles(LinearArgs a, hipStream_t st) {
     a.band_rows = 8;
     a.band = Div(tiles_n * a.band_rows);
     const unsigned grid = (a.work + 7) / 8 * 8;
-    if (a.k % 16) linear_tile_kernel<T, BM, BN, MT, S, true><<<grid, kThreads, 0, st>>>(a);
-    else linear_tile_kernel<T, BM, BN, MT, S, false><<<grid, kThreads, 0, st>>>(a);
+    linear_tile_kernel<T, BM, BN, MT, S><<<grid, kThreads, 0, st>>>(a);
 }
 
 template <class T, int MT>
@@ -323,12 +341,19 @@ template <class T>
 bool launch(LinearArgs a, hipStream_t st) {
     if ((a.m + 15) / 16 * ((a.n + 15) / 16) > 0x7ffffff0) return false;
     auto tiles = [&](int b) { return (a.m + b - 1) / b * ((a.n + b - 1) / b); };
-    if (tiles(256) >= 192) launch_tiles<T, 256, 256, 8, 2>(a, st);
-    else if (tiles(128) >= 256) launch_tiles<T, 128, 128, 4, 2>(a, st);
-    else if (a.m > 64 && a.k > 256) launch_tiles<T, 64, 64, 1, 4>(a, st);
-    else if (a.m <= 16 || a.k <= 256) launch_small<T, 1>(a, st);
-    else if (a.m <= 32) launch_small<T, 2>(a, st);
-    else launch_small<T, 4>(a, st);
+    // The largest tiles that still give most of the 256 compute units one
+    // (fewer loads a product), two workgroups a unit for those of 128; tiles of
+    // 64, three steps ahead, for the middle; straight from memory where there
+    // would be few of those.  Times in us with tiles of 256 / 128 / 64 / none:
+    // 16384 x 4096 x 512 63 / 69 / 119 / 295, 12000 x 1024 x 768 21 / 19 / 30 /
+    // 87, 2048 x 2048 x 2048 32 / 15 / 18 / 74, 512 x 4096 x 4096 50 / 26 / 16 /
+    // 74, 64 x 4096 x 4096 41 / 18 / 10 / 11, 48 x 1000 x 2000 22 / 10 / 7 / 4.
+    const bool fits = tiles(256) * 4 * 10 <= tiles(128) * 11;          // at most a tenth more of the edges
+    if (tiles(256) >= 192 && fits) launch_tiles<T, 256, 256, 8, 2>(a, st);
+    else if (tiles(128) >= 256) launch_tiles<T, 128, 128, 2, 2>(a, st);
+    else if (a.m > 32 && tiles(64) >= 64) launch_tiles<T, 64, 64, 1, 4>(a, st);
+    else if (a.m <= 16) launch_small<T, 1>(a, st);
+    else launch_small<T, 2>(a, st);
     return true;
 }
 
