@@ -170,29 +170,36 @@ __device__ __forceinline__ int clamp_to(int64_t v, int most) {
     return v < 0 ? 0 : v > most ? most : static_cast<int>(v);
 }
 
+// What of a wavefront's 32 tokens is surely on one page: a token (pages of 1 and
+// 2), the four that a lane has of each half (4 and 8), a half (16 and more).
+enum Pages { kTokens, kFours, kHalves };
+
 // Wavefronts of a SIMD that the registers are cut for (the most that spill
 // nothing).
-template <class T, int JV, bool kWhole, int R>
-constexpr int kWavesPerSimd = JV == 16 ? 2 : R == 2 ? 2 : JV == 8 ? (kParts<T> == 2 && kWhole ? 3 : 2) : 3;
+template <class T, int JV, int kPages, int R>
+constexpr int kWavesPerSimd = JV == 16 || R == 2 ? 2 : JV == 8 ? (kParts<T> == 2 && kPages != kTokens ? 3 : 2)
+                                                       : kPages == kFours && kParts<T> == 2 ? 5 : 3;
 
 // A wavefront's 32 tokens: where they are, then what they hold.
-template <int JV, bool kWhole>
+template <int JV, int kPages>
 struct Step {
     static constexpr int KK = JV >= 4 ? JV / 4 : 1;
-    int page[kWhole ? 2 : 1];       // kWhole: of the two halves, uniform; else of token lane & 31; -1: nothing to see
-    float2 sc[kWhole ? 2 : 1];      // the steps of keys and values
+    static constexpr int kLooks = kPages == kHalves ? 2 : 1;
+    int page[kLooks];               // kHalves: of the two, uniform; else of token lane & 31; -1: nothing to see
+    float2 sc[kLooks];              // the steps of keys and values
     i32x4 kv[2][KK];
     Columns<JV> vv[8];
 };
 
-// JV: columns of a lane, so heads of up to 16 JV.  kWhole: pages of at least
-// 16 tokens, one page to each half of a step.  NW: wavefronts that share a
-// workgroup's tokens.  R: row tiles of a wavefront, which share the keys'
+// JV: columns of a lane, so heads of up to 16 JV.  kPages: see Pages.  NW:
+// wavefronts that share a workgroup's tokens.  R: row tiles of a wavefront, which share the keys'
 // loads and the values' conversion.
-template <class T, int JV, bool kWhole, int NW, int R>
-__global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void attend_kernel(const AttendArgs a) {
+template <class T, int JV, int kPages, int NW, int R>
+__global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kPages, R>)) void attend_kernel(const AttendArgs a) {
     constexpr int N = kParts<T>;
     constexpr int KK = JV >= 4 ? JV / 4 : 1;
+    constexpr bool kWhole = kPages == kHalves;
+    constexpr int kLooks = Step<JV, kPages>::kLooks;
     const CacheView &c = a.c;
     const int lane = lane_id();
     const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -278,7 +285,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
     for (int i = 0; i < 4; i++) vat[i] = (4 * g + i) * width + vcol;
 
     // the pages of the step at t0 (whose table entries exist up to token n - 1)
-    auto look_up = [&](int t0, int (&page)[kWhole ? 2 : 1]) {
+    auto look_up = [&](int t0, int (&page)[kLooks]) {
         if constexpr (kWhole) {
 #pragma unroll
             for (int u = 0; u < 2; u++) {
@@ -287,14 +294,15 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
                 page[u] = p < n && p + 16 > first && static_cast<uint32_t>(got) < pages ? got : -1;
             }
         } else {
-            const int p = t0 + (lane & 31);
-            const int got = table[(c0r + (p < n ? p : n - 1)) >> c.shift];
-            page[0] = p < n && p >= first && static_cast<uint32_t>(got) < pages ? got : -1;
+            // kFours: as far as one of the four is seen
+            const int p = t0 + (lane & 31), from = kPages == kFours ? p & ~3 : p, to = kPages == kFours ? p | 3 : p;
+            const int got = table[(c0r + (from < n ? from : n - 1)) >> c.shift];
+            page[0] = from < n && to >= first && static_cast<uint32_t>(got) < pages ? got : -1;
         }
     };
 
     // the rows and steps of the step at t0, whose pages are known
-    auto fetch = [&](int t0, Step<JV, kWhole> &x) {
+    auto fetch = [&](int t0, Step<JV, kPages> &x) {
         if constexpr (kWhole) {
 #pragma unroll
             for (int u = 0; u < 2; u++) {
@@ -317,8 +325,18 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
 #pragma unroll
                 for (int kk = 0; kk < KK; kk++) x.kv[u][kk] = *reinterpret_cast<const i32x4 *>(kb + kcol[kk]);
             }
+            if constexpr (kPages == kFours) {
 #pragma unroll
-            for (int k = 0; k < 8; k++) {
+                for (int u = 0; u < 2; u++) {
+                    const int from = 16 * u + 4 * g;
+                    const uint32_t at = __builtin_amdgcn_ds_bpermute(4 * from, own);
+                    const int8_t *vb = data + static_cast<uint64_t>(at) * pitch + block + ((c0r + t0 + from) & pmask) * width + vcol;
+#pragma unroll
+                    for (int i = 0; i < 4; i++) x.vv[4 * u + i].load(vb + i * width);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < (kPages == kTokens ? 8 : 0); k++) {
                 const int from = 16 * (k >> 2) + 4 * g + (k & 3);
                 const uint32_t at = __builtin_amdgcn_ds_bpermute(4 * from, own);
                 x.vv[k].load(data + static_cast<uint64_t>(at) * pitch + block + ((c0r + t0 + from) & pmask) * width + vcol);
@@ -326,7 +344,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
         }
     };
 
-    auto multiply = [&](int t0, Step<JV, kWhole> &x) {
+    auto multiply = [&](int t0, Step<JV, kPages> &x) {
         // ---- steps of the lane's 8 tokens, which of them nobody sees ----
         int bad = 0;
         float ks[8], vs[8];
@@ -337,6 +355,10 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
                 ks[k] = x.sc[k >> 2].x;
                 vs[k] = ok ? x.sc[k >> 2].y : 0.0f;
                 if (!ok) bad |= 1 << k;
+            } else if (kPages == kFours && (k & 3) != 0) {
+                ks[k] = ks[k & ~3];
+                vs[k] = vs[k & ~3];
+                bad |= ((bad >> (k & ~3)) & 1) << k;
             } else {
                 const int from = 4 * (16 * (k >> 2) + 4 * g + (k & 3));
                 const float y = x.page[0] < 0 ? 0.0f : x.sc[0].y;
@@ -403,7 +425,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
             }
             // ---- the running maximum (of nothing where -inf meets a unit of 0: NaN, which fmaxf drops) ----
             float top;
-            if constexpr (kWhole) {                             // one unit for each half
+            if constexpr (kPages != kTokens) {                  // one unit for each half's four
                 top = fmaxf(fmaxf(fmaxf(dot[0], dot[1]), fmaxf(dot[2], dot[3])) * unit[0],
                             fmaxf(fmaxf(dot[4], dot[5]), fmaxf(dot[6], dot[7])) * unit[4]);
             } else {
@@ -472,38 +494,38 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kWhole, R>)) void
         if constexpr (!kAhead) {
             // the next step's pages are looked up while this one's rows come;
             // other wavefronts hide the rows' latency
-            Step<JV, kWhole> x;
+            Step<JV, kPages> x;
             look_up(t0, x.page);
             for (; t0 < n; t0 += kNext) {
                 fetch(t0, x);
-                int page[kWhole ? 2 : 1];
+                int page[kLooks];
                 look_up(t0 + kNext, page);
                 __builtin_amdgcn_sched_barrier(0);
                 multiply(t0, x);
 #pragma unroll
-                for (int u = 0; u < (kWhole ? 2 : 1); u++) x.page[u] = page[u];
+                for (int u = 0; u < kLooks; u++) x.page[u] = page[u];
             }
         } else {
             // two wavefronts a SIMD hide little: rows come a step ahead, too
-            Step<JV, kWhole> x, y;
+            Step<JV, kPages> x, y;
             look_up(t0, x.page);
             fetch(t0, x);
             look_up(t0 + kNext, y.page);
             for (; t0 < n; t0 += 2 * kNext) {
                 fetch(t0 + kNext, y);
-                int page[kWhole ? 2 : 1];
+                int page[kLooks];
                 look_up(t0 + 2 * kNext, page);
                 __builtin_amdgcn_sched_barrier(0);
                 multiply(t0, x);
 #pragma unroll
-                for (int u = 0; u < (kWhole ? 2 : 1); u++) x.page[u] = page[u];
+                for (int u = 0; u < kLooks; u++) x.page[u] = page[u];
                 if (t0 + kNext >= n) break;
                 fetch(t0 + 2 * kNext, x);
                 look_up(t0 + 3 * kNext, page);
                 __builtin_amdgcn_sched_barrier(0);
                 multiply(t0 + kNext, y);
 #pragma unroll
-                for (int u = 0; u < (kWhole ? 2 : 1); u++) y.page[u] = page[u];
+                for (int u = 0; u < kLooks; u++) y.page[u] = page[u];
             }
         }
     }
@@ -750,15 +772,15 @@ __global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(
             int kw[16][kWords], vw[16][kWords];
             unrolled<16>([&](auto J) {
                 constexpr int j = decltype(J)::value;
-                    const uint32_t at = from_lane<j>(own);
-                    const int8_t *k = data + static_cast<uint64_t>(at) * pitch + ((r0 + j) & pmask) * c.width;
-                    Columns<JV> x;
-                    x.load(k);
+                const uint32_t at = from_lane<j>(own);
+                const int8_t *k = data + static_cast<uint64_t>(at) * pitch + ((r0 + j) & pmask) * c.width;
+                Columns<JV> x;
+                x.load(k);
 #pragma unroll
-                    for (int w = 0; w < kWords; w++) kw[j][w] = x.w[w];
-                    x.load(k + block);
+                for (int w = 0; w < kWords; w++) kw[j][w] = x.w[w];
+                x.load(k + block);
 #pragma unroll
-                    for (int w = 0; w < kWords; w++) vw[j][w] = x.w[w];
+                for (int w = 0; w < kWords; w++) vw[j][w] = x.w[w];
             });
             float p[16];
 #pragma unroll
@@ -815,9 +837,6 @@ __global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(
 constexpr int64_t kFill = 2048;
 constexpr int64_t kMinChunk = 256;
 
-constexpr uint32_t kFewRows = 4;
-constexpr int64_t kFewTokens = 64;
-
 struct Plan {
     int64_t tile_rows;
     int64_t row_tiles;
@@ -851,18 +870,25 @@ Plan plan_of(const CacheView &c, int64_t num_seqs, int32_t pages_per_seq, int32_
     return p;
 }
 
-template <class T, int JV, bool kWhole>
+template <class T, int JV, int kPages>
 void launch(const AttendArgs &a, int nw, hipStream_t st) {
     // whole turns of the dies, of heads or of workgroups
     const unsigned grid = a.order == kHeadsInTurn ? (a.work / a.tiles.d + 7) / 8 * 8 * a.tiles.d : (a.work + 7) / 8 * 8;
     if constexpr (JV < 16) {
         if (a.tile_rows > kRows) {
-            attend_kernel<T, JV, kWhole, 4, 2><<<grid, 4 * kWave, 0, st>>>(a);
+            attend_kernel<T, JV, kPages, 4, 2><<<grid, 4 * kWave, 0, st>>>(a);
             return;
         }
     }
-    if (nw == 1) attend_kernel<T, JV, kWhole, 1, 1><<<grid, kWave, 0, st>>>(a);
-    else attend_kernel<T, JV, kWhole, 4, 1><<<grid, 4 * kWave, 0, st>>>(a);
+    if (nw == 1) attend_kernel<T, JV, kPages, 1, 1><<<grid, kWave, 0, st>>>(a);
+    else attend_kernel<T, JV, kPages, 4, 1><<<grid, 4 * kWave, 0, st>>>(a);
+}
+
+template <class T, int JV>
+void launch(const AttendArgs &a, int nw, hipStream_t st) {
+    if (a.c.tokens() >= 16) launch<T, JV, kHalves>(a, nw, st);
+    else if (a.c.tokens() >= 4) launch<T, JV, kFours>(a, nw, st);
+    else launch<T, JV, kTokens>(a, nw, st);
 }
 
 template <class T, int kLanes>
@@ -874,19 +900,35 @@ void launch_join(const AttendArgs &a, hipStream_t st) {
 
 template <class T>
 void launch(const AttendArgs &a, int nw, hipStream_t st) {
-    const bool whole = a.c.tokens() >= 16;
-    if (a.c.width <= 32) whole ? launch<T, 2, true>(a, nw, st) : launch<T, 2, false>(a, nw, st);
-    else if (a.c.width <= 64) whole ? launch<T, 4, true>(a, nw, st) : launch<T, 4, false>(a, nw, st);
-    else if (a.c.width <= 128) whole ? launch<T, 8, true>(a, nw, st) : launch<T, 8, false>(a, nw, st);
-    else whole ? launch<T, 16, true>(a, nw, st) : launch<T, 16, false>(a, nw, st);
+    if (a.c.width <= 32) launch<T, 2>(a, nw, st);
+    else if (a.c.width <= 64) launch<T, 4>(a, nw, st);
+    else if (a.c.width <= 128) launch<T, 8>(a, nw, st);
+    else launch<T, 16>(a, nw, st);
     if (!a.part_o) return;
     if (a.c.width <= 64) launch_join<T, 16>(a, st);
     else if (a.c.width <= 128) launch_join<T, 32>(a, st);
     else launch_join<T, 64>(a, st);
 }
 
-// Whether the kernel for few tokens is the faster one.
-bool few(const AttendArgs &a) { return a.rows <= kFewRows && (static_cast<int64_t>(a.s.pages_per_seq) << a.c.shift) <= kFewTokens; }
+// Whether the kernel for few tokens is the faster one: its work grows with
+// rows times tokens, the other's with tokens above 32.  12,000 sequences, 2
+// heads of 128, us here / there: 1 row of 16 tokens 22 / 49, of 32 39 / 50, of
+// 64 74 / 79; 2 rows of 16 42 / 50, of 32 75 / 51; 4 rows of 8 48 / 50, of 16
+// 79 / 51.
+bool few(const AttendArgs &a) {
+    const int64_t tokens = static_cast<int64_t>(a.s.pages_per_seq) << a.c.shift;
+    return a.rows * ((tokens + 15) / 16) <= 2 || (a.rows == 1 && tokens <= 64);
+}
+
+// Wavefronts that share a sequence's tokens.  One to itself needs no join
+// through LDS and leaves more of them resident, as long as there are many.  2
+// heads of 50, us with 1 / 4: 1000 sequences and heads, 64 tokens 8.0 / 9.7, 128
+// 11.3 / 10.6, 256 17 / 14; 4000 of 128 21 / 30, of 256 35 / 40, of 512 63 / 61;
+// 24,000 of 256 164 / 198, of 512 315 / 313.
+int wavefronts(const AttendArgs &a) {
+    const int64_t tokens = static_cast<int64_t>(a.s.pages_per_seq) << a.c.shift;
+    return tokens <= 64 || (tokens <= 256 && a.items.d >= 2048) ? 1 : 4;
+}
 
 template <class T>
 void launch_few(const AttendArgs &a, unsigned grid, hipStream_t st) {
@@ -986,8 +1028,7 @@ tgl_status tgl_cache_attend(const tgl_cache *cache, const tgl_heads *q, int32_t 
         else launch_few<bf16_t>(a, grid, st);
         return launch_status();
     }
-    // a wavefront alone where a sequence has at most two steps for it
-    const int nw = (static_cast<int64_t>(a.s.pages_per_seq) << a.c.shift) <= 2 * kTile ? 1 : 4;
+    const int nw = wavefronts(a);
     if (dtype == TGL_OUT_F32) launch<float>(a, nw, st);
     else launch<bf16_t>(a, nw, st);
     return launch_status();
