@@ -177,8 +177,7 @@ enum Pages { kTokens, kFours, kHalves };
 // Wavefronts of a SIMD that the registers are cut for (the most that spill
 // nothing).
 template <class T, int JV, int kPages, int R>
-constexpr int kWavesPerSimd = JV == 16 || R == 2 ? 2 : JV == 8 ? (kParts<T> == 2 && kPages != kTokens ? 3 : 2)
-                                                       : kPages == kFours && kParts<T> == 2 ? 5 : 3;
+constexpr int kWavesPerSimd = JV == 16 || R == 2 ? 2 : JV == 8 ? (kParts<T> == 2 && kPages != kTokens ? 3 : 2) : 4;
 
 // A wavefront's 32 tokens: where they are, then what they hold.
 template <int JV, int kPages>
@@ -414,20 +413,23 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kPages, R>)) void
                     unit[4 * u + i] = ks[4 * u + i] * to_log2[y];
                 }
             }
+            const float unit0 = unit[0], unit4 = unit[4];
             int hide = bad;
             if (masked) {
 #pragma unroll
                 for (int k = 0; k < 8; k++) {
                     const int p = t0 + 16 * (k >> 2) + 4 * g + (k & 3);
                     if (p < first || p >= last[y]) hide |= 1 << k;
-                    if ((hide >> k) & 1) dot[k] = -INFINITY;
+                    const bool hidden = (hide >> k) & 1;
+                    dot[k] = hidden ? -INFINITY : dot[k];
+                    unit[k] = hidden ? 1.0f : unit[k];          // -inf stays -inf whatever the page's step is
                 }
             }
             // ---- the running maximum (of nothing where -inf meets a unit of 0: NaN, which fmaxf drops) ----
             float top;
             if constexpr (kPages != kTokens) {                  // one unit for each half's four
-                top = fmaxf(fmaxf(fmaxf(dot[0], dot[1]), fmaxf(dot[2], dot[3])) * unit[0],
-                            fmaxf(fmaxf(dot[4], dot[5]), fmaxf(dot[6], dot[7])) * unit[4]);
+                top = fmaxf(fmaxf(fmaxf(dot[0], dot[1]), fmaxf(dot[2], dot[3])) * unit0,
+                            fmaxf(fmaxf(dot[4], dot[5]), fmaxf(dot[6], dot[7])) * unit4);
             } else {
                 top = dot[0] * unit[0];
 #pragma unroll
@@ -448,9 +450,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kPages, R>)) void
             float w[8];
 #pragma unroll
             for (int k = 0; k < 8; k++) {
-                float e = __builtin_fmaf(dot[k], unit[k], -from);
-                if (masked) e = (hide >> k) & 1 ? -INFINITY : e;
-                const float p = __builtin_amdgcn_exp2f(e);
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(dot[k], unit[k], -from));
                 l[y] += p;
                 w[k] = p * vw[k];
             }
