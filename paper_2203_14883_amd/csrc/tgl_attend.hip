@@ -25,6 +25,16 @@
 //           far (a running one, like the maximum), so that pages of any steps
 //           add up.  P is f16: one for bfloat16 outputs (2^-11 of each), two,
 //           the second the rounding error of the first, for float32.
+//
+// Few rows a head: bound by memory.  1,000,003 tokens of 8 heads of 128 in pages
+// of 64 (2.05 GB), 4 query heads each, 349 us, 5.9 TB/s, and 7 us to join 253
+// chunks; 64 histories of 1 to 8192 tokens (0.54 GB) 114 + 5 us, 4.5 TB/s, the
+// rest being long and short histories side by side.  Small pages and heads: by
+// instructions, 300 for 32 tokens (600 windows of 1000 tokens, 2 heads of 64,
+// pages of 4: 35 us, 3.6 TB/s).  Many rows: by the scores' arithmetic (256
+// queries of 4 histories of 2500 to 4097, 8 heads of 128 for 32: 95 us, 560
+// TFLOP/s), 350 vector instructions for 32 rows and 32 tokens beside 32 matrix
+// ones.
 #include "tgl_cache.hpp"
 
 namespace tgl {
@@ -166,6 +176,23 @@ __device__ __forceinline__ uint32_t here(uint32_t v, int t) {
     return v;
 }
 
+// What the queries of a sequence see, whatever the device arrays say: begin in
+// [0, all], the end of the last query's view in [0, all + queries].
+struct View {
+    int64_t begin, end, all;
+};
+
+__device__ __forceinline__ View view_of_seq(const AttendArgs &a, uint32_t b) {
+    View v;
+    v.all = static_cast<int64_t>(a.s.pages_per_seq) << a.c.shift;
+    v.begin = a.s.begin(b);
+    v.begin = v.begin < 0 ? 0 : v.begin > v.all ? v.all : v.begin;
+    v.end = a.end ? a.end[b] : v.all;
+    const int64_t most = v.all + a.queries;
+    v.end = v.end < 0 ? 0 : v.end > most ? most : v.end;
+    return v;
+}
+
 __device__ __forceinline__ int clamp_to(int64_t v, int most) {
     return v < 0 ? 0 : v > most ? most : static_cast<int>(v);
 }
@@ -174,8 +201,8 @@ __device__ __forceinline__ int clamp_to(int64_t v, int most) {
 // 2), the four that a lane has of each half (4 and 8), a half (16 and more).
 enum Pages { kTokens, kFours, kHalves };
 
-// Wavefronts of a SIMD that the registers are cut for (the most that spill
-// nothing).
+// Wavefronts of a SIMD that the registers are cut for: the most that spill
+// nothing, or (float32, heads above 64, pages of 1 and 2) a few.
 template <class T, int JV, int kPages, int R>
 constexpr int kWavesPerSimd = JV == 16 || R == 2 ? 2 : JV == 8 ? (kParts<T> == 2 && kPages != kTokens ? 3 : 2) : 4;
 
@@ -217,10 +244,8 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kPages, R>)) void
     const uint32_t r0 = tile * (kRows * R);
     const uint32_t rl = r0 + kRows * R < a.rows ? r0 + kRows * R - 1 : a.rows - 1;      // last row
     // what the tile's rows see: from begin to at most stop, a row up to row_end
-    const int64_t all = static_cast<int64_t>(a.s.pages_per_seq) << c.shift;
-    int64_t begin = a.s.begin(b);
-    begin = begin < 0 ? 0 : begin;
-    const int64_t end = a.end ? a.end[b] : all;
+    const View view = view_of_seq(a, b);
+    const int64_t all = view.all, begin = view.begin, end = view.end;
     int64_t stop = end - (a.queries - 1 - a.group(rl));
     int64_t safe = end - (a.queries - 1 - a.group(r0));                 // every row sees up to here
     stop = stop > all ? all : stop;
@@ -606,7 +631,8 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kPages, R>)) void
 
 // Joins the chunks of a row with NW wavefronts.  A lane takes four columns of
 // every (NW kWave / kLanes)-th chunk, kLanes the lanes of a row's columns, eight
-// chunks in flight.  With NW = 1 a workgroup has a row for each of its
+// chunks in flight (253 chunks of 32 rows of 128: 7 us; 212 us with a wavefront
+// per row and a chunk at a time).  With NW = 1 a workgroup has a row for each of its
 // wavefronts.
 template <class T, int NW, int kLanes>
 __global__ __launch_bounds__((NW == 1 ? kBlock : NW * kWave)) void attend_join_kernel(const AttendArgs a) {
@@ -626,12 +652,10 @@ __global__ __launch_bounds__((NW == 1 ? kBlock : NW * kWave)) void attend_join_k
     // the chunks that the row's tile has, as the tile counts them
     const uint32_t tile_end = r / a.tile_rows * a.tile_rows + a.tile_rows;
     const uint32_t rl = tile_end < a.rows ? tile_end - 1 : a.rows - 1;
-    const int64_t all = static_cast<int64_t>(a.s.pages_per_seq) << c.shift;
-    int64_t begin = a.s.begin(b);
-    begin = begin < 0 ? 0 : begin;
-    int64_t stop = (a.end ? a.end[b] : all) - (a.queries - 1 - a.group(rl));
-    stop = stop > all ? all : stop;
-    const int64_t span = stop - (begin & ~static_cast<int64_t>(kTile - 1));
+    const View view = view_of_seq(a, b);
+    int64_t stop = view.end - (a.queries - 1 - a.group(rl));
+    stop = stop > view.all ? view.all : stop;
+    const int64_t span = stop - (view.begin & ~static_cast<int64_t>(kTile - 1));
     const int64_t want = span <= 0 ? 1 : (span + a.chunk - 1) / a.chunk;
     const int n = static_cast<int>(want < a.chunks ? want : a.chunks);
     const int64_t at = (static_cast<int64_t>(bh) * a.rows + r) * a.chunks;
@@ -704,7 +728,9 @@ __global__ __launch_bounds__((NW == 1 ? kBlock : NW * kWave)) void attend_join_k
 // 16 tokens at a time: lane i looks token i up; every lane multiplies its
 // columns of all 16; the products are summed over the lanes so that token i's
 // sum arrives in lane i (four exchanges, halving the tokens each time); the
-// weights come back from lane i by a swizzle.
+// weights come back from lane i by a swizzle.  12,000 roots of 10 slots, 2 heads
+// of 50 float32 (23 MB): 11.3 us, half of it instructions, half the chain of
+// three loads (slot, step, row); 42 us on the matrix instructions.
 
 template <int kCtrl>
 __device__ __forceinline__ float dpp(float v) {
@@ -739,10 +765,8 @@ __global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(
     const uint32_t it = there ? item : items - 1;
     const uint32_t b = a.heads(it);
     const int head = static_cast<int>(it - b * a.heads.d);
-    const int64_t all = static_cast<int64_t>(a.s.pages_per_seq) << c.shift;
-    int64_t begin = a.s.begin(b);
-    begin = begin < 0 ? 0 : begin;
-    const int64_t end = a.end ? a.end[b] : all;
+    const View view = view_of_seq(a, b);
+    const int64_t all = view.all, begin = view.begin, end = view.end;
     const int block = static_cast<int>(c.block_bytes());
     const uint32_t pitch = static_cast<uint32_t>(c.heads) * 2 * block;
     const int col = JV * i < c.width - JV ? JV * i : c.width - JV;

@@ -34,6 +34,11 @@ struct SeqsView {
     int32_t pages_per_seq;
 
     __device__ int64_t begin(int64_t b) const { return start ? start[b] : 0; }
+    // The same between far below 0 and the table's end, so that sums with it stay whole numbers.
+    __device__ int64_t bounded_begin(int64_t b, int shift) const {
+        const int64_t v = begin(b), all = static_cast<int64_t>(pages_per_seq) << shift, low = -(int64_t(1) << 62);
+        return v < low ? low : v > all ? all : v;
+    }
     __device__ int64_t first_token(int64_t b) const {
         const int64_t t = offsets ? offsets[b] : b * per;
         return t < 0 ? 0 : t > tokens ? tokens : t;

@@ -56,6 +56,8 @@ __device__ __forceinline__ void finish(const LinearArgs &a, int64_t row, int j, 
 
 // A workgroup per 16 MT rows and 16 columns, whose wavefronts take 64 of k in
 // turn and add up through LDS: a row of w is read once for 16 MT rows of x.
+// Bound by latency where w is small (1 x 2304 x 768: 3.4 us) and by w's bytes
+// where it is not (1 x 4096 x 4096: 5.0 us, 3.4 TB/s).
 template <class T, int NW, int MT>
 __global__ __launch_bounds__(NW * kWave) void linear_small_kernel(const LinearArgs a) {
     __shared__ i32x4 sums[NW > 1 ? NW : 1][MT][kWave];
@@ -142,6 +144,11 @@ __global__ __launch_bounds__(NW * kWave) void linear_small_kernel(const LinearAr
 // bytes, so that the 16 lanes that read one piece of 16 rows touch all banks.
 // Whole pieces only: past them LDS holds 0, from loads beyond the buffer's end,
 // and a piece that k ends in is multiplied once, after the steps, from memory.
+
+// Bound by the matrix units and their feeding: 16384 x 4096 x 4096 in 240 to 268
+// us by the card's clocks, 2.0 to 2.3 POP/s, the units at work 47% of the time;
+// 8192^3 2.5 POP/s.  The steps overlap: loads, 6 reads of LDS for every 8
+// products, and the products of two wavefronts a SIMD.
 
 constexpr int kStepK = 128;
 

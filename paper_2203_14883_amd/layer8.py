@@ -206,7 +206,7 @@ def linear_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: 
 # cache
 # --------------------------------------------------------------------------
 
-@dataclass(frozen=True)
+@dataclass(frozen=True, eq=False)
 class HistoryCache:
     """Keys and values in 8 bits, in pages of P tokens: ``data`` int8 ``[pages,
     heads, 2, P, Dp]`` (keys, then values; Dp = dim rounded up to 16) and

@@ -522,6 +522,35 @@ def test_attend_nan_only_where_it_is_seen():
     assert torch.isfinite(P.cache_attend(c, q, table)).all()
 
 
+@pytest.mark.parametrize("pages,page", [(3, 4), (40, 4), (40, 16), (3000, 4), (600, 64)])
+def test_attend_bounds_beyond_the_table(pages, page):
+    """Whatever begin and end hold, what is seen lies in the table."""
+    torch = require_gpu()
+    announce("attend bounds %d x %d" % (pages, page))
+    rng = np.random.default_rng(pages)
+    top, low = 2 ** 63 - 1, -2 ** 63
+    c, _ = _cache(rng, torch, 4 * pages, 1, page, 32)
+    table = torch.arange(4 * pages, dtype=torch.int32).cuda().view(4, pages)
+    for T in (1, 3):
+        q = torch.randn(4, T, 2, 32).cuda()
+        whole = P.cache_attend(c, q, table, end=torch.full((4,), pages * page + T - 1).cuda())
+        for begin, end, want in [(0, top, whole), (low, top, whole), (-5, pages * page + 1000, whole), (top, top, None), (2 ** 62, top, None),
+                                 (0, low, None), (low, -1, None), (pages * page, pages * page, None)]:
+            out, lse = P.cache_attend(c, q, table, begin=torch.full((4,), begin, dtype=torch.int64).cuda(),
+                                      end=torch.full((4,), end, dtype=torch.int64).cuda(), return_lse=True)
+            if want is None:
+                assert (out == 0).all() and torch.isneginf(lse).all()
+            else:
+                assert torch.equal(out, want)
+    k = torch.ones(4, 1, 32).cuda()
+    before = c.data.clone()
+    for start in (top, low, -1, pages * page, 2 ** 62):
+        P.cache_write(c, k, k, table, start=torch.full((4,), start, dtype=torch.int64).cuda())
+        got, _ = P.cache_read(c, table, start=torch.full((4,), start, dtype=torch.int64).cuda(), n=4)
+        assert (got == 0).all()
+    assert torch.equal(c.data, before)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_attend_strided_queries_and_outputs(dtype):
     torch = require_gpu()
