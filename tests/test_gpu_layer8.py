@@ -444,6 +444,65 @@ def test_attend_nan_queries_and_keys(L, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,heads,T,group,length,page,dim", [
+    (1, 1, 20, 2, 9000, 16, 64),        # row tiles of a long history: both cut
+    (1, 2, 33, 1, 4500, 2, 100), (16, 2, 50, 1, 300, 16, 32), (11, 3, 9, 4, 150, 4, 50), (3, 1, 40, 2, 700, 32, 200), (8, 1, 5, 7, 90, 1, 128),
+])
+def test_attend_row_tiles(B, heads, T, group, length, page, dim, dtype):
+    torch = require_gpu()
+    announce("attend row tiles %d x %d x %d x %d of %d page %d dim %d %s" % (B, heads, T, group, length, page, dim, dtype))
+    rng = np.random.default_rng(B + T + length)
+    lengths = rng.integers(0, length + 1, B)
+    lengths[0] = length
+    _attend(torch, rng, dtype, page, heads, group, dim, T, lengths, holes=0.03)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_cache_io_through_views(dtype):
+    """Tables, inputs and outputs that are parts of larger tensors."""
+    torch = require_gpu()
+    announce("cache views %s" % dtype)
+    rng = np.random.default_rng(61)
+    heads, dim, page, B = 3, 50, 4, 6
+    c, oc = _cache(rng, torch, 40, heads, page, dim)
+    wide = torch.from_numpy(np.concatenate([np.full((B, 2), 39), rng.permutation(36).reshape(B, 6)], 1).astype(np.int32)).cuda()
+    tab = wide[:, 2:7]
+    x, xh = _up(torch, rng.standard_normal((heads, B * 17, dim + 5)), dtype)       # head-major
+    k = x[:, :, 2:dim + 2].transpose(0, 1)
+    kh = xh[:, :, 2:dim + 2].transpose(1, 0, 2)
+    P.cache_write(c, k, k, tab, start=torch.full((B,), 3, dtype=torch.int64).cuda())
+    oc.write(kh, kh, tab.cpu().numpy(), np.full(B, 3), np.arange(B + 1) * 17)
+    np.testing.assert_array_equal(c.data.cpu().numpy(), oc.data)
+    room = torch.full((2, B * 20, heads + 1, dim + 7), 3.0).cuda().to(_torch_type(torch, dtype))
+    ko, vo = room[0, :, 1:, 4:dim + 4], room[1, :, :heads, 1:dim + 1]
+    got = P.cache_read(c, tab, k=ko, v=vo)
+    assert got[0] is ko and got[1] is vo
+    want = np.concatenate([oc.tokens(tab.cpu().numpy(), b, range(20))[0] for b in range(B)]).astype(np.float32)
+    np.testing.assert_array_equal(_host(ko), want if dtype == "f32" else O.to_bf16(want))
+    assert (room[0, :, 0] == 3).all() and (room[0, :, :, :4] == 3).all() and (room[0, :, :, dim + 4:] == 3).all()
+    assert (room[1, :, heads] == 3).all() and (room[1, :, :, 0] == 3).all() and (room[1, :, :, dim + 1:] == 3).all()
+
+
+def test_offsets_that_make_no_sense_touch_nothing_else():
+    """Offsets are device data: whatever they hold, only pages of the table change and only tokens of the call are read."""
+    torch = require_gpu()
+    announce("odd offsets")
+    rng = np.random.default_rng(67)
+    c, _ = _cache(rng, torch, 60, 2, 4, 32)
+    table = torch.arange(40, dtype=torch.int32).cuda().view(4, 10)
+    spare = c.data[40:].clone()
+    k = torch.randn(30, 2, 32).cuda()
+    room = torch.full((34, 2, 32), 5.0).cuda()
+    for offs in ([0, 20, 10, 25, 30], [-7, -3, 4, 9, 1000], [30, 20, 10, 5, 0], [5, 5, 5, 5, 5], [2**62, 0, 2**62, -2**62, 3]):
+        o = torch.tensor(offs, dtype=torch.int64).cuda()
+        P.cache_write(c, k, k, table, start=torch.tensor([0, 3, 39, 2], dtype=torch.int64).cuda(), offsets=o)
+        P.cache_read(c, table, offsets=o, n=30, k=room[2:32], v=room[2:32].clone())
+    torch.cuda.synchronize()
+    assert torch.equal(c.data[40:], spare)
+    assert (room[:2] == 5).all() and (room[32:] == 5).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_attend_sharp_and_flat_scores(dtype):
     torch = require_gpu()
     announce("attend sharp and flat %s" % dtype)
