@@ -1,5 +1,5 @@
 // tgl_int8.hpp -- what the 8-bit operators share: element types, the rounding
-// of a set of numbers to bytes and a step, wave reductions, argument checks.
+// of a set of numbers to bytes and a step, wide accesses, argument checks.
 #pragma once
 
 #include "tgl_internal.hpp"
@@ -41,25 +41,6 @@ __device__ __forceinline__ float step_of(float a) {
 
 // 1 / s, or 0 where every byte is to be 0 (a step of 0 or NaN).
 __device__ __forceinline__ float inverse_step(float s) { return s > 0.0f ? 1.0f / s : 0.0f; }
-
-// x in units of the step, as a byte; v_rndne.  inv = 0 gives 0 whatever x is.
-__device__ __forceinline__ int to_byte(float x, float inv) {
-    return inv == 0.0f ? 0 : static_cast<int>(rintf(x * inv));
-}
-
-template <int W>
-__device__ __forceinline__ float group_max_nan(float v) {
-#pragma unroll
-    for (int d = W / 2; d >= 1; d >>= 1) v = max_nan(v, __shfl_xor(v, d, kWave));
-    return v;
-}
-
-template <int W>
-__device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-    for (int d = W / 2; d >= 1; d >>= 1) v += __shfl_xor(v, d, kWave);
-    return v;
-}
 
 // ---- loops over constants ----
 
