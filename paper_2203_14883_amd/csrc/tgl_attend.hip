@@ -8,11 +8,12 @@
 // wavefront takes 32 tokens at a time against it:
 //
 //   scores  S^T = K Q^T on the int8 matrix instructions.  The keys go in as
-//           they lie in the cache; a query row goes in as two signed bytes of
-//           a 16-bit whole number (bfloat16 queries) or three of a 24-bit one
-//           (float32), in units of its largest element / (127 * 256^(n-1)).
-//           The sums are exact; what is lost is that rounding, 2^-16 or 2^-24
-//           of the row's largest element.
+//           they lie in the cache; a query row goes in as three signed bytes of
+//           a 24-bit whole number, in units of its largest element / (127 *
+//           65536).  The sums are exact; what is lost is that rounding, 2^-24
+//           of the row's largest element.  (Two bytes would do for the large
+//           elements of a bfloat16 row, but one outlier among them would take
+//           the others' bits.)
 //   output  O^T = V^T P^T on the f16 ones.  S^T leaves every lane four tokens
 //           of a row per 16 x 16 tile, which is what P^T takes with the tokens
 //           in a fixed other order, so the probabilities never leave their
@@ -23,8 +24,8 @@
 //           makes it v 2^-9, exactly.
 //   P       carries the step of its token's page over the largest step seen so
 //           far (a running one, like the maximum), so that pages of any steps
-//           add up.  P is f16: one for bfloat16 outputs (2^-11 of each), two,
-//           the second the rounding error of the first, for float32.
+//           add up.  P is two f16, the second the rounding error of the
+//           first: 2^-22 of each weight.
 //
 // Few rows a head: bound by memory.  1,000,003 tokens of 8 heads of 128 in pages
 // of 64 (2.05 GB), 4 query heads each, 349 us, 5.9 TB/s, and 7 us to join 253
@@ -91,27 +92,19 @@ __device__ __forceinline__ uint32_t die_order(const AttendArgs &a) {
     return at >= per ? a.work : die * per + at;
 }
 
-template <class T>
-constexpr int kParts = 2;           // bytes of a query element
-template <>
-constexpr int kParts<float> = 3;
+constexpr int kParts = 3;           // bytes of a query element
 
 // Largest log2 of a weight relative to the running maximum before that is
 // raised, and the offset of all of them, so that f16 holds at most 2^14 (2^15
 // with a step that is up to twice the running one).
-template <class T>
-constexpr float kSlack = 8.0f;
-template <>
-constexpr float kSlack<float> = 1.0f;
-template <class T>
-constexpr float kOffset = 14.0f - kSlack<T>;
+constexpr float kSlack = 1.0f;
+constexpr float kOffset = 14.0f - kSlack;
 
 // The row's query as signed bytes, kk-th piece of 64 columns, part p (the
 // highest first); returns the size of one unit.  v + 0x808080 has, byte by
 // byte, the digits of v in base 256 between -128 and 127, each plus 128.
 template <class T, int KK>
-__device__ __forceinline__ float load_query(const AttendArgs &a, const T *q, bool there, int lane, i32x4 (&parts)[kParts<T>][KK]) {
-    constexpr int N = kParts<T>;
+__device__ __forceinline__ float load_query(const AttendArgs &a, const T *q, bool there, int lane, i32x4 (&parts)[kParts][KK]) {
     float x[KK][16];
     uint32_t bits = 0;              // of the largest magnitude: NaN above infinity above numbers
 #pragma unroll
@@ -128,7 +121,7 @@ __device__ __forceinline__ float load_query(const AttendArgs &a, const T *q, boo
     other = __shfl_xor(bits, 32, kWave);
     bits = other > bits ? other : bits;
     const float top = __builtin_bit_cast(float, bits);
-    constexpr float kUnits = N == 2 ? 127.0f * 256.0f : 127.0f * 65536.0f;
+    constexpr float kUnits = 127.0f * 65536.0f;
     // not finite: a NaN unit makes the row NaN; tiny: zeros
     const float unit = bits >= 0x7f800000u ? __builtin_nanf("") : top < kTiny ? 0.0f : top * (1.0f / kUnits);
     const float size = there ? inverse_step(unit) : 0.0f;
@@ -141,11 +134,11 @@ __device__ __forceinline__ float load_query(const AttendArgs &a, const T *q, boo
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 const float y = inv == 0.0f ? 0.0f : x[kk][4 * w + i] * inv;
-                v[i] = static_cast<int>(rintf(y)) + (N == 2 ? 0x8080 : 0x808080);
+                v[i] = static_cast<int>(rintf(y)) + 0x808080;
             }
 #pragma unroll
-            for (int p = 0; p < N; p++) {
-                const unsigned byte = N - 1 - p;
+            for (int p = 0; p < kParts; p++) {
+                const unsigned byte = kParts - 1 - p;
                 const unsigned two = 0x0c0c0000u | ((4 + byte) << 8) | byte;
                 const int ab = __builtin_amdgcn_perm(v[1], v[0], two), cd = __builtin_amdgcn_perm(v[3], v[2], two);
                 parts[p][kk][w] = (ab | (cd << 16)) ^ 0x80808080;
@@ -201,10 +194,9 @@ __device__ __forceinline__ int clamp_to(int64_t v, int most) {
 // 2), the four that a lane has of each half (4 and 8), a half (16 and more).
 enum Pages { kTokens, kFours, kHalves };
 
-// Wavefronts of a SIMD that the registers are cut for: the most that spill
-// nothing, or (float32, heads above 64, pages of 1 and 2) a few.
-template <class T, int JV, int kPages, int R>
-constexpr int kWavesPerSimd = JV == 16 || R == 2 ? 2 : JV == 8 ? (kParts<T> == 2 && kPages != kTokens ? 3 : 2) : 4;
+// Wavefronts of a SIMD that the registers are cut for.
+template <int JV, int R>
+constexpr int kWavesPerSimd = JV >= 8 || R == 2 ? 2 : 4;
 
 // A wavefront's 32 tokens: where they are, then what they hold.
 template <int JV, int kPages>
@@ -221,8 +213,7 @@ struct Step {
 // wavefronts that share a workgroup's tokens.  R: row tiles of a wavefront, which share the keys'
 // loads and the values' conversion.
 template <class T, int JV, int kPages, int NW, int R>
-__global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kPages, R>)) void attend_kernel(const AttendArgs a) {
-    constexpr int N = kParts<T>;
+__global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_kernel(const AttendArgs a) {
     constexpr int KK = JV >= 4 ? JV / 4 : 1;
     constexpr bool kWhole = kPages == kHalves;
     constexpr int kLooks = Step<JV, kPages>::kLooks;
@@ -259,7 +250,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kPages, R>)) void
     bool there[R];
     int64_t q_row[R];
     int q_head[R], last[R];
-    i32x4 qp[R][N][KK];
+    i32x4 qp[R][kParts][KK];
     float to_log2[R];
 #pragma unroll
     for (int y = 0; y < R; y++) {
@@ -422,9 +413,9 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kPages, R>)) void
             float dot[8], unit[8];
 #pragma unroll
             for (int u = 0; u < 2; u++) {
-                i32x4 acc[N];
+                i32x4 acc[kParts];
 #pragma unroll
-                for (int p = 0; p < N; p++) {
+                for (int p = 0; p < kParts; p++) {
                     acc[p] = i32x4{0, 0, 0, 0};
 #pragma unroll
                     for (int kk = 0; kk < KK; kk++)
@@ -432,9 +423,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kPages, R>)) void
                 }
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
-                    float d = static_cast<float>(acc[0][i] * 256 + acc[1][i]);
-                    if constexpr (N == 3) d = __builtin_fmaf(d, 256.0f, static_cast<float>(acc[2][i]));
-                    dot[4 * u + i] = d;
+                    dot[4 * u + i] = __builtin_fmaf(static_cast<float>(acc[0][i] * 256 + acc[1][i]), 256.0f, static_cast<float>(acc[2][i]));
                     unit[4 * u + i] = ks[4 * u + i] * to_log2[y];
                 }
             }
@@ -460,7 +449,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kPages, R>)) void
 #pragma unroll
                 for (int k = 1; k < 8; k++) top = fmaxf(top, dot[k] * unit[k]);
             }
-            if (__ballot(top > m[y] + kSlack<T>)) {
+            if (__ballot(top > m[y] + kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 16, kWave));
                 top = fmaxf(top, __shfl_xor(top, 32, kWave));
                 const float next = fmaxf(m[y], top);
@@ -471,7 +460,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kPages, R>)) void
                 m[y] = next;
             }
             // ---- weights ----
-            const float from = m[y] == -INFINITY ? 0.0f : m[y] - kOffset<T>;
+            const float from = m[y] == -INFINITY ? 0.0f : m[y] - kOffset;
             float w[8];
 #pragma unroll
             for (int k = 0; k < 8; k++) {
@@ -487,10 +476,8 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kPages, R>)) void
             for (int k = 0; k < 4; k++) {
                 const int pair = pack_f16(w[2 * k], w[2 * k + 1]);
                 hi[y][k] = pair;
-                if constexpr (N == 3) {
-                    const f16x2 h = __builtin_bit_cast(f16x2, pair);    // of a scalar: hi[y][k] would be read as hi[y][0]
-                    lo[y][k] = pack_f16(w[2 * k] - static_cast<float>(h[0]), w[2 * k + 1] - static_cast<float>(h[1]));
-                }
+                const f16x2 h = __builtin_bit_cast(f16x2, pair);        // of a scalar: hi[y][k] would be read as hi[y][0]
+                lo[y][k] = pack_f16(w[2 * k] - static_cast<float>(h[0]), w[2 * k + 1] - static_cast<float>(h[1]));
             }
         }
         // ---- output ----
@@ -506,14 +493,13 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kPages, R>)) void
 #pragma unroll
             for (int y = 0; y < R; y++) {
                 o[y][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, hi[y]), o[y][j], 0, 0, 0);
-                if constexpr (N == 3)
-                    o[y][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, lo[y]), o[y][j], 0, 0, 0);
+                o[y][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, lo[y]), o[y][j], 0, 0, 0);
             }
         }
     };
 
     constexpr int kNext = NW * kTile;
-    constexpr bool kAhead = kWhole && JV < 16 && !(JV == 8 && N == 3);      // as far as registers go
+    constexpr bool kAhead = kWhole && JV < 16 && !(JV == 8 && R == 2);      // as far as registers go
     int t0 = wave * kTile;
     if (t0 < n) {
         if constexpr (!kAhead) {
@@ -624,7 +610,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<T, JV, kPages, R>)) void
                 store_columns<T, JV>(out, JV * (4 * g + i), c.dim, v);
             }
             if (a.lse && g == 0)
-                a.lse[q_row[y] * (a.heads.d * a.group.d) + q_head[y]] = none ? -INFINITY : (m[y] - kOffset<T> + __builtin_amdgcn_logf(l[y])) / kLog2E;
+                a.lse[q_row[y] * (a.heads.d * a.group.d) + q_head[y]] = none ? -INFINITY : (m[y] - kOffset + __builtin_amdgcn_logf(l[y])) / kLog2E;
         }
     }
 }
@@ -717,7 +703,7 @@ __global__ __launch_bounds__((NW == 1 ? kBlock : NW * kWave)) void attend_join_k
     for (int k = 0; k < 4; k++) v[k] = none ? 0.0f : o[k] * norm;
     if (lane < kLanes && 4 * lane < c.width) store_columns<T, 4>(out, 4 * lane, c.dim, v);
     if (a.lse && lane == 0)
-        a.lse[q_row * (c.heads * a.group.d) + q_head] = none ? -INFINITY : (m - kOffset<T> + __builtin_amdgcn_logf(l)) / kLog2E;
+        a.lse[q_row * (c.heads * a.group.d) + q_head] = none ? -INFINITY : (m - kOffset + __builtin_amdgcn_logf(l)) / kLog2E;
 }
 
 // ---- few tokens -------------------------------------------------------------

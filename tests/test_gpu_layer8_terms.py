@@ -1,0 +1,114 @@
+"""Attention over an 8-bit cache where a row's terms differ by many orders of
+magnitude, against float64 and within bounds made of the row's own terms."""
+import math
+
+import numpy as np
+import pytest
+
+import paper_2203_14883_amd as P
+from gpu_util import announce, require_gpu
+from oracle import layer8 as O
+from test_gpu_layer8 import HALF, TYPES, _cache, _host, _tables, _torch_type, _up
+
+pytestmark = pytest.mark.gpu
+
+
+def _bounds(dtype, oc, qh, table, begin, end, scale, want):
+    """Bound of every output's error from the terms p_j |v_j| that it sums.
+
+    With e a bound of the error of a score: a query element is held to 2^-24 of
+    the row's largest; products, sums of at most 256 of them (16 in turn and a
+    tree) and the exponential's argument are float32, 24 roundings at the most.
+    A mean of values whose weights are each off by a factor exp(+-2 e) moves by 2 e
+    of sum p |v|.  Weights are held to 2^-22 of themselves, and to 2^-36 of the row's
+    largest p times step; exponentials to 2^-21; sums are float32, length / 16
+    terms in turn at the least parallel."""
+    B, T, H, D = qh.shape
+    g = H // oc.data.shape[1]
+    all_ = table.shape[1] * oc.P
+    tol = np.zeros(qh.shape)
+    for b in range(B):
+        a = 0 if begin is None else max(0, int(begin[b]))
+        e = all_ if end is None else min(all_, int(end[b]))
+        k, v, ok = oc.tokens(table, b, range(a, max(a, e)))
+        pages = [oc.page(table, b, p // oc.P) for p in range(a, max(a, e))]
+        for t in range(T):
+            see = ok.copy()
+            see[max(0, (all_ if end is None else int(end[b])) - (T - 1 - t) - a):] = False
+            if not see.any():
+                continue
+            step = oc.scales[np.array(pages)[see]][:, :, 1].astype(np.float64)
+            for h in range(H):
+                ks, vs, q = k[see, h // g], v[see, h // g], qh[b, t, h].astype(np.float64)
+                s = ks @ q * scale
+                p = np.exp(s - s.max())
+                p /= p.sum()
+                err = abs(scale) * HALF * (np.abs(q).max() * np.abs(ks).sum(1).max() + 24 * (np.abs(ks) @ np.abs(q)).max())
+                sums = p @ np.abs(vs)
+                tol[b, t, h] = sums * (2 * err + 2.0 ** -20 + (16 + len(p) / 16) * HALF) + len(p) * 127 * 2.0 ** -36 * (p * step[:, h // g]).max()
+    return tol + (2.0 ** -8 * np.abs(want) if dtype == "bf16" else 0)
+
+
+def _check(torch, dtype, c, oc, q, qh, table, begin, end, scale):
+    kw = {}
+    if begin is not None:
+        kw["begin"] = torch.from_numpy(np.asarray(begin, np.int64)).cuda()
+    if end is not None:
+        kw["end"] = torch.from_numpy(np.asarray(end, np.int64)).cuda()
+    out = _host(P.cache_attend(c, q, torch.from_numpy(table).cuda(), scale=scale, **kw))
+    with np.errstate(over="ignore"):
+        want, _ = oc.attend(qh, table, begin, end, scale)
+    tol = _bounds(dtype, oc, qh, table, begin, end, scale, want)
+    assert np.isfinite(out).all()
+    over = np.abs(out - want) / np.maximum(tol, 1e-300)
+    assert np.all(np.abs(out - want) <= tol), "largest error %.3g of its bound" % over.max()
+    return out
+
+
+# what a call of so many places, rows and sequences runs: few tokens; one wavefront; four; chunks; two row tiles
+LAYOUTS = [(1, 1, 1, 10, 3), (4, 1, 1, 48, 2), (1, 1, 3, 60, 2), (16, 2, 3, 64, 2), (1, 1, 2, 300, 2), (4, 1, 2, 300, 3), (16, 2, 2, 300, 2),
+           (64, 1, 1, 300, 1), (16, 1, 2, 3000, 1), (2, 1, 1, 2000, 1), (16, 1, 20, 200, 2), (4, 1, 40, 1500, 1)]
+
+
+@pytest.mark.parametrize("page,heads,group,length,B", LAYOUTS)
+def test_attend_bfloat16_small_elements_beside_a_large_one(page, heads, group, length, B):
+    """One column of the query is 4096 times the others, where every key is 0: the others make the scores."""
+    torch = require_gpu()
+    announce("bfloat16 query with an outlier, page %d rows %d tokens %d" % (page, group, length))
+    rng = np.random.default_rng(length + group)
+    D, need = 64, -(-length // page)
+    c, oc = _cache(rng, torch, B * need, heads, page, D)
+    oc.data[:, :, 0, :, 5] = 0
+    c.data[:, :, 0, :, 5] = 0
+    table = _tables(rng, np.full(B, need), need, B * need)
+    qh = rng.standard_normal((B, 1, heads * group, D))
+    qh[..., 5] = 4096
+    q, qh = _up(torch, qh, "bf16")
+    _check(torch, "bf16", c, oc, q, qh, table, None, np.full(B, length), 1 / math.sqrt(D))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("page,group,length", [(1, 1, 12), (1, 3, 60), (16, 3, 64), (16, 2, 200), (4, 2, 200), (1, 2, 200), (16, 20, 200)])
+def test_attend_weights_whose_terms_cancel(page, group, length, dtype):
+    """A last token that takes away what the others add up to: what is left shows how the weights are held."""
+    torch = require_gpu()
+    announce("terms that cancel, page %d rows %d tokens %d %s" % (page, group, length, dtype))
+    rng = np.random.default_rng(length * 3 + group)
+    D, need = 32, -(-length // page)
+    c, oc = _cache(rng, torch, need, 1, page, D)
+    oc.scales[..., 0] = 2.0 ** -12
+    oc.scales[..., 1] = 0.5
+    oc.data[:, 0, 0] = rng.integers(-3, 4, oc.data[:, 0, 0].shape)
+    table = _tables(rng, np.array([need]), need, need)
+    qh = np.ones((1, 1, group, D)) * (1 + np.arange(group)[:, None] % 2)
+    last, row = oc.page(table, 0, (length - 1) // page), (length - 1) % page
+    oc.data[last, 0, 0, row] = 127
+    scale = 0.75 * math.log(length) / (127 * D * 2.0 ** -12)         # its weight is length^0.75 of the others'
+    q, qh = _up(torch, qh, dtype)
+    k, v, _ = oc.tokens(table, 0, range(length))
+    p = np.exp((k[:, 0] @ qh[0, 0, 0].astype(np.float64)) * scale)
+    take = -(p[:-1] @ v[:-1, 0]) / p[-1] / 0.5                      # so the terms of every other row cancel
+    oc.data[last, 0, 1, row, :D] = np.clip(np.rint(take), -127, 127)
+    c.data.copy_(torch.from_numpy(oc.data))
+    c.scales.copy_(torch.from_numpy(oc.scales))
+    _check(torch, dtype, c, oc, q, qh, table, None, np.array([length]), scale)
