@@ -22,10 +22,12 @@
 //           column's bytes with v_perm.  A byte b ^ 0x80 = v + 128 read as the bits
 //           of an f16 is (v + 128) 2^-24, and one packed fused multiply-add
 //           makes it v 2^-9, exactly.
-//   P       carries the step of its token's page over the largest step seen so
-//           far (a running one, like the maximum), so that pages of any steps
-//           add up.  P is two f16, the second the rounding error of the
-//           first: 2^-22 of each weight.
+//   P       carries the step of its token's page.  Its unit is a row's own: a
+//           power of two that follows the largest exponential times step that
+//           the row has summed, so that what has weight keeps its bits, however
+//           large the steps are of what has none or is not seen.  P is two f16,
+//           the second the rounding error of the first: 2^-22 of each weight,
+//           or 2^-36 of the largest.
 //
 // Few rows a head: bound by memory.  1,000,003 tokens of 8 heads of 128 in pages
 // of 64 (2.05 GB), 4 query heads each, 349 us, 5.9 TB/s, and 7 us to join 253
@@ -94,11 +96,15 @@ __device__ __forceinline__ uint32_t die_order(const AttendArgs &a) {
 
 constexpr int kParts = 3;           // bytes of a query element
 
-// Largest log2 of a weight relative to the running maximum before that is
-// raised, and the offset of all of them, so that f16 holds at most 2^14 (2^15
-// with a step that is up to twice the running one).
-constexpr float kSlack = 1.0f;
-constexpr float kOffset = 14.0f - kSlack;
+// Exponentials are taken relative to a whole power of two, which is raised when
+// one of them would pass 2^kSlack: their sum is float32 and has room.
+constexpr float kSlack = 4.0f;
+
+// Exponential times step in the row's unit is f16.  One that would pass kLimit
+// makes the unit larger, so that it lies in [2^(kTop - 1), 2^kTop).  kFinest is the
+// inverse of the smallest unit, which is the first: steps are at least 2^-107.
+constexpr float kLimit = 32768.0f, kFinest = 0x1p126f;
+constexpr int kTop = 12;
 
 // The row's query as signed bytes, kk-th piece of 64 columns, part p (the
 // highest first); returns the size of one unit.  v + 0x808080 has, byte by
@@ -268,15 +274,15 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
     }
 
     f32x4 o[R][JV];
-    float m[R], l[R];
+    float m[R], l[R], inv[R];                                   // inv: of the unit that o is in, 2^-9 of it
 #pragma unroll
     for (int y = 0; y < R; y++) {
         m[y] = -INFINITY;
         l[y] = 0.0f;
+        inv[y] = kFinest;
 #pragma unroll
         for (int j = 0; j < JV; j++) o[y][j] = f32x4{0, 0, 0, 0};
     }
-    float step = 0x1p-126f, inv = 0x1p126f;                     // the running step of values
 
     const uint32_t width = c.width;
     const uint32_t block = width << c.shift;
@@ -387,25 +393,6 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
         if constexpr (kWhole) masked = masked || x.page[0] < 0 || x.page[1] < 0;
         else masked = masked || __ballot(x.page[0] < 0) != 0;
 
-        // ---- the running step of values ----
-        float big = fmaxf(fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3])), fmaxf(fmaxf(vs[4], vs[5]), fmaxf(vs[6], vs[7])));
-        if (__ballot(big > 2.0f * step)) {
-            if constexpr (!kWhole) {                            // else the same in every lane
-                big = fmaxf(big, __shfl_xor(big, 16, kWave));
-                big = fmaxf(big, __shfl_xor(big, 32, kWave));
-            }
-            const float f = step / big;
-#pragma unroll
-            for (int y = 0; y < R; y++)
-#pragma unroll
-                for (int j = 0; j < JV; j++) o[y][j] *= f;
-            step = big;
-            inv = 1.0f / big;
-        }
-
-        float vw[8];
-#pragma unroll
-        for (int k = 0; k < 8; k++) vw[k] = vs[k] * inv;
         i32x4 hi[R], lo[R];
 #pragma unroll
         for (int y = 0; y < R; y++) {
@@ -452,32 +439,54 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
             if (__ballot(top > m[y] + kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 16, kWave));
                 top = fmaxf(top, __shfl_xor(top, 32, kWave));
-                const float next = fmaxf(m[y], top);
-                const float f = m[y] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[y] - next);
-                l[y] *= f;
+                const float next = fmaxf(m[y], ceilf(top));
+                if (m[y] != -INFINITY) {
+                    // o stays as it is: relative to the new maximum its unit is smaller
+                    const float finer = inv[y] * __builtin_amdgcn_exp2f(next - m[y]);
+                    l[y] *= __builtin_amdgcn_exp2f(m[y] - next);
+                    inv[y] = finer > kFinest ? kFinest : finer;
+                    if (finer > kFinest) {
 #pragma unroll
-                for (int j = 0; j < JV; j++) o[y][j] *= f;
+                        for (int j = 0; j < JV; j++) o[y][j] *= kFinest / finer;
+                    }
+                }
                 m[y] = next;
             }
-            // ---- weights ----
-            const float from = m[y] == -INFINITY ? 0.0f : m[y] - kOffset;
+            // ---- weights, times steps ----
+            const float from = m[y] == -INFINITY ? 0.0f : m[y];
             float w[8];
 #pragma unroll
             for (int k = 0; k < 8; k++) {
                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(dot[k], unit[k], -from));
                 l[y] += p;
-                w[k] = p * vw[k];
+                w[k] = p * vs[k];
             }
             if (masked) {
 #pragma unroll
                 for (int k = 0; k < 8; k++) w[k] = (hide >> k) & 1 ? 0.0f : w[k];    // a step that is not seen may be NaN
             }
+            // ---- the row's unit ----
+            float big = fmaxf(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])), fmaxf(fmaxf(w[4], w[5]), fmaxf(w[6], w[7])));
+            if (__ballot(big * inv[y] > kLimit)) {
+                big = fmaxf(big, __shfl_xor(big, 16, kWave));
+                big = fmaxf(big, __shfl_xor(big, 32, kWave));
+                if (big * inv[y] > kLimit) {
+                    const float next = ldexpf(1.0f, kTop - __builtin_amdgcn_frexp_expf(big));
+#pragma unroll
+                    for (int j = 0; j < JV; j++) o[y][j] *= next / inv[y];
+                    inv[y] = next;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 8; k++) w[k] *= inv[y];
 #pragma unroll
             for (int k = 0; k < 4; k++) {
-                const int pair = pack_f16(w[2 * k], w[2 * k + 1]);
+                int pair = pack_f16(w[2 * k], w[2 * k + 1]);
+                asm("" : "+v"(pair));                                   // or each half would be converted once more by itself
                 hi[y][k] = pair;
                 const f16x2 h = __builtin_bit_cast(f16x2, pair);        // of a scalar: hi[y][k] would be read as hi[y][0]
-                lo[y][k] = pack_f16(w[2 * k] - static_cast<float>(h[0]), w[2 * k + 1] - static_cast<float>(h[1]));
+                lo[y][k] = pack_f16(__builtin_fmaf(static_cast<float>(h[0]), -1.0f, w[2 * k]),
+                                    __builtin_fmaf(static_cast<float>(h[1]), -1.0f, w[2 * k + 1]));
             }
         }
         // ---- output ----
@@ -549,7 +558,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
     for (int y = 0; y < R; y++) {
         l[y] += __shfl_xor(l[y], 16, kWave);
         l[y] += __shfl_xor(l[y], 32, kWave);
-        float back = step * 512.0f;
+        float back = 512.0f / inv[y];
         if constexpr (NW > 1) {
             if (y > 0) __syncthreads();
             if (lane < 16) {
@@ -610,7 +619,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
                 store_columns<T, JV>(out, JV * (4 * g + i), c.dim, v);
             }
             if (a.lse && g == 0)
-                a.lse[q_row[y] * (a.heads.d * a.group.d) + q_head[y]] = none ? -INFINITY : (m[y] - kOffset + __builtin_amdgcn_logf(l[y])) / kLog2E;
+                a.lse[q_row[y] * (a.heads.d * a.group.d) + q_head[y]] = none ? -INFINITY : (m[y] + __builtin_amdgcn_logf(l[y])) / kLog2E;
         }
     }
 }
@@ -703,7 +712,7 @@ __global__ __launch_bounds__((NW == 1 ? kBlock : NW * kWave)) void attend_join_k
     for (int k = 0; k < 4; k++) v[k] = none ? 0.0f : o[k] * norm;
     if (lane < kLanes && 4 * lane < c.width) store_columns<T, 4>(out, 4 * lane, c.dim, v);
     if (a.lse && lane == 0)
-        a.lse[q_row * (c.heads * a.group.d) + q_head] = none ? -INFINITY : (m - kOffset + __builtin_amdgcn_logf(l)) / kLog2E;
+        a.lse[q_row * (c.heads * a.group.d) + q_head] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) / kLog2E;
 }
 
 // ---- few tokens -------------------------------------------------------------

@@ -112,3 +112,93 @@ def test_attend_weights_whose_terms_cancel(page, group, length, dtype):
     c.data.copy_(torch.from_numpy(oc.data))
     c.scales.copy_(torch.from_numpy(oc.scales))
     _check(torch, dtype, c, oc, q, qh, table, None, np.array([length]), scale)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("ratio", [2.0 ** 12, 2.0 ** 24, 2.0 ** 32, 2.0 ** 60, 2.0 ** 100])
+@pytest.mark.parametrize("page,heads,group,length,B", LAYOUTS)
+def test_attend_a_large_step_without_weight(page, heads, group, length, B, ratio, dtype):
+    """A first page whose step is ratio times the others' and whose scores lie so far below that its terms are as small as theirs."""
+    torch = require_gpu()
+    announce("large step %g, page %d rows %d tokens %d %s" % (ratio, page, group, length, dtype))
+    rng = np.random.default_rng(length + group)
+    D, need = 32, -(-length // page)
+    c, oc = _cache(rng, torch, B * need, heads, page, D)
+    oc.scales[:] = 2.0 ** -6
+    oc.data[:, :, 0] = rng.integers(-9, 10, oc.data[:, :, 0].shape)
+    oc.data[:, :, 1, :, :D] = 100
+    table = _tables(rng, np.full(B, need), need, B * need)
+    qh = np.ones((B, 1, heads * group, D))
+    scale = 1 / math.sqrt(D)
+    below = (math.log(ratio) + 3) / (D * scale)
+    for b in range(B):
+        for at in (0, need // 2):           # the first page, and one that comes later
+            oc.data[table[b, at], :, 0] = -127
+            oc.scales[table[b, at], :, 0] = below / 127
+            oc.scales[table[b, at], :, 1] *= ratio
+    c.data.copy_(torch.from_numpy(oc.data))
+    c.scales.copy_(torch.from_numpy(oc.scales))
+    q, qh = _up(torch, qh, dtype)
+    _check(torch, dtype, c, oc, q, qh, table, None, np.full(B, length), scale)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("page,heads,group,length,B", LAYOUTS)
+def test_attend_terms_of_any_size(page, heads, group, length, B, dtype):
+    """Steps from 1e-20 to 1e20 in no order, scores up to 40 either way: any token may make the output."""
+    torch = require_gpu()
+    announce("terms of any size, page %d rows %d tokens %d %s" % (page, group, length, dtype))
+    rng = np.random.default_rng(7 * length + group)
+    D, need = 16, -(-length // page)
+    c, oc = _cache(rng, torch, B * need, heads, page, D)
+    oc.scales[..., 1] = 10.0 ** rng.uniform(-20, 20, oc.scales[..., 1].shape)
+    oc.scales[..., 0] = 40.0 / 127 / D
+    oc.data[:, :, 0, :, :D] = rng.integers(-127, 128, oc.data.shape[:2] + (page, 1))
+    c.data.copy_(torch.from_numpy(oc.data))
+    c.scales.copy_(torch.from_numpy(oc.scales))
+    table = _tables(rng, np.full(B, need), need, B * need)
+    q, qh = _up(torch, rng.uniform(0.2, 1, (B, 1, heads * group, 1)) * np.ones(D), dtype)
+    _check(torch, dtype, c, oc, q, qh, table, None, np.full(B, length), 1.0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("up", [1, -1])
+@pytest.mark.parametrize("page,group,length", [(1, 2, 60), (16, 2, 300), (4, 1, 900), (2, 2, 3000), (16, 9, 300)])
+def test_attend_scores_that_rise_while_steps_fall(page, group, length, up, dtype):
+    """Scores grow along the history by 75 in all while steps shrink as fast, or the other way."""
+    torch = require_gpu()
+    announce("rising scores %d, page %d rows %d tokens %d %s" % (up, page, group, length, dtype))
+    rng = np.random.default_rng(length)
+    D, need = 16, -(-length // page)
+    c, oc = _cache(rng, torch, need, 1, page, D)
+    along = np.linspace(0, 1, need) if up > 0 else np.linspace(1, 0, need)
+    table = np.arange(need, dtype=np.int32)[None]
+    oc.data[:, 0, 0, :, :D] = 127
+    oc.scales[:, 0, 0] = np.maximum(along, 1e-3) * 75 / 127 / D
+    oc.scales[:, 0, 1] = np.exp(-75 * along + 20)
+    c.data.copy_(torch.from_numpy(oc.data))
+    c.scales.copy_(torch.from_numpy(oc.scales))
+    q, qh = _up(torch, np.ones((1, 1, group, D)), dtype)
+    _check(torch, dtype, c, oc, q, qh, table, None, np.array([length]), 1.0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("page,group,T,length", [(1, 1, 3, 50), (1, 1, 3, 300), (4, 2, 5, 300), (16, 1, 3, 146), (16, 4, 9, 290), (1, 1, 40, 200), (1, 2, 3, 3000)])
+def test_attend_a_later_event_changes_no_earlier_query(page, group, T, length, dtype):
+    """The newest tokens have steps 2^40 times the others': queries that do not see them are as they are without."""
+    torch = require_gpu()
+    announce("later event, page %d rows %d queries %d tokens %d %s" % (page, group, T, length, dtype))
+    rng = np.random.default_rng(length + T)
+    D, need = 48, -(-length // page)
+    c, oc = _cache(rng, torch, need, 1, page, D)
+    table = np.arange(need, dtype=np.int32)[None]
+    oc.scales[:] = 1 / 64
+    new = (length - 1) // page              # the page that the newest token is on
+    oc.scales[new] = (1 / 64, 2.0 ** 34)
+    c.scales.copy_(torch.from_numpy(oc.scales))
+    q, qh = _up(torch, rng.standard_normal((1, T, group, D)), dtype)
+    out = _check(torch, dtype, c, oc, q, qh, table, None, np.array([length]), 1 / math.sqrt(D))
+    for t in range(T):
+        if length - (T - 1 - t) <= new * page:                              # sees none of that page
+            _check(torch, dtype, c, oc, q[:, t:t + 1], qh[:, t:t + 1], table, None, np.array([length - (T - 1 - t)]), 1 / math.sqrt(D))
+            assert np.abs(out[0, t]).max() < 100
