@@ -551,6 +551,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
     }
 
     // ---- join the lanes of a row, then the wavefronts ----
+    // what is joined is means, with weights of at most 1: sums of values could overflow
     constexpr int kPad = 16 * JV + 4;
     __shared__ float so[NW > 1 ? NW - 1 : 1][kRows][kPad];
     __shared__ float sm[NW][kRows], sl[NW][kRows];
@@ -558,7 +559,8 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
     for (int y = 0; y < R; y++) {
         l[y] += __shfl_xor(l[y], 16, kWave);
         l[y] += __shfl_xor(l[y], 32, kWave);
-        float back = 512.0f / inv[y];
+        const float back = 512.0f / inv[y];
+        float norm = l[y] == 0.0f ? 0.0f : back / l[y];         // a NaN among what is seen stays one
         if constexpr (NW > 1) {
             if (y > 0) __syncthreads();
             if (lane < 16) {
@@ -569,38 +571,42 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
 #pragma unroll
                 for (int i = 0; i < 4; i++)
 #pragma unroll
-                    for (int j = 0; j < JV; j++) so[wave - 1][i16][JV * (4 * g + i) + j] = o[y][j][i] * back;
+                    for (int j = 0; j < JV; j++) so[wave - 1][i16][JV * (4 * g + i) + j] = o[y][j][i] * norm;
             }
             __syncthreads();
             if (wave == 0) {
                 float all_m = m[y];
 #pragma unroll
                 for (int w = 1; w < NW; w++) all_m = fmaxf(all_m, sm[w][i16]);
-                const float f0 = m[y] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[y] - all_m);
-                l[y] *= f0;
-#pragma unroll
-                for (int j = 0; j < JV; j++) o[y][j] *= back * f0;
-                back = 1.0f;
+                float f[NW];
+                f[0] = m[y] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[y] - all_m);
+                l[y] *= f[0];
 #pragma unroll
                 for (int w = 1; w < NW; w++) {
-                    const float f = sm[w][i16] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][i16] - all_m);
-                    l[y] += sl[w][i16] * f;
+                    f[w] = sl[w][i16] * (sm[w][i16] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][i16] - all_m));
+                    l[y] += f[w];
+                }
+                const float part = l[y] == 0.0f ? 0.0f : 1.0f / l[y];
+#pragma unroll
+                for (int j = 0; j < JV; j++) o[y][j] *= back * (f[0] * part);
+#pragma unroll
+                for (int w = 1; w < NW; w++)
 #pragma unroll
                     for (int i = 0; i < 4; i++)
 #pragma unroll
-                        for (int j = 0; j < JV; j++) o[y][j][i] += so[w - 1][i16][JV * (4 * g + i) + j] * f;
-                }
+                        for (int j = 0; j < JV; j++) o[y][j][i] += so[w - 1][i16][JV * (4 * g + i) + j] * (f[w] * part);
                 m[y] = all_m;
+                norm = 1.0f;
             }
         }
-        const bool none = l[y] == 0.0f;             // a NaN among what is seen stays one
+        const bool none = l[y] == 0.0f;
         if (wave == 0 && there[y] && a.part_o) {
             const int64_t at = (static_cast<int64_t>(bh) * a.rows + r0 + kRows * y + i16) * a.chunks + chunk;
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 float v[JV];
 #pragma unroll
-                for (int j = 0; j < JV; j++) v[j] = o[y][j][i] * back;
+                for (int j = 0; j < JV; j++) v[j] = o[y][j][i] * norm;
                 store_columns<float, JV>(a.part_o + at * width, JV * (4 * g + i), width, v);
             }
             if (g == 0) {
@@ -610,7 +616,6 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
         }
         if (wave == 0 && there[y] && !a.part_o) {
             T *out = static_cast<T *>(a.out) + q_row[y] * a.ot + q_head[y] * a.oh;
-            const float norm = none ? 0.0f : back / l[y];
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 float v[JV];
@@ -624,7 +629,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
     }
 }
 
-// Joins the chunks of a row with NW wavefronts.  A lane takes four columns of
+// Joins the chunks of a row, a mean each, with NW wavefronts.  A lane takes four columns of
 // every (NW kWave / kLanes)-th chunk, kLanes the lanes of a row's columns, eight
 // chunks in flight (253 chunks of 32 rows of 128: 7 us; 212 us with a wavefront
 // per row and a chunk at a time).  With NW = 1 a workgroup has a row for each of its
@@ -668,6 +673,21 @@ __global__ __launch_bounds__((NW == 1 ? kBlock : NW * kWave)) void attend_join_k
         for (int y = 0; y < NW; y++) m = fmaxf(m, sm[y]);
     }
     float l = 0.0f;
+    for (int i = wave * kWave + lane; i < n; i += NW * kWave) {
+        const float2 w = ml[i];
+        l += w.y * (w.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(w.x - m));
+    }
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) l += __shfl_xor(l, d, kWave);
+    if constexpr (NW > 1) {
+        if (lane == 0) sl[wave] = l;
+        __syncthreads();
+        l = 0.0f;
+#pragma unroll
+        for (int y = 0; y < NW; y++) l += sl[y];
+    }
+    const bool none = l == 0.0f;
+    const float part = none ? 0.0f : 1.0f / l;
     f32x4 o = {0, 0, 0, 0};
     for (int i0 = (wave * kWave + lane) / kLanes; i0 < n; i0 += kStep * kStride) {
         f32x4 v[kStep];
@@ -681,35 +701,25 @@ __global__ __launch_bounds__((NW == 1 ? kBlock : NW * kWave)) void attend_join_k
 #pragma unroll
         for (int y = 0; y < kStep; y++) {
             if (i0 + y * kStride >= n) continue;
-            const float f = w[y].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(w[y].x - m);
-            l += w[y].y * f;
-            o += v[y] * f;
+            o += v[y] * (w[y].y * (w[y].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(w[y].x - m)) * part);
         }
     }
     // the wavefront's other chunks, then the other wavefronts
 #pragma unroll
-    for (int d = kLanes; d < kWave; d <<= 1) {
-        l += __shfl_xor(l, d, kWave);
+    for (int d = kLanes; d < kWave; d <<= 1)
 #pragma unroll
         for (int k = 0; k < 4; k++) o[k] += __shfl_xor(o[k], d, kWave);
-    }
     if constexpr (NW > 1) {
         if (lane < kLanes) *reinterpret_cast<f32x4 *>(&so[wave][4 * lane]) = o;
-        if (lane == 0) sl[wave] = l;
         __syncthreads();
         if (wave > 0) return;
 #pragma unroll
-        for (int y = 1; y < NW; y++) {
-            l += sl[y];
-            o += *reinterpret_cast<const f32x4 *>(&so[y][4 * (lane % kLanes)]);
-        }
+        for (int y = 1; y < NW; y++) o += *reinterpret_cast<const f32x4 *>(&so[y][4 * (lane % kLanes)]);
     }
-    const bool none = l == 0.0f;
     T *out = static_cast<T *>(a.out) + q_row * a.ot + q_head * a.oh;
-    const float norm = 1.0f / l;
     float v[4];
 #pragma unroll
-    for (int k = 0; k < 4; k++) v[k] = none ? 0.0f : o[k] * norm;
+    for (int k = 0; k < 4; k++) v[k] = none ? 0.0f : o[k];
     if (lane < kLanes && 4 * lane < c.width) store_columns<T, 4>(out, 4 * lane, c.dim, v);
     if (a.lse && lane == 0)
         a.lse[q_row * (c.heads * a.group.d) + q_head] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) / kLog2E;
@@ -748,6 +758,8 @@ template <int J>
 __device__ __forceinline__ int from_lane(int v) {
     return __builtin_amdgcn_ds_swizzle(v, (J << 5) | 0x10);
 }
+
+constexpr float kFew = 64.0f;       // tokens at most, see few()
 
 template <class T, int JV>
 __global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(const AttendArgs a) {
@@ -823,7 +835,7 @@ __global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(
             m = next;
             const float e = __builtin_amdgcn_exp2f(s - (m == -INFINITY ? 0.0f : m));
             l = l * f + e;
-            const int w = __builtin_bit_cast(int, page < 0 ? 0.0f : e * sc.y);
+            const int w = __builtin_bit_cast(int, page < 0 ? 0.0f : e * (sc.y * (1.0f / kFew)));     // the sum stays below the largest value
 #pragma unroll
             for (int k = 0; k < JV; k++) o[k] *= f;
             unrolled<16>([&](auto J) {
@@ -839,7 +851,7 @@ __global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(
         l += dpp<kXor2>(l);
         l += dpp<kXor1>(l);
         const bool none = l == 0.0f;
-        const float norm = 1.0f / l;
+        const float norm = kFew / l;
 #pragma unroll
         for (int k = 0; k < JV; k++) o[k] = none ? 0.0f : o[k] * norm;
         if (there) {
@@ -936,7 +948,7 @@ void launch(const AttendArgs &a, int nw, hipStream_t st) {
 // 79 / 51.
 bool few(const AttendArgs &a) {
     const int64_t tokens = static_cast<int64_t>(a.s.pages_per_seq) << a.c.shift;
-    return a.rows * ((tokens + 15) / 16) <= 2 || (a.rows == 1 && tokens <= 64);
+    return a.rows * ((tokens + 15) / 16) <= 2 || (a.rows == 1 && tokens <= static_cast<int64_t>(kFew));
 }
 
 // Wavefronts that share a sequence's tokens.  One to itself needs no join

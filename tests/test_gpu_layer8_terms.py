@@ -202,3 +202,21 @@ def test_attend_a_later_event_changes_no_earlier_query(page, group, T, length, d
         if length - (T - 1 - t) <= new * page:                              # sees none of that page
             _check(torch, dtype, c, oc, q[:, t:t + 1], qh[:, t:t + 1], table, None, np.array([length - (T - 1 - t)]), 1 / math.sqrt(D))
             assert np.abs(out[0, t]).max() < 100
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("page,heads,group,length,B", LAYOUTS)
+def test_attend_values_near_the_largest_float(page, heads, group, length, B, dtype):
+    """A mean of values near 1.7e38 is such a value, however many there are."""
+    torch = require_gpu()
+    announce("large values, page %d rows %d tokens %d %s" % (page, group, length, dtype))
+    rng = np.random.default_rng(length + 2 * group)
+    D, need = 32, -(-length // page)
+    c, oc = _cache(rng, torch, B * need, heads, page, D)
+    oc.scales[..., 1] = 2.0 ** 120
+    oc.data[:, :, 1, :, :D] = rng.integers(90, 128, oc.data[:, :, 1, :, :D].shape)
+    c.data.copy_(torch.from_numpy(oc.data))
+    c.scales.copy_(torch.from_numpy(oc.scales))
+    table = _tables(rng, np.full(B, need), need, B * need)
+    q, qh = _up(torch, rng.standard_normal((B, 1, heads * group, D)), dtype)
+    _check(torch, dtype, c, oc, q, qh, table, None, np.full(B, length), 1 / math.sqrt(D))
