@@ -731,7 +731,9 @@ tgl_status tgl_cache_read(const tgl_cache *cache, const tgl_heads *k, const tgl_
  *   score_j = scale * <q, k_j>
  *   out = sum_j exp(score_j) v_j / sum_j exp(score_j)
  *   lse = log(sum_j exp(score_j))
- * over what it sees; where that is nothing, out = 0 and lse = -inf.  Query
+ * over what it sees; where that is nothing, out = 0 and lse = -inf.  A row
+ * that sees something and whose largest score is not finite in float32, or whose
+ * query is not, is NaN.  Query
  * head h reads the cache's head h / (q_heads / heads).  Sampled slots are a
  * cache of one-token pages with the slots' neighbour ids as the table.
  *   q          [device] num_seqs * queries x q_heads x dim elements of type dtype

@@ -48,6 +48,7 @@ using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
 
 constexpr int kRows = 16;           // rows of a tile
 constexpr int kTile = 32;           // tokens of a wavefront's step
+constexpr float kLowest = -3.4028235e38f;
 constexpr float kLog2E = 1.44269504088896340736f;
 
 enum Order { kInTurn, kHeadsInTurn, kStretches };
@@ -275,11 +276,13 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
 
     f32x4 o[R][JV];
     float m[R], l[R], inv[R];                                   // inv: of the unit that o is in, 2^-9 of it
+    int unseen[R];                                              // bit k: none of the lane's k-th tokens was seen
 #pragma unroll
     for (int y = 0; y < R; y++) {
         m[y] = -INFINITY;
         l[y] = 0.0f;
         inv[y] = kFinest;
+        unseen[y] = 0xff;
 #pragma unroll
         for (int j = 0; j < JV; j++) o[y][j] = f32x4{0, 0, 0, 0};
     }
@@ -426,6 +429,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
                     unit[k] = hidden ? 1.0f : unit[k];          // -inf stays -inf whatever the page's step is
                 }
             }
+            unseen[y] &= hide;
             // ---- the running maximum (of nothing where -inf meets a unit of 0: NaN, which fmaxf drops) ----
             float top;
             if constexpr (kPages != kTokens) {                  // one unit for each half's four
@@ -559,6 +563,10 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
     for (int y = 0; y < R; y++) {
         l[y] += __shfl_xor(l[y], 16, kWave);
         l[y] += __shfl_xor(l[y], 32, kWave);
+        // -inf is the maximum of nothing; seen scores of -inf have a maximum below every other
+        const bool seen = __shfl_xor(unseen[y], 16, kWave) != 0xff || __shfl_xor(unseen[y], 32, kWave) != 0xff ||
+                          __shfl_xor(unseen[y], 48, kWave) != 0xff || unseen[y] != 0xff;
+        if (m[y] == -INFINITY && seen) m[y] = kLowest;
         const float back = 512.0f / inv[y];
         float norm = l[y] == 0.0f ? 0.0f : back / l[y];         // a NaN among what is seen stays one
         if constexpr (NW > 1) {
@@ -599,7 +607,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
                 norm = 1.0f;
             }
         }
-        const bool none = l[y] == 0.0f;
+        const bool none = m[y] == -INFINITY;
         if (wave == 0 && there[y] && a.part_o) {
             const int64_t at = (static_cast<int64_t>(bh) * a.rows + r0 + kRows * y + i16) * a.chunks + chunk;
 #pragma unroll
@@ -615,6 +623,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
             }
         }
         if (wave == 0 && there[y] && !a.part_o) {
+            if (!none && l[y] == 0.0f) l[y] = norm = __builtin_nanf("");    // the largest score is infinite
             T *out = static_cast<T *>(a.out) + q_row[y] * a.ot + q_head[y] * a.oh;
 #pragma unroll
             for (int i = 0; i < 4; i++) {
@@ -686,7 +695,8 @@ __global__ __launch_bounds__((NW == 1 ? kBlock : NW * kWave)) void attend_join_k
 #pragma unroll
         for (int y = 0; y < NW; y++) l += sl[y];
     }
-    const bool none = l == 0.0f;
+    const bool none = m == -INFINITY;
+    if (!none && l == 0.0f) l = __builtin_nanf("");         // the largest score is infinite
     const float part = none ? 0.0f : 1.0f / l;
     f32x4 o = {0, 0, 0, 0};
     for (int i0 = (wave * kWave + lane) / kLanes; i0 < n; i0 += kStep * kStride) {
@@ -790,8 +800,12 @@ __global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(
         const int n = there ? clamp_to(stop - begin, 1 << 30) : 0;
         float q[JV];
         load_columns<T, JV>(static_cast<const T *>(a.q) + q_row * a.qt + q_head * a.qh, JV * i, c.dim, q);
+        bool odd = false, seen = false;             // an element that is no number; a token that is seen
 #pragma unroll
-        for (int k = 0; k < JV; k++) q[k] *= a.scale * kLog2E;
+        for (int k = 0; k < JV; k++) {
+            q[k] *= a.scale * kLog2E;
+            odd |= !(fabsf(q[k]) < INFINITY);
+        }
         float m = -INFINITY, l = 0.0f, o[JV] = {};
         for (int j0 = 0; __any(j0 < n); j0 += 16) {
             int page = -1;
@@ -826,6 +840,7 @@ __global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(
             scatter_sum<2, kXor2, 2>(p, i);
             scatter_sum<1, kXor1, 1>(p, i);
             const float s = page < 0 ? -INFINITY : p[0] * sc.x;
+            seen |= page >= 0;
             float top = fmaxf(s, dpp<kXor8>(s));
             top = fmaxf(top, dpp<kXor7>(top));
             top = fmaxf(top, dpp<kXor2>(top));
@@ -850,7 +865,8 @@ __global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(
         l += dpp<kXor7>(l);
         l += dpp<kXor2>(l);
         l += dpp<kXor1>(l);
-        const bool none = l == 0.0f;
+        const bool none = group_ballot<16>(seen) == 0, bad = group_ballot<16>(odd) != 0;
+        if (l == 0.0f || bad) l = __builtin_nanf("");       // every score -inf, or a query that is no number
         const float norm = kFew / l;
 #pragma unroll
         for (int k = 0; k < JV; k++) o[k] = none ? 0.0f : o[k] * norm;

@@ -363,7 +363,7 @@ def cache_attend(cache: HistoryCache, q: torch.Tensor, table: torch.Tensor, begi
     a table of a node's pages is attention over its history, and the
     neighbour ids of sampled slots over one-token pages is attention over
     the sampled neighbours.  ``scale`` defaults to ``1 / sqrt(dim)``.  Rows that
-    see nothing are 0.  Queries are held to 2^-24 of their row's largest element and
+    see nothing are 0; rows whose largest score is no finite number are NaN.  Queries are held to 2^-24 of their row's largest element and
     weights to 2^-22 of themselves, in either type.  Returns ``out`` like q, and with ``return_lse`` the
     logarithm of each row's sum of exponentials, float32 ``[B(, T), q_heads]``."""
     dev = _cache_device(cache)

@@ -220,3 +220,37 @@ def test_attend_values_near_the_largest_float(page, heads, group, length, B, dty
     table = _tables(rng, np.full(B, need), need, B * need)
     q, qh = _up(torch, rng.standard_normal((B, 1, heads * group, D)), dtype)
     _check(torch, dtype, c, oc, q, qh, table, None, np.full(B, length), 1 / math.sqrt(D))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("page,group,T,length", [(1, 1, 1, 1), (1, 1, 1, 10), (4, 1, 1, 60), (1, 2, 1, 16), (1, 3, 1, 60), (16, 2, 2, 64), (1, 2, 1, 300),
+                                                 (16, 2, 1, 300), (4, 1, 1, 3000), (16, 20, 1, 200)])
+def test_attend_scores_that_are_no_numbers(page, group, T, length, dtype):
+    """A row whose largest score is not finite is NaN, whichever sign made it; one that sees nothing is 0."""
+    torch = require_gpu()
+    announce("scores without end, page %d rows %d x %d tokens %d %s" % (page, group, T, length, dtype))
+    D, need = 16, -(-length // page)
+    B = 4
+    near = 7 * (2.0 ** -20 + (16 + length / 16) * HALF)                     # bfloat16: rounded to 7 itself
+    data = torch.zeros(need, 1, 2, page, D, dtype=torch.int8).cuda()
+    data[:, 0, 0] = 3
+    data[:, 0, 1] = 7
+    c = P.HistoryCache(data, torch.ones(need, 1, 2).cuda(), D)
+    table = torch.arange(need, dtype=torch.int32).cuda().expand(B, need)
+    end = torch.tensor([length, 0, length, length + T - 1]).cuda()
+    for value, finite in [(math.inf, 0), (-math.inf, 0), (math.nan, 0), (2.0 ** 127, 0), (-2.0 ** 127, 0), (1.0, 1)]:
+        for scale in (1.0, -1.0):
+            q = torch.ones(B, T, group, D).cuda().to(_torch_type(torch, dtype))
+            q[:2, :, 0] = value
+            q[3, -1, group - 1, 11] = value
+            out, lse = P.cache_attend(c, q, table, end=end, scale=scale, return_lse=True)
+            out, lse = _host(out), lse.cpu().numpy()
+            what = "%g, scale %g" % (value, scale)
+            assert (out[1] == 0).all() and np.isneginf(lse[1]).all(), what
+            if finite:
+                assert (np.abs(out[[0, 2], -1] - 7) <= near).all(), what
+                continue
+            assert np.isnan(out[0, -1, 0]).all() and np.isnan(lse[0, -1, 0]), what
+            assert (np.abs(out[2, -1] - 7) <= near).all() and np.isfinite(lse[2, -1]).all(), what
+            if not np.isfinite(value):
+                assert np.isnan(out[3, -1, group - 1]).all() and np.isnan(lse[3, -1, group - 1]), what
