@@ -770,6 +770,7 @@ __device__ __forceinline__ int from_lane(int v) {
 }
 
 constexpr float kFew = 64.0f;       // tokens at most, see few()
+constexpr float kRoom = 32768.0f;   // 127 columns of 256: sums of query times bytes stay in range where scores do
 
 template <class T, int JV>
 __global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(const AttendArgs a) {
@@ -803,7 +804,7 @@ __global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(
         bool odd = false, seen = false;             // an element that is no number; a token that is seen
 #pragma unroll
         for (int k = 0; k < JV; k++) {
-            q[k] *= a.scale * kLog2E;
+            q[k] *= a.scale * (kLog2E / kRoom);
             odd |= !(fabsf(q[k]) < INFINITY);
         }
         float m = -INFINITY, l = 0.0f, o[JV] = {};
@@ -839,7 +840,7 @@ __global__ __launch_bounds__(kBlock, (JV == 16 ? 2 : 4)) void attend_few_kernel(
             scatter_sum<4, kXor7, 4>(p, i);
             scatter_sum<2, kXor2, 2>(p, i);
             scatter_sum<1, kXor1, 1>(p, i);
-            const float s = page < 0 ? -INFINITY : p[0] * sc.x;
+            const float s = page < 0 ? -INFINITY : p[0] * sc.x * kRoom;
             seen |= page >= 0;
             float top = fmaxf(s, dpp<kXor8>(s));
             top = fmaxf(top, dpp<kXor7>(top));

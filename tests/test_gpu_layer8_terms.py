@@ -254,3 +254,28 @@ def test_attend_scores_that_are_no_numbers(page, group, T, length, dtype):
             assert (np.abs(out[2, -1] - 7) <= near).all() and np.isfinite(lse[2, -1]).all(), what
             if not np.isfinite(value):
                 assert np.isnan(out[3, -1, group - 1]).all() and np.isnan(lse[3, -1, group - 1]), what
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("page,group,length", [(1, 1, 10), (1, 3, 60), (1, 2, 300), (4, 2, 300), (1, 1, 3000)])
+def test_attend_a_score_far_below_has_no_weight(page, group, length, dtype):
+    """Scores of minus infinity beside finite ones weigh nothing; a hidden infinite one does not count."""
+    torch = require_gpu()
+    announce("scores far below, page %d rows %d tokens %d %s" % (page, group, length, dtype))
+    D, need = 16, -(-length // page)
+    data = torch.zeros(need, 1, 2, page, D, dtype=torch.int8).cuda()
+    data[:, 0, 0] = 100
+    data[:, 0, 1] = 7
+    near = 7 * (2.0 ** -20 + (16 + length / 16) * HALF)
+    scales = torch.full((need, 1, 2), 1e-36).cuda()
+    scales[..., 1] = 1.0
+    scales[::2, 0, 0] = 1e5
+    scales[::2, 0, 1] = 1000.0
+    c = P.HistoryCache(data, scales, D)
+    table = torch.arange(need, dtype=torch.int32).cuda()[None]
+    q = torch.full((1, group, D), -1e37).cuda().to(_torch_type(torch, dtype))
+    out, lse = P.cache_attend(c, q, table, scale=1.0, return_lse=True)
+    assert ((out.float() - 7).abs() <= near).all() and torch.isfinite(lse).all()
+    table[0, ::2] = -1
+    out = P.cache_attend(c, -q, table, scale=1.0)
+    assert ((out.float() - 7).abs() <= near).all()
