@@ -738,7 +738,9 @@ tgl_status tgl_cache_read(const tgl_cache *cache, const tgl_heads *k, const tgl_
  * cache of one-token pages with the slots' neighbour ids as the table.
  *   q          [device] num_seqs * queries x q_heads x dim elements of type dtype
  *   q_heads    a multiple of the cache's heads, at most TGL_MAX_HEADS
- *   queries    >= 1
+ *   queries    >= 1; num_seqs * queries * q_heads below 2^31, and of one sequence
+ *              heads times tiles of 16 or 32 rows (queries of a head's group) times
+ *              chunks of its table below about 2^24 (TGL_EINVAL beyond)
  *   seqs       start is begin (NULL: 0); end is `end`; offsets must be NULL
  *   end        [device] int64[num_seqs], or NULL: pages_per_seq * page_tokens
  *   out        [device] like q, of the same type

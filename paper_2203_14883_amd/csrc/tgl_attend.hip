@@ -985,6 +985,30 @@ void launch_few(const AttendArgs &a, unsigned grid, hipStream_t st) {
     else attend_few_kernel<T, 16><<<grid, kBlock, 0, st>>>(a);
 }
 
+// The part of a call that is n sequences from b on.
+AttendArgs slice(AttendArgs a, int64_t b, int64_t n, size_t elem) {
+    const int64_t row = b * a.queries, items = n * a.c.heads;
+    a.s.table += b * a.s.table_stride;
+    if (a.s.start) a.s.start += b;
+    if (a.end) a.end += b;
+    a.s.seqs = static_cast<int32_t>(n);
+    a.q = static_cast<const char *>(a.q) + row * a.qt * static_cast<int64_t>(elem);
+    a.out = static_cast<char *>(a.out) + row * a.ot * static_cast<int64_t>(elem);
+    if (a.lse) a.lse += row * a.c.heads * a.group.d;
+    a.items = Div(static_cast<uint32_t>(items));
+    a.work = static_cast<uint32_t>(items * a.tiles.d * a.chunks);
+    a.all_rows = static_cast<uint32_t>(items * a.rows);
+    const int64_t units = items * a.chunks;
+    a.order = a.tiles.d == 1 ? kInTurn : units >= 32 || units % 8 == 0 ? kHeadsInTurn : kStretches;
+    return a;
+}
+
+template <class T>
+void launch(const AttendArgs &a, hipStream_t st) {
+    if (few(a)) launch_few<T>(a, static_cast<unsigned>((a.items.d + 15) / 16), st);
+    else launch<T>(a, wavefronts(a), st);
+}
+
 // Rows without anything to see: zeros.
 template <class T>
 __global__ __launch_bounds__(kBlock) void attend_none_kernel(const AttendArgs a) {
@@ -1052,33 +1076,28 @@ tgl_status tgl_cache_attend(const tgl_cache *cache, const tgl_heads *q, int32_t 
         else attend_none_kernel<bf16_t><<<grid, kBlock, 0, st>>>(a);
         return launch_status();
     }
-    const int64_t work = seqs->num_seqs * a.c.heads * p.row_tiles * p.chunks;
-    if (work > 0x7fffff00 - 8 * p.row_tiles) return TGL_EINVAL;
     a.rows = static_cast<uint32_t>(queries * group);
     a.row_of = Div(a.rows);
-    a.all_rows = a.rows * a.s.seqs * a.c.heads;
     a.chunk = p.chunk;
-    a.work = static_cast<uint32_t>(work);
     a.tile_rows = static_cast<uint32_t>(p.tile_rows);
     a.tiles = Div(static_cast<uint32_t>(p.row_tiles));
     a.chunks = static_cast<uint32_t>(p.chunks);
-    a.items = Div(static_cast<uint32_t>(seqs->num_seqs * a.c.heads));
     a.heads = Div(a.c.heads);
-    const int64_t units = seqs->num_seqs * a.c.heads * p.chunks;
-    a.order = p.row_tiles == 1 ? kInTurn : units >= 32 || units % 8 == 0 ? kHeadsInTurn : kStretches;
     if (p.part_o) {
         a.part_o = static_cast<float *>(workspace);
         a.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + p.part_o);
     }
-    if (few(a)) {
-        const unsigned grid = static_cast<unsigned>((a.s.seqs * int64_t(a.c.heads) + 15) / 16);
-        if (dtype == TGL_OUT_F32) launch_few<float>(a, grid, st);
-        else launch_few<bf16_t>(a, grid, st);
-        return launch_status();
+    // A launch has fewer than 2^32 threads: as many sequences at a time as keep
+    // to that.  Their launches follow each other, so they share the workspace.
+    int64_t most = ((int64_t(1) << 24) - 1 - 8 * p.row_tiles) / (a.c.heads * p.row_tiles * p.chunks);   // of 256 threads
+    const int64_t joins = ((int64_t(1) << 22) - 1) / (static_cast<int64_t>(a.c.heads) * a.rows);        // of 1024
+    if (p.part_o && most > joins) most = joins;
+    if (most < 1) return TGL_EINVAL;
+    for (int64_t b = 0; b < seqs->num_seqs; b += most) {
+        const AttendArgs part = slice(a, b, seqs->num_seqs - b < most ? seqs->num_seqs - b : most, elem_size(dtype));
+        if (dtype == TGL_OUT_F32) launch<float>(part, st);
+        else launch<bf16_t>(part, st);
     }
-    const int nw = wavefronts(a);
-    if (dtype == TGL_OUT_F32) launch<float>(a, nw, st);
-    else launch<bf16_t>(a, nw, st);
     return launch_status();
 }
 
