@@ -600,8 +600,8 @@ tgl_status tgl_time_encode(const float *dt, int64_t n, const int64_t *count, int
  *   h = x + r;  sum[i] = h in x's type
  *   t = h * weight;  (q[i], s) = t in 8 bits
  *   scale[i] = s / sqrt(mean(h^2) + eps)
- * so that q * scale = h / rms(h) * weight.  h, t and the mean are float32
- * (the mean is of h before its rounding to x's type).  Without the norm
+ * so that q * scale = h / rms(h) * weight.  h and t are float32, the mean 64
+ * bits (of h before its rounding to x's type).  Without the norm
  * (normalize = 0): scale[i] = s, eps is not read; with weight NULL too, this
  * is the plain rounding of rows, for weights and for rows that need no norm.
  *   x, residual  [device] n rows of dim elements of type dtype; residual may

@@ -6,7 +6,8 @@
 //
 // The norm's factor 1 / sqrt(mean + eps) is common to a row, so it drops out
 // of the bytes and enters the scale alone: bytes do not depend on the order in
-// which the mean's sum is taken.
+// which the mean's sum is taken.  Squares are summed in 64 bits: float32 ones of
+// finite rows leave the range above 2^63 and below 2^-63.
 #include "tgl_int8.hpp"
 
 namespace tgl {
@@ -31,6 +32,14 @@ struct NormArgs {
 
 constexpr int kRun = 8;             // elements of a lane's access
 
+// step / sqrt(mean + eps), in float32 where that has the range.
+__device__ __forceinline__ float normed_step(const NormArgs &a, float step, double squares) {
+    if (!a.normalize) return step;
+    const double x = squares / a.dim + a.eps;
+    if (x > 0x1p-100 && x < 0x1p100) return step / sqrtf(static_cast<float>(x));
+    return static_cast<float>(step / sqrt(x));
+}
+
 // L lanes per row, which stays in registers: H runs of 8 elements a lane.  The
 // weights of a lane's columns stay there too, over all rows it takes.  Bound by
 // memory: 12,000 rows of 768 bfloat16 with a residual (64 MB) 15.4 us, 4.2 TB/s
@@ -39,7 +48,8 @@ constexpr int kRun = 8;             // elements of a lane's access
 template <class T, int L, int H>
 __global__ __launch_bounds__(kBlock) void norm_kernel(const NormArgs a) {
     constexpr int kWaves = L / kWave;           // of a row
-    __shared__ float tops[kBlock / kWave], parts[kBlock / kWave];
+    __shared__ float tops[kBlock / kWave];
+    __shared__ double parts[kBlock / kWave];
     const int i = threadIdx.x % L;
     const int group = threadIdx.x / L;
     const int runs = round16(a.dim) / kRun;
@@ -72,12 +82,12 @@ __global__ __launch_bounds__(kBlock) void norm_kernel(const NormArgs a) {
                 }
             }
         }
-        float squares = 0.0f;
+        double squares = 0.0;
         uint32_t bits = 0;              // of the largest magnitude: NaN above infinity above numbers
 #pragma unroll
         for (int h = 0; h < H; h++) {
 #pragma unroll
-            for (int k = 0; k < kRun; k++) squares = __builtin_fmaf(v[h][k], v[h][k], squares);
+            for (int k = 0; k < kRun; k++) squares = __builtin_fma(static_cast<double>(v[h][k]), static_cast<double>(v[h][k]), squares);
             if (a.sum && there && i + h * L < runs)
                 store_columns<T, kRun>(static_cast<T *>(a.sum) + row * a.ss, (i + h * L) * kRun, a.dim, v[h]);
 #pragma unroll
@@ -100,7 +110,7 @@ __global__ __launch_bounds__(kBlock) void norm_kernel(const NormArgs a) {
                 parts[threadIdx.x / kWave] = squares;
             }
             __syncthreads();
-            squares = 0.0f;
+            squares = 0.0;
 #pragma unroll
             for (int y = 0; y < kWaves; y++) {
                 squares += parts[group * kWaves + y];
@@ -119,7 +129,7 @@ __global__ __launch_bounds__(kBlock) void norm_kernel(const NormArgs a) {
                 *reinterpret_cast<i32x2 *>(a.q + row * a.qs + (i + h * L) * kRun) = q;
             }
         }
-        if (i == 0) a.scale[row] = a.normalize ? s / sqrtf(squares / static_cast<float>(a.dim) + a.eps) : s;
+        if (i == 0) a.scale[row] = normed_step(a, s, squares);
     }
 }
 
@@ -127,11 +137,12 @@ __global__ __launch_bounds__(kBlock) void norm_kernel(const NormArgs a) {
 // over each, the second mostly from L2.
 template <class T>
 __global__ __launch_bounds__(kBlock) void norm_long_kernel(const NormArgs a) {
-    __shared__ float tops[kBlock / kWave], parts[kBlock / kWave];
+    __shared__ float tops[kBlock / kWave];
+    __shared__ double parts[kBlock / kWave];
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const T *x = static_cast<const T *>(a.x) + row * a.xs;
         const T *r = a.r ? static_cast<const T *>(a.r) + row * a.rs : nullptr;
-        float squares = 0.0f;
+        double squares = 0.0;
         uint32_t bits = 0;
         auto hold = [&](int n, float (&h)[kRun], float (&t)[kRun]) {
             load_columns<T, kRun>(x, n * kRun, a.dim, h);
@@ -152,7 +163,7 @@ __global__ __launch_bounds__(kBlock) void norm_long_kernel(const NormArgs a) {
             hold(n, h, t);
 #pragma unroll
             for (int k = 0; k < kRun; k++) {
-                squares = __builtin_fmaf(h[k], h[k], squares);
+                squares = __builtin_fma(static_cast<double>(h[k]), static_cast<double>(h[k]), squares);
                 const uint32_t y = __builtin_bit_cast(uint32_t, t[k]) & 0x7fffffffu;
                 bits = y > bits ? y : bits;
             }
@@ -169,7 +180,7 @@ __global__ __launch_bounds__(kBlock) void norm_long_kernel(const NormArgs a) {
             parts[threadIdx.x / kWave] = squares;
         }
         __syncthreads();
-        squares = 0.0f;
+        squares = 0.0;
 #pragma unroll
         for (int y = 0; y < kBlock / kWave; y++) {
             squares += parts[y];
@@ -185,7 +196,7 @@ __global__ __launch_bounds__(kBlock) void norm_long_kernel(const NormArgs a) {
             *reinterpret_cast<i32x2 *>(a.q + row * a.qs + n * kRun) = q;
             if (a.sum) store_columns<T, kRun>(static_cast<T *>(a.sum) + row * a.ss, n * kRun, a.dim, h);
         }
-        if (threadIdx.x == 0) a.scale[row] = a.normalize ? s / sqrtf(squares / static_cast<float>(a.dim) + a.eps) : s;
+        if (threadIdx.x == 0) a.scale[row] = normed_step(a, s, squares);
     }
 }
 
