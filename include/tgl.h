@@ -588,7 +588,7 @@ tgl_status tgl_time_encode(const float *dt, int64_t n, const int64_t *count, int
  * or TGL_OUT_BF16 (2-byte aligned).  Strides are in elements.
  */
 #define TGL_MAX_ROW_DIM    (1 << 20)  /* elements of a row of tgl_norm_quant    */
-#define TGL_MAX_LINEAR_K   131072     /* its int32 sums cannot overflow         */
+#define TGL_MAX_LINEAR_K   131072     /* sums of any bytes in 32 bits are exact */
 #define TGL_MAX_LINEAR_OUT (1 << 20)
 #define TGL_MAX_HEAD_DIM   256
 #define TGL_MAX_HEADS      1024

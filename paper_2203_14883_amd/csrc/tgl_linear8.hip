@@ -39,6 +39,10 @@ __device__ __forceinline__ i32x4 mask_piece(i32x4 v, int c, int k) {
     return v;
 }
 
+// An int32 sum, which of 2^17 products of -128 with itself is 2^31: no other sum
+// has those bits, since the least is -128 * 127 * 2^17.
+__device__ __forceinline__ float sum_of(int v) { return v == INT32_MIN ? 0x1p31f : static_cast<float>(v); }
+
 // Scales, bias, the one rounding: N outputs of a row from column j on.
 template <class T, int N>
 __device__ __forceinline__ void finish(const LinearArgs &a, int64_t row, int j, const int (&sum)[N], const float (&ws)[N], const float (&bias)[N]) {
@@ -46,7 +50,7 @@ __device__ __forceinline__ void finish(const LinearArgs &a, int64_t row, int j, 
     float y[N];
 #pragma unroll
     for (int i = 0; i < N; i++) {
-        y[i] = static_cast<float>(sum[i]) * xs * ws[i];
+        y[i] = sum_of(sum[i]) * xs * ws[i];
         if (a.bias) y[i] += bias[i];
     }
     store_columns<T, N>(static_cast<T *>(a.out) + row * a.ostride, j, a.n, y);

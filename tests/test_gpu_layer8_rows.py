@@ -32,3 +32,18 @@ def test_norm_of_rows_of_any_size(size, eps, dim, dtype):
     if eps == 0 or size > 1:
         rms = np.sqrt(np.mean((got / wh) ** 2, 1))
         assert np.all(np.abs(rms - 1) <= 0.05)
+
+
+@pytest.mark.parametrize("m", [1, 20, 300])
+@pytest.mark.parametrize("k", [131071, 131072])
+def test_linear_i8_of_the_smallest_bytes(k, m):
+    """Sums of (-128)^2 reach 2^31 at the largest k."""
+    torch = require_gpu()
+    announce("linear_i8 of -128, %d rows, k %d" % (m, k))
+    x = torch.full((m, O.round16(k)), -128, dtype=torch.int8).cuda()[:, :k]
+    w = torch.full((900, O.round16(k)), -128, dtype=torch.int8).cuda()[:, :k]
+    w[1] = 127
+    w[2, ::2] = 127
+    y = P.linear_i8(x, torch.ones(m).cuda(), w, torch.ones(900).cuda(), out_dtype=torch.float32).double()
+    for j, total in ((0, 128 * 128 * k), (1, -128 * 127 * k), (2, 128 * 128 * (k // 2) - 128 * 127 * (k - k // 2))):
+        assert (y[:, j] - float(total)).abs().max() <= abs(total) * 2.0 ** -24
