@@ -349,8 +349,7 @@ void launch_small(LinearArgs a, hipStream_t st) {
 }
 
 template <class T>
-bool launch(LinearArgs a, hipStream_t st) {
-    if ((a.m + 15) / 16 * ((a.n + 15) / 16) > 0x7ffffff0) return false;
+void launch(const LinearArgs &a, hipStream_t st) {
     auto tiles = [&](int b) { return (a.m + b - 1) / b * ((a.n + b - 1) / b); };
     // The largest tiles that still give most of the 256 compute units one
     // (fewer loads a product), two workgroups a unit for those of 128; tiles of
@@ -365,7 +364,20 @@ bool launch(LinearArgs a, hipStream_t st) {
     else if (a.m > 32 && tiles(64) >= 64) launch_tiles<T, 64, 64, 1, 4>(a, st);
     else if (a.m <= 16) launch_small<T, 1>(a, st);
     else launch_small<T, 2>(a, st);
-    return true;
+}
+
+// A launch has fewer than 2^32 threads: as many rows at a time as keep to that
+// with tiles of 64 and 256 threads, or of 128 and 512.
+template <class T>
+void launch_parts(LinearArgs a, hipStream_t st) {
+    const int64_t most = (int64_t(1) << 25) / ((a.n + 15) / 16) / 16 * 256, all = a.m;
+    for (int64_t row = 0; row < all; row += most) {
+        a.m = all - row < most ? all - row : most;
+        launch<T>(a, st);
+        a.x += most * a.xstride;
+        a.xs += most;
+        a.out = static_cast<T *>(a.out) + most * a.ostride;
+    }
 }
 
 }  // namespace
@@ -402,7 +414,8 @@ tgl_status tgl_linear_i8(const int8_t *x, int64_t x_stride, const float *x_scale
     a.m = m;
     a.n = n;
     a.k = k;
-    if (!(out_type == TGL_OUT_F32 ? launch<float>(a, st) : launch<bf16_t>(a, st))) return TGL_EINVAL;
+    if (out_type == TGL_OUT_F32) launch_parts<float>(a, st);
+    else launch_parts<bf16_t>(a, st);
     return launch_status();
 }
 

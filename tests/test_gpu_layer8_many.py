@@ -33,3 +33,16 @@ def test_attend_many_sequences(places, group, bounded):
     want = (values[see.long().clamp(min=0)] * there).sum(1) / count.clamp(min=1)
     assert ((out[..., 0].float() - want[:, None]).abs() <= 2.0 ** -8 * want.abs()[:, None] + 1e-30).all()
     assert ((lse.exp() - count[:, None]).abs() <= 1e-5).all()
+
+
+def test_linear_i8_of_many_rows():
+    """2^30 rows and a few, all of them the same bytes with a scale each."""
+    torch = require_gpu()
+    m, k = (1 << 30) + 37, 16
+    announce("linear_i8 of %d rows" % m)
+    x = torch.arange(-7, 9, dtype=torch.int8, device="cuda")
+    w = torch.arange(100, 116, dtype=torch.int8, device="cuda")
+    total = float((x.long() * w.long()).sum())
+    scale = torch.rand(m, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    y = P.linear_i8(x.expand(m, k), scale, w[None], torch.ones(1, device="cuda"))
+    assert torch.equal(y[:, 0], (scale * total).bfloat16())
