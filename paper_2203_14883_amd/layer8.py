@@ -235,6 +235,9 @@ class HistoryCache:
         object.__setattr__(self, "_view", c_cache(d.data_ptr() if pages else None, s.data_ptr() if pages else None,
                                                   pages, P, heads, self.dim, 0))
 
+    def __reduce__(self):                   # copies and pickles: the view is made anew, of the copy's tensors
+        return type(self), (self.data, self.scales, self.dim)
+
     @classmethod
     def empty(cls, num_pages: int, heads: int, dim: int, page_tokens: int = 1, device="cuda") -> "HistoryCache":
         """A cache of that many pages, zeros everywhere."""
