@@ -6,7 +6,8 @@ histories (``cache_write``, ``cache_read``) and attended over
 (include/tgl.h has the definitions).
 
 Rounding to 8 bits has no gradient: tensors that require one are refused
-while gradients are recorded (use ``torch.no_grad()`` or ``detach()``).  With
+while gradients are recorded (use ``torch.no_grad()`` or ``detach()``), and so
+are those that carry a forward-mode tangent.  With
 ``stream``, work is enqueued there and outputs are allocated for it; inputs
 made on another stream must be ready, as for every call of the library.
 """
@@ -18,6 +19,7 @@ from dataclasses import dataclass, field
 from typing import Optional
 
 import torch
+from torch.autograd import forward_ad
 
 from .binding import OUT_BF16, OUT_F32, _check, c_cache, c_heads, c_seqs, lib
 
@@ -51,20 +53,20 @@ def _device(t: torch.Tensor, name: str) -> int:
     dev = t.get_device()
     if dev < 0 or dev != torch._C._cuda_getDevice():
         raise ValueError("%s must be on the current device, not on %s" % (name, t.device))
-    if t.requires_grad:
-        _no_gradient(name)
+    if t.requires_grad or forward_ad._current_level >= 0:
+        _no_gradient(t, name)
     return dev
 
 
 def _also(t: torch.Tensor, name: str, dev: int):
     if t.get_device() != dev:
         raise ValueError("%s must be on the current device, not on %s" % (name, t.device))
-    if t.requires_grad:
-        _no_gradient(name)
+    if t.requires_grad or forward_ad._current_level >= 0:
+        _no_gradient(t, name)
 
 
-def _no_gradient(name: str):
-    if torch.is_grad_enabled():
+def _no_gradient(t: torch.Tensor, name: str):
+    if (t.requires_grad and torch.is_grad_enabled()) or forward_ad.unpack_dual(t).tangent is not None:
         raise ValueError("%s requires a gradient, and rounding to 8 bits has none" % name)
 
 
