@@ -288,6 +288,7 @@ def _cache_device(cache: HistoryCache) -> int:
     dev = cache.data.get_device()
     if dev < 0 or dev != torch._C._cuda_getDevice():
         raise ValueError("the cache must be on the current device")
+    _also(cache.scales, "the cache's scales", dev)
     return dev
 
 
