@@ -284,6 +284,11 @@ def _heads(t: torch.Tensor, name: str, n: int, heads: int, dim: int) -> c_heads:
     return c_heads(t.data_ptr() or None, token, head)
 
 
+def _apart(t: torch.Tensor, name: str):
+    if any(stride == 0 and size > 1 for stride, size in zip(t.stride(), t.shape)):
+        raise ValueError("%s's rows overlap" % name)
+
+
 def _cache_device(cache: HistoryCache) -> int:
     dev = cache.data.get_device()
     if dev < 0 or dev != torch._C._cuda_getDevice():
@@ -349,6 +354,8 @@ def cache_read(cache: HistoryCache, table: torch.Tensor, start: Optional[torch.T
         ot = _type(k.dtype, "k")
         _also(k, "k", dev)
         _also(v, "v", dev)
+        _apart(k, "k")
+        _apart(v, "v")
     kh, vh = _heads(k, "k", n, view.heads, view.dim), _heads(v, "v", n, view.heads, view.dim)
     s = lib().tgl_cache_read(C.byref(view), C.byref(kh), C.byref(vh), ot, n, C.byref(sq), _raw_stream(stream, dev))
     if s:
@@ -404,6 +411,7 @@ def cache_attend(cache: HistoryCache, q: torch.Tensor, table: torch.Tensor, begi
         if out.dtype != q.dtype or out.shape != shape:
             raise ValueError("out must have q's type and shape")
         _also(out, "out", dev)
+        _apart(out, "out")
     qh, oh = _heads(_flat(q, "q", rows), "q", rows, H, dim), _heads(_flat(out, "out", rows), "out", rows, H, dim)
     s = L.tgl_cache_attend(C.byref(view), C.byref(qh), H, T, dt, C.byref(sq), last,
                            1.0 / math.sqrt(dim) if scale is None else scale, C.byref(oh),
