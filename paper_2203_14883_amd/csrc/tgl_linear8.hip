@@ -175,11 +175,11 @@ __global__ __launch_bounds__(BM / (16 * MT) * (BN / 64) * kWave, 2) void linear_
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int g = lane >> 4, i16 = lane & 15;
     // the 8 dies take workgroups in turn: each gets a contiguous stretch of
-    // tiles, walked in bands of kBand tiles of rows
+    // tiles, walked in bands of band_rows tiles of rows
     const uint32_t per = (a.work + 7) / 8;
     const uint32_t id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= per || id >= a.work) return;
-    const uint32_t band = a.band(id);                       // tiles_n * kBand tiles
+    const uint32_t band = a.band(id);                       // tiles_n * band_rows tiles
     const uint32_t in_band = id - band * a.band.d;
     const uint32_t rows_left = a.tiles_m - band * a.band_rows;
     const uint32_t height = rows_left < a.band_rows ? rows_left : a.band_rows;
@@ -340,11 +340,10 @@ void launch_tiles(LinearArgs a, hipStream_t st) {
 template <class T, int MT>
 void launch_small(LinearArgs a, hipStream_t st) {
     a.tiles_n = Div((a.n + 15) / 16);
-    const int64_t tiles = (a.m + 16 * MT - 1) / (16 * MT) * a.tiles_n.d;
-    const unsigned grid = static_cast<unsigned>(tiles);
+    const unsigned grid = static_cast<unsigned>((a.m + 16 * MT - 1) / (16 * MT) * a.tiles_n.d);
     // wavefronts that share a tile's k, while tiles alone do not fill the card
-    if (tiles >= 4096 || a.k <= 64) linear_small_kernel<T, 1, MT><<<grid, kWave, 0, st>>>(a);
-    else if (tiles >= 1024 || a.k <= 512) linear_small_kernel<T, 4, MT><<<grid, 4 * kWave, 0, st>>>(a);
+    if (a.k <= 64) linear_small_kernel<T, 1, MT><<<grid, kWave, 0, st>>>(a);
+    else if (grid >= 1024 || a.k <= 512) linear_small_kernel<T, 4, MT><<<grid, 4 * kWave, 0, st>>>(a);
     else linear_small_kernel<T, 8, MT><<<grid, 8 * kWave, 0, st>>>(a);
 }
 
