@@ -6,9 +6,10 @@ attends from a root to its neighbours with keys and values made from theirs
 
 * by node: one token per node, overwritten when the node's row changes; a root
   attends over the neighbours that the sampler picked, whose ids are the
-  pages;
-* by history: a node's events one after another in pages of 16; a root attends
-  over the newest of its own past.
+  pages (keys of the neighbour's state alone: the edge and the time between
+  root and slot are one per slot, for which a node's page has no room);
+* by history: a node's events one after another in pages of 16, their keys made
+  with the time since the last one; a root attends over the newest of its own past.
 
     python examples/serve_attention.py [--batches N] [--edges N]
 """

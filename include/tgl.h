@@ -749,7 +749,8 @@ tgl_status tgl_cache_read(const tgl_cache *cache, const tgl_heads *k, const tgl_
  *              aligned (NULL where that is 0)
  * Scores, maxima, sums and the output are accumulated in float32 or exactly.
  * Of the operands, a query element is held to 2^-24 of the largest one of its row
- * and head, and a weight exp(score_j) to 2^-22 of itself, for either type.
+ * and head (as 0 where that is below 2^-100), and a weight exp(score_j) to 2^-22 of
+ * itself, for either type.
  * Never synchronises.  Errors: TGL_EINVAL, TGL_ENOSPACE, TGL_EDEVICE.
  */
 size_t tgl_cache_attend_workspace(const tgl_cache *cache, const tgl_seqs *seqs, int32_t q_heads, int64_t queries);

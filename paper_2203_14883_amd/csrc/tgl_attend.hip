@@ -30,14 +30,16 @@
 //           or 2^-36 of the largest.
 //
 // Few rows a head: bound by memory.  1,000,003 tokens of 8 heads of 128 in pages
-// of 64 (2.05 GB), 4 query heads each, 349 us, 5.9 TB/s, and 7 us to join 253
+// of 64 (2.05 GB), 4 query heads each, 350 us, 5.9 TB/s, and 8 us to join 253
 // chunks; 64 histories of 1 to 8192 tokens (0.54 GB) 114 + 5 us, 4.5 TB/s, the
-// rest being long and short histories side by side.  Small pages and heads: by
-// instructions, 300 for 32 tokens (600 windows of 1000 tokens, 2 heads of 64,
-// pages of 4: 35 us, 3.6 TB/s).  Many rows: by the scores' arithmetic (256
-// queries of 4 histories of 2500 to 4097, 8 heads of 128 for 32: 95 us, 560
-// TFLOP/s), 350 vector instructions for 32 rows and 32 tokens beside 32 matrix
-// ones.
+// rest being long and short histories side by side; float32 queries the same.
+// Small pages and heads: half by instructions, 330 for 32 tokens, half by the
+// latency of rows that are not loaded a step ahead (600 windows of 1000 tokens,
+// 2 heads of 64, pages of 4: 37 us, 3.5 TB/s).  Many rows: by the scores'
+// arithmetic (256 queries of 4 histories of 2500 to 4097, 8 heads of 128 for 32:
+// 130 us, 410 TFLOP/s), 460 vector instructions for 32 rows and 32 tokens beside
+// 56 matrix ones.  (With a query in two bytes and P in one f16: 95 us, and
+// outputs that are off by that rounding.)
 #include "tgl_cache.hpp"
 
 namespace tgl {
@@ -640,7 +642,7 @@ __global__ __launch_bounds__(NW * kWave, (kWavesPerSimd<JV, R>)) void attend_ker
 
 // Joins the chunks of a row, a mean each, with NW wavefronts.  A lane takes four columns of
 // every (NW kWave / kLanes)-th chunk, kLanes the lanes of a row's columns, eight
-// chunks in flight (253 chunks of 32 rows of 128: 7 us; 212 us with a wavefront
+// chunks in flight (253 chunks of 32 rows of 128: 8 us; 212 us with a wavefront
 // per row and a chunk at a time).  With NW = 1 a workgroup has a row for each of its
 // wavefronts.
 template <class T, int NW, int kLanes>
@@ -744,8 +746,8 @@ __global__ __launch_bounds__((NW == 1 ? kBlock : NW * kWave)) void attend_join_k
 // columns of all 16; the products are summed over the lanes so that token i's
 // sum arrives in lane i (four exchanges, halving the tokens each time); the
 // weights come back from lane i by a swizzle.  12,000 roots of 10 slots, 2 heads
-// of 50 float32 (23 MB): 11.3 us, half of it instructions, half the chain of
-// three loads (slot, step, row); 42 us on the matrix instructions.
+// of 50 float32 (23 MB): 11.8 us, half of it instructions, half the chain of
+// three loads (slot, step, row); 40 us on the matrix instructions.
 
 template <int kCtrl>
 __device__ __forceinline__ float dpp(float v) {
@@ -960,9 +962,9 @@ void launch(const AttendArgs &a, int nw, hipStream_t st) {
 
 // Whether the kernel for few tokens is the faster one: its work grows with
 // rows times tokens, the other's with tokens above 32.  12,000 sequences, 2
-// heads of 128, us here / there: 1 row of 16 tokens 22 / 49, of 32 39 / 50, of
-// 64 74 / 79; 2 rows of 16 42 / 50, of 32 75 / 51; 4 rows of 8 48 / 50, of 16
-// 79 / 51.
+// heads of 128, us here / there: 1 row of 16 tokens 23 / 51, of 32 39 / 51, of
+// 64 72 / 77; 2 rows of 16 41 / 51, of 32 76 / 53; 4 rows of 8 50 / 52, of 16
+// 79 / 52.
 bool few(const AttendArgs &a) {
     const int64_t tokens = static_cast<int64_t>(a.s.pages_per_seq) << a.c.shift;
     return a.rows * ((tokens + 15) / 16) <= 2 || (a.rows == 1 && tokens <= static_cast<int64_t>(kFew));
@@ -970,9 +972,9 @@ bool few(const AttendArgs &a) {
 
 // Wavefronts that share a sequence's tokens.  One to itself needs no join
 // through LDS and leaves more of them resident, as long as there are many.  2
-// heads of 50, us with 1 / 4: 1000 sequences and heads, 64 tokens 8.0 / 9.7, 128
-// 11.3 / 10.6, 256 17 / 14; 4000 of 128 21 / 30, of 256 35 / 40, of 512 63 / 61;
-// 24,000 of 256 164 / 198, of 512 315 / 313.
+// heads of 50, 3 rows, us with 1 / 4: 1000 sequences and heads, 64 tokens 6.5 / 7.6,
+// 128 8.1 / 9.0, 256 12.2 / 11.2; 4000 of 128 17 / 28, of 256 28 / 35, of 512
+// 48 / 49; 24,000 of 256 122 / 183, of 512 227 / 264.
 int wavefronts(const AttendArgs &a) {
     const int64_t tokens = static_cast<int64_t>(a.s.pages_per_seq) << a.c.shift;
     return tokens <= 64 || (tokens <= 256 && a.items.d >= 2048) ? 1 : 4;

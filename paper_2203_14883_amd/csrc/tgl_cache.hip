@@ -217,7 +217,8 @@ __device__ __forceinline__ int64_t last_at_most(const SeqsView &s, int64_t token
 // then all stream its heads, 16 bytes of keys and of values a lane, past the
 // caches.  Bound by memory: the tokens above read back (0.63 GB read, 1.26
 // written) in 374 us, 5.1 TB/s; 120,000 slots of 2 heads of 50 float32 from 2M
-// one-token pages in 39 us, 3.0 TB/s, rows of 256 bytes at random places (50 us
+// one-token pages in 39 us, 42 MB read and 123 written (96 of them numbers: rows
+// of 200 bytes leave lines that are written in parts), 4.2 TB/s (50 us
 // with stores of 32 bytes a lane through the caches).
 template <class T>
 __global__ __launch_bounds__(kBlock) void read_kernel(const IoArgs a) {

@@ -61,7 +61,7 @@ __device__ __forceinline__ void finish(const LinearArgs &a, int64_t row, int j, 
 // A workgroup per 16 MT rows and 16 columns, whose wavefronts take 64 of k in
 // turn and add up through LDS: a row of w is read once for 16 MT rows of x.
 // Bound by latency where w is small (1 x 2304 x 768: 3.4 us) and by w's bytes
-// where it is not (1 x 4096 x 4096: 5.0 us, 3.4 TB/s).
+// where it is not (1 x 4096 x 4096: 4.8 us, 3.5 TB/s).
 template <class T, int NW, int MT>
 __global__ __launch_bounds__(NW * kWave) void linear_small_kernel(const LinearArgs a) {
     __shared__ i32x4 sums[NW > 1 ? NW : 1][MT][kWave];
@@ -149,9 +149,10 @@ __global__ __launch_bounds__(NW * kWave) void linear_small_kernel(const LinearAr
 // Whole pieces only: past them LDS holds 0, from loads beyond the buffer's end,
 // and a piece that k ends in is multiplied once, after the steps, from memory.
 
-// Bound by the matrix units and their feeding: 16384 x 4096 x 4096 in 240 to 268
-// us by the card's clocks, 2.0 to 2.3 POP/s, the units at work 47% of the time;
-// 8192^3 2.5 POP/s.  The steps overlap: loads, 6 reads of LDS for every 8
+// Bound by the matrix units and their feeding: 16384 x 4096 x 4096 in 252 to 272
+// us by the card's clocks, 2.0 to 2.2 POP/s, the units at work 47% of the time;
+// 8192^3 in 413 us, 2.7 POP/s.  One row of 65,536 columns (128 x 128 tiles, of
+// 268 MB of weights) 41 us, 6.5 TB/s.  The steps overlap: loads, 6 reads of LDS for every 8
 // products, and the products of two wavefronts a SIMD.
 
 constexpr int kStepK = 128;

@@ -42,8 +42,8 @@ __device__ __forceinline__ float normed_step(const NormArgs &a, float step, doub
 
 // L lanes per row, which stays in registers: H runs of 8 elements a lane.  The
 // weights of a lane's columns stay there too, over all rows it takes.  Bound by
-// memory: 12,000 rows of 768 bfloat16 with a residual (64 MB) 15.4 us, 4.2 TB/s
-// (34 us in two passes over each row); one row 3.2 us, two latencies of memory
+// memory: 12,000 rows of 768 bfloat16 with a residual (64 MB) 16.4 us, 3.9 TB/s
+// (34 us in two passes over each row); one row 3.4 us, two latencies of memory
 // and the exchanges of two sums.
 template <class T, int L, int H>
 __global__ __launch_bounds__(kBlock) void norm_kernel(const NormArgs a) {
