@@ -1099,8 +1099,9 @@ tgl_status tgl_cache_attend(const tgl_cache *cache, const tgl_heads *q, int32_t 
         const AttendArgs part = slice(a, b, seqs->num_seqs - b < most ? seqs->num_seqs - b : most, elem_size(dtype));
         if (dtype == TGL_OUT_F32) launch<float>(part, st);
         else launch<bf16_t>(part, st);
+        if (launch_status() != TGL_OK) return TGL_EDEVICE;
     }
-    return launch_status();
+    return TGL_OK;
 }
 
 }  // extern "C"

@@ -369,15 +369,17 @@ void launch(const LinearArgs &a, hipStream_t st) {
 // A launch has fewer than 2^32 threads: as many rows at a time as keep to that
 // with tiles of 64 and 256 threads, or of 128 and 512.
 template <class T>
-void launch_parts(LinearArgs a, hipStream_t st) {
+tgl_status launch_parts(LinearArgs a, hipStream_t st) {
     const int64_t most = (int64_t(1) << 25) / ((a.n + 15) / 16) / 16 * 256, all = a.m;
     for (int64_t row = 0; row < all; row += most) {
         a.m = all - row < most ? all - row : most;
         launch<T>(a, st);
+        if (launch_status() != TGL_OK) return TGL_EDEVICE;
         a.x += most * a.xstride;
         a.xs += most;
         a.out = static_cast<T *>(a.out) + most * a.ostride;
     }
+    return TGL_OK;
 }
 
 }  // namespace
@@ -414,9 +416,7 @@ tgl_status tgl_linear_i8(const int8_t *x, int64_t x_stride, const float *x_scale
     a.m = m;
     a.n = n;
     a.k = k;
-    if (out_type == TGL_OUT_F32) launch_parts<float>(a, st);
-    else launch_parts<bf16_t>(a, st);
-    return launch_status();
+    return out_type == TGL_OUT_F32 ? launch_parts<float>(a, st) : launch_parts<bf16_t>(a, st);
 }
 
 }  // extern "C"
