@@ -1,9 +1,6 @@
 """What the 8-bit operators refuse because no launch could take it (host checks only)."""
-import ctypes as C
-
-import paper_2203_14883_amd as P
 from paper_2203_14883_amd import binding as B
-from test_abi_layer8 import FAKE, _attend, _cache, _seqs
+from test_abi_layer8 import _attend, _cache, _seqs
 
 
 def test_attend_refuses_a_sequence_of_more_tiles_than_a_launch_has():
