@@ -203,7 +203,8 @@ __device__ __forceinline__ int clamp_to(int64_t v, int most) {
 // 2), the four that a lane has of each half (4 and 8), a half (16 and more).
 enum Pages { kTokens, kFours, kHalves };
 
-// Wavefronts of a SIMD that the registers are cut for.
+// Wavefronts of a SIMD that the registers are cut for: the most that spill
+// nothing, or (pages of 1 and 2, heads above 32) a few.
 template <int JV, int R>
 constexpr int kWavesPerSimd = JV >= 8 || R == 2 ? 2 : 4;
 
