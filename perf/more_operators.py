@@ -191,11 +191,11 @@ def _plain_linear_backward(s, dy, x, w, order, ends, bias):
 
 
 def _plain_norm(x, res, gamma, beta):
-    h = x.float() if res is None else x.float() + res.float()
-    rounded = h.to(x.dtype)
+    kept = x if res is None else (x.float() + res.float()).to(x.dtype)
+    h = kept.float()
     c = h - h.mean(1, keepdim=True)
     rstd = 1 / torch.sqrt(c.square().mean(1, keepdim=True) + EPS)
-    return (c * rstd * gamma + beta).to(x.dtype), rounded
+    return (c * rstd * gamma + beta).to(x.dtype), kept
 
 
 def _plain_norm_backward(dy, h, gamma, dh):
@@ -342,8 +342,7 @@ def _exact_norm(case, s):
     if case["kind"] == "norm":
         return _normed(s["x"].double(), s["gamma"], s["beta"])[0]
     h = s["x"].double() + s["res"].double()
-    y = _normed(h, s["gamma"], s["beta"])[0]
-    _, xh, sd = _normed(h.to(s["type"]).double(), s["gamma"], s["beta"])    # backward has h as it is kept
+    y, xh, sd = _normed(h.to(s["type"]).double(), s["gamma"], s["beta"])    # the norm is of the sum as it is kept
     dx, dgamma, dbeta = _norm_gradients(s["dy"], xh, sd, s["gamma"])
     return y, h, dx + s["dh"].double(), dgamma, dbeta
 
