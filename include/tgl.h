@@ -760,6 +760,138 @@ tgl_status tgl_cache_attend(const tgl_cache *cache, const tgl_heads *q, int32_t 
                             void *stream);
 
 /* ------------------------------------------------------------------------ */
+/* Rows of several types, layer norm: training a temporal attention layer   */
+/* (Sections 2.1, 2.2) in float32 and bfloat16, with gradients              */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Element types of rows and weights: TGL_OUT_F32 (4-byte aligned) or
+ * TGL_OUT_BF16 (2-byte aligned); strides are in elements and may be 0 or
+ * negative for what is only read.  Biases, the norm's weights and the gradients
+ * of both are float32.  Products are summed in float32, what is rounded to
+ * bfloat16 is rounded once, to nearest, and results do not change from run to
+ * run: every sum is taken in one order.
+ */
+#define TGL_MAX_TYPES     1024
+#define TGL_MAX_TYPED_DIM 65536       /* columns of rows and weights              */
+#define TGL_MAX_NORM_DIM  16384
+
+/*
+ * Rows sorted by their type.
+ *   type of row i = types[i], or with ids types[ids[i]], none where ids[i] is
+ *   outside [0, num_ids) (PAD slots carry -1) or the type is outside [0, num_types)
+ *   order[0..n)    [device] the rows of type 0, then of type 1, ..., then those of
+ *                  no type, each in ascending order
+ *   offsets[g]     [device] where type g begins in order; offsets[num_types]:
+ *                  where the rows of no type begin
+ *   types      [device] n (with ids: num_ids) int32, or int64 where types64 = 1
+ *   ids        [device] int32[n] or NULL (then num_ids is not read)
+ *   n          in [0, 2^31);  num_types in [1, TGL_MAX_TYPES]
+ *   workspace  [device] at least tgl_group_rows_workspace(...) bytes, 256-byte
+ *              aligned (NULL where that is 0)
+ * Never synchronises.  Errors: TGL_EINVAL, TGL_ENOSPACE, TGL_EDEVICE.
+ */
+size_t tgl_group_rows_workspace(int64_t n, int32_t num_types);
+tgl_status tgl_group_rows(const void *types, int32_t types64, int64_t num_ids, const int32_t *ids, int64_t n,
+                          int32_t num_types, int32_t *order, int64_t *offsets, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/*
+ * The rows of a call by type, as tgl_group_rows leaves them: type g has the
+ * rows order[p], p in [offsets[g], offsets[g + 1]).  With order NULL row p
+ * itself.  offsets[0] counts as 0, offsets do not decrease, and what lies at
+ * or beyond offsets[num_types] has no type.  Offsets are taken as within [0, n] and
+ * places of order outside [0, n) are skipped; a row must be in order once.
+ */
+typedef struct tgl_row_groups {
+    const int32_t *order;   /* [device] n, or NULL      */
+    const int64_t *offsets; /* [device] num_types + 1   */
+    int64_t n;              /* in [0, 2^31)             */
+    int32_t num_types;      /* in [1, TGL_MAX_TYPES]    */
+    int32_t reserved;       /* 0                        */
+} tgl_row_groups;
+
+/* Weights of every type: element (g, o, i) at g * type_stride + o * row_stride
+ * + i, o < out and i < in, both in [1, TGL_MAX_TYPED_DIM]. */
+typedef struct tgl_typed_weights {
+    const void *ptr;        /* [device] */
+    int64_t type_stride;
+    int64_t row_stride;     /* at least in */
+    int32_t out;
+    int32_t in;
+} tgl_typed_weights;
+
+/*
+ * Products of rows with their type's weights, and their gradients: with W and b of
+ * row i's type
+ *   y[i]  = W x[i] + b                             (0 for rows of no type)
+ *   dx[i] = W^T dy[i]                              (0 for rows of no type)
+ *   dW[g] = sum over the rows i of type g of dy[i] x[i]^T,  db[g] = the sum of dy[i]
+ * Rows of no type are not read.
+ *   x, dx      [device] n rows of w->in elements;  y, dy: of w->out elements
+ *   bias       [device] float[num_types][out], contiguous, or NULL
+ *   dw         [device] elements [num_types][out][in], contiguous; 0 for types
+ *              without rows;  db [device] float[num_types][out] or NULL
+ *   outputs may not overlap inputs
+ *   workspace  [device] at least the matching *_workspace() bytes, 256-byte
+ *              aligned (NULL where that is 0)
+ * Never synchronise.  Errors: TGL_EINVAL, TGL_ENOSPACE, TGL_EDEVICE.
+ */
+tgl_status tgl_linear_typed(const tgl_row_groups *groups, const void *x, int64_t x_stride,
+                            const tgl_typed_weights *w, const float *bias, void *y, int64_t y_stride,
+                            int32_t dtype, void *stream);
+tgl_status tgl_linear_typed_grad_x(const tgl_row_groups *groups, const void *dy, int64_t dy_stride,
+                                   const tgl_typed_weights *w, void *dx, int64_t dx_stride, int32_t dtype,
+                                   void *stream);
+size_t tgl_linear_typed_grad_w_workspace(const tgl_row_groups *groups, int32_t out, int32_t in, int32_t dtype);
+tgl_status tgl_linear_typed_grad_w(const tgl_row_groups *groups, const void *dy, int64_t dy_stride, const void *x,
+                                   int64_t x_stride, int32_t out, int32_t in, void *dw, float *db, int32_t dtype,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Residual addition and layer norm of rows.  For every row, with x = x[i],
+ * r = residual[i]:
+ *   h = x + r in x's type (x itself without a residual);  sum[i] = h
+ *   mean = mean(h);  rstd = 1 / sqrt(mean((h - mean)^2) + eps);  stats[i] = (mean, rstd)
+ *   y[i] = (h - mean) * rstd * weight + bias
+ * Both means are sums of 64 bits.
+ *   x, residual  [device] n rows of dim elements of type dtype; residual may be
+ *                NULL (then sum must be)
+ *   weight, bias [device] float[dim], or NULL for ones and zeros
+ *   dim          in [1, TGL_MAX_NORM_DIM]
+ *   y, sum       [device] n rows of dim elements; sum may be x or residual itself
+ *                (with its stride), and with a residual may not be NULL; y may be x
+ *                itself where there is no residual
+ *   stats        [device] double[n][2], or NULL
+ * Never synchronises.  Errors: TGL_EINVAL, TGL_EDEVICE.
+ */
+tgl_status tgl_layer_norm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride,
+                          const float *weight, const float *bias, int64_t n, int32_t dim, int32_t dtype, float eps,
+                          void *y, int64_t y_stride, void *sum, int64_t sum_stride, double *stats, void *stream);
+
+/*
+ * Gradients of tgl_layer_norm: with xh = (h - mean) * rstd and g = dy * weight
+ *   dx[i]   = (g - mean(g) - xh * mean(g * xh)) * rstd  (+ dsum[i])
+ *   dweight = sum over rows of dy * xh,  dbias = sum over rows of dy
+ * dx is the gradient of x and of the residual.
+ *   dy, h, dsum  [device] n rows of dim elements of type dtype; h is sum (x without
+ *                a residual), dsum the gradient that reaches h itself, or NULL
+ *   stats        [device] double[n][2], of tgl_layer_norm
+ *   dx           [device] n rows of dim elements, or NULL; it may be dy or dsum
+ *                itself, with its stride
+ *   dweight, dbias  [device] float[dim]; either may be NULL
+ *   workspace    [device] at least tgl_layer_norm_grad_workspace(...) bytes,
+ *                256-byte aligned; not read where dweight and dbias are NULL
+ * Sums are taken in 64 bits.  Never synchronises.  Errors: TGL_EINVAL,
+ * TGL_ENOSPACE, TGL_EDEVICE.
+ */
+size_t tgl_layer_norm_grad_workspace(int64_t n, int32_t dim);
+tgl_status tgl_layer_norm_grad(const void *dy, int64_t dy_stride, const void *h, int64_t h_stride,
+                               const double *stats, const float *weight, const void *dsum, int64_t dsum_stride,
+                               int64_t n, int32_t dim, int32_t dtype, void *dx, int64_t dx_stride, float *dweight,
+                               float *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------ */
 /* Kernel timers (instrumentation for benchmarks)                           */
 /* ------------------------------------------------------------------------ */
 

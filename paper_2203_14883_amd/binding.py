@@ -44,7 +44,10 @@ EXPORTS = ("tgl_version", "tgl_status_str", "tgl_tcsr_build_workspace", "tgl_tcs
            "tgl_sample_ex", "tgl_sample_noalloc", "tgl_pointers_reset", "tgl_mfg_workspace", "tgl_mfg_export",
            "tgl_gather", "tgl_time_encode",
            "tgl_norm_quant", "tgl_linear_i8", "tgl_cache_write", "tgl_cache_read",
-           "tgl_cache_attend_workspace", "tgl_cache_attend", "tgl_timer_enable",
+           "tgl_cache_attend_workspace", "tgl_cache_attend",
+           "tgl_group_rows_workspace", "tgl_group_rows", "tgl_linear_typed", "tgl_linear_typed_grad_x",
+           "tgl_linear_typed_grad_w_workspace", "tgl_linear_typed_grad_w",
+           "tgl_layer_norm", "tgl_layer_norm_grad_workspace", "tgl_layer_norm_grad", "tgl_timer_enable",
            "tgl_timer_disable", "tgl_timer_read", "tgl_timer_reset", "tgl_timer_select")
 
 
@@ -97,6 +100,16 @@ class c_seqs(C.Structure):
 
 class c_heads(C.Structure):
     _fields_ = [("ptr", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class c_row_groups(C.Structure):
+    _fields_ = [("order", C.c_void_p), ("offsets", C.c_void_p), ("n", C.c_int64), ("num_types", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class c_typed_weights(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("type_stride", C.c_int64), ("row_stride", C.c_int64), ("out", C.c_int32),
+                ("in_", C.c_int32)]
 
 
 _lib: Optional[C.CDLL] = None
@@ -164,6 +177,25 @@ def lib() -> C.CDLL:
     L.tgl_cache_attend.restype = i32
     L.tgl_cache_attend.argtypes = [C.POINTER(c_cache), C.POINTER(c_heads), i32, i64, i32, C.POINTER(c_seqs), P, f32,
                                    C.POINTER(c_heads), P, P, C.c_size_t, P]
+    groups, weights, size = C.POINTER(c_row_groups), C.POINTER(c_typed_weights), C.c_size_t
+    L.tgl_group_rows_workspace.restype = size
+    L.tgl_group_rows_workspace.argtypes = [i64, i32]
+    L.tgl_group_rows.restype = i32
+    L.tgl_group_rows.argtypes = [P, i32, i64, P, i64, i32, P, P, P, size, P]
+    L.tgl_linear_typed.restype = i32
+    L.tgl_linear_typed.argtypes = [groups, P, i64, weights, P, P, i64, i32, P]
+    L.tgl_linear_typed_grad_x.restype = i32
+    L.tgl_linear_typed_grad_x.argtypes = [groups, P, i64, weights, P, i64, i32, P]
+    L.tgl_linear_typed_grad_w_workspace.restype = size
+    L.tgl_linear_typed_grad_w_workspace.argtypes = [groups, i32, i32, i32]
+    L.tgl_linear_typed_grad_w.restype = i32
+    L.tgl_linear_typed_grad_w.argtypes = [groups, P, i64, P, i64, i32, i32, P, P, i32, P, size, P]
+    L.tgl_layer_norm.restype = i32
+    L.tgl_layer_norm.argtypes = [P, i64, P, i64, P, P, i64, i32, i32, f32, P, i64, P, i64, P, P]
+    L.tgl_layer_norm_grad_workspace.restype = size
+    L.tgl_layer_norm_grad_workspace.argtypes = [i64, i32]
+    L.tgl_layer_norm_grad.restype = i32
+    L.tgl_layer_norm_grad.argtypes = [P, i64, P, i64, P, P, P, i64, i64, i32, i32, P, i64, P, P, P, size, P]
     L.tgl_timer_enable.restype = i32
     L.tgl_timer_enable.argtypes = [i32]
     L.tgl_timer_disable.restype = i32
