@@ -3,7 +3,9 @@
 //   y[i] = W x[i] + b;  dx[i] = W^T dy[i];  dW = sum dy[i] x[i]^T;  db = sum dy[i]
 // over the rows i of a type, whose places are known on the device only: the grid has
 // room for as many tiles as there can be, and each finds its type and rows.
-#include "tgl_typed.hpp"
+#include <type_traits>
+
+#include "tgl_typed_tile.hpp"
 
 namespace tgl {
 namespace {
@@ -30,207 +32,241 @@ struct SumsArgs {               // dW and db
     int64_t dys, xs;
     int32_t out, in;
     int32_t rows;               // of a stretch
+    int32_t tile;
     int32_t tiles_in, tiles;    // tiles of dW
-    int32_t stretches;          // there is room for
+    uint32_t stretches;         // there is room for
 };
 
-constexpr int kTile = 64;
-constexpr int kBytes = 128;     // of a tile's row in LDS
-
-__device__ __forceinline__ int swizzle(int r) { return (r >> 1) & 7; }
-
-template <class T>
-__device__ __forceinline__ void put_piece(int8_t *tile, int r, int p, const i32x4 &v) {
-    *reinterpret_cast<i32x4 *>(tile + r * kBytes + ((p ^ swizzle(r)) * 16)) = v;
+// Tile `id` of rows x cols, in bands of `band` rows walked column by column, so
+// that tiles of neighbouring numbers share what they read.
+__device__ __forceinline__ void banded(uint32_t id, uint32_t rows, uint32_t cols, uint32_t band, uint32_t &r, uint32_t &c) {
+    const uint32_t b = id / (band * cols), in = id - b * band * cols;
+    const uint32_t left = rows - b * band, height = left < band ? left : band;
+    c = in / height;
+    r = b * band + (in - c * height);
 }
 
-template <class T>
-__device__ __forceinline__ i32x4 get_piece(const int8_t *tile, int r, int p) {
-    return *reinterpret_cast<const i32x4 *>(tile + r * kBytes + ((p ^ swizzle(r)) * 16));
+// A workgroup's number among `work`: the 8 dies take workgroups in turn, and each
+// gets a contiguous stretch of the work.  False if there is none left.
+__device__ __forceinline__ bool die_major(uint32_t work, uint32_t &id) {
+    const uint32_t per = (work + 7) / 8, at = blockIdx.x >> 3;
+    id = (blockIdx.x & 7) * per + at;
+    return at < per && id < work;
 }
 
-// kPiece elements that lie across kPiece rows of a tile, at element e of each.
-template <class T>
-__device__ __forceinline__ void put_across(int8_t *tile, int r, int e, const i32x4 &v) {
-    const Run<T, kPiece<T>> x = __builtin_bit_cast(Run<T, kPiece<T>>, v);
-#pragma unroll
-    for (int i = 0; i < kPiece<T>; i++) {
-        const int p = e / kPiece<T>, in = e % kPiece<T>;
-        *reinterpret_cast<T *>(tile + (r + i) * kBytes + ((p ^ swizzle(r + i)) * 16) + in * sizeof(T)) = x.t[i];
-    }
-}
-
-// 64 x 64 outputs of 4 wavefronts, 32 x 32 each; `b` are a tile's output columns.
-template <class T>
-__device__ __forceinline__ void multiply_tile(const int8_t *a, const int8_t *b, int wm, int wn, f32x4 (&acc)[2][2]) {
-    const int i16 = lane_id() & 15, g = lane_id() >> 4;
-#pragma unroll
-    for (int h = 0; h < 2; h++) {
-        i32x4 x[2], w[2];
-#pragma unroll
-        for (int i = 0; i < 2; i++) {
-            x[i] = get_piece<T>(a, wm * 32 + i * 16 + i16, 4 * h + g);
-            w[i] = get_piece<T>(b, wn * 32 + i * 16 + i16, 4 * h + g);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; i++)
-#pragma unroll
-            for (int j = 0; j < 2; j++) acc[i][j] = multiply_pieces<T>(w[j], x[i], acc[i][j]);
-    }
-}
-
-template <class T, bool kAcross>
-__global__ __launch_bounds__(kBlock) void rows_kernel(const RowsArgs a) {
-    __shared__ __attribute__((aligned(16))) int8_t at[kTile * kBytes];
-    __shared__ __attribute__((aligned(16))) int8_t bt[kTile * kBytes];
-    constexpr int kStep = kBytes / sizeof(T), E = kPiece<T>;
-    const uint32_t tm = blockIdx.x / a.tiles_n;
-    const int n0 = (blockIdx.x % a.tiles_n) * kTile;
+// BM rows of one type times BN columns; a wavefront has 64 columns.
+template <class T, bool kAcross, int BM, int BN, int NW, bool kDirect>
+__global__ __launch_bounds__(NW * kWave, 2) void rows_kernel(const RowsArgs a) {
+    constexpr int kWaveN = BN / 64, MT = BM / (NW / kWaveN) / 16, NT = 4;
+    // one object each: so the compiler sees that a step's reads do not wait for the others' loads
+    __shared__ __attribute__((aligned(1024))) int8_t buf0[(BM + BN) * kStepBytes];
+    __shared__ __attribute__((aligned(1024))) int8_t buf1[(BM + BN) * kStepBytes];
+    uint32_t id, tm, tn;
+    const uint32_t tiles_m = count_stretches<true>(a.g, BM, 0);
+    if (!die_major(tiles_m * a.tiles_n, id)) return;
+    banded(id, tiles_m, a.tiles_n, 8, tm, tn);
     Stretch s;
-    if (!find_stretch<true>(a.g, tm, kTile, 0, s)) return;
-    const int lane = lane_id(), wave = threadIdx.x / kWave;
-    const int i16 = lane & 15, g = lane >> 4, wm = wave >> 1, wn = wave & 1;
-    f32x4 acc[2][2] = {};
+    if (!find_stretch<true>(a.g, tm, BM, 0, s)) return;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wm = wave / kWaveN, wn = wave % kWaveN;
+    const int n0 = tn * BN;
+    f32x4 acc[MT][NT] = {};
     if (s.type < a.g.num_types) {
-        const T *w = static_cast<const T *>(a.w) + s.type * a.wt;
-        const int r0 = threadIdx.x / 8, p = threadIdx.x % 8;        // rows r0 and r0 + 32
-        const T *row[2];
+        using X = Along<T, BM, NW, kDirect>;
+        using W = std::conditional_t<kAcross, Across<T, BN, NW, kDirect>, Along<T, BN, NW, kDirect>>;
+        X x;
+        W w;
+        x.length = a.k;
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
-            const int64_t at = row_at(a.g, s.begin + r0 + 32 * i, s.end);
-            row[i] = at < 0 ? nullptr : static_cast<const T *>(a.x) + at * a.xs;
+        for (int f = 0; f < X::kFetch; f++) {
+            const int64_t row = row_at(a.g, s.begin + X::edge(wave, f), s.end);
+            x.set(wave, f, static_cast<const T *>(a.x) + (row < 0 ? 0 : row) * a.xs);
         }
-        for (int k0 = 0; k0 < a.k; k0 += kStep) {
-            __syncthreads();
+        const T *weights = static_cast<const T *>(a.w) + s.type * a.wt;
+        if constexpr (kAcross) {
+            w.set(wave, weights, a.ws, a.k, n0, a.n);
+        } else {
+            w.length = a.k;
 #pragma unroll
-            for (int i = 0; i < 2; i++) put_piece<T>(at, r0 + 32 * i, p, load_piece(row[i], k0 + p * E, a.k));
-            if constexpr (!kAcross) {
-#pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    const int c = n0 + r0 + 32 * i;
-                    put_piece<T>(bt, r0 + 32 * i, p, load_piece(c < a.n ? w + c * a.ws : nullptr, k0 + p * E, a.k));
-                }
-            } else {
-                for (int t = threadIdx.x; t < kStep * (kTile / E); t += kBlock) {
-                    const int k = t / (kTile / E), c = t % (kTile / E) * E;
-                    put_across<T>(bt, c, k, load_piece(k0 + k < a.k ? w + (k0 + k) * a.ws : nullptr, n0 + c, a.n));
-                }
+            for (int f = 0; f < W::kFetch; f++) {
+                const int c = n0 + W::edge(wave, f);
+                w.set(wave, f, weights + (c < a.n ? c : a.n - 1) * a.ws);
             }
-            __syncthreads();
-            multiply_tile<T>(at, bt, wm, wn, acc);
         }
+        multiply_steps<T, false, kAcross>(
+            (a.k + kStep<T> - 1) / kStep<T>, buf0, buf1, acc,
+            [&](int step, int8_t *buf) {
+                x.fetch(wave, step, buf);
+                w.fetch(wave, step, buf + BM * kStepBytes);
+            },
+            [&](int8_t *buf) {
+                x.store(wave, buf);
+                w.store(wave, buf + BM * kStepBytes);
+            },
+            [&](const int8_t *buf, int h, i32x4(&xv)[MT], i32x4(&wv)[NT]) {
+                W::read(buf + BM * kStepBytes, wn * 64, h, wv);
+                X::read(buf, wm * MT * 16, h, xv);
+            },
+            [](const i32x4(&)[MT], const i32x4(&)[NT]) {});
     }
+    const float *bias = a.bias && s.type < a.g.num_types ? a.bias + static_cast<int64_t>(s.type) * a.n : nullptr;
+    int64_t row[MT];
 #pragma unroll
-    for (int i = 0; i < 2; i++) {
-        const int64_t row = row_at(a.g, s.begin + wm * 32 + i * 16 + i16, s.end);
-        if (row < 0) continue;
+    for (int i = 0; i < MT; i++) row[i] = row_at(a.g, s.begin + wm * MT * 16 + tile_row<T, false, MT>(i), s.end);
 #pragma unroll
-        for (int j = 0; j < 2; j++) {
-            const int c = n0 + wn * 32 + j * 16 + 4 * g;
-            float v[4];
+    for (int i = 0; i < MT; i++) {
+        if (row[i] < 0) continue;
+        T *y = static_cast<T *>(a.y) + row[i] * a.ys;
+        tile_columns<T, kAcross>(acc[i], [&](int c, const float(&v)[4]) {
+            const int col = n0 + wn * 64 + c;
+            if (col >= a.n) return;
+            float out[4] = {v[0], v[1], v[2], v[3]};
+            if (bias) {
+                float b[4];
+                load_columns<float, 4>(bias, col, a.n, b);
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                v[e] = acc[i][j][e];
-                if (a.bias && s.type < a.g.num_types && c + e < a.n) v[e] += a.bias[static_cast<int64_t>(s.type) * a.n + c + e];
+                for (int e = 0; e < 4; e++) out[e] += b[e];
             }
-            if (c < a.n) store_columns<T, 4>(static_cast<T *>(a.y) + row * a.ys, c, a.n, v);
-        }
+            store_columns<T, 4>(y, col, a.n, out);
+        });
     }
+    (void)lane;
 }
 
-template <class T>
-__global__ __launch_bounds__(kBlock) void sums_kernel(const SumsArgs a) {
-    __shared__ __attribute__((aligned(16))) int8_t at[kTile * kBytes];
-    __shared__ __attribute__((aligned(16))) int8_t bt[kTile * kBytes];
-    constexpr int kStep = kBytes / sizeof(T), E = kPiece<T>;
-    const uint32_t stretch = blockIdx.x / a.tiles;
-    const int tile = blockIdx.x % a.tiles;
-    const int o0 = tile / a.tiles_in * kTile, c0 = tile % a.tiles_in * kTile;
+// BM rows times BN columns of dW, over a stretch of a type's rows.
+template <class T, int BM, int BN, int NW, bool kDirect>
+__global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
+    constexpr int kWaveN = BN / 64, MT = BM / (NW / kWaveN) / 16, NT = 4;
+    __shared__ __attribute__((aligned(1024))) int8_t buf0[(BM + BN) * kStepBytes];
+    __shared__ __attribute__((aligned(1024))) int8_t buf1[(BM + BN) * kStepBytes];
+    uint32_t id, to, ti;
+    const uint32_t stretches = count_stretches<false>(a.g, a.rows, 1);
+    if (!die_major((stretches < a.stretches ? stretches : a.stretches) * a.tiles, id)) return;
+    const uint32_t stretch = id / a.tiles;
+    banded(id - stretch * a.tiles, a.tiles / a.tiles_in, a.tiles_in, 4, to, ti);
+    const int o0 = to * BM, c0 = ti * BN;
     Stretch s;
     if (!find_stretch<false>(a.g, stretch, a.rows, 1, s)) return;
-    const int lane = lane_id(), wave = threadIdx.x / kWave;
-    const int i16 = lane & 15, g = lane >> 4, wm = wave >> 1, wn = wave & 1;
-    f32x4 acc[2][2] = {};
-    float sum = 0.0f;
-    for (int64_t p0 = s.begin; p0 < s.end; p0 += kStep) {
-        __syncthreads();
-        for (int t = threadIdx.x; t < kStep * (kTile / E); t += kBlock) {
-            const int k = t / (kTile / E), c = t % (kTile / E) * E;
-            const int64_t row = row_at(a.g, p0 + k, s.end);
-            put_across<T>(at, c, k, load_piece(row < 0 ? nullptr : static_cast<const T *>(a.dy) + row * a.dys, o0 + c, a.out));
-            put_across<T>(bt, c, k, load_piece(row < 0 ? nullptr : static_cast<const T *>(a.x) + row * a.xs, c0 + c, a.in));
-        }
-        __syncthreads();
-        multiply_tile<T>(at, bt, wm, wn, acc);
-        if (a.db && c0 == 0 && threadIdx.x < kTile)
-            for (int p = 0; p < 8; p++) {
-                const Run<T, E> v = __builtin_bit_cast(Run<T, E>, get_piece<T>(at, threadIdx.x, p));
-                for (int i = 0; i < E; i++) sum += as_float(v.t[i]);
-            }
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wm = wave / kWaveN, wn = wave % kWaveN;
+    f32x4 acc[MT][NT] = {};
+    constexpr int kSums = (MT + kWaveN - 1) / kWaveN;
+    float sum[kSums] = {};                      // of dy, tiles wn, wn + kWaveN, ... of the wavefront's rows
+    const bool want_sum = a.db && ti == 0;
+    using D = Gathered<T, BM, NW, kDirect>;
+    using X = Gathered<T, BN, NW, kDirect>;
+    const int steps = static_cast<int>((s.end - s.begin + kStep<T> - 1) / kStep<T>);
+    if (steps > 0) {
+        D d;
+        X x;
+        d.set(static_cast<const T *>(a.dy), a.dys, o0, a.out);
+        x.set(static_cast<const T *>(a.x), a.xs, c0, a.in);
+        auto rows_of = [&](int step) {
+            return static_cast<int32_t>(row_at(a.g, s.begin + static_cast<int64_t>(step) * kStep<T> + wave * D::kOwn + lane % D::kOwn, s.end));
+        };
+        int32_t ids = rows_of(0);
+        multiply_steps<T, true, true>(
+            steps, buf0, buf1, acc,
+            [&](int step, int8_t *buf) {
+                d.fetch(wave, ids, buf);
+                x.fetch(wave, ids, buf + BM * kStepBytes);
+                ids = rows_of(step + 1);
+            },
+            [&](int8_t *buf) {
+                d.store(wave, buf);
+                x.store(wave, buf + BM * kStepBytes);
+            },
+            [&](const int8_t *buf, int h, i32x4(&dv)[MT], i32x4(&xv)[NT]) {
+                X::read(buf + BM * kStepBytes, wn * 64, h, xv);
+                D::read(buf, wm * MT * 16, h, dv);
+            },
+            [&](const i32x4(&dv)[MT], const i32x4(&)[NT]) {
+                if (!want_sum) return;
+#pragma unroll
+                for (int i = 0; i < MT; i++) {
+                    if (i % kWaveN != wn) continue;
+                    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            sum[i / kWaveN] += __builtin_bit_cast(float, dv[i][e] << 16);
+                            sum[i / kWaveN] += __builtin_bit_cast(float, dv[i][e] & static_cast<int>(0xffff0000u));
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; e++) sum[i / kWaveN] += element<T, true>(dv, i, e);
+                    }
+                }
+            });
     }
     const int64_t outs = static_cast<int64_t>(a.out) * a.in;
 #pragma unroll
-    for (int i = 0; i < 2; i++) {
-        const int o = o0 + wm * 32 + i * 16 + i16;
-        if (o >= a.out) continue;
-#pragma unroll
-        for (int j = 0; j < 2; j++) {
-            const int c = c0 + wn * 32 + j * 16 + 4 * g;
-            const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-            if (c >= a.in) continue;
-            if (s.count == 1) store_columns<T, 4>(static_cast<T *>(a.dw) + s.type * outs + static_cast<int64_t>(o) * a.in, c, a.in, v);
-            else store_columns<float, 4>(a.parts + stretch * outs + static_cast<int64_t>(o) * a.in, c, a.in, v);
+    for (int i = 0; i < MT; i++) {
+        const int o = o0 + wm * MT * 16 + tile_row<T, true, MT>(i);
+        if (want_sum && i % kWaveN == wn) {
+            float v = sum[i / kWaveN];
+            v += __shfl_xor(v, 16, kWave);
+            v += __shfl_xor(v, 32, kWave);
+            if (lane < 16 && o < a.out) {
+                if (s.count == 1) a.db[static_cast<int64_t>(s.type) * a.out + o] = v;
+                else a.parts_b[static_cast<int64_t>(stretch) * a.out + o] = v;
+            }
         }
-    }
-    if (a.db && c0 == 0 && threadIdx.x < kTile && o0 + static_cast<int>(threadIdx.x) < a.out) {
-        const int o = o0 + threadIdx.x;
-        if (s.count == 1) a.db[static_cast<int64_t>(s.type) * a.out + o] = sum;
-        else a.parts_b[static_cast<int64_t>(stretch) * a.out + o] = sum;
+        if (o >= a.out) continue;
+        tile_columns<T, true>(acc[i], [&](int c, const float(&v)[4]) {
+            const int col = c0 + wn * 64 + c;
+            if (col >= a.in) return;
+            if (s.count == 1) store_columns<T, 4>(static_cast<T *>(a.dw) + s.type * outs + static_cast<int64_t>(o) * a.in, col, a.in, v);
+            else store_columns<float, 4>(a.parts + stretch * outs + static_cast<int64_t>(o) * a.in, col, a.in, v);
+        });
     }
 }
 
 // The stretches of a type together, one after another.
 template <class T>
-__global__ __launch_bounds__(kBlock) void sums_join_kernel(const SumsArgs a, int32_t blocks) {
+__global__ __launch_bounds__(kBlock) void sums_join_kernel(const SumsArgs a, uint32_t blocks) {
     const int type = blockIdx.x / blocks;
-    // the type's first stretch and their number
-    int64_t first = 0;
-    int32_t count = 0;
-    for (int t = 0; t <= type; t++) {
-        int64_t begin = t == 0 ? 0 : a.g.offsets[t], end = a.g.offsets[t + 1];
-        begin = begin < 0 ? 0 : begin > a.g.n ? a.g.n : begin;
-        end = end > a.g.n ? a.g.n : end < begin ? begin : end;
-        first += count;
-        count = static_cast<int32_t>((end - begin + a.rows - 1) / a.rows);
-        if (count < 1) count = 1;
-    }
+    int64_t first;
+    const int32_t count = stretches_of_type(a.g, type, a.rows, 1, first);
     if (count == 1 || first + count > a.stretches) return;      // offsets that decrease: nothing to read
     const int64_t outs = static_cast<int64_t>(a.out) * a.in;
     for (int64_t i = static_cast<int64_t>(blockIdx.x % blocks) * kBlock + threadIdx.x; i < outs + (a.db ? a.out : 0);
          i += static_cast<int64_t>(blocks) * kBlock) {
+        const int64_t step = i < outs ? outs : a.out;
         const float *p = i < outs ? a.parts + first * outs + i : a.parts_b + first * a.out + (i - outs);
         float sum = 0.0f;
-        for (int32_t c = 0; c < count; c++) sum += p[c * (i < outs ? outs : a.out)];
+#pragma unroll 4
+        for (int32_t c = 0; c < count; c++) sum += p[c * step];
         if (i < outs) static_cast<T *>(a.dw)[type * outs + i] = from_float<T>(sum);
         else a.db[static_cast<int64_t>(type) * a.out + (i - outs)] = sum;
     }
 }
 
-// Rows of a stretch: as many stretches as give the card two workgroups a unit.
-int32_t stretch_rows(int64_t n, int32_t out, int32_t in) {
-    const int64_t tiles = static_cast<int64_t>((out + kTile - 1) / kTile) * ((in + kTile - 1) / kTile);
-    const int64_t most = (512 + tiles - 1) / tiles;
-    int64_t rows = (n + most - 1) / most;
-    if (rows < 256) rows = 256;
-    return static_cast<int32_t>(rows < (1 << 30) ? (rows + 63) / 64 * 64 : 1 << 30);
+constexpr int kTarget = 512;            // workgroups that fill the card
+
+// The tiles of a call's outputs: the largest of which there are still enough.
+int tile_of(int64_t rows, int64_t cols) {
+    auto tiles = [&](int64_t t) { return (rows + t - 1) / t * ((cols + t - 1) / t); };
+    return tiles(256) >= 192 ? 256 : tiles(128) >= 256 ? 128 : 64;
+}
+
+// dW: its tiles, and the rows of a stretch, of which there are as many as fill the card.
+void plan_sums(SumsArgs &a, int32_t dtype) {
+    const bool wide = dtype == TGL_OUT_BF16 && a.out >= 192 && a.in >= 192 && a.g.n / a.g.num_types >= 2048;
+    a.tile = wide ? 256 : a.out > 64 && a.in > 64 && a.g.n / a.g.num_types >= 512 ? 128 : 64;
+    a.tiles_in = (a.in + a.tile - 1) / a.tile;
+    a.tiles = (a.out + a.tile - 1) / a.tile * a.tiles_in;
+    const int64_t most = (kTarget + a.tiles - 1) / a.tiles;
+    int64_t rows = (a.g.n + most - 1) / most;
+    if (rows < 512) rows = 512;
+    a.rows = static_cast<int32_t>(rows < (1 << 30) ? (rows + 63) / 64 * 64 : 1 << 30);
+    a.stretches = static_cast<uint32_t>(a.g.n / a.rows + a.g.num_types);
 }
 
 size_t carve(SumsArgs &a, void *base) {
     Carver c(base);
-    const size_t stretches = static_cast<size_t>(a.g.n / a.rows + a.g.num_types);
     if (a.g.n <= a.rows) return 0;              // no type is cut
-    a.parts = c.take<float>(stretches * a.out * a.in);
-    a.parts_b = c.take<float>(stretches * a.out);
+    a.parts = c.take<float>(static_cast<size_t>(a.stretches) * a.out * a.in);
+    a.parts_b = c.take<float>(static_cast<size_t>(a.stretches) * a.out);
     return c.size();
 }
 
@@ -245,9 +281,31 @@ bool valid_dims(int32_t out, int32_t in) {
 
 Groups groups_of(const tgl_row_groups *g) { return Groups{g->order, g->offsets, g->n, g->num_types}; }
 
+bool wide_rows(const void *p, int64_t stride, size_t e) { return aligned(p, 16) && stride * static_cast<int64_t>(e) % 16 == 0; }
+
+constexpr int64_t kMostBlocks = int64_t(1) << 22;       // of a launch, whose threads are fewer than 2^32
+
+template <class T, bool kAcross, int B, int NW, bool kDirect>
+tgl_status launch_rows(RowsArgs a, hipStream_t st) {
+    a.tiles_n = (a.n + B - 1) / B;
+    const int64_t work = (a.g.n / B + a.g.num_types + 1) * a.tiles_n;
+    if (work > kMostBlocks) return TGL_EINVAL;
+    rows_kernel<T, kAcross, B, B, NW, kDirect><<<static_cast<unsigned>((work + 7) / 8 * 8), NW * kWave, 0, st>>>(a);
+    return launch_status();
+}
+
+template <class T, bool kAcross>
+tgl_status launch_rows(const RowsArgs &a, bool direct, hipStream_t st) {
+    const int tile = tile_of(a.g.n, a.n);
+    if (!direct) return tile == 64 ? launch_rows<T, kAcross, 64, 4, false>(a, st) : launch_rows<T, kAcross, 128, 4, false>(a, st);
+    if constexpr (sizeof(T) == 2)
+        if (tile == 256) return launch_rows<T, kAcross, 256, 8, true>(a, st);
+    return tile == 64 ? launch_rows<T, kAcross, 64, 4, true>(a, st) : launch_rows<T, kAcross, 128, 4, true>(a, st);
+}
+
 template <bool kAcross>
-tgl_status launch_rows(const tgl_row_groups *groups, const void *x, int64_t x_stride, const tgl_typed_weights *w,
-                       const float *bias, void *y, int64_t y_stride, int32_t dtype, void *stream) {
+tgl_status rows_call(const tgl_row_groups *groups, const void *x, int64_t x_stride, const tgl_typed_weights *w,
+                     const float *bias, void *y, int64_t y_stride, int32_t dtype, void *stream) {
     if (!valid_groups(groups) || !w || !valid_dims(w->out, w->in) || !is_elem_type(dtype) || w->row_stride < w->in)
         return TGL_EINVAL;
     const size_t e = elem_size(dtype);
@@ -257,13 +315,26 @@ tgl_status launch_rows(const tgl_row_groups *groups, const void *x, int64_t x_st
     if (groups->n == 0) return TGL_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();
-    RowsArgs a{groups_of(groups), x, w->ptr, bias, y, x_stride, w->row_stride, w->type_stride, y_stride, k, n, 0};
-    a.tiles_n = (n + kTile - 1) / kTile;
-    const int64_t tiles = (groups->n / kTile + groups->num_types + 1) * a.tiles_n;
-    if (tiles >= (int64_t(1) << 24)) return TGL_EINVAL;
-    if (dtype == TGL_OUT_F32) rows_kernel<float, kAcross><<<static_cast<unsigned>(tiles), kBlock, 0, st>>>(a);
-    else rows_kernel<bf16_t, kAcross><<<static_cast<unsigned>(tiles), kBlock, 0, st>>>(a);
+    const RowsArgs a{groups_of(groups), x, w->ptr, bias, y, x_stride, w->row_stride, w->type_stride, y_stride, k, n, 0};
+    const bool direct = wide_rows(x, x_stride, e) && wide_rows(w->ptr, w->row_stride, e) && w->type_stride * e % 16 == 0 &&
+                        k * e % 16 == 0 && (!kAcross || n * e % 16 == 0);
+    return dtype == TGL_OUT_F32 ? launch_rows<float, kAcross>(a, direct, st) : launch_rows<bf16_t, kAcross>(a, direct, st);
+}
+
+template <class T, int B, int NW, bool kDirect>
+tgl_status launch_sums(const SumsArgs &a, hipStream_t st) {
+    const int64_t work = static_cast<int64_t>(a.stretches) * a.tiles;
+    if (work > kMostBlocks) return TGL_EINVAL;
+    sums_kernel<T, B, B, NW, kDirect><<<static_cast<unsigned>((work + 7) / 8 * 8), NW * kWave, 0, st>>>(a);
     return launch_status();
+}
+
+template <class T>
+tgl_status launch_sums(const SumsArgs &a, bool direct, hipStream_t st) {
+    if (!direct) return a.tile == 64 ? launch_sums<T, 64, 4, false>(a, st) : launch_sums<T, 128, 4, false>(a, st);
+    if constexpr (sizeof(T) == 2)
+        if (a.tile == 256) return launch_sums<T, 256, 8, true>(a, st);
+    return a.tile == 64 ? launch_sums<T, 64, 4, true>(a, st) : launch_sums<T, 128, 4, true>(a, st);
 }
 
 }  // namespace
@@ -276,13 +347,13 @@ extern "C" {
 tgl_status tgl_linear_typed(const tgl_row_groups *groups, const void *x, int64_t x_stride,
                             const tgl_typed_weights *w, const float *bias, void *y, int64_t y_stride,
                             int32_t dtype, void *stream) {
-    return launch_rows<false>(groups, x, x_stride, w, bias, y, y_stride, dtype, stream);
+    return rows_call<false>(groups, x, x_stride, w, bias, y, y_stride, dtype, stream);
 }
 
 tgl_status tgl_linear_typed_grad_x(const tgl_row_groups *groups, const void *dy, int64_t dy_stride,
                                    const tgl_typed_weights *w, void *dx, int64_t dx_stride, int32_t dtype,
                                    void *stream) {
-    return launch_rows<true>(groups, dy, dy_stride, w, nullptr, dx, dx_stride, dtype, stream);
+    return rows_call<true>(groups, dy, dy_stride, w, nullptr, dx, dx_stride, dtype, stream);
 }
 
 size_t tgl_linear_typed_grad_w_workspace(const tgl_row_groups *groups, int32_t out, int32_t in, int32_t dtype) {
@@ -291,7 +362,7 @@ size_t tgl_linear_typed_grad_w_workspace(const tgl_row_groups *groups, int32_t o
     a.g = groups_of(groups);
     a.out = out;
     a.in = in;
-    a.rows = stretch_rows(a.g.n, out, in);
+    plan_sums(a, dtype);
     return carve(a, nullptr);
 }
 
@@ -302,25 +373,36 @@ tgl_status tgl_linear_typed_grad_w(const tgl_row_groups *groups, const void *dy,
     const size_t e = elem_size(dtype);
     if (!aligned(dy, e) || !aligned(x, e) || !aligned(dw, e) || !aligned(db, 4) || !dw) return TGL_EINVAL;
     if (groups->n > 0 && (!dy || !x)) return TGL_EINVAL;
-    SumsArgs a{groups_of(groups), dy, x, dw, db, nullptr, nullptr, dy_stride, x_stride, out, in, 0, 0, 0, 0};
-    a.rows = stretch_rows(a.g.n, out, in);
+    SumsArgs a{};
+    a.g = groups_of(groups);
+    a.dy = dy;
+    a.x = x;
+    a.dw = dw;
+    a.db = db;
+    a.dys = dy_stride;
+    a.xs = x_stride;
+    a.out = out;
+    a.in = in;
+    plan_sums(a, dtype);
+    const bool direct = wide_rows(dy, dy_stride, e) && wide_rows(x, x_stride, e) && out * e % 16 == 0 && in * e % 16 == 0;
+    if (!direct && a.tile == 256) {             // 128 through registers
+        a.tile = 128;
+        a.tiles_in = (in + 127) / 128;
+        a.tiles = (out + 127) / 128 * a.tiles_in;
+    }
     const size_t need = carve(a, nullptr);
     if (need) {
         if (!workspace || workspace_bytes < need) return TGL_ENOSPACE;
         if (!aligned(workspace, 256)) return TGL_EINVAL;
         carve(a, workspace);
     }
-    a.tiles_in = (in + kTile - 1) / kTile;
-    a.tiles = (out + kTile - 1) / kTile * a.tiles_in;
-    a.stretches = static_cast<int32_t>(a.g.n / a.rows + a.g.num_types);
-    const int64_t grid = static_cast<int64_t>(a.stretches) * a.tiles;
-    if (grid >= (int64_t(1) << 24)) return TGL_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();
-    if (dtype == TGL_OUT_F32) sums_kernel<float><<<static_cast<unsigned>(grid), kBlock, 0, st>>>(a);
-    else sums_kernel<bf16_t><<<static_cast<unsigned>(grid), kBlock, 0, st>>>(a);
-    if (!need || launch_status() != TGL_OK) return launch_status();
-    const int32_t blocks = 64;
+    const tgl_status done = dtype == TGL_OUT_F32 ? launch_sums<float>(a, direct, st) : launch_sums<bf16_t>(a, direct, st);
+    if (!need || done != TGL_OK) return done;
+    // types that are cut are few: a workgroup for every 2048 outputs of each, 2048 in all at most
+    const int64_t each = (static_cast<int64_t>(out) * in + 2047) / 2048, most = (2048 + a.g.num_types - 1) / a.g.num_types;
+    const uint32_t blocks = static_cast<uint32_t>(each < most ? each : most);
     const unsigned join = static_cast<unsigned>(a.g.num_types) * blocks;
     if (dtype == TGL_OUT_F32) sums_join_kernel<float><<<join, kBlock, 0, st>>>(a, blocks);
     else sums_join_kernel<bf16_t><<<join, kBlock, 0, st>>>(a, blocks);

@@ -1,0 +1,322 @@
+// tgl_typed_tile.hpp -- a tile of a matrix product on the matrix units: BM x BN
+// outputs of a workgroup, whose operands come through LDS in steps of 128 bytes
+// of the sum's axis.
+//
+// A side is what one operand brings to a step: B rows of the tile's edge times
+// 128 bytes of the sum's axis.  It lies in LDS as the memory has it, so that
+// loads go straight there, 16 bytes a lane:
+//   along   the sum's axis is the one that memory runs along: B rows of 128 bytes,
+//           and a lane reads a piece of 16 bytes of one row;
+//   across  the sum's axis goes from row to row of memory: a row of LDS holds
+//           the B elements of one place of the sum's axis, and the reads turn
+//           them (bfloat16: the transposing read of LDS; float32: a lane takes
+//           four columns, and so a column of four tiles).
+// Pieces are permuted within their rows (an exclusive or with bits of the row),
+// so that what a read touches lies in different banks.
+#pragma once
+
+#include "tgl_typed.hpp"
+
+namespace tgl {
+
+constexpr int kStepBytes = 128;
+template <class T>
+constexpr int kStep = kStepBytes / static_cast<int>(sizeof(T));     // of the sum's axis
+
+using lds_t = __attribute__((address_space(3))) void;
+using global_t = __attribute__((address_space(1))) const void;
+
+// Where lanes read what is beyond the sum's axis.
+static __device__ const i32x4 kZeros = {0, 0, 0, 0};
+
+template <class T>
+__device__ __forceinline__ void to_lds(const T *from, int8_t *to) {
+    __builtin_amdgcn_global_load_lds((global_t *)(from), (lds_t *)to, 16, 0, 0);
+}
+
+// Whether a lane's pieces are four columns of one place of the sum's axis
+// each (of four tiles), and not four places of one column.
+template <class T, bool kAcross, int N>
+constexpr bool kQuads = sizeof(T) == 4 && kAcross && N % 4 == 0;
+
+// ---- sides ----
+//
+// Each wavefront brings kFetch times 1024 bytes of a side.  kDirect: row starts
+// and strides are multiples of 16 bytes and so is the sum's axis, or the edge's
+// length where it is the one that memory runs along; memory goes straight to LDS.
+// Otherwise it goes through registers: load() a step ahead, store() after.
+
+// `along`: rows[f] are the lane's rows of the tile's edge.
+template <class T, int B, int NW, bool kDirect>
+struct Along {
+    static constexpr int kFetch = B / 8 / NW;
+    static_assert(B % (8 * NW) == 0, "the wavefronts fetch as much each");
+    const T *row[kFetch];       // kDirect: at the lane's piece
+    i32x4 held[kDirect ? 1 : kFetch];
+    int length;                 // of the sum's axis
+
+    static __device__ __forceinline__ int swizzle(int r) { return (r >> 1) & 7; }
+    static __device__ __forceinline__ int edge(int wave, int f) { return (wave * kFetch + f) * 8 + (lane_id() >> 3); }
+    static __device__ __forceinline__ int column(int wave, int f) { return ((lane_id() & 7) ^ swizzle(edge(wave, f))) * kPiece<T>; }
+
+    // A row that is not there may be any row: what comes of it is not stored.
+    __device__ __forceinline__ void set(int wave, int f, const T *p) { row[f] = kDirect ? p + column(wave, f) : p; }
+
+    __device__ __forceinline__ void fetch(int wave, int step, int8_t *buf) {
+        const int k = step * kStep<T>;
+        const bool whole = k + kStep<T> <= length;
+#pragma unroll
+        for (int f = 0; f < kFetch; f++) {
+            if constexpr (kDirect) {
+                const T *p = row[f] + k;
+                if (!whole && k + column(wave, f) >= length) p = reinterpret_cast<const T *>(&kZeros);
+                to_lds(p, buf + (wave * kFetch + f) * 1024);
+            } else {
+                held[f] = load_piece(row[f], k + column(wave, f), length);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(int wave, int8_t *buf) {
+        if constexpr (!kDirect)
+#pragma unroll
+            for (int f = 0; f < kFetch; f++) *reinterpret_cast<i32x4 *>(buf + (wave * kFetch + f) * 1024 + lane_id() * 16) = held[f];
+    }
+    // The lane's pieces of `N` tiles of 16 rows from `first` on, of half h of a step.
+    template <int N>
+    static __device__ __forceinline__ void read(const int8_t *buf, int first, int h, i32x4 (&v)[N]) {
+        const int r = first + (lane_id() & 15);
+        const int8_t *p = buf + r * kStepBytes + (((4 * h + (lane_id() >> 4)) ^ swizzle(r)) * 16);
+#pragma unroll
+        for (int i = 0; i < N; i++) v[i] = *reinterpret_cast<const i32x4 *>(p + i * 16 * kStepBytes);
+    }
+};
+
+// What both kinds of `across` share: where a lane's bytes go and come from.
+template <class T, int B, int NW>
+struct AcrossLayout {
+    static constexpr int kPieces = B * static_cast<int>(sizeof(T)) / 16;      // of a row of LDS
+    static constexpr int kRows = kWave / kPieces;                             // of a fetch
+    static constexpr int kFetch = kStep<T> / kRows / NW;
+    static_assert(kPieces <= kWave && kStep<T> % (kRows * NW) == 0, "the wavefronts fetch as much each");
+
+    static __device__ __forceinline__ int swizzle(int k) {
+        if constexpr (sizeof(T) == 4) return k & 12;
+        return ((k & 3) << 1) | (kPieces >= 16 ? k & 8 : 0);
+    }
+    // The lane's place of the sum's axis in a step, and its columns of the edge.
+    static __device__ __forceinline__ int place(int wave, int f) { return (wave * kFetch + f) * kRows + lane_id() / kPieces; }
+    static __device__ __forceinline__ int column(int wave, int f) {
+        return ((lane_id() % kPieces) ^ swizzle(place(wave, f))) * kPiece<T>;
+    }
+
+    template <int N>
+    static __device__ __forceinline__ void read(const int8_t *buf, int first, int h, i32x4 (&v)[N]) {
+        const int i16 = lane_id() & 15, g = lane_id() >> 4;
+        if constexpr (sizeof(T) == 2) {
+            using words_t = __attribute__((address_space(3))) i16x4;
+            const int k = 8 * g + (i16 >> 2);           // + 32 h + 4 q, which the swizzle does not see
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const int c = first + 16 * i + 4 * (i16 & 3);
+                const int8_t *p = buf + (32 * h + k) * (kPieces * 16) + (((c >> 3) ^ swizzle(k)) * 16) + (c & 4) * 2;
+                const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((words_t *)(p));
+                const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((words_t *)(p + 4 * kPieces * 16));
+                v[i] = __builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        } else if constexpr (kQuads<T, true, N>) {
+            // v[4 t + i]: place i of the lane's four, a column of each of tiles 4 t to 4 t + 3
+#pragma unroll
+            for (int t = 0; t < N / 4; t++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    v[4 * t + i] = *reinterpret_cast<const i32x4 *>(buf + (16 * h + 4 * g + i) * (kPieces * 16) +
+                                                                    (((first / 4 + 16 * t + i16) ^ (4 * g)) * 16));
+        } else {
+#pragma unroll
+            for (int t = 0; t < N; t++) {
+                const int c = first + 16 * t + i16;
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    v[t][i] = *reinterpret_cast<const int *>(buf + (16 * h + 4 * g + i) * (kPieces * 16) +
+                                                             (((c >> 2) ^ (4 * g)) * 16) + (c & 3) * 4);
+            }
+        }
+    }
+};
+
+// `across` with rows of memory one after another: a type's weights.
+template <class T, int B, int NW, bool kDirect>
+struct Across : AcrossLayout<T, B, NW> {
+    using L = AcrossLayout<T, B, NW>;
+    using L::kFetch;
+    const T *row[kFetch];       // kDirect: at the lane's piece
+    i32x4 held[kDirect ? 1 : kFetch];
+    int64_t stride;
+    int length, first, edge;    // of the sum's axis; the tile's first column; columns in all
+
+    __device__ __forceinline__ void set(int wave, const T *base, int64_t stride_, int length_, int first_, int edge_) {
+        stride = stride_;
+        length = length_;
+        first = first_;
+        edge = edge_;
+#pragma unroll
+        for (int f = 0; f < kFetch; f++) {
+            const int c = first + L::column(wave, f);
+            row[f] = base + L::place(wave, f) * stride + (kDirect ? (c < edge ? c : 0) : 0);
+        }
+    }
+    __device__ __forceinline__ void fetch(int wave, int step, int8_t *buf) {
+        const int k = step * kStep<T>;
+        const bool whole = k + kStep<T> <= length;
+#pragma unroll
+        for (int f = 0; f < kFetch; f++) {
+            const T *p = row[f] + k * stride;
+            const bool there = whole || k + L::place(wave, f) < length;
+            if constexpr (kDirect) to_lds(there ? p : reinterpret_cast<const T *>(&kZeros), buf + (wave * kFetch + f) * 1024);
+            else held[f] = load_piece(there ? p : nullptr, first + L::column(wave, f), edge);
+        }
+    }
+    __device__ __forceinline__ void store(int wave, int8_t *buf) {
+        if constexpr (!kDirect)
+#pragma unroll
+            for (int f = 0; f < kFetch; f++) *reinterpret_cast<i32x4 *>(buf + (wave * kFetch + f) * 1024 + lane_id() * 16) = held[f];
+    }
+};
+
+// `across` with rows of memory that places of order name.
+template <class T, int B, int NW, bool kDirect>
+struct Gathered : AcrossLayout<T, B, NW> {
+    using L = AcrossLayout<T, B, NW>;
+    using L::kFetch;
+    static constexpr int kOwn = kStep<T> / NW;          // rows of a wavefront in a step
+    i32x4 held[kDirect ? 1 : kFetch];
+    const T *base;
+    int64_t stride;
+    int first, edge;
+
+    __device__ __forceinline__ void set(const T *base_, int64_t stride_, int first_, int edge_) {
+        base = base_;
+        stride = stride_;
+        first = first_;
+        edge = edge_;
+    }
+    // ids: lane l has the row of the wavefront's place l % kOwn, or -1.
+    __device__ __forceinline__ void fetch(int wave, int32_t ids, int8_t *buf) {
+#pragma unroll
+        for (int f = 0; f < kFetch; f++) {
+            const int32_t id = __shfl(ids, f * L::kRows + lane_id() / L::kPieces, kWave);
+            const int c = first + L::column(wave, f);
+            if constexpr (kDirect)
+                to_lds(id < 0 ? reinterpret_cast<const T *>(&kZeros) : base + id * stride + (c < edge ? c : 0),
+                       buf + (wave * kFetch + f) * 1024);
+            else
+                held[f] = load_piece(id < 0 ? nullptr : base + id * stride, c, edge);
+        }
+    }
+    __device__ __forceinline__ void store(int wave, int8_t *buf) {
+        if constexpr (!kDirect)
+#pragma unroll
+            for (int f = 0; f < kFetch; f++) *reinterpret_cast<i32x4 *>(buf + (wave * kFetch + f) * 1024 + lane_id() * 16) = held[f];
+    }
+};
+
+// ---- products of what was read ----
+//
+// x are M tiles of output rows, w are N tiles of output columns.
+
+// float32: what a lane has of tile t at place k of its four.
+template <class T, bool kAcross, int N>
+__device__ __forceinline__ float element(const i32x4 (&v)[N], int t, int k) {
+    if constexpr (kQuads<T, kAcross, N>) return __builtin_bit_cast(f32x4, v[t / 4 * 4 + k])[t % 4];
+    else return __builtin_bit_cast(f32x4, v[t])[k];
+}
+
+template <class T, bool kAcrossX, bool kAcrossW, int M, int N>
+__device__ __forceinline__ void multiply(const i32x4 (&x)[M], const i32x4 (&w)[N], f32x4 (&acc)[M][N]) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < M; i++)
+#pragma unroll
+            for (int j = 0; j < N; j++)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[j]), __builtin_bit_cast(bf16x8, x[i]),
+                                                                    acc[i][j], 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+#pragma unroll
+            for (int i = 0; i < M; i++)
+#pragma unroll
+                for (int j = 0; j < N; j++)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(element<T, kAcrossW>(w, j, k), element<T, kAcrossX>(x, i, k),
+                                                                     acc[i][j], 0, 0, 0);
+    }
+}
+
+// The output row, within a wavefront's rows, of a lane's tile i.
+template <class T, bool kAcross, int M>
+__device__ __forceinline__ int tile_row(int i) {
+    const int i16 = lane_id() & 15;
+    return kQuads<T, kAcross, M> ? 64 * (i / 4) + 4 * i16 + i % 4 : 16 * i + i16;
+}
+
+// f(column, four values): a lane's outputs of tile row i, four consecutive columns at a time.
+template <class T, bool kAcross, int N, class F>
+__device__ __forceinline__ void tile_columns(const f32x4 (&acc)[N], const F &f) {
+    const int g = lane_id() >> 4;
+    if constexpr (kQuads<T, kAcross, N>) {
+#pragma unroll
+        for (int t = 0; t < N / 4; t++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const float v[4] = {acc[4 * t][e], acc[4 * t + 1][e], acc[4 * t + 2][e], acc[4 * t + 3][e]};
+                f(64 * t + 16 * g + 4 * e, v);
+            }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; j++) {
+            const float v[4] = {acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
+            f(16 * j + 4 * g, v);
+        }
+    }
+}
+
+// All loads, and all reads of LDS, of this wavefront are done, then of the others.
+// __syncthreads by itself would do; nothing may be moved across it.
+__device__ __forceinline__ void meet() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);         // vmcnt(0), lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// The steps of a tile.  fetch(step, buffer) brings a step's sides, store(buffer)
+// puts them where they went through registers, read(buffer, h, x, w) takes half a step,
+// used(x, w) is shown every half once.  Buffers are filled a step ahead, and the
+// first half of a step is read while the second half of the one before is multiplied.
+template <class T, bool kAcrossX, bool kAcrossW, int M, int N, class Fetch, class Store, class Read, class Used>
+__device__ __forceinline__ void multiply_steps(int steps, int8_t *buf0, int8_t *buf1, f32x4 (&acc)[M][N], const Fetch &fetch,
+                                               const Store &store, const Read &read, const Used &used) {
+    i32x4 x0[M], w0[N], x1[M], w1[N];
+    fetch(0, buf0);
+    store(buf0);
+    meet();
+    if (steps > 1) fetch(1, buf1);
+    read(buf0, 0, x0, w0);
+    auto one = [&](int step, int8_t *buf, int8_t *other) {
+        read(buf, 1, x1, w1);
+        used(x0, w0);
+        multiply<T, kAcrossX, kAcrossW>(x0, w0, acc);
+        if (step + 1 < steps) store(other);
+        meet();
+        if (step + 2 < steps) fetch(step + 2, buf);
+        if (step + 1 < steps) read(other, 0, x0, w0);
+        used(x1, w1);
+        multiply<T, kAcrossX, kAcrossW>(x1, w1, acc);
+    };
+    for (int step = 0; step < steps; step += 2) {
+        one(step, buf0, buf1);
+        if (step + 1 < steps) one(step + 1, buf1, buf0);
+    }
+}
+
+}  // namespace tgl
