@@ -103,16 +103,14 @@ __global__ __launch_bounds__(NW * kWave, 2) void rows_kernel(const RowsArgs a) {
                 x.store(wave, buf);
                 w.store(wave, buf + BM * kStepBytes);
             },
-            [&](const int8_t *buf, int h, i32x4(&xv)[MT], i32x4(&wv)[NT]) {
-                W::read(buf + BM * kStepBytes, wn * 64, h, wv);
-                X::read(buf, wm * MT * 16, h, xv);
-            },
-            [](const i32x4(&)[MT], const i32x4(&)[NT]) {});
+            [&](const int8_t *buf, int h, int first, auto &v) { X::read(buf, 0, (wm * MT + first) * 16, h, v); },
+            [&](const int8_t *buf, int h, i32x4(&v)[NT]) { W::read(buf, BM * kStepBytes, wn * 64, h, v); },
+            [](const auto &, int) {});
     }
     const float *bias = a.bias && s.type < a.g.num_types ? a.bias + static_cast<int64_t>(s.type) * a.n : nullptr;
-    int64_t row[MT];
+    int32_t row[MT];
 #pragma unroll
-    for (int i = 0; i < MT; i++) row[i] = row_at(a.g, s.begin + wm * MT * 16 + tile_row<T, false, MT>(i), s.end);
+    for (int i = 0; i < MT; i++) row[i] = static_cast<int32_t>(row_at(a.g, s.begin + wm * MT * 16 + tile_row<T, false, MT>(i), s.end));
 #pragma unroll
     for (int i = 0; i < MT; i++) {
         if (row[i] < 0) continue;
@@ -161,39 +159,41 @@ __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
         X x;
         d.set(static_cast<const T *>(a.dy), a.dys, o0, a.out);
         x.set(static_cast<const T *>(a.x), a.xs, c0, a.in);
-        auto rows_of = [&](int step) {
-            return static_cast<int32_t>(row_at(a.g, s.begin + static_cast<int64_t>(step) * kStep<T> + wave * D::kOwn + lane % D::kOwn, s.end));
-        };
-        int32_t ids = rows_of(0);
+        // The lane's row of a step, from order a step earlier: looked at only when it is used, since that waits for every
+        // load before it.
+        const int32_t mine = wave * D::kOwn + lane % D::kOwn, places = static_cast<int32_t>(s.end - s.begin);
+        auto place_of = [&](int step) { return step * kStep<T> + mine < places ? step * kStep<T> + mine : places - 1; };
+        int32_t ids = a.g.order ? a.g.order[s.begin + place_of(0)] : 0;
         multiply_steps<T, true, true>(
             steps, buf0, buf1, acc,
             [&](int step, int8_t *buf) {
-                d.fetch(wave, ids, buf);
-                x.fetch(wave, ids, buf + BM * kStepBytes);
-                ids = rows_of(step + 1);
+                int32_t id = a.g.order ? ids : static_cast<int32_t>(s.begin) + place_of(step);
+                if (step * kStep<T> + mine >= places || id >= a.g.n) id = -1;
+                d.fetch(wave, id, buf);
+                x.fetch(wave, id, buf + BM * kStepBytes);
+                if (a.g.order) ids = a.g.order[s.begin + place_of(step + 1)];
             },
             [&](int8_t *buf) {
                 d.store(wave, buf);
                 x.store(wave, buf + BM * kStepBytes);
             },
-            [&](const int8_t *buf, int h, i32x4(&dv)[MT], i32x4(&xv)[NT]) {
-                X::read(buf + BM * kStepBytes, wn * 64, h, xv);
-                D::read(buf, wm * MT * 16, h, dv);
-            },
-            [&](const i32x4(&dv)[MT], const i32x4(&)[NT]) {
+            [&](const int8_t *buf, int h, int first, auto &v) { D::read(buf, 0, (wm * MT + first) * 16, h, v); },
+            [&](const int8_t *buf, int h, i32x4(&v)[NT]) { X::read(buf, BM * kStepBytes, wn * 64, h, v); },
+            [&](const auto &dv, int first) {
                 if (!want_sum) return;
 #pragma unroll
-                for (int i = 0; i < MT; i++) {
-                    if (i % kWaveN != wn) continue;
+                for (int i = 0; i < kGroup<MT>; i++) {
+                    if (i % kWaveN != wn) continue;             // first is a multiple of 4, or 0
+                    float &v = sum[(first + i) / kWaveN];
                     if constexpr (sizeof(T) == 2) {
 #pragma unroll
                         for (int e = 0; e < 4; e++) {
-                            sum[i / kWaveN] += __builtin_bit_cast(float, dv[i][e] << 16);
-                            sum[i / kWaveN] += __builtin_bit_cast(float, dv[i][e] & static_cast<int>(0xffff0000u));
+                            v += __builtin_bit_cast(float, dv[i][e] << 16);
+                            v += __builtin_bit_cast(float, dv[i][e] & static_cast<int>(0xffff0000u));
                         }
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 4; e++) sum[i / kWaveN] += element<T, true>(dv, i, e);
+                        for (int e = 0; e < 4; e++) v += element<T, true>(dv, i, e);
                     }
                 }
             });
@@ -317,7 +317,7 @@ tgl_status rows_call(const tgl_row_groups *groups, const void *x, int64_t x_stri
     (void)hipGetLastError();
     const RowsArgs a{groups_of(groups), x, w->ptr, bias, y, x_stride, w->row_stride, w->type_stride, y_stride, k, n, 0};
     const bool direct = wide_rows(x, x_stride, e) && wide_rows(w->ptr, w->row_stride, e) && w->type_stride * e % 16 == 0 &&
-                        k * e % 16 == 0 && (!kAcross || n * e % 16 == 0);
+                        k * e % 16 == 0 && (!kAcross || (n * e % 16 == 0 && w->row_stride < (1 << 26)));
     return dtype == TGL_OUT_F32 ? launch_rows<float, kAcross>(a, direct, st) : launch_rows<bf16_t, kAcross>(a, direct, st);
 }
 

@@ -39,6 +39,14 @@ __device__ __forceinline__ void to_lds(const T *from, int8_t *to) {
 template <class T, bool kAcross, int N>
 constexpr bool kQuads = sizeof(T) == 4 && kAcross && N % 4 == 0;
 
+// A place in a buffer, as a number that the compiler does not see through: a read is
+// then an access of that buffer and no other, and does not wait for loads that
+// are on their way to the other one.
+__device__ __forceinline__ int opaque(int at) {
+    asm("" : "+v"(at));
+    return at;
+}
+
 // ---- sides ----
 //
 // Each wavefront brings kFetch times 1024 bytes of a side.  kDirect: row starts
@@ -83,11 +91,11 @@ struct Along {
     }
     // The lane's pieces of `N` tiles of 16 rows from `first` on, of half h of a step.
     template <int N>
-    static __device__ __forceinline__ void read(const int8_t *buf, int first, int h, i32x4 (&v)[N]) {
+    static __device__ __forceinline__ void read(const int8_t *buf, int side, int first, int h, i32x4 (&v)[N]) {
         const int r = first + (lane_id() & 15);
-        const int8_t *p = buf + r * kStepBytes + (((4 * h + (lane_id() >> 4)) ^ swizzle(r)) * 16);
+        const int at = opaque(side + r * kStepBytes + (((4 * h + (lane_id() >> 4)) ^ swizzle(r)) * 16));
 #pragma unroll
-        for (int i = 0; i < N; i++) v[i] = *reinterpret_cast<const i32x4 *>(p + i * 16 * kStepBytes);
+        for (int i = 0; i < N; i++) v[i] = *reinterpret_cast<const i32x4 *>(buf + (at + i * 16 * kStepBytes));
     }
 };
 
@@ -110,7 +118,7 @@ struct AcrossLayout {
     }
 
     template <int N>
-    static __device__ __forceinline__ void read(const int8_t *buf, int first, int h, i32x4 (&v)[N]) {
+    static __device__ __forceinline__ void read(const int8_t *buf, int side, int first, int h, i32x4 (&v)[N]) {
         const int i16 = lane_id() & 15, g = lane_id() >> 4;
         if constexpr (sizeof(T) == 2) {
             using words_t = __attribute__((address_space(3))) i16x4;
@@ -118,27 +126,26 @@ struct AcrossLayout {
 #pragma unroll
             for (int i = 0; i < N; i++) {
                 const int c = first + 16 * i + 4 * (i16 & 3);
-                const int8_t *p = buf + (32 * h + k) * (kPieces * 16) + (((c >> 3) ^ swizzle(k)) * 16) + (c & 4) * 2;
-                const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((words_t *)(p));
-                const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((words_t *)(p + 4 * kPieces * 16));
+                const int at = opaque(side + (32 * h + k) * (kPieces * 16) + (((c >> 3) ^ swizzle(k)) * 16) + (c & 4) * 2);
+                const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((words_t *)(buf + at));
+                const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((words_t *)(buf + (at + 4 * kPieces * 16)));
                 v[i] = __builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
             }
         } else if constexpr (kQuads<T, true, N>) {
             // v[4 t + i]: place i of the lane's four, a column of each of tiles 4 t to 4 t + 3
 #pragma unroll
-            for (int t = 0; t < N / 4; t++)
+            for (int t = 0; t < N / 4; t++) {
+                const int at = opaque(side + (16 * h + 4 * g) * (kPieces * 16) + (((first / 4 + 16 * t + i16) ^ (4 * g)) * 16));
 #pragma unroll
-                for (int i = 0; i < 4; i++)
-                    v[4 * t + i] = *reinterpret_cast<const i32x4 *>(buf + (16 * h + 4 * g + i) * (kPieces * 16) +
-                                                                    (((first / 4 + 16 * t + i16) ^ (4 * g)) * 16));
+                for (int i = 0; i < 4; i++) v[4 * t + i] = *reinterpret_cast<const i32x4 *>(buf + (at + i * kPieces * 16));
+            }
         } else {
 #pragma unroll
             for (int t = 0; t < N; t++) {
                 const int c = first + 16 * t + i16;
+                const int at = opaque(side + (16 * h + 4 * g) * (kPieces * 16) + (((c >> 2) ^ (4 * g)) * 16) + (c & 3) * 4);
 #pragma unroll
-                for (int i = 0; i < 4; i++)
-                    v[t][i] = *reinterpret_cast<const int *>(buf + (16 * h + 4 * g + i) * (kPieces * 16) +
-                                                             (((c >> 2) ^ (4 * g)) * 16) + (c & 3) * 4);
+                for (int i = 0; i < 4; i++) v[t][i] = *reinterpret_cast<const int *>(buf + (at + i * kPieces * 16));
             }
         }
     }
@@ -149,31 +156,34 @@ template <class T, int B, int NW, bool kDirect>
 struct Across : AcrossLayout<T, B, NW> {
     using L = AcrossLayout<T, B, NW>;
     using L::kFetch;
-    const T *row[kFetch];       // kDirect: at the lane's piece
     i32x4 held[kDirect ? 1 : kFetch];
+    const T *base;
     int64_t stride;
     int length, first, edge;    // of the sum's axis; the tile's first column; columns in all
 
-    __device__ __forceinline__ void set(int wave, const T *base, int64_t stride_, int length_, int first_, int edge_) {
+    __device__ __forceinline__ void set(int wave, const T *base_, int64_t stride_, int length_, int first_, int edge_) {
+        base = base_ + wave * (kFetch * L::kRows) * stride_;
         stride = stride_;
         length = length_;
         first = first_;
         edge = edge_;
-#pragma unroll
-        for (int f = 0; f < kFetch; f++) {
-            const int c = first + L::column(wave, f);
-            row[f] = base + L::place(wave, f) * stride + (kDirect ? (c < edge ? c : 0) : 0);
-        }
     }
     __device__ __forceinline__ void fetch(int wave, int step, int8_t *buf) {
         const int k = step * kStep<T>;
         const bool whole = k + kStep<T> <= length;
 #pragma unroll
         for (int f = 0; f < kFetch; f++) {
-            const T *p = row[f] + k * stride;
-            const bool there = whole || k + L::place(wave, f) < length;
-            if constexpr (kDirect) to_lds(there ? p : reinterpret_cast<const T *>(&kZeros), buf + (wave * kFetch + f) * 1024);
-            else held[f] = load_piece(there ? p : nullptr, first + L::column(wave, f), edge);
+            const int c = first + L::column(wave, f);
+            if constexpr (kDirect) {
+                // a wavefront's rows begin at one place; the lane's is not far from there
+                const T *p = base + (k + f * L::kRows) * stride;
+                const uint32_t at = lane_id() / L::kPieces * static_cast<uint32_t>(stride) + (c < edge ? c : 0);
+                if (whole || k + L::place(wave, f) < length) to_lds(p + at, buf + (wave * kFetch + f) * 1024);
+                else to_lds(reinterpret_cast<const T *>(&kZeros), buf + (wave * kFetch + f) * 1024);
+            } else {
+                const bool there = whole || k + L::place(wave, f) < length;
+                held[f] = load_piece(there ? base + (k + f * L::kRows + lane_id() / L::kPieces) * stride : nullptr, c, edge);
+            }
         }
     }
     __device__ __forceinline__ void store(int wave, int8_t *buf) {
@@ -222,8 +232,6 @@ struct Gathered : AcrossLayout<T, B, NW> {
 
 // ---- products of what was read ----
 //
-// x are M tiles of output rows, w are N tiles of output columns.
-
 // float32: what a lane has of tile t at place k of its four.
 template <class T, bool kAcross, int N>
 __device__ __forceinline__ float element(const i32x4 (&v)[N], int t, int k) {
@@ -231,15 +239,16 @@ __device__ __forceinline__ float element(const i32x4 (&v)[N], int t, int k) {
     else return __builtin_bit_cast(f32x4, v[t])[k];
 }
 
-template <class T, bool kAcrossX, bool kAcrossW, int M, int N>
-__device__ __forceinline__ void multiply(const i32x4 (&x)[M], const i32x4 (&w)[N], f32x4 (&acc)[M][N]) {
+// acc[first + i][j] += x[i] w[j]: x are tiles of output rows, w of output columns.
+template <class T, bool kAcrossX, bool kAcrossW, int M, int N, int A>
+__device__ __forceinline__ void multiply(const i32x4 (&x)[M], const i32x4 (&w)[N], int first, f32x4 (&acc)[A][N]) {
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int i = 0; i < M; i++)
 #pragma unroll
             for (int j = 0; j < N; j++)
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[j]), __builtin_bit_cast(bf16x8, x[i]),
-                                                                    acc[i][j], 0, 0, 0);
+                acc[first + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[j]), __builtin_bit_cast(bf16x8, x[i]),
+                                                                            acc[first + i][j], 0, 0, 0);
     } else {
 #pragma unroll
         for (int k = 0; k < 4; k++)
@@ -247,8 +256,8 @@ __device__ __forceinline__ void multiply(const i32x4 (&x)[M], const i32x4 (&w)[N
             for (int i = 0; i < M; i++)
 #pragma unroll
                 for (int j = 0; j < N; j++)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(element<T, kAcrossW>(w, j, k), element<T, kAcrossX>(x, i, k),
-                                                                     acc[i][j], 0, 0, 0);
+                    acc[first + i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(element<T, kAcrossW>(w, j, k), element<T, kAcrossX>(x, i, k),
+                                                                             acc[first + i][j], 0, 0, 0);
     }
 }
 
@@ -284,34 +293,51 @@ __device__ __forceinline__ void tile_columns(const f32x4 (&acc)[N], const F &f) 
 // __syncthreads by itself would do; nothing may be moved across it.
 __device__ __forceinline__ void meet() {
     asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0x0070);         // vmcnt(0), lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
     asm volatile("" ::: "memory");
 }
 
+// Tiles of output rows that are read together.
+template <int M>
+constexpr int kGroup = M < 4 ? M : 4;
+
 // The steps of a tile.  fetch(step, buffer) brings a step's sides, store(buffer)
-// puts them where they went through registers, read(buffer, h, x, w) takes half a step,
-// used(x, w) is shown every half once.  Buffers are filled a step ahead, and the
-// first half of a step is read while the second half of the one before is multiplied.
-template <class T, bool kAcrossX, bool kAcrossW, int M, int N, class Fetch, class Store, class Read, class Used>
+// puts them where they went through registers, read_x(buffer, h, first, x) and
+// read_w(buffer, h, w) take half a step's tiles, used(x, first) is shown every x once.
+// Buffers are filled a step ahead.  What is multiplied next is read while the
+// tiles before it are multiplied, over the step's end too.
+template <class T, bool kAcrossX, bool kAcrossW, int M, int N, class Fetch, class Store, class ReadX, class ReadW, class Used>
 __device__ __forceinline__ void multiply_steps(int steps, int8_t *buf0, int8_t *buf1, f32x4 (&acc)[M][N], const Fetch &fetch,
-                                               const Store &store, const Read &read, const Used &used) {
-    i32x4 x0[M], w0[N], x1[M], w1[N];
+                                               const Store &store, const ReadX &read_x, const ReadW &read_w, const Used &used) {
+    constexpr int K = kGroup<M>, kGroups = M / K, kUnits = 2 * kGroups;
+    i32x4 x[2][K], w[2][N];
     fetch(0, buf0);
     store(buf0);
     meet();
     if (steps > 1) fetch(1, buf1);
-    read(buf0, 0, x0, w0);
+    read_x(buf0, 0, 0, x[0]);
+    read_w(buf0, 0, w[0]);
     auto one = [&](int step, int8_t *buf, int8_t *other) {
-        read(buf, 1, x1, w1);
-        used(x0, w0);
-        multiply<T, kAcrossX, kAcrossW>(x0, w0, acc);
-        if (step + 1 < steps) store(other);
-        meet();
-        if (step + 2 < steps) fetch(step + 2, buf);
-        if (step + 1 < steps) read(other, 0, x0, w0);
-        used(x1, w1);
-        multiply<T, kAcrossX, kAcrossW>(x1, w1, acc);
+        unrolled<kUnits>([&](auto U) {
+            constexpr int u = decltype(U)::value, h = u / kGroups, next = u + 1;
+            if constexpr (next < kUnits) {
+                read_x(buf, next / kGroups, next % kGroups * K, x[next & 1]);
+                if constexpr (next == kGroups) read_w(buf, 1, w[1]);
+            } else {
+                if (step + 1 < steps) store(other);
+                meet();
+                if (step + 2 < steps) fetch(step + 2, buf);
+                if (step + 1 < steps) {
+                    read_x(other, 0, 0, x[0]);
+                    read_w(other, 0, w[0]);
+                }
+            }
+            used(x[u & 1], u % kGroups * K);
+            multiply<T, kAcrossX, kAcrossW>(x[u & 1], w[h], u % kGroups * K, acc);
+        });
     };
     for (int step = 0; step < steps; step += 2) {
         one(step, buf0, buf1);
