@@ -11,12 +11,12 @@
 // numbers leave that type's range, and a mean that is large beside the
 // distances would lose their bits in 32.  The card does 64-bit sums and
 // products at the rate of float32's, and memory bounds these kernels.
-#include "tgl_int8.hpp"
+#include <type_traits>
+
+#include "tgl_typed.hpp"
 
 namespace tgl {
 namespace {
-
-constexpr int kRun = 8;             // elements of a lane's access
 
 struct NormArgs {
     const void *x;
@@ -45,14 +45,40 @@ struct GradArgs {
     int32_t dim;
 };
 
+// What the lane whose number differs in bit D has (for D = 4 and 8: one of the
+// other half's, which all have the same by then).  In registers: exchanges through LDS
+// would be most of a row's time.
+template <int D>
+__device__ __forceinline__ double exchanged(double v) {
+    const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+    uint32_t half[2] = {static_cast<uint32_t>(bits), static_cast<uint32_t>(bits >> 32)};
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        if constexpr (D < 16) {
+            constexpr int kControl = D == 1 ? 0xb1 : D == 2 ? 0x4e : D == 4 ? 0x141 : 0x140;   // quads, half rows, rows of 16
+            half[i] = __builtin_amdgcn_update_dpp(0, half[i], kControl, 0xf, 0xf, true);
+        } else {
+            const auto both = D == 16 ? __builtin_amdgcn_permlane16_swap(half[i], half[i], false, false)
+                                      : __builtin_amdgcn_permlane32_swap(half[i], half[i], false, false);
+            half[i] = lane_id() & D ? both[0] : both[1];
+        }
+    }
+    return __builtin_bit_cast(double, static_cast<uint64_t>(half[1]) << 32 | half[0]);
+}
+
 // Sum over the L lanes of a row, in all of them.  `lds` has one number per wavefront of
 // the workgroup and is free again after the next barrier.
 template <int L, int N>
 __device__ __forceinline__ void row_sum(double (&v)[N], double (*lds)[N]) {
 #pragma unroll
-    for (int d = (L < kWave ? L : kWave) / 2; d >= 1; d >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; i++) v[i] += __shfl_xor(v[i], d, kWave);
+    for (int i = 0; i < N; i++) {
+        v[i] += exchanged<1>(v[i]);
+        v[i] += exchanged<2>(v[i]);
+        v[i] += exchanged<4>(v[i]);
+        if constexpr (L >= 16) v[i] += exchanged<8>(v[i]);
+        if constexpr (L >= 32) v[i] += exchanged<16>(v[i]);
+        if constexpr (L >= 64) v[i] += exchanged<32>(v[i]);
+    }
     if constexpr (L > kWave) {
         constexpr int kWaves = L / kWave;
         const int wave = threadIdx.x / kWave, first = wave / kWaves * kWaves;
@@ -68,168 +94,251 @@ __device__ __forceinline__ void row_sum(double (&v)[N], double (*lds)[N]) {
     }
 }
 
-// A lane's columns of the weights (or what stands for none).
-template <int L, int H>
-__device__ __forceinline__ void load_weights(const float *w, int i, int runs, int dim, float without, float (&v)[H][kRun]) {
-#pragma unroll
-    for (int h = 0; h < H; h++) {
-#pragma unroll
-        for (int k = 0; k < kRun; k++) v[h][k] = without;
-        if (w && i + h * L < runs) load_columns<float, kRun>(w, (i + h * L) * kRun, dim, v[h]);
-    }
+constexpr int E = 4;                // elements of a run, a lane's access
+
+// A run as whole words, which are taken apart where its elements are used: so nothing waits for a load before that.
+template <class T>
+using run_t = std::conditional_t<sizeof(T) == 2, i32x2, i32x4>;
+
+template <class T>
+__device__ __forceinline__ float run_at(const run_t<T> &v, int k) {
+    if constexpr (sizeof(T) == 2) return __builtin_bit_cast(float, k & 1 ? v[k / 2] & static_cast<int>(0xffff0000u) : v[k / 2] << 16);
+    else return __builtin_bit_cast(f32x4, v)[k];
 }
+
+// Run h of lane i of a row's L begins at column (i + h L) E.  Zeros beyond the row.
+template <class T, int L>
+__device__ __forceinline__ run_t<T> load_run(const void *p, int64_t at, int i, int h, int dim) {
+    using word_t = run_t<T> __attribute__((aligned(alignof(T))));
+    const T *row = static_cast<const T *>(p) + at;
+    const int c = (i + h * L) * E;
+    if (c + E <= dim) return *reinterpret_cast<const word_t *>(row + c);
+    Run<T, E> v = {};
+#pragma unroll
+    for (int k = 0; k < E; k++)
+        if (c + k < dim) v.t[k] = row[c + k];
+    return __builtin_bit_cast(run_t<T>, v);
+}
+
+// A row in the registers of L lanes.
+template <class T, int L, int H>
+struct Held {
+    run_t<T> v[H];
+    __device__ __forceinline__ void load(const void *p, int64_t at, int i, int dim) {
+#pragma unroll
+        for (int h = 0; h < H; h++) v[h] = load_run<T, L>(p, at, i, h, dim);
+    }
+    __device__ __forceinline__ float at(int h, int k) const { return run_at<T>(v[h], k); }
+};
 
 template <class T, int L, int H>
-__device__ __forceinline__ void load_row(const void *p, int64_t at, int i, int runs, int dim, float (&v)[H][kRun]) {
+__device__ __forceinline__ void store_row(void *p, int64_t at, int i, int dim, const float (&v)[H][E]) {
+#pragma unroll
+    for (int h = 0; h < H; h++)
+        if ((i + h * L) * E < dim) store_columns<T, E>(static_cast<T *>(p) + at, (i + h * L) * E, dim, v[h]);
+}
+
+// A lane's columns of the weights, or what stands for none.
+template <class T, int L, int H>
+__device__ __forceinline__ void load_weights(const float *w, int i, int dim, float without, float (&v)[H][E]) {
 #pragma unroll
     for (int h = 0; h < H; h++) {
 #pragma unroll
-        for (int k = 0; k < kRun; k++) v[h][k] = 0.0f;
-        if (i + h * L < runs) load_columns<T, kRun>(static_cast<const T *>(p) + at, (i + h * L) * kRun, dim, v[h]);
+        for (int k = 0; k < E; k++) v[h][k] = without;
+        if (w && (i + h * L) * E < dim) load_columns<float, E>(w, (i + h * L) * E, dim, v[h]);
     }
 }
 
-template <class T, int L, int H, int kThreads>
+// Bound by memory, as long as enough of it is on its way: the next row is loaded
+// before this one is worked on, where registers have room (kAhead).
+template <class T, int L, int H, int kThreads, bool kAhead>
 __global__ __launch_bounds__(kThreads) void norm_kernel(const NormArgs a) {
     __shared__ double lds[2][kThreads / kWave][1];
-    const int i = threadIdx.x % L;
-    const int runs = (a.dim + kRun - 1) / kRun;
-    float w[H][kRun], b[H][kRun];
-    load_weights<L, H>(a.w, i, runs, a.dim, 1.0f, w);
-    load_weights<L, H>(a.b, i, runs, a.dim, 0.0f, b);
     constexpr int kRows = kThreads / L;
-    for (int64_t at = static_cast<int64_t>(blockIdx.x) * kRows; at < a.n; at += static_cast<int64_t>(gridDim.x) * kRows) {
-        const bool there = at + threadIdx.x / L < a.n;
-        const int64_t row = there ? at + threadIdx.x / L : a.n - 1;
-        float v[H][kRun];
-        load_row<T, L, H>(a.x, row * a.xs, i, runs, a.dim, v);
-        if (a.r) {
-            float r[H][kRun];
-            load_row<T, L, H>(a.r, row * a.rs, i, runs, a.dim, r);
+    const int i = threadIdx.x % L, sub = threadIdx.x / L;
+    float w[H][E], b[H][E];
+    load_weights<T, L, H>(a.w, i, a.dim, 1.0f, w);
+    load_weights<T, L, H>(a.b, i, a.dim, 0.0f, b);
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * kRows;
+    auto row_of = [&](int64_t at) { return at + sub < a.n ? at + sub : a.n - 1; };
+    Held<T, L, H> x, r, next_x, next_r;
+    auto load = [&](int64_t at, Held<T, L, H> &x, Held<T, L, H> &r) {
+        x.load(a.x, row_of(at) * a.xs, i, a.dim);
+        if (a.r) r.load(a.r, row_of(at) * a.rs, i, a.dim);
+    };
+    int64_t at = static_cast<int64_t>(blockIdx.x) * kRows;
+    load(at, x, r);
+    for (; at < a.n; at += stride) {
+        if (kAhead && at + stride < a.n) load(at + stride, next_x, next_r);
+        const bool there = at + sub < a.n;
+        const int64_t row = row_of(at);
+        float v[H][E];
 #pragma unroll
-            for (int h = 0; h < H; h++) {
+        for (int h = 0; h < H; h++)
 #pragma unroll
-                for (int k = 0; k < kRun; k++) v[h][k] = as_float(from_float<T>(v[h][k] + r[h][k]));
-                if (there && i + h * L < runs)
-                    store_columns<T, kRun>(static_cast<T *>(a.sum) + row * a.ss, (i + h * L) * kRun, a.dim, v[h]);
+            for (int k = 0; k < E; k++) {
+                v[h][k] = x.at(h, k);
+                if (a.r) v[h][k] = as_float(from_float<T>(v[h][k] + r.at(h, k)));
             }
-        }
+        if (a.r && there) store_row<T, L, H>(a.sum, row * a.ss, i, a.dim, v);
         double sum[1] = {0.0};
 #pragma unroll
         for (int h = 0; h < H; h++)
 #pragma unroll
-            for (int k = 0; k < kRun; k++) sum[0] += v[h][k];       // 0 beyond the row
+            for (int k = 0; k < E; k++) sum[0] += v[h][k];
         row_sum<L>(sum, lds[0]);
         const double mean = sum[0] / a.dim;
         double squares[1] = {0.0};
 #pragma unroll
         for (int h = 0; h < H; h++)
 #pragma unroll
-            for (int k = 0; k < kRun; k++) {
-                const double c = (i + h * L) * kRun + k < a.dim ? v[h][k] - mean : 0.0;
+            for (int k = 0; k < E; k++) {
+                const double c = (i + h * L) * E + k < a.dim ? v[h][k] - mean : 0.0;
                 squares[0] = __builtin_fma(c, c, squares[0]);
             }
         row_sum<L>(squares, lds[1]);
         const double rstd = 1.0 / sqrt(squares[0] / a.dim + a.eps);
-        if (!there) continue;
+        if (there) {
 #pragma unroll
-        for (int h = 0; h < H; h++) {
-            if (i + h * L < runs) {
+            for (int h = 0; h < H; h++)
 #pragma unroll
-                for (int k = 0; k < kRun; k++)
+                for (int k = 0; k < E; k++)
                     v[h][k] = __builtin_fmaf(static_cast<float>((v[h][k] - mean) * rstd), w[h][k], b[h][k]);
-                store_columns<T, kRun>(static_cast<T *>(a.y) + row * a.ys, (i + h * L) * kRun, a.dim, v[h]);
+            store_row<T, L, H>(a.y, row * a.ys, i, a.dim, v);
+            if (a.stats && i == 0) {
+                a.stats[2 * row] = mean;
+                a.stats[2 * row + 1] = rstd;
             }
         }
-        if (a.stats && i == 0) {
-            a.stats[2 * row] = mean;
-            a.stats[2 * row + 1] = rstd;
+        if constexpr (kAhead) {
+            x = next_x;
+            r = next_r;
+        } else {
+            if (at + stride < a.n) load(at + stride, x, r);
         }
     }
 }
 
-template <class T, int L, int H, int kThreads, bool kParams>
+// As norm_kernel.  Rows too wide to stay beside the sums of the weights' gradients
+// (!kHold) are read again, mostly from L2, once their means are known.
+template <class T, int L, int H, int kThreads, bool kHold, bool kParams>
 __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const GradArgs a) {
     __shared__ double lds[2][kThreads / kWave][2];
-    const int i = threadIdx.x % L;
-    const int runs = (a.dim + kRun - 1) / kRun;
-    float w[H][kRun];
-    load_weights<L, H>(a.w, i, runs, a.dim, 1.0f, w);
-    double dw[kParams ? H : 1][kRun], db[kParams ? H : 1][kRun];
-    if constexpr (kParams) {
+    constexpr int kRows = kThreads / L, kColumns = L * H * E;
+    const int i = threadIdx.x % L, sub = threadIdx.x / L;
+    float w[H][E];
+    load_weights<T, L, H>(a.w, i, a.dim, 1.0f, w);
+    double dw[kParams ? H : 1][E] = {}, db[kParams ? H : 1][E] = {};
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * kRows;
+    auto row_of = [&](int64_t at) { return at + sub < a.n ? at + sub : a.n - 1; };
+    Held<T, L, kHold ? H : 1> dy, x, dh, next_dy, next_x, next_dh;
+    double mean, rstd, next_mean = 0.0, next_rstd = 0.0;
+    auto load = [&](int64_t at, auto &dy, auto &x, auto &dh, double &mean, double &rstd) {
+        const int64_t row = row_of(at);
+        if constexpr (kHold) {
+            dy.load(a.dy, row * a.dys, i, at + sub < a.n ? a.dim : 0);
+            x.load(a.h, row * a.hs, i, a.dim);
+            if (a.dh) dh.load(a.dh, row * a.dhs, i, a.dim);
+        }
+        mean = a.stats[2 * row];
+        rstd = a.stats[2 * row + 1];
+    };
+    int64_t at = static_cast<int64_t>(blockIdx.x) * kRows;
+    load(at, dy, x, dh, mean, rstd);
+    int turn = 0;
+    for (; at < a.n; at += stride) {
+        if (at + stride < a.n) load(at + stride, next_dy, next_x, next_dh, next_mean, next_rstd);
+        const bool there = at + sub < a.n;
+        const int64_t row = row_of(at);
+        const int dim = there ? a.dim : 0;
+        auto run_of = [&](const auto &held, const void *p, int64_t stride, int h) {
+            if constexpr (kHold) return held.v[h];
+            else return load_run<T, L>(p, row * stride, i, h, dim);
+        };
+        // (h - mean) rstd; beyond the row, and beyond the rows, 0, as dy is
+        auto normed = [&](const run_t<T> &v, int h, int k) {
+            return (i + h * L) * E + k < dim ? static_cast<float>((run_at<T>(v, k) - mean) * rstd) : 0.0f;
+        };
+        // weights are held as 32 bits: made 64 anew for every row
 #pragma unroll
         for (int h = 0; h < H; h++)
 #pragma unroll
-            for (int k = 0; k < kRun; k++) dw[h][k] = db[h][k] = 0.0;
-    }
-    constexpr int kRows = kThreads / L;
-    int turn = 0;
-    for (int64_t at = static_cast<int64_t>(blockIdx.x) * kRows; at < a.n; at += static_cast<int64_t>(gridDim.x) * kRows) {
-        const bool there = at + threadIdx.x / L < a.n;
-        const int64_t row = there ? at + threadIdx.x / L : a.n - 1;
-        float xh[H][kRun], dy[H][kRun];
-        load_row<T, L, H>(a.h, row * a.hs, i, runs, a.dim, xh);
-        load_row<T, L, H>(a.dy, row * a.dys, i, runs, a.dim, dy);
-        const double mean = a.stats[2 * row], rstd = a.stats[2 * row + 1];
+            for (int k = 0; k < E; k++) asm("" : "+v"(w[h][k]));
         double sums[2] = {0.0, 0.0};
 #pragma unroll
-        for (int h = 0; h < H; h++)
-#pragma unroll
-            for (int k = 0; k < kRun; k++) {
-                xh[h][k] = static_cast<float>((xh[h][k] - mean) * rstd);
-                const double d = dy[h][k], g = d * w[h][k];             // 0 beyond the row
-                if ((i + h * L) * kRun + k < a.dim) {
-                    sums[0] += g;
-                    sums[1] = __builtin_fma(g, static_cast<double>(xh[h][k]), sums[1]);
-                    if constexpr (kParams) {
-                        if (there) {
-                            dw[h][k] = __builtin_fma(d, static_cast<double>(xh[h][k]), dw[h][k]);
-                            db[h][k] += d;
-                        }
-                    }
-                }
-            }
-        if (!a.dx) continue;
-        row_sum<L>(sums, lds[turn]);
-        turn ^= 1;
-        if (!there) continue;
-        const double c1 = sums[0] / a.dim, c2 = sums[1] / a.dim;
-        float dh[H][kRun];
-        if (a.dh) load_row<T, L, H>(a.dh, row * a.dhs, i, runs, a.dim, dh);
-#pragma unroll
         for (int h = 0; h < H; h++) {
-            if (i + h * L < runs) {
+            const run_t<T> dv = run_of(dy, a.dy, a.dys, h), xv = run_of(x, a.h, a.hs, h);
 #pragma unroll
-                for (int k = 0; k < kRun; k++) {
-                    const double g = static_cast<double>(dy[h][k]) * w[h][k];
-                    const double d = __builtin_fma(-c2, static_cast<double>(xh[h][k]), g - c1) * rstd;
-                    dy[h][k] = static_cast<float>(a.dh ? d + dh[h][k] : d);
+            for (int k = 0; k < E; k++) {
+                const double d = run_at<T>(dv, k), t = normed(xv, h, k), g = d * w[h][k];
+                sums[0] += g;
+                sums[1] = __builtin_fma(g, t, sums[1]);
+                if constexpr (kParams) {
+                    dw[h][k] = __builtin_fma(d, t, dw[h][k]);
+                    db[h][k] += d;
                 }
-                store_columns<T, kRun>(static_cast<T *>(a.dx) + row * a.dxs, (i + h * L) * kRun, a.dim, dy[h]);
             }
         }
+        if (a.dx) {
+            row_sum<L>(sums, lds[turn]);
+            turn ^= 1;
+            const double c1 = sums[0] / a.dim, c2 = sums[1] / a.dim;
+            if constexpr (kHold) {
+                // taken apart anew: 64-bit numbers kept from above would cost a wavefront a SIMD
+#pragma unroll
+                for (int h = 0; h < H; h++) {
+                    asm("" : "+v"(dy.v[h]), "+v"(x.v[h]));
+#pragma unroll
+                    for (int k = 0; k < E; k++) asm("" : "+v"(w[h][k]));
+                }
+            }
+            if (there) {
+#pragma unroll
+                for (int h = 0; h < H; h++) {
+                    const int c = (i + h * L) * E;
+                    if (c >= a.dim) continue;
+                    const run_t<T> dv = run_of(dy, a.dy, a.dys, h), xv = run_of(x, a.h, a.hs, h);
+                    run_t<T> hv = {};
+                    if (a.dh) hv = run_of(dh, a.dh, a.dhs, h);
+                    float v[E];
+#pragma unroll
+                    for (int k = 0; k < E; k++) {
+                        const double g = static_cast<double>(run_at<T>(dv, k)) * w[h][k];
+                        const double d = __builtin_fma(-c2, static_cast<double>(normed(xv, h, k)), g - c1) * rstd;
+                        v[k] = static_cast<float>(a.dh ? d + run_at<T>(hv, k) : d);
+                    }
+                    store_columns<T, E>(static_cast<T *>(a.dx) + row * a.dxs, c, a.dim, v);
+                }
+            }
+        }
+        if constexpr (kHold) {
+            dy = next_dy;
+            x = next_x;
+            dh = next_dh;
+        }
+        mean = next_mean;
+        rstd = next_rstd;
     }
     if constexpr (kParams) {
         // the workgroup's rows together: first those of a wavefront, then its wavefronts one after another
-        __shared__ double cols[L >= kWave || kThreads > kWave ? 2 : 1][L * H * kRun > 2048 ? 1 : L * H * kRun];
+        constexpr int kWavesOfRow = L > kWave ? L / kWave : 1, kGroups = kThreads / kWave / kWavesOfRow;
+        __shared__ double cols[2][kGroups > 1 ? kColumns : 1];
         double *part = a.parts + static_cast<int64_t>(blockIdx.x) * 2 * a.dim;
 #pragma unroll
         for (int d = L; d < kWave; d <<= 1)
 #pragma unroll
             for (int h = 0; h < H; h++)
 #pragma unroll
-                for (int k = 0; k < kRun; k++) {
+                for (int k = 0; k < E; k++) {
                     dw[h][k] += __shfl_xor(dw[h][k], d, kWave);
                     db[h][k] += __shfl_xor(db[h][k], d, kWave);
                 }
-        constexpr int kWavesOfRow = L > kWave ? L / kWave : 1;
-        constexpr int kGroups = kThreads / kWave / kWavesOfRow;
         if constexpr (kGroups == 1) {
 #pragma unroll
             for (int h = 0; h < H; h++)
 #pragma unroll
-                for (int k = 0; k < kRun; k++) {
-                    const int c = (i + h * L) * kRun + k;
+                for (int k = 0; k < E; k++) {
+                    const int c = (i + h * L) * E + k;
                     if (c < a.dim && threadIdx.x < L) {
                         part[c] = dw[h][k];
                         part[a.dim + c] = db[h][k];
@@ -244,8 +353,8 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const GradArgs a) {
 #pragma unroll
                     for (int h = 0; h < H; h++)
 #pragma unroll
-                        for (int k = 0; k < kRun; k++) {
-                            const int c = (h * kRun + k) * L + i;           // lanes beside each other
+                        for (int k = 0; k < E; k++) {
+                            const int c = (h * E + k) * L + i;              // lanes beside each other
                             cols[0][c] = g == 0 ? dw[h][k] : cols[0][c] + dw[h][k];
                             cols[1][c] = g == 0 ? db[h][k] : cols[1][c] + db[h][k];
                         }
@@ -253,7 +362,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const GradArgs a) {
             }
             __syncthreads();
             for (int c = threadIdx.x; c < a.dim; c += kThreads) {
-                const int run = c / kRun, h = run / L, at = (h * kRun + c % kRun) * L + run % L;
+                const int run = c / E, at = (run / L * E + c % E) * L + run % L;
                 part[c] = cols[0][at];
                 part[a.dim + c] = cols[1][at];
             }
@@ -284,31 +393,35 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const double *parts, in
     }
 }
 
-// Workgroups of a call at most: the weights are read once for each, and their
-// gradients' sums written once.
-constexpr int64_t kBlocks = 4096;
+// Workgroups of a call at most: each takes several rows in turn, and reads the
+// weights and writes the sums of their gradients once.
+constexpr int64_t kBlocks = 2048;
 int64_t grad_blocks(int32_t dim) { return dim <= 1024 ? 1024 : dim <= 4096 ? 512 : 256; }
 
-// f(lanes of a row, runs of a lane, threads of a workgroup) for a row's width.
-template <bool kGrad, class F>
+// f(lanes of a row, runs of a lane, threads of a workgroup, whether a row stays in registers) for a row's width.
+template <class F>
 void with_shape(int32_t dim, const F &f) {
-    if (dim <= 64) f(Const<8>(), Const<1>(), Const<256>());
-    else if (dim <= 128) f(Const<16>(), Const<1>(), Const<256>());
-    else if (dim <= 256) f(Const<32>(), Const<1>(), Const<256>());
-    else if (dim <= 512) f(Const<64>(), Const<1>(), Const<256>());
-    else if (dim <= 1024) f(Const<64>(), Const<2>(), Const<256>());
-    else if (dim <= 2048) f(Const<256>(), Const<1>(), Const<256>());
-    else if (dim <= 4096) f(Const<512>(), Const<1>(), Const<512>());
-    else if (dim <= 8192) f(Const<1024>(), Const<1>(), Const<1024>());
-    else f(Const<1024>(), Const<2>(), Const<1024>());
+    using Yes = std::true_type;
+    using No = std::false_type;
+    if (dim <= 32) f(Const<8>(), Const<1>(), Const<256>(), Yes());
+    else if (dim <= 64) f(Const<16>(), Const<1>(), Const<256>(), Yes());
+    else if (dim <= 128) f(Const<32>(), Const<1>(), Const<256>(), Yes());
+    else if (dim <= 256) f(Const<64>(), Const<1>(), Const<256>(), Yes());
+    else if (dim <= 512) f(Const<64>(), Const<2>(), Const<256>(), Yes());
+    else if (dim <= 768) f(Const<64>(), Const<3>(), Const<256>(), Yes());
+    else if (dim <= 1024) f(Const<128>(), Const<2>(), Const<256>(), Yes());
+    else if (dim <= 2048) f(Const<256>(), Const<2>(), Const<256>(), Yes());
+    else if (dim <= 4096) f(Const<512>(), Const<2>(), Const<512>(), Yes());
+    else if (dim <= 8192) f(Const<512>(), Const<4>(), Const<512>(), No());
+    else f(Const<512>(), Const<8>(), Const<512>(), No());
 }
 
 template <class T>
 tgl_status launch_norm(const NormArgs &a, hipStream_t st) {
-    with_shape<false>(a.dim, [&](auto L, auto H, auto N) {
+    with_shape(a.dim, [&](auto L, auto H, auto N, auto Hold) {
         constexpr int kL = decltype(L)::value, kH = decltype(H)::value, kN = decltype(N)::value;
         const int64_t blocks = (a.n + kN / kL - 1) / (kN / kL);
-        norm_kernel<T, kL, kH, kN><<<static_cast<unsigned>(blocks < kBlocks ? blocks : kBlocks), kN, 0, st>>>(a);
+        norm_kernel<T, kL, kH, kN, decltype(Hold)::value><<<static_cast<unsigned>(blocks < kBlocks ? blocks : kBlocks), kN, 0, st>>>(a);
     });
     return launch_status();
 }
@@ -316,11 +429,11 @@ tgl_status launch_norm(const NormArgs &a, hipStream_t st) {
 template <class T, bool kParams>
 int64_t launch_grad(const GradArgs &a, hipStream_t st) {
     int64_t count = 0;
-    with_shape<true>(a.dim, [&](auto L, auto H, auto N) {
+    with_shape(a.dim, [&](auto L, auto H, auto N, auto Hold) {
         constexpr int kL = decltype(L)::value, kH = decltype(H)::value, kN = decltype(N)::value;
         const int64_t most = grad_blocks(a.dim), blocks = (a.n + kN / kL - 1) / (kN / kL);
         count = blocks < most ? blocks : most;
-        norm_grad_kernel<T, kL, kH, kN, kParams><<<static_cast<unsigned>(count), kN, 0, st>>>(a);
+        norm_grad_kernel<T, kL, kH, kN, decltype(Hold)::value, kParams><<<static_cast<unsigned>(count), kN, 0, st>>>(a);
     });
     return count;
 }
