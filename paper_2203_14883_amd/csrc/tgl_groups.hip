@@ -39,7 +39,7 @@ template <class K>
 __device__ __forceinline__ uint32_t bin_of(const GroupArgs &a, int64_t row) {
     int64_t t;
     if (a.ids) {
-        const int32_t id = a.ids[row];
+        const int32_t id = __builtin_nontemporal_load(a.ids + row);       // read once: the nodes' types stay in the caches
         t = id >= 0 && id < a.num_ids ? static_cast<const K *>(a.types)[id] : -1;
     } else {
         t = static_cast<const K *>(a.types)[row];
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void group_count_kernel(const GroupArgs a
 #pragma unroll
         for (int i = 0; i < kAhead; i++) {
             const bool there = row + i * kWave < end;
-            if (a.kept && there) a.kept[row + i * kWave] = static_cast<uint16_t>(bin[i]);
+            if (a.kept && there) __builtin_nontemporal_store(static_cast<uint16_t>(bin[i]), a.kept + row + i * kWave);
             const uint64_t same = same_bin(bin[i], a.bits, __ballot(there));
             if (there && rank_below(same) == 0) atomicAdd(&count[wave][bin[i]], static_cast<uint32_t>(__popcll(same)));
         }

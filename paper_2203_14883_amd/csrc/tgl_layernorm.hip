@@ -106,12 +106,18 @@ __device__ __forceinline__ float run_at(const run_t<T> &v, int k) {
     else return __builtin_bit_cast(f32x4, v)[k];
 }
 
-// Run h of lane i of a row's L begins at column (i + h L) E.  Zeros beyond the row.
-template <class T, int L>
+// Run h of lane i of a row's L begins at column (i + h L) E.  Zeros beyond the
+// row; kWhole: rows end with a run.
+template <class T, int L, bool kWhole>
 __device__ __forceinline__ run_t<T> load_run(const void *p, int64_t at, int i, int h, int dim) {
     using word_t = run_t<T> __attribute__((aligned(alignof(T))));
     const T *row = static_cast<const T *>(p) + at;
     const int c = (i + h * L) * E;
+    if constexpr (kWhole) {
+        run_t<T> v = {};
+        if (c < dim) v = *reinterpret_cast<const word_t *>(row + c);
+        return v;
+    }
     if (c + E <= dim) return *reinterpret_cast<const word_t *>(row + c);
     Run<T, E> v = {};
 #pragma unroll
@@ -121,21 +127,27 @@ __device__ __forceinline__ run_t<T> load_run(const void *p, int64_t at, int i, i
 }
 
 // A row in the registers of L lanes.
-template <class T, int L, int H>
+template <class T, int L, int H, bool kWhole>
 struct Held {
     run_t<T> v[H];
     __device__ __forceinline__ void load(const void *p, int64_t at, int i, int dim) {
 #pragma unroll
-        for (int h = 0; h < H; h++) v[h] = load_run<T, L>(p, at, i, h, dim);
+        for (int h = 0; h < H; h++) v[h] = load_run<T, L, kWhole>(p, at, i, h, dim);
     }
     __device__ __forceinline__ float at(int h, int k) const { return run_at<T>(v[h], k); }
 };
 
-template <class T, int L, int H>
+// E columns from c < dim on.
+template <class T, bool kWhole>
+__device__ __forceinline__ void store_run(void *p, int64_t at, int c, int dim, const float (&v)[E]) {
+    store_columns<T, E>(static_cast<T *>(p) + at, c, kWhole ? c + E : dim, v);
+}
+
+template <class T, int L, int H, bool kWhole>
 __device__ __forceinline__ void store_row(void *p, int64_t at, int i, int dim, const float (&v)[H][E]) {
 #pragma unroll
     for (int h = 0; h < H; h++)
-        if ((i + h * L) * E < dim) store_columns<T, E>(static_cast<T *>(p) + at, (i + h * L) * E, dim, v[h]);
+        if ((i + h * L) * E < dim) store_run<T, kWhole>(p, at, (i + h * L) * E, dim, v[h]);
 }
 
 // A lane's columns of the weights, or what stands for none.
@@ -151,7 +163,7 @@ __device__ __forceinline__ void load_weights(const float *w, int i, int dim, flo
 
 // Bound by memory, as long as enough of it is on its way: the next row is loaded
 // before this one is worked on, where registers have room (kAhead).
-template <class T, int L, int H, int kThreads, bool kAhead>
+template <class T, int L, int H, int kThreads, bool kAhead, bool kWhole>
 __global__ __launch_bounds__(kThreads) void norm_kernel(const NormArgs a) {
     __shared__ double lds[2][kThreads / kWave][1];
     constexpr int kRows = kThreads / L;
@@ -161,8 +173,8 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const NormArgs a) {
     load_weights<T, L, H>(a.b, i, a.dim, 0.0f, b);
     const int64_t stride = static_cast<int64_t>(gridDim.x) * kRows;
     auto row_of = [&](int64_t at) { return at + sub < a.n ? at + sub : a.n - 1; };
-    Held<T, L, H> x, r, next_x, next_r;
-    auto load = [&](int64_t at, Held<T, L, H> &x, Held<T, L, H> &r) {
+    Held<T, L, H, kWhole> x, r, next_x, next_r;
+    auto load = [&](int64_t at, auto &x, auto &r) {
         x.load(a.x, row_of(at) * a.xs, i, a.dim);
         if (a.r) r.load(a.r, row_of(at) * a.rs, i, a.dim);
     };
@@ -180,7 +192,7 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const NormArgs a) {
                 v[h][k] = x.at(h, k);
                 if (a.r) v[h][k] = as_float(from_float<T>(v[h][k] + r.at(h, k)));
             }
-        if (a.r && there) store_row<T, L, H>(a.sum, row * a.ss, i, a.dim, v);
+        if (a.r && there) store_row<T, L, H, kWhole>(a.sum, row * a.ss, i, a.dim, v);
         double sum[1] = {0.0};
 #pragma unroll
         for (int h = 0; h < H; h++)
@@ -193,7 +205,7 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const NormArgs a) {
         for (int h = 0; h < H; h++)
 #pragma unroll
             for (int k = 0; k < E; k++) {
-                const double c = (i + h * L) * E + k < a.dim ? v[h][k] - mean : 0.0;
+                const double c = (i + h * L) * E + (kWhole ? 0 : k) < a.dim ? v[h][k] - mean : 0.0;
                 squares[0] = __builtin_fma(c, c, squares[0]);
             }
         row_sum<L>(squares, lds[1]);
@@ -204,7 +216,7 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const NormArgs a) {
 #pragma unroll
                 for (int k = 0; k < E; k++)
                     v[h][k] = __builtin_fmaf(static_cast<float>((v[h][k] - mean) * rstd), w[h][k], b[h][k]);
-            store_row<T, L, H>(a.y, row * a.ys, i, a.dim, v);
+            store_row<T, L, H, kWhole>(a.y, row * a.ys, i, a.dim, v);
             if (a.stats && i == 0) {
                 a.stats[2 * row] = mean;
                 a.stats[2 * row + 1] = rstd;
@@ -219,96 +231,174 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const NormArgs a) {
     }
 }
 
-// As norm_kernel.  Rows too wide to stay beside the sums of the weights' gradients
-// (!kHold) are read again, mostly from L2, once their means are known.
-template <class T, int L, int H, int kThreads, bool kHold, bool kParams>
+// Rows of a lane whose products are summed in 32 bits before they join its 64-bit sums.
+constexpr int kChain = 32;
+
+// As norm_kernel, but 64-bit numbers for all of it would take more than memory
+// does (52 operations an element, 280 us for 132,000 rows of 768 bfloat16 with a sum's
+// gradient, where these take 18): distances from the mean are taken from its upper and
+// its lower bits, (h - upper) - lower, which loses nothing that 32 bits could hold, and a row's
+// means and the weights' gradients are sums of 64 bits of a lane's few elements, or kChain rows,
+// in 32.  Rows that leave float32's range on the way are worked in 64.  Rows too
+// wide for the registers (!kHold) are read again, mostly from L2, once their means are known.
+template <class T, int L, int H, int kThreads, bool kHold, bool kWhole, bool kParams>
 __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const GradArgs a) {
     __shared__ double lds[2][kThreads / kWave][2];
     constexpr int kRows = kThreads / L, kColumns = L * H * E;
+    constexpr int kWavesOfRow = L > kWave ? L / kWave : 1, kGroups = kThreads / kWave / kWavesOfRow;
+    __shared__ double cols[2][kParams && kGroups > 1 ? kColumns : 1];
     const int i = threadIdx.x % L, sub = threadIdx.x / L;
     float w[H][E];
     load_weights<T, L, H>(a.w, i, a.dim, 1.0f, w);
-    double dw[kParams ? H : 1][E] = {}, db[kParams ? H : 1][E] = {};
+    float dw[kParams ? H : 1][E] = {}, db[kParams ? H : 1][E] = {};
     const int64_t stride = static_cast<int64_t>(gridDim.x) * kRows;
-    auto row_of = [&](int64_t at) { return at + sub < a.n ? at + sub : a.n - 1; };
-    Held<T, L, kHold ? H : 1> dy, x, dh, next_dy, next_x, next_dh;
+
+    Held<T, L, kHold ? H : 1, kWhole> dy, x, dh, next_dy, next_x, next_dh;
     double mean, rstd, next_mean = 0.0, next_rstd = 0.0;
+    // rows beyond the last are zeros
     auto load = [&](int64_t at, auto &dy, auto &x, auto &dh, double &mean, double &rstd) {
-        const int64_t row = row_of(at);
-        if constexpr (kHold) {
-            dy.load(a.dy, row * a.dys, i, at + sub < a.n ? a.dim : 0);
-            x.load(a.h, row * a.hs, i, a.dim);
-            if (a.dh) dh.load(a.dh, row * a.dhs, i, a.dim);
-        }
-        mean = a.stats[2 * row];
-        rstd = a.stats[2 * row + 1];
-    };
-    int64_t at = static_cast<int64_t>(blockIdx.x) * kRows;
-    load(at, dy, x, dh, mean, rstd);
-    int turn = 0;
-    for (; at < a.n; at += stride) {
-        if (at + stride < a.n) load(at + stride, next_dy, next_x, next_dh, next_mean, next_rstd);
         const bool there = at + sub < a.n;
-        const int64_t row = row_of(at);
-        const int dim = there ? a.dim : 0;
-        auto run_of = [&](const auto &held, const void *p, int64_t stride, int h) {
-            if constexpr (kHold) return held.v[h];
-            else return load_run<T, L>(p, row * stride, i, h, dim);
+        const int64_t row = there ? at + sub : a.n - 1;
+        if constexpr (kHold) {
+            const int dim = there ? a.dim : 0;
+            dy.load(a.dy, row * a.dys, i, dim);
+            x.load(a.h, row * a.hs, i, dim);
+            if (a.dh) dh.load(a.dh, row * a.dhs, i, dim);
+        }
+        mean = there ? a.stats[2 * row] : 0.0;
+        rstd = there ? a.stats[2 * row + 1] : 0.0;
+    };
+    // The lanes' sums of the weights' gradients to the workgroup's: first those of a
+    // wavefront, then its wavefronts one after another.
+    auto flush = [&](bool first) {
+        double *part = a.parts + static_cast<int64_t>(blockIdx.x) * 2 * a.dim;
+        auto add = [&](int c, double x, double y) {
+            part[c] = first ? x : part[c] + x;
+            part[a.dim + c] = first ? y : part[a.dim + c] + y;
         };
-        // (h - mean) rstd; beyond the row, and beyond the rows, 0, as dy is
-        auto normed = [&](const run_t<T> &v, int h, int k) {
-            return (i + h * L) * E + k < dim ? static_cast<float>((run_at<T>(v, k) - mean) * rstd) : 0.0f;
-        };
-        // weights are held as 32 bits: made 64 anew for every row
+        if constexpr (kGroups == 1) {
+#pragma unroll
+            for (int h = 0; h < H; h++)
+#pragma unroll
+                for (int k = 0; k < E; k++)
+                    if ((i + h * L) * E + k < a.dim) add((i + h * L) * E + k, dw[h][k], db[h][k]);
+        } else {
+            const int group = threadIdx.x / kWave / kWavesOfRow;
+            const bool owner = L >= kWave || lane_id() < L;
+            for (int g = 0; g < kGroups; g++) {
+                __syncthreads();
+                if (g != group) continue;
+#pragma unroll
+                for (int h = 0; h < H; h++)
+#pragma unroll
+                    for (int k = 0; k < E; k++) {
+                        double x = dw[h][k], y = db[h][k];
+#pragma unroll
+                        for (int d = L; d < kWave; d <<= 1) {
+                            x += __shfl_xor(x, d, kWave);
+                            y += __shfl_xor(y, d, kWave);
+                        }
+                        const int c = (h * E + k) * L + i;                  // lanes beside each other
+                        if (owner) {
+                            cols[0][c] = g == 0 ? x : cols[0][c] + x;
+                            cols[1][c] = g == 0 ? y : cols[1][c] + y;
+                        }
+                    }
+            }
+            __syncthreads();
+            for (int c = threadIdx.x; c < a.dim; c += kThreads) {
+                const int run = c / E, at = (run / L * E + c % E) * L + run % L;
+                add(c, cols[0][at], cols[1][at]);
+            }
+        }
 #pragma unroll
         for (int h = 0; h < H; h++)
 #pragma unroll
-            for (int k = 0; k < E; k++) asm("" : "+v"(w[h][k]));
-        double sums[2] = {0.0, 0.0};
+            for (int k = 0; k < E; k++) dw[h][k] = db[h][k] = 0.0f;
+    };
+    int64_t at = static_cast<int64_t>(blockIdx.x) * kRows;
+    load(at, dy, x, dh, mean, rstd);
+    int turn = 0, rows = 0;
+    bool flushed = false;
+    for (; at < a.n; at += stride) {
+        if (at + stride < a.n) load(at + stride, next_dy, next_x, next_dh, next_mean, next_rstd);
+        const bool there = at + sub < a.n;
+        const int64_t row = there ? at + sub : a.n - 1;
+        const int dim = there ? a.dim : 0;
+        const bool ordinary = fabs(mean) < 0x1p100 && rstd > 0x1p-60 && rstd < 0x1p60;
+        const float upper = static_cast<float>(mean), lower = static_cast<float>(mean - upper), scale = static_cast<float>(rstd);
+        auto run_of = [&](const auto &held, const void *p, int64_t stride, int h) {
+            if constexpr (kHold) return held.v[h];
+            else return load_run<T, L, kWhole>(p, row * stride, i, h, dim);
+        };
+        auto normed = [&](float v) { return ((v - upper) - lower) * scale; };
+        // beyond the row 0, as dy is there: the product need not be a number
+        auto normed_wide = [&](float v, int c) { return c < dim ? static_cast<float>((v - mean) * rstd) : 0.0f; };
+        float xh[kHold ? H : 1][E];
+        float part[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int h = 0; h < H; h++) {
             const run_t<T> dv = run_of(dy, a.dy, a.dys, h), xv = run_of(x, a.h, a.hs, h);
+            float t[E];
+            if (ordinary) {
+#pragma unroll
+                for (int k = 0; k < E; k++) t[k] = normed(run_at<T>(xv, k));
+            } else {
+#pragma unroll
+                for (int k = 0; k < E; k++) t[k] = normed_wide(run_at<T>(xv, k), (i + h * L) * E + k);
+            }
 #pragma unroll
             for (int k = 0; k < E; k++) {
-                const double d = run_at<T>(dv, k), t = normed(xv, h, k), g = d * w[h][k];
-                sums[0] += g;
-                sums[1] = __builtin_fma(g, t, sums[1]);
+                const float d = run_at<T>(dv, k), g = d * w[h][k];
+                part[0] += g;
+                part[1] = __builtin_fmaf(g, t[k], part[1]);
                 if constexpr (kParams) {
-                    dw[h][k] = __builtin_fma(d, t, dw[h][k]);
+                    dw[h][k] = __builtin_fmaf(d, t[k], dw[h][k]);
                     db[h][k] += d;
                 }
+                if constexpr (kHold) xh[h][k] = t[k];
             }
         }
         if (a.dx) {
+            double sums[2] = {part[0], part[1]};
             row_sum<L>(sums, lds[turn]);
             turn ^= 1;
-            const double c1 = sums[0] / a.dim, c2 = sums[1] / a.dim;
-            if constexpr (kHold) {
-                // taken apart anew: 64-bit numbers kept from above would cost a wavefront a SIMD
-#pragma unroll
-                for (int h = 0; h < H; h++) {
-                    asm("" : "+v"(dy.v[h]), "+v"(x.v[h]));
-#pragma unroll
-                    for (int k = 0; k < E; k++) asm("" : "+v"(w[h][k]));
-                }
-            }
+            const double inv = 1.0 / a.dim, c1 = sums[0] * inv, c2 = sums[1] * inv;
+            const float c1f = static_cast<float>(c1), c2f = static_cast<float>(c2);
             if (there) {
 #pragma unroll
                 for (int h = 0; h < H; h++) {
                     const int c = (i + h * L) * E;
                     if (c >= a.dim) continue;
-                    const run_t<T> dv = run_of(dy, a.dy, a.dys, h), xv = run_of(x, a.h, a.hs, h);
-                    run_t<T> hv = {};
+                    const run_t<T> dv = run_of(dy, a.dy, a.dys, h);
+                    run_t<T> xv = {}, hv = {};
+                    if constexpr (!kHold) xv = run_of(x, a.h, a.hs, h);
                     if (a.dh) hv = run_of(dh, a.dh, a.dhs, h);
                     float v[E];
+                    if (ordinary) {
 #pragma unroll
-                    for (int k = 0; k < E; k++) {
-                        const double g = static_cast<double>(run_at<T>(dv, k)) * w[h][k];
-                        const double d = __builtin_fma(-c2, static_cast<double>(normed(xv, h, k)), g - c1) * rstd;
-                        v[k] = static_cast<float>(a.dh ? d + run_at<T>(hv, k) : d);
+                        for (int k = 0; k < E; k++) {
+                            const float t = kHold ? xh[kHold ? h : 0][k] : normed(run_at<T>(xv, k));
+                            v[k] = __builtin_fmaf(-c2f, t, run_at<T>(dv, k) * w[h][k] - c1f) * scale;
+                            if (a.dh) v[k] += run_at<T>(hv, k);
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < E; k++) {
+                            const double t = kHold ? xh[kHold ? h : 0][k] : normed_wide(run_at<T>(xv, k), c + k);
+                            const double d = __builtin_fma(-c2, t, static_cast<double>(run_at<T>(dv, k)) * w[h][k] - c1) * rstd;
+                            v[k] = static_cast<float>(a.dh ? d + run_at<T>(hv, k) : d);
+                        }
                     }
-                    store_columns<T, E>(static_cast<T *>(a.dx) + row * a.dxs, c, a.dim, v);
+                    store_run<T, kWhole>(a.dx, row * a.dxs, c, a.dim, v);
                 }
+            }
+        }
+        if constexpr (kParams) {
+            if (++rows == kChain) {
+                flush(!flushed);
+                flushed = true;
+                rows = 0;
             }
         }
         if constexpr (kHold) {
@@ -320,53 +410,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const GradArgs a) {
         rstd = next_rstd;
     }
     if constexpr (kParams) {
-        // the workgroup's rows together: first those of a wavefront, then its wavefronts one after another
-        constexpr int kWavesOfRow = L > kWave ? L / kWave : 1, kGroups = kThreads / kWave / kWavesOfRow;
-        __shared__ double cols[2][kGroups > 1 ? kColumns : 1];
-        double *part = a.parts + static_cast<int64_t>(blockIdx.x) * 2 * a.dim;
-#pragma unroll
-        for (int d = L; d < kWave; d <<= 1)
-#pragma unroll
-            for (int h = 0; h < H; h++)
-#pragma unroll
-                for (int k = 0; k < E; k++) {
-                    dw[h][k] += __shfl_xor(dw[h][k], d, kWave);
-                    db[h][k] += __shfl_xor(db[h][k], d, kWave);
-                }
-        if constexpr (kGroups == 1) {
-#pragma unroll
-            for (int h = 0; h < H; h++)
-#pragma unroll
-                for (int k = 0; k < E; k++) {
-                    const int c = (i + h * L) * E + k;
-                    if (c < a.dim && threadIdx.x < L) {
-                        part[c] = dw[h][k];
-                        part[a.dim + c] = db[h][k];
-                    }
-                }
-        } else {
-            const int group = threadIdx.x / kWave / kWavesOfRow;
-            const bool owner = L >= kWave || lane_id() < L;
-            for (int g = 0; g < kGroups; g++) {
-                __syncthreads();
-                if (g == group && owner) {
-#pragma unroll
-                    for (int h = 0; h < H; h++)
-#pragma unroll
-                        for (int k = 0; k < E; k++) {
-                            const int c = (h * E + k) * L + i;              // lanes beside each other
-                            cols[0][c] = g == 0 ? dw[h][k] : cols[0][c] + dw[h][k];
-                            cols[1][c] = g == 0 ? db[h][k] : cols[1][c] + db[h][k];
-                        }
-                }
-            }
-            __syncthreads();
-            for (int c = threadIdx.x; c < a.dim; c += kThreads) {
-                const int run = c / E, at = (run / L * E + c % E) * L + run % L;
-                part[c] = cols[0][at];
-                part[a.dim + c] = cols[1][at];
-            }
-        }
+        if (rows || !flushed) flush(!flushed);
     }
 }
 
@@ -421,7 +465,9 @@ tgl_status launch_norm(const NormArgs &a, hipStream_t st) {
     with_shape(a.dim, [&](auto L, auto H, auto N, auto Hold) {
         constexpr int kL = decltype(L)::value, kH = decltype(H)::value, kN = decltype(N)::value;
         const int64_t blocks = (a.n + kN / kL - 1) / (kN / kL);
-        norm_kernel<T, kL, kH, kN, decltype(Hold)::value><<<static_cast<unsigned>(blocks < kBlocks ? blocks : kBlocks), kN, 0, st>>>(a);
+        const unsigned grid = static_cast<unsigned>(blocks < kBlocks ? blocks : kBlocks);
+        if (a.dim % E == 0) norm_kernel<T, kL, kH, kN, decltype(Hold)::value, true><<<grid, kN, 0, st>>>(a);
+        else norm_kernel<T, kL, kH, kN, decltype(Hold)::value, false><<<grid, kN, 0, st>>>(a);
     });
     return launch_status();
 }
@@ -433,7 +479,9 @@ int64_t launch_grad(const GradArgs &a, hipStream_t st) {
         constexpr int kL = decltype(L)::value, kH = decltype(H)::value, kN = decltype(N)::value;
         const int64_t most = grad_blocks(a.dim), blocks = (a.n + kN / kL - 1) / (kN / kL);
         count = blocks < most ? blocks : most;
-        norm_grad_kernel<T, kL, kH, kN, decltype(Hold)::value, kParams><<<static_cast<unsigned>(count), kN, 0, st>>>(a);
+        const unsigned grid = static_cast<unsigned>(count);
+        if (a.dim % E == 0) norm_grad_kernel<T, kL, kH, kN, decltype(Hold)::value, true, kParams><<<grid, kN, 0, st>>>(a);
+        else norm_grad_kernel<T, kL, kH, kN, decltype(Hold)::value, false, kParams><<<grid, kN, 0, st>>>(a);
     });
     return count;
 }
