@@ -26,13 +26,14 @@ struct GroupArgs {
     int64_t n;
     int32_t *order;
     int64_t *offsets;
-    uint32_t *counts;       // [bins][chunks]: rows of a bin in a wavefront's chunk, then in all chunks before it
+    uint32_t *counts;       // [bins][pitch]: rows of a bin in a wavefront's chunk, then in all chunks before it
     uint32_t *totals;       // [bins]
     uint16_t *kept;         // bins that were looked up, or null
     int32_t num_types;
     int32_t bits;           // of a bin
     int32_t chunk;          // rows of a wavefront
     int32_t chunks;
+    int32_t pitch;          // chunks, rounded up to 8
 };
 
 template <class K>
@@ -146,33 +147,44 @@ __global__ __launch_bounds__(kThreads) void group_count_kernel(const GroupArgs a
 #pragma unroll
         for (int i = 0; i < kAhead; i++) {
             const bool there = row + i * kWave < end;
-            if (a.kept && there) __builtin_nontemporal_store(static_cast<uint16_t>(bin[i]), a.kept + row + i * kWave);
+            if (a.kept && there) a.kept[row + i * kWave] = static_cast<uint16_t>(bin[i]);
             const uint64_t same = same_bin(bin[i], a.bits, __ballot(there));
             if (there && rank_below(same) == 0) atomicAdd(&count[wave][bin[i]], static_cast<uint32_t>(__popcll(same)));
         }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    for (int b = lane_id(); b < bins; b += kWave) a.counts[static_cast<int64_t>(b) * a.chunks + chunk] = count[wave][b];
+    for (int b = lane_id(); b < bins; b += kWave) a.counts[static_cast<int64_t>(b) * a.pitch + chunk] = count[wave][b];
 }
 
-// A workgroup per bin: its rows in all chunks before each, and in all.
+// A workgroup per bin: its rows in all chunks before each, and in all.  A thread has 8
+// chunks, of the 8192 at most.
 __global__ __launch_bounds__(kThreads) void group_scan_kernel(const GroupArgs a) {
+    using four_t = uint32_t __attribute__((ext_vector_type(4)));
     __shared__ uint32_t parts[kWaves];
-    uint32_t *count = a.counts + static_cast<int64_t>(blockIdx.x) * a.chunks;
-    const int per = (a.chunks + kThreads - 1) / kThreads;       // consecutive ones of a thread, at most 8
-    const int first = threadIdx.x * per;
-    uint32_t v[8], sum = 0;
+    const int first = threadIdx.x * 8;
+    four_t *count = reinterpret_cast<four_t *>(a.counts + static_cast<int64_t>(blockIdx.x) * a.pitch + first);
+    four_t v[2] = {};
+    if (first < a.pitch) {
+        v[0] = count[0];
+        v[1] = count[1];
+    }
+    uint32_t sum = 0;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-        v[i] = i < per && first + i < a.chunks ? count[first + i] : 0;
-        sum += v[i];
+        if (first + i >= a.chunks) v[i / 4][i % 4] = 0;             // what lies behind the chunks
+        sum += v[i / 4][i % 4];
     }
     uint32_t at = before_thread(sum, parts);
     if (threadIdx.x == kThreads - 1) a.totals[blockIdx.x] = at + sum;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-        if (i < per && first + i < a.chunks) count[first + i] = at;
-        at += v[i];
+        const uint32_t own = v[i / 4][i % 4];
+        v[i / 4][i % 4] = at;
+        at += own;
+    }
+    if (first < a.pitch) {
+        count[0] = v[0];
+        count[1] = v[1];
     }
 }
 
@@ -195,7 +207,7 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(const GroupArgs a
         for (int b = t; b < bins; b += kThreads) a.offsets[b] = begin[b];
     if (chunk >= a.chunks) return;
     for (int b = lane_id(); b < bins; b += kWave)
-        count[wave][b] = begin[b] + a.counts[static_cast<int64_t>(b) * a.chunks + chunk];
+        count[wave][b] = begin[b] + a.counts[static_cast<int64_t>(b) * a.pitch + chunk];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     const int64_t end = (chunk + 1) * a.chunk < a.n ? (chunk + 1) * a.chunk : a.n;
     for (int64_t row = chunk * a.chunk + lane_id(); row < end + lane_id(); row += kAhead * kWave) {
@@ -225,7 +237,7 @@ int64_t chunk_rows(int64_t n, int32_t num_types) {
 
 size_t carve(GroupArgs &a, void *base) {
     Carver c(base);
-    a.counts = c.take<uint32_t>(static_cast<size_t>(a.chunks) * (a.num_types + 1));
+    a.counts = c.take<uint32_t>(static_cast<size_t>(a.pitch) * (a.num_types + 1));
     a.totals = c.take<uint32_t>(kBins);
     a.kept = c.take<uint16_t>(static_cast<size_t>(a.n));
     return c.size();
@@ -235,6 +247,7 @@ bool split(GroupArgs &a) {
     if (a.n <= kFew) return false;
     a.chunk = static_cast<int32_t>(chunk_rows(a.n, a.num_types));
     a.chunks = static_cast<int32_t>((a.n + a.chunk - 1) / a.chunk);
+    a.pitch = (a.chunks + 7) & ~7;
     return true;
 }
 
