@@ -46,12 +46,26 @@ __device__ __forceinline__ void banded(uint32_t id, uint32_t rows, uint32_t cols
     r = b * band + (in - c * height);
 }
 
-// A workgroup's number among `work`: the 8 dies take workgroups in turn, and each
-// gets a contiguous stretch of the work.  False if there is none left.
-__device__ __forceinline__ bool die_major(uint32_t work, uint32_t &id) {
-    const uint32_t per = (work + 7) / 8, at = blockIdx.x >> 3;
+// A workgroup's number among `work` pieces of work: the 8 dies take workgroups in
+// turn, and each gets a contiguous stretch.  False if there is none for it; `at`, the
+// workgroup's number within its die, then is the number among those that come after.
+__device__ __forceinline__ bool die_major(uint32_t work, uint32_t &at, uint32_t &id) {
+    const uint32_t per = (work + 7) / 8;
     id = (blockIdx.x & 7) * per + at;
-    return at < per && id < work;
+    at = at < per ? ~0u : at - per;
+    return at == ~0u && id < work;
+}
+
+// Zeros for a tile of the rows of no type.
+template <class T, int BM, int BN>
+__device__ __forceinline__ void clear_tile(const RowsArgs &a, int64_t begin, int n0) {
+    constexpr float kNone[4] = {};
+    const int cols = a.n - n0 < BN ? a.n - n0 : BN;
+    for (int i = threadIdx.x; i < BM * (BN / 4); i += blockDim.x) {
+        const int64_t row = row_at(a.g, begin + i / (BN / 4), a.g.n);
+        const int c = i % (BN / 4) * 4;
+        if (row >= 0 && c < cols) store_columns<T, 4>(static_cast<T *>(a.y) + row * a.ys, n0 + c, a.n, kNone);
+    }
 }
 
 // BM rows of one type times BN columns; a wavefront has 64 columns.
@@ -61,17 +75,25 @@ __global__ __launch_bounds__(NW * kWave, 2) void rows_kernel(const RowsArgs a) {
     // one object each: so the compiler sees that a step's reads do not wait for the others' loads
     __shared__ __attribute__((aligned(1024))) int8_t buf0[(BM + BN) * kStepBytes];
     __shared__ __attribute__((aligned(1024))) int8_t buf1[(BM + BN) * kStepBytes];
-    uint32_t id, tm, tn;
-    const uint32_t tiles_m = count_stretches<true>(a.g, BM, 0);
-    if (!die_major(tiles_m * a.tiles_n, id)) return;
+    uint32_t at = blockIdx.x >> 3, id, tm, tn;
+    Stretches cut(a.g, BM, 0);
+    const uint32_t tiles_m = cut.all();
+    if (!die_major(tiles_m * a.tiles_n, at, id)) {
+        // rows of no type, which every die has its part of
+        const int64_t begin = typed_rows(a.g);
+        const uint32_t clear = static_cast<uint32_t>((a.g.n - begin + BM - 1) / BM) * a.tiles_n;
+        if (at != ~0u && die_major(clear, at, id))
+            clear_tile<T, BM, BN>(a, begin + static_cast<int64_t>(id / a.tiles_n) * BM, id % a.tiles_n * BN);
+        return;
+    }
     banded(id, tiles_m, a.tiles_n, 8, tm, tn);
     Stretch s;
-    if (!find_stretch<true>(a.g, tm, BM, 0, s)) return;
-    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    if (!cut.find(tm, s)) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wm = wave / kWaveN, wn = wave % kWaveN;
     const int n0 = tn * BN;
     f32x4 acc[MT][NT] = {};
-    if (s.type < a.g.num_types) {
+    {
         using X = Along<T, BM, NW, kDirect>;
         using W = std::conditional_t<kAcross, Across<T, BN, NW, kDirect>, Along<T, BN, NW, kDirect>>;
         X x;
@@ -107,7 +129,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void rows_kernel(const RowsArgs a) {
             [&](const int8_t *buf, int h, i32x4(&v)[NT]) { W::read(buf, BM * kStepBytes, wn * 64, h, v); },
             [](const auto &, int) {});
     }
-    const float *bias = a.bias && s.type < a.g.num_types ? a.bias + static_cast<int64_t>(s.type) * a.n : nullptr;
+    const float *bias = a.bias ? a.bias + static_cast<int64_t>(s.type) * a.n : nullptr;
     int32_t row[MT];
 #pragma unroll
     for (int i = 0; i < MT; i++) row[i] = static_cast<int32_t>(row_at(a.g, s.begin + wm * MT * 16 + tile_row<T, false, MT>(i), s.end));
@@ -128,7 +150,6 @@ __global__ __launch_bounds__(NW * kWave, 2) void rows_kernel(const RowsArgs a) {
             store_columns<T, 4>(y, col, a.n, out);
         });
     }
-    (void)lane;
 }
 
 // BM rows times BN columns of dW, over a stretch of a type's rows.
@@ -137,14 +158,15 @@ __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
     constexpr int kWaveN = BN / 64, MT = BM / (NW / kWaveN) / 16, NT = 4;
     __shared__ __attribute__((aligned(1024))) int8_t buf0[(BM + BN) * kStepBytes];
     __shared__ __attribute__((aligned(1024))) int8_t buf1[(BM + BN) * kStepBytes];
-    uint32_t id, to, ti;
-    const uint32_t stretches = count_stretches<false>(a.g, a.rows, 1);
-    if (!die_major((stretches < a.stretches ? stretches : a.stretches) * a.tiles, id)) return;
+    uint32_t at = blockIdx.x >> 3, id, to, ti;
+    Stretches cut(a.g, a.rows, 1);
+    const uint32_t stretches = cut.all();
+    if (!die_major((stretches < a.stretches ? stretches : a.stretches) * a.tiles, at, id)) return;
     const uint32_t stretch = id / a.tiles;
     banded(id - stretch * a.tiles, a.tiles / a.tiles_in, a.tiles_in, 4, to, ti);
     const int o0 = to * BM, c0 = ti * BN;
     Stretch s;
-    if (!find_stretch<false>(a.g, stretch, a.rows, 1, s)) return;
+    if (!cut.find(stretch, s)) return;
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wm = wave / kWaveN, wn = wave % kWaveN;
     f32x4 acc[MT][NT] = {};
@@ -226,7 +248,7 @@ template <class T>
 __global__ __launch_bounds__(kBlock) void sums_join_kernel(const SumsArgs a, uint32_t blocks) {
     const int type = blockIdx.x / blocks;
     int64_t first;
-    const int32_t count = stretches_of_type(a.g, type, a.rows, 1, first);
+    const int32_t count = Stretches(a.g, a.rows, 1).of_type(type, first);
     if (count == 1 || first + count > a.stretches) return;      // offsets that decrease: nothing to read
     const int64_t outs = static_cast<int64_t>(a.out) * a.in;
     for (int64_t i = static_cast<int64_t>(blockIdx.x % blocks) * kBlock + threadIdx.x; i < outs + (a.db ? a.out : 0);
@@ -288,7 +310,7 @@ constexpr int64_t kMostBlocks = int64_t(1) << 22;       // of a launch, whose th
 template <class T, bool kAcross, int B, int NW, bool kDirect>
 tgl_status launch_rows(RowsArgs a, hipStream_t st) {
     a.tiles_n = (a.n + B - 1) / B;
-    const int64_t work = (a.g.n / B + a.g.num_types + 1) * a.tiles_n;
+    const int64_t work = (a.g.n / B + a.g.num_types + 1) * a.tiles_n + 8;        // a die rounds up twice
     if (work > kMostBlocks) return TGL_EINVAL;
     rows_kernel<T, kAcross, B, B, NW, kDirect><<<static_cast<unsigned>((work + 7) / 8 * 8), NW * kWave, 0, st>>>(a);
     return launch_status();
@@ -296,7 +318,7 @@ tgl_status launch_rows(RowsArgs a, hipStream_t st) {
 
 template <class T, bool kAcross>
 tgl_status launch_rows(const RowsArgs &a, bool direct, hipStream_t st) {
-    const int tile = tile_of(a.g.n, a.n);
+    const int tile = sizeof(T) == 4 ? 64 : tile_of(a.g.n, a.n);
     if (!direct) return tile == 64 ? launch_rows<T, kAcross, 64, 4, false>(a, st) : launch_rows<T, kAcross, 128, 4, false>(a, st);
     if constexpr (sizeof(T) == 2)
         if (tile == 256) return launch_rows<T, kAcross, 256, 8, true>(a, st);

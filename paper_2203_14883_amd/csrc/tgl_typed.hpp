@@ -18,10 +18,10 @@ struct Groups {
     int32_t num_types;
 };
 
-// A number that all lanes have, held once for all.
-__device__ __forceinline__ int64_t uniform(int64_t v) {
-    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v));
-    const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(static_cast<uint64_t>(v) >> 32));
+// What one lane has, for all.
+__device__ __forceinline__ int64_t lane_of(int64_t v, int lane) {
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(v), lane);
+    const uint32_t hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(static_cast<uint64_t>(v) >> 32), lane);
     return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
@@ -33,72 +33,90 @@ struct Stretch {
     int64_t begin, end;
 };
 
-// The places of 64 types from `first` on, a lane each, cut into stretches of
-// `rows`: types without rows have `least`, and the rows of no type follow the last
-// type where kNone.
-template <bool kNone>
-__device__ __forceinline__ int32_t stretches_of(const Groups &g, int first, int32_t rows, int32_t least, int64_t &begin, int64_t &end) {
-    const int t = first + lane_id();
-    begin = end = 0;
-    if (t >= g.num_types + (kNone ? 1 : 0)) return 0;
-    begin = t == 0 ? 0 : g.offsets[t];
-    end = t == g.num_types ? g.n : g.offsets[t + 1];
-    begin = begin < 0 ? 0 : begin > g.n ? g.n : begin;
-    end = end > g.n ? g.n : end < begin ? begin : end;
-    const int32_t count = static_cast<int32_t>((end - begin + rows - 1) / rows);
-    return count < least ? least : count;
+// Inclusive sum over the 64 lanes, in registers: these sums stand before every tile's first load.
+__device__ __forceinline__ uint32_t lanes_sum(uint32_t v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // within rows of 16: 1, 2, 4, 8 lanes below
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // a row's last to the row above it
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // the lower half's last to the upper half
+    return v;
 }
 
-// Stretches in all.  Asked by whole wavefronts, as the next is.
-template <bool kNone>
-__device__ __forceinline__ uint32_t count_stretches(const Groups &g, int32_t rows, int32_t least) {
-    uint32_t all = 0;
-    for (int first = 0; first < g.num_types + (kNone ? 1 : 0); first += kWave) {
-        int64_t begin, end;
-        const uint32_t upto = wave_inclusive_sum(static_cast<uint32_t>(stretches_of<kNone>(g, first, rows, least, begin, end)));
-        all += __builtin_amdgcn_readlane(upto, kWave - 1);
-    }
-    return all;
-}
+// The types of a call, 64 at a time, cut into stretches of `rows` places: types
+// without rows have `least`.  Asked by whole wavefronts, whose lanes have a type each.
+struct Stretches {
+    const Groups &g;
+    int32_t rows, least;
+    int64_t begin, end;         // of the lane's type
+    int32_t count;
+    uint32_t upto;              // stretches of types up to the lane's, from `first` on
 
-// Stretch number `at`; false beyond the last.
-template <bool kNone>
-__device__ __forceinline__ bool find_stretch(const Groups &g, uint32_t at, int32_t rows, int32_t least, Stretch &s) {
-    uint32_t before = 0;
-    for (int first = 0; first < g.num_types + (kNone ? 1 : 0); first += kWave) {
-        int64_t begin, end;
-        const int32_t count = stretches_of<kNone>(g, first, rows, least, begin, end);
-        const uint32_t upto = before + wave_inclusive_sum(static_cast<uint32_t>(count));
-        const uint64_t past = __ballot(at < upto);
-        if (past) {
-            const int lane = __builtin_ctzll(past);
-            s.type = first + lane;
-            s.count = __builtin_amdgcn_readlane(count, lane);
-            s.index = static_cast<int32_t>(at - (__builtin_amdgcn_readlane(upto, lane) - s.count));
-            const int64_t b = uniform(__shfl(begin, lane, kWave)), e = uniform(__shfl(end, lane, kWave));
-            s.begin = b + static_cast<int64_t>(s.index) * rows;
-            s.end = s.begin + rows < e ? s.begin + rows : e;
-            return true;
+    __device__ __forceinline__ Stretches(const Groups &g_, int32_t rows_, int32_t least_) : g(g_), rows(rows_), least(least_) {}
+
+    __device__ __forceinline__ void take(int first) {
+        const int t = first + lane_id();
+        begin = end = 0;
+        count = 0;
+        if (t < g.num_types) {
+            begin = t == 0 ? 0 : g.offsets[t];
+            end = g.offsets[t + 1];
+            begin = begin < 0 ? 0 : begin > g.n ? g.n : begin;
+            end = end > g.n ? g.n : end < begin ? begin : end;
+            count = static_cast<int32_t>((end - begin + rows - 1) / rows);
+            if (count < least) count = least;
         }
-        before = __builtin_amdgcn_readlane(upto, kWave - 1);
+        upto = lanes_sum(static_cast<uint32_t>(count));
     }
-    return false;
-}
-
-// The stretches of a type and, in first, how many there are before them.
-__device__ __forceinline__ int32_t stretches_of_type(const Groups &g, int32_t type, int32_t rows, int32_t least, int64_t &first) {
-    first = 0;
-    for (int t = 0;; t += kWave) {
-        int64_t begin, end;
-        const int32_t count = stretches_of<false>(g, t, rows, least, begin, end);
-        const uint32_t upto = wave_inclusive_sum(static_cast<uint32_t>(count));
-        if (type < t + kWave) {
-            const int32_t own = __builtin_amdgcn_readlane(count, type - t);
-            first += __builtin_amdgcn_readlane(upto, type - t) - own;
-            return own;
+    // Stretches in all.
+    __device__ __forceinline__ uint32_t all() {
+        uint32_t sum = 0;
+        for (int first = 0; first < g.num_types; first += kWave) {
+            take(first);
+            sum += __builtin_amdgcn_readlane(upto, kWave - 1);
         }
-        first += __builtin_amdgcn_readlane(upto, kWave - 1);
+        return sum;
     }
+    // Stretch number `at`; false beyond the last.  After all().
+    __device__ __forceinline__ bool find(uint32_t at, Stretch &s) {
+        uint32_t before = 0;
+        for (int first = 0; first < g.num_types; first += kWave) {
+            if (g.num_types > kWave) take(first);           // otherwise they are still there
+            const uint64_t past = __ballot(at < before + upto);
+            if (past) {
+                const int lane = __builtin_ctzll(past);
+                s.type = first + lane;
+                s.count = __builtin_amdgcn_readlane(count, lane);
+                s.index = static_cast<int32_t>(at - (before + __builtin_amdgcn_readlane(upto, lane) - s.count));
+                const int64_t b = lane_of(begin, lane), e = lane_of(end, lane);
+                s.begin = b + static_cast<int64_t>(s.index) * rows;
+                s.end = s.begin + rows < e ? s.begin + rows : e;
+                return true;
+            }
+            before += __builtin_amdgcn_readlane(upto, kWave - 1);
+        }
+        return false;
+    }
+    // The number of a type's stretches and, in first, of those before them.
+    __device__ __forceinline__ int32_t of_type(int32_t type, int64_t &before) {
+        before = 0;
+        for (int first = 0;; first += kWave) {
+            take(first);
+            if (type < first + kWave) {
+                const int32_t own = __builtin_amdgcn_readlane(count, type - first);
+                before += __builtin_amdgcn_readlane(upto, type - first) - own;
+                return own;
+            }
+            before += __builtin_amdgcn_readlane(upto, kWave - 1);
+        }
+    }
+};
+
+// Where the rows of no type begin.
+__device__ __forceinline__ int64_t typed_rows(const Groups &g) {
+    const int64_t v = g.offsets[g.num_types];
+    return v < 0 ? 0 : v > g.n ? g.n : v;
 }
 
 // The row at a place of order, or -1 if there is none.
