@@ -68,42 +68,23 @@ __device__ __forceinline__ void clear_tile(const RowsArgs &a, int64_t begin, int
     }
 }
 
-// BM rows of one type times BN columns; a wavefront has 64 columns.
-template <class T, bool kAcross, int BM, int BN, int NW, bool kDirect>
-__global__ __launch_bounds__(NW * kWave, 2) void rows_kernel(const RowsArgs a) {
-    constexpr int kWaveN = BN / 64, MT = BM / (NW / kWaveN) / 16, NT = 4;
-    // one object each: so the compiler sees that a step's reads do not wait for the others' loads
-    __shared__ __attribute__((aligned(1024))) int8_t buf0[(BM + BN) * kStepBytes];
-    __shared__ __attribute__((aligned(1024))) int8_t buf1[(BM + BN) * kStepBytes];
-    uint32_t at = blockIdx.x >> 3, id, tm, tn;
-    Stretches cut(a.g, BM, 0);
-    const uint32_t tiles_m = cut.all();
-    if (!die_major(tiles_m * a.tiles_n, at, id)) {
-        // rows of no type, which every die has its part of
-        const int64_t begin = typed_rows(a.g);
-        const uint32_t clear = static_cast<uint32_t>((a.g.n - begin + BM - 1) / BM) * a.tiles_n;
-        if (at != ~0u && die_major(clear, at, id))
-            clear_tile<T, BM, BN>(a, begin + static_cast<int64_t>(id / a.tiles_n) * BM, id % a.tiles_n * BN);
-        return;
-    }
-    banded(id, tiles_m, a.tiles_n, 8, tm, tn);
-    Stretch s;
-    if (!cut.find(tm, s)) return;
+// ROWS rows of one type, BM of them at most, times BN columns; a wavefront has 64 columns.
+template <class T, bool kAcross, int ROWS, int BM, int BN, int NW, int SB, bool kDirect>
+__device__ __forceinline__ void rows_tile(const RowsArgs &a, const Stretch &s, int n0, int8_t (&steps_of)[2][(BM + BN) * SB]) {
+    constexpr int kWaveN = BN / 64, MT = ROWS / (NW / kWaveN) / 16, NT = 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wm = wave / kWaveN, wn = wave % kWaveN;
-    const int n0 = tn * BN;
     f32x4 acc[MT][NT] = {};
+    using X = Along<T, ROWS, NW, SB, kDirect>;
+    using W = std::conditional_t<kAcross, Across<T, BN, NW, SB, kDirect>, Along<T, BN, NW, SB, kDirect>>;
     {
-        using X = Along<T, BM, NW, kDirect>;
-        using W = std::conditional_t<kAcross, Across<T, BN, NW, kDirect>, Along<T, BN, NW, kDirect>>;
         X x;
         W w;
         x.length = a.k;
+        int32_t row[X::kFetch];
+        rows_at(a.g, s.end, [&](int f) { return s.begin + X::edge(wave, f); }, row);
 #pragma unroll
-        for (int f = 0; f < X::kFetch; f++) {
-            const int64_t row = row_at(a.g, s.begin + X::edge(wave, f), s.end);
-            x.set(wave, f, static_cast<const T *>(a.x) + (row < 0 ? 0 : row) * a.xs);
-        }
+        for (int f = 0; f < X::kFetch; f++) x.set(wave, f, static_cast<const T *>(a.x) + (row[f] < 0 ? 0 : row[f]) * a.xs);
         const T *weights = static_cast<const T *>(a.w) + s.type * a.wt;
         if constexpr (kAcross) {
             w.set(wave, weights, a.ws, a.k, n0, a.n);
@@ -115,24 +96,20 @@ __global__ __launch_bounds__(NW * kWave, 2) void rows_kernel(const RowsArgs a) {
                 w.set(wave, f, weights + (c < a.n ? c : a.n - 1) * a.ws);
             }
         }
-        multiply_steps<T, false, kAcross>(
-            (a.k + kStep<T> - 1) / kStep<T>, buf0, buf1, acc,
-            [&](int step, int8_t *buf) {
-                x.fetch(wave, step, buf);
-                w.fetch(wave, step, buf + BM * kStepBytes);
-            },
+        multiply_steps<T, false, kAcross, SB>(
+            (a.k + kStep<T, SB> - 1) / kStep<T, SB>, [&](int i) { return steps_of[i]; }, acc,
+            [&](int step, int8_t *buf) { x.fetch(wave, step, buf); },
+            [&](int step, int8_t *buf) { w.fetch(wave, step, buf + BM * SB); },
             [&](int8_t *buf) {
                 x.store(wave, buf);
-                w.store(wave, buf + BM * kStepBytes);
+                w.store(wave, buf + BM * SB);
             },
             [&](const int8_t *buf, int h, int first, auto &v) { X::read(buf, 0, (wm * MT + first) * 16, h, v); },
-            [&](const int8_t *buf, int h, i32x4(&v)[NT]) { W::read(buf, BM * kStepBytes, wn * 64, h, v); },
-            [](const auto &, int) {});
+            [&](const int8_t *buf, int h, i32x4(&v)[NT]) { W::read(buf, BM * SB, wn * 64, h, v); }, [](const auto &, int) {});
     }
     const float *bias = a.bias ? a.bias + static_cast<int64_t>(s.type) * a.n : nullptr;
     int32_t row[MT];
-#pragma unroll
-    for (int i = 0; i < MT; i++) row[i] = static_cast<int32_t>(row_at(a.g, s.begin + wm * MT * 16 + tile_row<T, false, MT>(i), s.end));
+    rows_at(a.g, s.end, [&](int i) { return s.begin + wm * MT * 16 + tile_row<T, false, MT>(i); }, row);
 #pragma unroll
     for (int i = 0; i < MT; i++) {
         if (row[i] < 0) continue;
@@ -152,18 +129,55 @@ __global__ __launch_bounds__(NW * kWave, 2) void rows_kernel(const RowsArgs a) {
     }
 }
 
+template <class T, bool kAcross, int BM, int BN, int NW, int SB, bool kDirect>
+__global__ __launch_bounds__(NW * kWave, 2) void rows_kernel(const RowsArgs a) {
+    __shared__ __attribute__((aligned(1024))) int8_t steps_of[2][(BM + BN) * SB];
+    uint32_t at = blockIdx.x >> 3, id, tm, tn;
+    Stretches cut(a.g, BM, 0, 0);
+    const uint32_t tiles_m = cut.all();
+    if (!die_major(tiles_m * a.tiles_n, at, id)) {
+        // rows of no type, which every die has its part of
+        const int64_t begin = typed_rows(a.g);
+        const uint32_t clear = static_cast<uint32_t>((a.g.n - begin + BM - 1) / BM) * a.tiles_n;
+        if (at != ~0u && die_major(clear, at, id))
+            clear_tile<T, BM, BN>(a, begin + static_cast<int64_t>(id / a.tiles_n) * BM, id % a.tiles_n * BN);
+        return;
+    }
+    banded(id, tiles_m, a.tiles_n, 8, tm, tn);
+    Stretch s;
+    if (!cut.find(tm, s)) return;
+    // a type's last rows fill half a tile as often as not: half the products then (16,384 rows of 8 types, 4096
+    // x 4096 in bfloat16: 68 tiles of rows where 64 would do, 646 us without)
+    if constexpr (BM == 256) {
+        if (s.end - s.begin <= BM / 2) {
+            rows_tile<T, kAcross, BM / 2, BM, BN, NW, SB, kDirect>(a, s, tn * BN, steps_of);
+            return;
+        }
+    }
+    rows_tile<T, kAcross, BM, BM, BN, NW, SB, kDirect>(a, s, tn * BN, steps_of);
+}
+
 // BM rows times BN columns of dW, over a stretch of a type's rows.
-template <class T, int BM, int BN, int NW, bool kDirect>
+template <class T, int BM, int BN, int NW, int SB, bool kDirect>
 __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
     constexpr int kWaveN = BN / 64, MT = BM / (NW / kWaveN) / 16, NT = 4;
-    __shared__ __attribute__((aligned(1024))) int8_t buf0[(BM + BN) * kStepBytes];
-    __shared__ __attribute__((aligned(1024))) int8_t buf1[(BM + BN) * kStepBytes];
-    uint32_t at = blockIdx.x >> 3, id, to, ti;
-    Stretches cut(a.g, a.rows, 1);
-    const uint32_t stretches = cut.all();
-    if (!die_major((stretches < a.stretches ? stretches : a.stretches) * a.tiles, at, id)) return;
-    const uint32_t stretch = id / a.tiles;
-    banded(id - stretch * a.tiles, a.tiles / a.tiles_in, a.tiles_in, 4, to, ti);
+    __shared__ __attribute__((aligned(1024))) int8_t steps_of[2][(BM + BN) * SB];
+    // A stretch's tiles, which read the same rows, go to one die.  Many stretches, whose lengths differ, go to the
+    // dies in turn; few are cut into tiles for all dies.
+    uint32_t at = blockIdx.x >> 3, stretch, tile, to, ti;
+    if (a.stretches >= 64) {
+        stretch = at / a.tiles * 8 + (blockIdx.x & 7);
+        tile = at % a.tiles;
+        if (stretch >= a.stretches) return;
+    } else {
+        uint32_t id;
+        if (!die_major(a.stretches * a.tiles, at, id)) return;
+        stretch = id / a.tiles;
+        tile = id - stretch * a.tiles;
+    }
+    banded(tile, a.tiles / a.tiles_in, a.tiles_in, 4, to, ti);
+    Stretches cut(a.g, a.rows, 1, kStep<T, SB>);
+    if (a.g.num_types <= kWave) cut.take(0);
     const int o0 = to * BM, c0 = ti * BN;
     Stretch s;
     if (!cut.find(stretch, s)) return;
@@ -173,34 +187,30 @@ __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
     constexpr int kSums = (MT + kWaveN - 1) / kWaveN;
     float sum[kSums] = {};                      // of dy, tiles wn, wn + kWaveN, ... of the wavefront's rows
     const bool want_sum = a.db && ti == 0;
-    using D = Gathered<T, BM, NW, kDirect>;
-    using X = Gathered<T, BN, NW, kDirect>;
-    const int steps = static_cast<int>((s.end - s.begin + kStep<T> - 1) / kStep<T>);
-    if (steps > 0) {
+    using D = Gathered<T, BM, NW, SB, kDirect>;
+    using X = Gathered<T, BN, NW, SB, kDirect>;
+    if (s.end > s.begin) {
         D d;
         X x;
         d.set(static_cast<const T *>(a.dy), a.dys, o0, a.out);
         x.set(static_cast<const T *>(a.x), a.xs, c0, a.in);
-        // The lane's row of a step, from order a step earlier: looked at only when it is used, since that waits for every
-        // load before it.
-        const int32_t mine = wave * D::kOwn + lane % D::kOwn, places = static_cast<int32_t>(s.end - s.begin);
-        auto place_of = [&](int step) { return step * kStep<T> + mine < places ? step * kStep<T> + mine : places - 1; };
-        int32_t ids = a.g.order ? a.g.order[s.begin + place_of(0)] : 0;
-        multiply_steps<T, true, true>(
-            steps, buf0, buf1, acc,
-            [&](int step, int8_t *buf) {
-                int32_t id = a.g.order ? ids : static_cast<int32_t>(s.begin) + place_of(step);
-                if (step * kStep<T> + mine >= places || id >= a.g.n) id = -1;
-                d.fetch(wave, id, buf);
-                x.fetch(wave, id, buf + BM * kStepBytes);
-                if (a.g.order) ids = a.g.order[s.begin + place_of(step + 1)];
+        Places<kStep<T, SB> / NW> places(a.g, s.begin, s.end, wave * (kStep<T, SB> / NW));
+        multiply_steps<T, true, true, SB>(
+            static_cast<int>((s.end - s.begin + kStep<T, SB> - 1) / kStep<T, SB>), [&](int i) { return steps_of[i]; }, acc,
+            [&](int, int8_t *buf) {
+                places.advance(kStep<T, SB>);
+                d.fetch(wave, places, buf);
+            },
+            [&](int, int8_t *buf) {
+                x.fetch(wave, places, buf + BM * SB);
+                places.load();
             },
             [&](int8_t *buf) {
                 d.store(wave, buf);
-                x.store(wave, buf + BM * kStepBytes);
+                x.store(wave, buf + BM * SB);
             },
             [&](const int8_t *buf, int h, int first, auto &v) { D::read(buf, 0, (wm * MT + first) * 16, h, v); },
-            [&](const int8_t *buf, int h, i32x4(&v)[NT]) { X::read(buf, BM * kStepBytes, wn * 64, h, v); },
+            [&](const int8_t *buf, int h, i32x4(&v)[NT]) { X::read(buf, BM * SB, wn * 64, h, v); },
             [&](const auto &dv, int first) {
                 if (!want_sum) return;
 #pragma unroll
@@ -243,27 +253,37 @@ __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
     }
 }
 
-// The stretches of a type together, one after another.
+// The stretches of a type together, one after another: four outputs a thread.
 template <class T>
 __global__ __launch_bounds__(kBlock) void sums_join_kernel(const SumsArgs a, uint32_t blocks) {
     const int type = blockIdx.x / blocks;
     int64_t first;
-    const int32_t count = Stretches(a.g, a.rows, 1).of_type(type, first);
+    const int32_t count = Stretches(a.g, a.rows, 1, 0).of_type(type, first);
     if (count == 1 || first + count > a.stretches) return;      // offsets that decrease: nothing to read
     const int64_t outs = static_cast<int64_t>(a.out) * a.in;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x % blocks) * kBlock + threadIdx.x; i < outs + (a.db ? a.out : 0);
-         i += static_cast<int64_t>(blocks) * kBlock) {
-        const int64_t step = i < outs ? outs : a.out;
-        const float *p = i < outs ? a.parts + first * outs + i : a.parts_b + first * a.out + (i - outs);
-        float sum = 0.0f;
-#pragma unroll 4
-        for (int32_t c = 0; c < count; c++) sum += p[c * step];
-        if (i < outs) static_cast<T *>(a.dw)[type * outs + i] = from_float<T>(sum);
-        else a.db[static_cast<int64_t>(type) * a.out + (i - outs)] = sum;
+    auto join = [&](const float *parts, int64_t n, int64_t i, float (&sum)[4]) {
+        // as many loads on their way as there are registers for
+#pragma unroll 8
+        for (int32_t c = 0; c < count; c++) {
+            float v[4];
+            load_columns<float, 4>(parts + (first + c) * n + i, 0, n - i < 4 ? static_cast<int>(n - i) : 4, v);
+#pragma unroll
+            for (int e = 0; e < 4; e++) sum[e] += v[e];
+        }
+    };
+    const int64_t step = static_cast<int64_t>(blocks) * kBlock * 4;
+    for (int64_t i = (static_cast<int64_t>(blockIdx.x % blocks) * kBlock + threadIdx.x) * 4; i < outs; i += step) {
+        float sum[4] = {};
+        join(a.parts, outs, i, sum);
+        store_columns<T, 4>(static_cast<T *>(a.dw) + type * outs + i, 0, outs - i < 4 ? static_cast<int>(outs - i) : 4, sum);
+    }
+    if (!a.db) return;
+    for (int64_t i = (static_cast<int64_t>(blockIdx.x % blocks) * kBlock + threadIdx.x) * 4; i < a.out; i += step) {
+        float sum[4] = {};
+        join(a.parts_b, a.out, i, sum);
+        store_columns<float, 4>(a.db + static_cast<int64_t>(type) * a.out + i, 0, a.out - i < 4 ? static_cast<int>(a.out - i) : 4, sum);
     }
 }
-
-constexpr int kTarget = 512;            // workgroups that fill the card
 
 // The tiles of a call's outputs: the largest of which there are still enough.
 int tile_of(int64_t rows, int64_t cols) {
@@ -274,12 +294,13 @@ int tile_of(int64_t rows, int64_t cols) {
 // dW: its tiles, and the rows of a stretch, of which there are as many as fill the card.
 void plan_sums(SumsArgs &a, int32_t dtype) {
     const bool wide = dtype == TGL_OUT_BF16 && a.out >= 192 && a.in >= 192 && a.g.n / a.g.num_types >= 2048;
-    a.tile = wide ? 256 : a.out > 64 && a.in > 64 && a.g.n / a.g.num_types >= 512 ? 128 : 64;
+    a.tile = wide ? 256 : dtype == TGL_OUT_BF16 && a.out > 64 && a.in > 64 && a.g.n / a.g.num_types >= 512 ? 128 : 64;
     a.tiles_in = (a.in + a.tile - 1) / a.tile;
     a.tiles = (a.out + a.tile - 1) / a.tile * a.tiles_in;
-    const int64_t most = (kTarget + a.tiles - 1) / a.tiles;
+    const int64_t target = a.tile == 256 ? 512 : a.tile == 128 ? 1024 : 2560;        // twice what runs at a time
+    const int64_t most = (target + a.tiles - 1) / a.tiles;
     int64_t rows = (a.g.n + most - 1) / most;
-    if (rows < 512) rows = 512;
+    if (rows < 256) rows = 256;
     a.rows = static_cast<int32_t>(rows < (1 << 30) ? (rows + 63) / 64 * 64 : 1 << 30);
     a.stretches = static_cast<uint32_t>(a.g.n / a.rows + a.g.num_types);
 }
@@ -305,6 +326,7 @@ Groups groups_of(const tgl_row_groups *g) { return Groups{g->order, g->offsets, 
 
 bool wide_rows(const void *p, int64_t stride, size_t e) { return aligned(p, 16) && stride * static_cast<int64_t>(e) % 16 == 0; }
 
+constexpr int kStepBytes = 128;                         // of the sum's axis
 constexpr int64_t kMostBlocks = int64_t(1) << 22;       // of a launch, whose threads are fewer than 2^32
 
 template <class T, bool kAcross, int B, int NW, bool kDirect>
@@ -312,17 +334,20 @@ tgl_status launch_rows(RowsArgs a, hipStream_t st) {
     a.tiles_n = (a.n + B - 1) / B;
     const int64_t work = (a.g.n / B + a.g.num_types + 1) * a.tiles_n + 8;        // a die rounds up twice
     if (work > kMostBlocks) return TGL_EINVAL;
-    rows_kernel<T, kAcross, B, B, NW, kDirect><<<static_cast<unsigned>((work + 7) / 8 * 8), NW * kWave, 0, st>>>(a);
+    rows_kernel<T, kAcross, B, B, NW, kStepBytes, kDirect><<<static_cast<unsigned>((work + 7) / 8 * 8), NW * kWave, 0, st>>>(a);
     return launch_status();
 }
 
 template <class T, bool kAcross>
 tgl_status launch_rows(const RowsArgs &a, bool direct, hipStream_t st) {
-    const int tile = sizeof(T) == 4 ? 64 : tile_of(a.g.n, a.n);
-    if (!direct) return tile == 64 ? launch_rows<T, kAcross, 64, 4, false>(a, st) : launch_rows<T, kAcross, 128, 4, false>(a, st);
-    if constexpr (sizeof(T) == 2)
-        if (tile == 256) return launch_rows<T, kAcross, 256, 8, true>(a, st);
-    return tile == 64 ? launch_rows<T, kAcross, 64, 4, true>(a, st) : launch_rows<T, kAcross, 128, 4, true>(a, st);
+    // float32's products take 16 times as long as bfloat16's, so loads are no matter and the smallest tiles waste least:
+    // 120,000 rows of 272 -> 128 in tiles of 64 98 us, of 128 112; 40,000 of 272 -> 100 47 and 55
+    if constexpr (sizeof(T) == 2) {
+        const int tile = tile_of(a.g.n, a.n);
+        if (tile == 256 && direct) return launch_rows<T, kAcross, 256, 8, true>(a, st);
+        if (tile >= 128) return direct ? launch_rows<T, kAcross, 128, 4, true>(a, st) : launch_rows<T, kAcross, 128, 4, false>(a, st);
+    }
+    return direct ? launch_rows<T, kAcross, 64, 4, true>(a, st) : launch_rows<T, kAcross, 64, 4, false>(a, st);
 }
 
 template <bool kAcross>
@@ -345,18 +370,19 @@ tgl_status rows_call(const tgl_row_groups *groups, const void *x, int64_t x_stri
 
 template <class T, int B, int NW, bool kDirect>
 tgl_status launch_sums(const SumsArgs &a, hipStream_t st) {
-    const int64_t work = static_cast<int64_t>(a.stretches) * a.tiles;
+    const int64_t work = (static_cast<int64_t>(a.stretches) + 7) / 8 * 8 * a.tiles;
     if (work > kMostBlocks) return TGL_EINVAL;
-    sums_kernel<T, B, B, NW, kDirect><<<static_cast<unsigned>((work + 7) / 8 * 8), NW * kWave, 0, st>>>(a);
+    sums_kernel<T, B, B, NW, kStepBytes, kDirect><<<static_cast<unsigned>(work), NW * kWave, 0, st>>>(a);
     return launch_status();
 }
 
 template <class T>
 tgl_status launch_sums(const SumsArgs &a, bool direct, hipStream_t st) {
-    if (!direct) return a.tile == 64 ? launch_sums<T, 64, 4, false>(a, st) : launch_sums<T, 128, 4, false>(a, st);
-    if constexpr (sizeof(T) == 2)
+    if constexpr (sizeof(T) == 2) {
         if (a.tile == 256) return launch_sums<T, 256, 8, true>(a, st);
-    return a.tile == 64 ? launch_sums<T, 64, 4, true>(a, st) : launch_sums<T, 128, 4, true>(a, st);
+        if (a.tile == 128) return direct ? launch_sums<T, 128, 4, true>(a, st) : launch_sums<T, 128, 4, false>(a, st);
+    }
+    return direct ? launch_sums<T, 64, 4, true>(a, st) : launch_sums<T, 64, 4, false>(a, st);
 }
 
 }  // namespace
@@ -422,8 +448,8 @@ tgl_status tgl_linear_typed_grad_w(const tgl_row_groups *groups, const void *dy,
     (void)hipGetLastError();
     const tgl_status done = dtype == TGL_OUT_F32 ? launch_sums<float>(a, direct, st) : launch_sums<bf16_t>(a, direct, st);
     if (!need || done != TGL_OK) return done;
-    // types that are cut are few: a workgroup for every 2048 outputs of each, 2048 in all at most
-    const int64_t each = (static_cast<int64_t>(out) * in + 2047) / 2048, most = (2048 + a.g.num_types - 1) / a.g.num_types;
+    // a workgroup for every 1024 outputs of a type, 4096 in all: most types are not cut
+    const int64_t each = (static_cast<int64_t>(out) * in + 1023) / 1024, most = (4096 + a.g.num_types - 1) / a.g.num_types;
     const uint32_t blocks = static_cast<uint32_t>(each < most ? each : most);
     const unsigned join = static_cast<unsigned>(a.g.num_types) * blocks;
     if (dtype == TGL_OUT_F32) sums_join_kernel<float><<<join, kBlock, 0, st>>>(a, blocks);

@@ -48,12 +48,13 @@ __device__ __forceinline__ uint32_t lanes_sum(uint32_t v) {
 // without rows have `least`.  Asked by whole wavefronts, whose lanes have a type each.
 struct Stretches {
     const Groups &g;
-    int32_t rows, least;
+    int32_t rows, least, even;  // even > 0: a type's stretches are alike, in units of `even` places
     int64_t begin, end;         // of the lane's type
     int32_t count;
     uint32_t upto;              // stretches of types up to the lane's, from `first` on
 
-    __device__ __forceinline__ Stretches(const Groups &g_, int32_t rows_, int32_t least_) : g(g_), rows(rows_), least(least_) {}
+    __device__ __forceinline__ Stretches(const Groups &g_, int32_t rows_, int32_t least_, int32_t even_)
+        : g(g_), rows(rows_), least(least_), even(even_) {}
 
     __device__ __forceinline__ void take(int first) {
         const int t = first + lane_id();
@@ -90,8 +91,10 @@ struct Stretches {
                 s.count = __builtin_amdgcn_readlane(count, lane);
                 s.index = static_cast<int32_t>(at - (before + __builtin_amdgcn_readlane(upto, lane) - s.count));
                 const int64_t b = lane_of(begin, lane), e = lane_of(end, lane);
-                s.begin = b + static_cast<int64_t>(s.index) * rows;
-                s.end = s.begin + rows < e ? s.begin + rows : e;
+                int32_t each = rows;
+                if (even > 0 && s.count > 1) each = static_cast<int32_t>((e - b + s.count - 1) / s.count + even - 1) / even * even;
+                s.begin = b + static_cast<int64_t>(s.index) * each;
+                s.end = s.begin + each < e ? s.begin + each : e;
                 return true;
             }
             before += __builtin_amdgcn_readlane(upto, kWave - 1);
@@ -124,6 +127,22 @@ __device__ __forceinline__ int64_t row_at(const Groups &g, int64_t place, int64_
     if (place >= end) return -1;
     const int64_t row = g.order ? g.order[place] : place;
     return row >= 0 && row < g.n ? row : -1;
+}
+
+// The same at N places, place(0), place(1), ..., of [begin, end), which is not empty: all of them
+// on their way at a time.
+template <int N, class F>
+__device__ __forceinline__ void rows_at(const Groups &g, int64_t end, const F &place, int32_t (&row)[N]) {
+    if (g.order) {
+#pragma unroll
+        for (int i = 0; i < N; i++) row[i] = g.order[place(i) < end ? place(i) : end - 1];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i++) row[i] = static_cast<int32_t>(place(i));
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++)
+        if (place(i) >= end || row[i] >= g.n) row[i] = -1;
 }
 
 // ---- 16 bytes of a row ----
