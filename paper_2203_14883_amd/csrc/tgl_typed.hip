@@ -96,7 +96,7 @@ __device__ __forceinline__ void rows_tile(const RowsArgs &a, const Stretch &s, i
                 w.set(wave, f, weights + (c < a.n ? c : a.n - 1) * a.ws);
             }
         }
-        multiply_steps<T, false, kAcross, SB>(
+        multiply_steps<T, false, kAcross, true, SB>(
             (a.k + kStep<T, SB> - 1) / kStep<T, SB>, [&](int i) { return steps_of[i]; }, acc,
             [&](int step, int8_t *buf) { x.fetch(wave, step, buf); },
             [&](int step, int8_t *buf) { w.fetch(wave, step, buf + BM * SB); },
@@ -165,19 +165,20 @@ __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
     // A stretch's tiles, which read the same rows, go to one die.  Many stretches, whose lengths differ, go to the
     // dies in turn; few are cut into tiles for all dies.
     uint32_t at = blockIdx.x >> 3, stretch, tile, to, ti;
+    Stretches cut(a.g, a.rows, 1, kStep<T, SB>);
     if (a.stretches >= 64) {
         stretch = at / a.tiles * 8 + (blockIdx.x & 7);
         tile = at % a.tiles;
         if (stretch >= a.stretches) return;
+        if (a.g.num_types <= kWave) cut.take(0);
     } else {
+        const uint32_t stretches = cut.all();
         uint32_t id;
-        if (!die_major(a.stretches * a.tiles, at, id)) return;
+        if (!die_major((stretches < a.stretches ? stretches : a.stretches) * a.tiles, at, id)) return;
         stretch = id / a.tiles;
         tile = id - stretch * a.tiles;
     }
     banded(tile, a.tiles / a.tiles_in, a.tiles_in, 4, to, ti);
-    Stretches cut(a.g, a.rows, 1, kStep<T, SB>);
-    if (a.g.num_types <= kWave) cut.take(0);
     const int o0 = to * BM, c0 = ti * BN;
     Stretch s;
     if (!cut.find(stretch, s)) return;
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
         d.set(static_cast<const T *>(a.dy), a.dys, o0, a.out);
         x.set(static_cast<const T *>(a.x), a.xs, c0, a.in);
         Places<kStep<T, SB> / NW> places(a.g, s.begin, s.end, wave * (kStep<T, SB> / NW));
-        multiply_steps<T, true, true, SB>(
+        multiply_steps<T, true, true, false, SB>(
             static_cast<int>((s.end - s.begin + kStep<T, SB> - 1) / kStep<T, SB>), [&](int i) { return steps_of[i]; }, acc,
             [&](int, int8_t *buf) {
                 places.advance(kStep<T, SB>);

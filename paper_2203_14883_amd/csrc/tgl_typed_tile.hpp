@@ -349,14 +349,14 @@ constexpr int kGroup = M < 4 ? M : 4;
 // x once.  Buffers are filled a step ahead; what is multiplied next is read while the tiles
 // before it are multiplied, over a step's end too.  Loads are taken no faster than the
 // memory's pipe has room, and a wavefront does nothing else until they are: so a step's two sides
-// are asked for apart, with products between.
+// are asked for apart (kApart), with products between, unless both need a look at LDS before that.
 //
 // Bound by the matrix units at the clocks that the card's power leaves them: 16384 x 4096 x 4096 in
 // bfloat16, one type, 493 us and its rows' gradient 470, where the library's products take 449 and
 // 525; without its loads 350 to 365, without its reads of LDS 420 to 440.  Three and four buffers of half a
 // step each, wavefronts that take turns at multiplying and loading, and 4 wavefronts of 128 x 128
 // outputs measured the same or up to a fifth more.
-template <class T, bool kAcrossX, bool kAcrossW, int SB, int M, int N, class Buffer, class FetchX, class FetchW, class Store, class ReadX,
+template <class T, bool kAcrossX, bool kAcrossW, bool kApart, int SB, int M, int N, class Buffer, class FetchX, class FetchW, class Store, class ReadX,
           class ReadW, class Used>
 __device__ __forceinline__ void multiply_steps(int steps, const Buffer &buffer, f32x4 (&acc)[M][N], const FetchX &fetch_x,
                                                const FetchW &fetch_w, const Store &store, const ReadX &read_x, const ReadW &read_w,
@@ -385,12 +385,15 @@ __device__ __forceinline__ void multiply_steps(int steps, const Buffer &buffer, 
                     read_x(buffer(turn), next / kGroups, next % kGroups * K, x[next & 1]);
                     if constexpr (next % kGroups == 0) read_w(buffer(turn), next / kGroups, w[next / kGroups]);
                     // the other side of what the last step began to bring
-                    if constexpr (u == 0)
+                    if constexpr (u == 0 && kApart)
                         if (step > 0 && step + 1 < steps) fetch_w(step + 1, buffer(1 - turn));
                 } else {
                     if (step + 1 < steps) store(buffer(1 - turn));
                     meet();
-                    if (step + 2 < steps) fetch_x(step + 2, buffer(turn));
+                    if (step + 2 < steps) {
+                        fetch_x(step + 2, buffer(turn));
+                        if constexpr (!kApart) fetch_w(step + 2, buffer(turn));
+                    }
                     if (step + 1 < steps) {
                         read_x(buffer(1 - turn), 0, 0, x[0]);
                         read_w(buffer(1 - turn), 0, w[0]);
