@@ -157,6 +157,67 @@ __global__ __launch_bounds__(NW * kWave, 2) void rows_kernel(const RowsArgs a) {
     rows_tile<T, kAcross, BM, BM, BN, NW, SB, kDirect>(a, s, tn * BN, steps_of);
 }
 
+// Few rows: a workgroup per 16 rows of a type and 16 columns, operands straight
+// from memory.  Its wavefronts take pieces of the sum's axis in turn and add up through LDS, in
+// their order.  Bound by latency where the weights are small (a row of 768 -> 2304 bfloat16 5 us, in
+// tiles of 64 8) and by their bytes where they are not.
+template <class T, int NW>
+__global__ __launch_bounds__(NW * kWave) void rows_few_kernel(const RowsArgs a) {
+    __shared__ f32x4 sums[NW][kWave];
+    constexpr int kAhead = 4;                   // pieces of a lane on their way
+    Stretches cut(a.g, 16, 0, 0);
+    const uint32_t tiles_m = cut.all(), tm = blockIdx.x / a.tiles_n;
+    const int n0 = static_cast<int>(blockIdx.x - tm * a.tiles_n) * 16;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    if (tm >= tiles_m) {
+        const int64_t begin = typed_rows(a.g) + static_cast<int64_t>(tm - tiles_m) * 16;
+        if (begin < a.g.n) clear_tile<T, 16, 16>(a, begin, n0);
+        return;
+    }
+    Stretch s;
+    if (!cut.find(tm, s)) return;
+    int32_t row[1];
+    rows_at(a.g, s.end, [&](int) { return s.begin + (lane & 15); }, row);
+    const T *x = static_cast<const T *>(a.x) + (row[0] < 0 ? 0 : row[0]) * a.xs;
+    const int c = n0 + (lane & 15);
+    const T *w = static_cast<const T *>(a.w) + s.type * a.wt + (c < a.n ? c : a.n - 1) * a.ws;
+    constexpr int E = kPiece<T>, kLength = 4 * E;               // of the sum's axis that a wavefront takes at a time
+    using word_t = i32x4 __attribute__((aligned(alignof(T))));
+    f32x4 acc[1][1] = {};
+    int k = wave * kLength + (lane >> 4) * E;
+    const int mine = wave * kLength;
+    for (; mine + (k - (mine + (lane >> 4) * E)) + (kAhead - 1) * NW * kLength + kLength <= a.k; k += kAhead * NW * kLength) {
+        i32x4 xv[kAhead][1], wv[kAhead][1];
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            wv[u][0] = *reinterpret_cast<const word_t *>(w + k + u * NW * kLength);
+            xv[u][0] = *reinterpret_cast<const word_t *>(x + k + u * NW * kLength);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) multiply<T, false, false>(xv[u], wv[u], 0, acc);
+    }
+    for (; k - (lane >> 4) * E < a.k; k += NW * kLength) {
+        const i32x4 xv[1] = {load_piece(x, k, a.k)}, wv[1] = {load_piece(w, k, a.k)};
+        multiply<T, false, false>(xv, wv, 0, acc);
+    }
+    sums[wave][lane] = acc[0][0];
+    __syncthreads();
+    if (wave != 0 || row[0] < 0) return;
+    f32x4 sum = sums[0][lane];
+#pragma unroll
+    for (int i = 1; i < NW; i++) sum += sums[i][lane];
+    const int col = n0 + 4 * (lane >> 4);
+    if (col >= a.n) return;
+    float out[4] = {sum[0], sum[1], sum[2], sum[3]};
+    if (a.bias) {
+        float b[4];
+        load_columns<float, 4>(a.bias + static_cast<int64_t>(s.type) * a.n, col, a.n, b);
+#pragma unroll
+        for (int e = 0; e < 4; e++) out[e] += b[e];
+    }
+    store_columns<T, 4>(static_cast<T *>(a.y) + row[0] * a.ys, col, a.n, out);
+}
+
 // BM rows times BN columns of dW, over a stretch of a type's rows.
 template <class T, int BM, int BN, int NW, int SB, bool kDirect>
 __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
@@ -327,6 +388,7 @@ Groups groups_of(const tgl_row_groups *g) { return Groups{g->order, g->offsets, 
 
 bool wide_rows(const void *p, int64_t stride, size_t e) { return aligned(p, 16) && stride * static_cast<int64_t>(e) % 16 == 0; }
 
+constexpr int kFewRows = 64;                            // that are not worth tiles
 constexpr int kStepBytes = 128;                         // of the sum's axis
 constexpr int64_t kMostBlocks = int64_t(1) << 22;       // of a launch, whose threads are fewer than 2^32
 
@@ -339,8 +401,19 @@ tgl_status launch_rows(RowsArgs a, hipStream_t st) {
     return launch_status();
 }
 
+template <class T>
+tgl_status launch_few(RowsArgs a, hipStream_t st) {
+    a.tiles_n = (a.n + 15) / 16;
+    const unsigned grid = static_cast<unsigned>((a.g.n / 16 + a.g.num_types + 2) * a.tiles_n);
+    if (a.k * sizeof(T) <= 512) rows_few_kernel<T, 4><<<grid, 4 * kWave, 0, st>>>(a);
+    else rows_few_kernel<T, 8><<<grid, 8 * kWave, 0, st>>>(a);
+    return launch_status();
+}
+
 template <class T, bool kAcross>
 tgl_status launch_rows(const RowsArgs &a, bool direct, hipStream_t st) {
+    if constexpr (!kAcross)
+        if (a.g.n <= kFewRows && (a.g.n / 16 + a.g.num_types + 2) * ((a.n + 15) / 16) <= (1 << 18)) return launch_few<T>(a, st);
     // float32's products take 16 times as long as bfloat16's, so loads are no matter and the smallest tiles waste least:
     // 120,000 rows of 272 -> 128 in tiles of 64 98 us, of 128 112; 40,000 of 272 -> 100 47 and 55
     if constexpr (sizeof(T) == 2) {
