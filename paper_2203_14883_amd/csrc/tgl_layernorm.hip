@@ -420,8 +420,10 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const double *parts, in
     const int64_t c = static_cast<int64_t>(blockIdx.x) * 16 + threadIdx.x % 16;
     const int slice = threadIdx.x / 16;
     double sum = 0.0;
-    if (c < 2 * static_cast<int64_t>(dim))
+    if (c < 2 * static_cast<int64_t>(dim)) {
+#pragma unroll 8
         for (int p = slice; p < count; p += 64) sum += parts[static_cast<int64_t>(p) * 2 * dim + c];
+    }
     sum += __shfl_xor(sum, 16, kWave);
     sum += __shfl_xor(sum, 32, kWave);
     if (lane_id() < 16) lds[threadIdx.x / kWave][lane_id()] = sum;
@@ -437,8 +439,8 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const double *parts, in
     }
 }
 
-// Workgroups of a call at most: each takes several rows in turn, and reads the
-// weights and writes the sums of their gradients once.
+// Workgroups of a call at most: each takes several rows in turn, four where there
+// are enough for every compute unit, and reads the weights and writes the sums of their gradients once.
 constexpr int64_t kBlocks = 2048;
 int64_t grad_blocks(int32_t dim) { return dim <= 1024 ? 1024 : dim <= 4096 ? 512 : 256; }
 
@@ -478,7 +480,7 @@ int64_t launch_grad(const GradArgs &a, hipStream_t st) {
     with_shape(a.dim, [&](auto L, auto H, auto N, auto Hold) {
         constexpr int kL = decltype(L)::value, kH = decltype(H)::value, kN = decltype(N)::value;
         const int64_t most = grad_blocks(a.dim), blocks = (a.n + kN / kL - 1) / (kN / kL);
-        count = blocks < most ? blocks : most;
+        count = blocks < 256 ? blocks : blocks / 4 < 256 ? 256 : blocks / 4 < most ? blocks / 4 : most;
         const unsigned grid = static_cast<unsigned>(count);
         if (a.dim % E == 0) norm_grad_kernel<T, kL, kH, kN, decltype(Hold)::value, true, kParams><<<grid, kN, 0, st>>>(a);
         else norm_grad_kernel<T, kL, kH, kN, decltype(Hold)::value, false, kParams><<<grid, kN, 0, st>>>(a);

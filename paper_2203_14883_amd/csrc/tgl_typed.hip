@@ -347,10 +347,12 @@ __global__ __launch_bounds__(kBlock) void sums_join_kernel(const SumsArgs a, uin
     }
 }
 
-// The tiles of a call's outputs: the largest of which there are still enough.
+// The tiles of a call's outputs in bfloat16: the largest of which there are still enough.  us
+// of tiles of 256 / 128 / 64: 132,000 rows of 768 -> 256 90 / - / 121, 12,000 of 768 -> 1024 33 / 35 / 43, 20,000 of 16 types
+// 58 / - / 73, 40,000 of 272 -> 128 - / 14 / 15.
 int tile_of(int64_t rows, int64_t cols) {
     auto tiles = [&](int64_t t) { return (rows + t - 1) / t * ((cols + t - 1) / t); };
-    return tiles(256) >= 192 ? 256 : tiles(128) >= 256 ? 128 : 64;
+    return tiles(256) >= 160 ? 256 : tiles(128) >= 256 ? 128 : 64;
 }
 
 // dW: its tiles, and the rows of a stretch, of which there are as many as fill the card.
@@ -388,7 +390,6 @@ Groups groups_of(const tgl_row_groups *g) { return Groups{g->order, g->offsets, 
 
 bool wide_rows(const void *p, int64_t stride, size_t e) { return aligned(p, 16) && stride * static_cast<int64_t>(e) % 16 == 0; }
 
-constexpr int kFewRows = 64;                            // that are not worth tiles
 constexpr int kStepBytes = 128;                         // of the sum's axis
 constexpr int64_t kMostBlocks = int64_t(1) << 22;       // of a launch, whose threads are fewer than 2^32
 
@@ -399,6 +400,15 @@ tgl_status launch_rows(RowsArgs a, hipStream_t st) {
     if (work > kMostBlocks) return TGL_EINVAL;
     rows_kernel<T, kAcross, B, B, NW, kStepBytes, kDirect><<<static_cast<unsigned>((work + 7) / 8 * 8), NW * kWave, 0, st>>>(a);
     return launch_status();
+}
+
+// Whether a call is too small for tiles of 64, by its tiles of 16: up to 900 of them; in float32, whose products
+// take long, also where they cover half of what tiles of 64 would, as those of many types with few rows.  us of tiles
+// of 64 / 16: bfloat16 65 x 768 x 1024 of 4 types 7.7 / 5.4, 1801 x 272 x 100 of 3 5.1 / 4.4, 200 x 768 x 1024 of 4 7.9 / 8.4,
+// of 64 17 / 22; float32 19.9 / 8.1, 9.4 / 5.7, 20 / 13.8, 70 / 37, 1000 x 768 x 768 of 3 23 / 39.
+bool few_rows(const RowsArgs &a, size_t e) {
+    auto tiles = [&](int64_t t) { return (a.g.n / t + (a.g.n < a.g.num_types ? a.g.n : a.g.num_types)) * ((a.n + t - 1) / t); };
+    return tiles(16) <= 900 || (e == 4 && tiles(16) <= 8192 && 2 * tiles(16) <= 16 * tiles(64));
 }
 
 template <class T>
@@ -413,7 +423,7 @@ tgl_status launch_few(RowsArgs a, hipStream_t st) {
 template <class T, bool kAcross>
 tgl_status launch_rows(const RowsArgs &a, bool direct, hipStream_t st) {
     if constexpr (!kAcross)
-        if (a.g.n <= kFewRows && (a.g.n / 16 + a.g.num_types + 2) * ((a.n + 15) / 16) <= (1 << 18)) return launch_few<T>(a, st);
+        if (few_rows(a, sizeof(T))) return launch_few<T>(a, st);
     // float32's products take 16 times as long as bfloat16's, so loads are no matter and the smallest tiles waste least:
     // 120,000 rows of 272 -> 128 in tiles of 64 98 us, of 128 112; 40,000 of 272 -> 100 47 and 55
     if constexpr (sizeof(T) == 2) {

@@ -18,7 +18,7 @@ for every call of the library.
 from __future__ import annotations
 
 import ctypes as C
-from dataclasses import dataclass
+from dataclasses import dataclass, field
 from typing import Optional
 
 import torch
@@ -113,6 +113,7 @@ class RowGroups:
     neither is checked (kernels stay within the rows whatever they hold)."""
     offsets: torch.Tensor
     order: Optional[torch.Tensor] = None
+    _view: Optional[c_row_groups] = field(init=False, repr=False, compare=False, default=None)
 
     def __post_init__(self):
         f, o = self.offsets, self.order
@@ -123,6 +124,10 @@ class RowGroups:
                 raise ValueError("order must be a contiguous int32 vector")
             if o.get_device() != f.get_device():
                 raise ValueError("order and offsets must be on the same device")
+            object.__setattr__(self, "_view", c_row_groups(o.data_ptr() or None, f.data_ptr(), o.shape[0], self.num_types, 0))
+
+    def __reduce__(self):                   # copies and pickles: the view is made anew, of the copy's tensors
+        return type(self), (self.offsets, self.order)
 
     @property
     def num_types(self) -> int:
@@ -130,11 +135,13 @@ class RowGroups:
 
     def c_view(self, n: int, dev: int) -> c_row_groups:
         """The groups of a call with n rows."""
-        o = self.order
-        if o is not None and o.shape[0] != n:
-            raise ValueError("the groups are of %d rows, not of %d" % (o.shape[0], n))
         _also(self.offsets, "the groups", dev)
-        return c_row_groups(None if o is None else o.data_ptr() or None, self.offsets.data_ptr(), n, self.num_types, 0)
+        v = self._view
+        if v is None:
+            return c_row_groups(None, self.offsets.data_ptr(), n, self.num_types, 0)
+        if v.n != n:
+            raise ValueError("the groups are of %d rows, not of %d" % (v.n, n))
+        return v
 
 
 def group_rows(types: torch.Tensor, num_types: int, ids: Optional[torch.Tensor] = None, stream=None) -> RowGroups:
