@@ -27,14 +27,15 @@ struct SumsArgs {               // dW and db
     const void *x;
     void *dw;
     float *db;
-    float *parts;               // [stretches][out][in] sums of types cut into several, then [stretches][out]
-    float *parts_b;
+    float *parts;               // [room][out][in] sums of the stretches of types that are cut into several
+    float *parts_b;             // [room][out]
     int64_t dys, xs;
     int32_t out, in;
     int32_t rows;               // of a stretch
     int32_t tile;
     int32_t tiles_in, tiles;    // tiles of dW
-    uint32_t stretches;         // there is room for
+    uint32_t stretches;         // at most
+    uint32_t room;              // of those of types that are cut, at most
 };
 
 // Tile `id` of rows x cols, in bands of `band` rows walked column by column, so
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
     banded(tile, a.tiles / a.tiles_in, a.tiles_in, 4, to, ti);
     const int o0 = to * BM, c0 = ti * BN;
     Stretch s;
-    if (!cut.find(stretch, s)) return;
+    if (!cut.find(stretch, s) || (s.count > 1 && s.part >= a.room)) return;     // (offsets that decrease)
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wm = wave / kWaveN, wn = wave % kWaveN;
     f32x4 acc[MT][NT] = {};
@@ -302,7 +303,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
             v += __shfl_xor(v, 32, kWave);
             if (lane < 16 && o < a.out) {
                 if (s.count == 1) a.db[static_cast<int64_t>(s.type) * a.out + o] = v;
-                else a.parts_b[static_cast<int64_t>(stretch) * a.out + o] = v;
+                else a.parts_b[static_cast<int64_t>(s.part) * a.out + o] = v;
             }
         }
         if (o >= a.out) continue;
@@ -310,7 +311,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
             const int col = c0 + wn * 64 + c;
             if (col >= a.in) return;
             if (s.count == 1) store_columns<T, 4>(static_cast<T *>(a.dw) + s.type * outs + static_cast<int64_t>(o) * a.in, col, a.in, v);
-            else store_columns<float, 4>(a.parts + stretch * outs + static_cast<int64_t>(o) * a.in, col, a.in, v);
+            else store_columns<float, 4>(a.parts + s.part * outs + static_cast<int64_t>(o) * a.in, col, a.in, v);
         });
     }
 }
@@ -320,8 +321,8 @@ template <class T>
 __global__ __launch_bounds__(kBlock) void sums_join_kernel(const SumsArgs a, uint32_t blocks) {
     const int type = blockIdx.x / blocks;
     int64_t first;
-    const int32_t count = Stretches(a.g, a.rows, 1, 0).of_type(type, first);
-    if (count == 1 || first + count > a.stretches) return;      // offsets that decrease: nothing to read
+    const int32_t count = Stretches(a.g, a.rows, 1, 1).of_type(type, first);
+    if (count == 1 || first + count > a.room) return;      // offsets that decrease: nothing to read
     const int64_t outs = static_cast<int64_t>(a.out) * a.in;
     auto join = [&](const float *parts, int64_t n, int64_t i, float (&sum)[4]) {
         // as many loads on their way as there are registers for
@@ -367,13 +368,14 @@ void plan_sums(SumsArgs &a, int32_t dtype) {
     if (rows < 256) rows = 256;
     a.rows = static_cast<int32_t>(rows < (1 << 30) ? (rows + 63) / 64 * 64 : 1 << 30);
     a.stretches = static_cast<uint32_t>(a.g.n / a.rows + a.g.num_types);
+    a.room = static_cast<uint32_t>(2 * (a.g.n / a.rows));       // a type of more than `rows` has fewer than twice its share
 }
 
 size_t carve(SumsArgs &a, void *base) {
     Carver c(base);
     if (a.g.n <= a.rows) return 0;              // no type is cut
-    a.parts = c.take<float>(static_cast<size_t>(a.stretches) * a.out * a.in);
-    a.parts_b = c.take<float>(static_cast<size_t>(a.stretches) * a.out);
+    a.parts = c.take<float>(static_cast<size_t>(a.room) * a.out * a.in);
+    a.parts_b = c.take<float>(static_cast<size_t>(a.room) * a.out);
     return c.size();
 }
 
@@ -391,13 +393,14 @@ Groups groups_of(const tgl_row_groups *g) { return Groups{g->order, g->offsets, 
 bool wide_rows(const void *p, int64_t stride, size_t e) { return aligned(p, 16) && stride * static_cast<int64_t>(e) % 16 == 0; }
 
 constexpr int kStepBytes = 128;                         // of the sum's axis
-constexpr int64_t kMostBlocks = int64_t(1) << 22;       // of a launch, whose threads are fewer than 2^32
+template <int NW>
+constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - 1) / (NW * kWave);     // of a launch, whose threads are fewer than 2^32
 
 template <class T, bool kAcross, int B, int NW, bool kDirect>
 tgl_status launch_rows(RowsArgs a, hipStream_t st) {
     a.tiles_n = (a.n + B - 1) / B;
     const int64_t work = (a.g.n / B + a.g.num_types + 1) * a.tiles_n + 8;        // a die rounds up twice
-    if (work > kMostBlocks) return TGL_EINVAL;
+    if (work + 8 > kMostBlocks<NW>) return TGL_EINVAL;
     rows_kernel<T, kAcross, B, B, NW, kStepBytes, kDirect><<<static_cast<unsigned>((work + 7) / 8 * 8), NW * kWave, 0, st>>>(a);
     return launch_status();
 }
@@ -455,7 +458,7 @@ tgl_status rows_call(const tgl_row_groups *groups, const void *x, int64_t x_stri
 template <class T, int B, int NW, bool kDirect>
 tgl_status launch_sums(const SumsArgs &a, hipStream_t st) {
     const int64_t work = (static_cast<int64_t>(a.stretches) + 7) / 8 * 8 * a.tiles;
-    if (work > kMostBlocks) return TGL_EINVAL;
+    if (work + 8 > kMostBlocks<NW>) return TGL_EINVAL;
     sums_kernel<T, B, B, NW, kStepBytes, kDirect><<<static_cast<unsigned>(work), NW * kWave, 0, st>>>(a);
     return launch_status();
 }

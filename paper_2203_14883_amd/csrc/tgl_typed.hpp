@@ -30,6 +30,7 @@ struct Stretch {
     int32_t type;               // num_types for rows of no type
     int32_t count;              // stretches of the type
     int32_t index;              // this one's number among them
+    uint32_t part;              // and among those of types that are cut into several
     int64_t begin, end;
 };
 
@@ -51,7 +52,7 @@ struct Stretches {
     int32_t rows, least, even;  // even > 0: a type's stretches are alike, in units of `even` places
     int64_t begin, end;         // of the lane's type
     int32_t count;
-    uint32_t upto;              // stretches of types up to the lane's, from `first` on
+    uint32_t upto, upto_cut;    // stretches of types up to the lane's, from `first` on; of those that are cut
 
     __device__ __forceinline__ Stretches(const Groups &g_, int32_t rows_, int32_t least_, int32_t even_)
         : g(g_), rows(rows_), least(least_), even(even_) {}
@@ -69,6 +70,7 @@ struct Stretches {
             if (count < least) count = least;
         }
         upto = lanes_sum(static_cast<uint32_t>(count));
+        if (even > 0) upto_cut = lanes_sum(count > 1 ? static_cast<uint32_t>(count) : 0u);
     }
     // Stretches in all.
     __device__ __forceinline__ uint32_t all() {
@@ -81,7 +83,7 @@ struct Stretches {
     }
     // Stretch number `at`; false beyond the last.  After all().
     __device__ __forceinline__ bool find(uint32_t at, Stretch &s) {
-        uint32_t before = 0;
+        uint32_t before = 0, before_cut = 0;
         for (int first = 0; first < g.num_types; first += kWave) {
             if (g.num_types > kWave) take(first);           // otherwise they are still there
             const uint64_t past = __ballot(at < before + upto);
@@ -92,26 +94,28 @@ struct Stretches {
                 s.index = static_cast<int32_t>(at - (before + __builtin_amdgcn_readlane(upto, lane) - s.count));
                 const int64_t b = lane_of(begin, lane), e = lane_of(end, lane);
                 int32_t each = rows;
+                s.part = even > 0 ? before_cut + __builtin_amdgcn_readlane(upto_cut, lane) - s.count + s.index : 0;
                 if (even > 0 && s.count > 1) each = static_cast<int32_t>((e - b + s.count - 1) / s.count + even - 1) / even * even;
                 s.begin = b + static_cast<int64_t>(s.index) * each;
                 s.end = s.begin + each < e ? s.begin + each : e;
                 return true;
             }
             before += __builtin_amdgcn_readlane(upto, kWave - 1);
+            if (even > 0) before_cut += __builtin_amdgcn_readlane(upto_cut, kWave - 1);
         }
         return false;
     }
-    // The number of a type's stretches and, in first, of those before them.
+    // The number of a type's stretches and, in before, of those of cut types before them.
     __device__ __forceinline__ int32_t of_type(int32_t type, int64_t &before) {
         before = 0;
         for (int first = 0;; first += kWave) {
             take(first);
             if (type < first + kWave) {
                 const int32_t own = __builtin_amdgcn_readlane(count, type - first);
-                before += __builtin_amdgcn_readlane(upto, type - first) - own;
+                before += __builtin_amdgcn_readlane(upto_cut, type - first) - (own > 1 ? own : 0);
                 return own;
             }
-            before += __builtin_amdgcn_readlane(upto, kWave - 1);
+            before += __builtin_amdgcn_readlane(upto_cut, kWave - 1);
         }
     }
 };

@@ -102,6 +102,9 @@ def test_weights_gradient_refuses():
     assert need > 0
     assert _grad_w(groups=many, bytes=need - 1) == B.ENOSPACE and _grad_w(groups=many, ws=None) == B.ENOSPACE
     assert _grad_w(groups=many, ws=FAKE + 4) == B.EINVAL
+    # parts are kept of types that are cut into several only, whatever the number of types
+    some = _groups(n=130_000, G=300)
+    assert P.lib().tgl_linear_typed_grad_w_workspace(C.byref(some), 4096, 1024, 0) < 12 * 4096 * 1024 * 4
 
 
 def _norm(**kw):

@@ -150,7 +150,8 @@ def test_linear_typed_of_many_rows(torch, n, k, out, G, empty, dtype):
     """Sums over rows in several parts, tiles of every size."""
     announce("linear_typed of many %d x %d -> %d, %d types, %s" % (n, k, out, G, dtype))
     rng = np.random.default_rng(n + k + out)
-    t = np.minimum(rng.geometric(0.5, n) - 1, G - 1)
+    t = np.minimum(rng.geometric(0.5, n) - 1, G - 1)        # some types have many rows, others few or none
+    t = (t * 37 + 3) % G
     t[rng.random(n) < empty] = -1
     x, _ = _up(torch, rng.standard_normal((n, k)), dtype)
     w, _ = _up(torch, rng.standard_normal((G, out, k)), dtype)
