@@ -145,7 +145,7 @@ def test_linear_typed(torch, n, k, out, G, dtype):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("n,k,out,G,empty", [(5000, 272, 100, 3, 0.1), (5003, 100, 272, 2, 0.0), (20_000, 64, 72, 40, 0.3), (3001, 520, 776, 2, 0.0),
                                              (9000, 128, 256, 1, 0.0), (4096, 768, 1024, 3, 0.05), (2500, 1023, 515, 2, 0.1), (1500, 1024, 2304, 1, 0.0),
-                                             (70_000, 48, 33, 3, 0.9)])
+                                             (70_000, 48, 33, 3, 0.9), (40_000, 200, 264, 200, 0.0), (50_000, 256, 512, 6, 0.02)])
 def test_linear_typed_of_many_rows(torch, n, k, out, G, empty, dtype):
     """Sums over rows in several parts, tiles of every size."""
     announce("linear_typed of many %d x %d -> %d, %d types, %s" % (n, k, out, G, dtype))
