@@ -226,11 +226,13 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(const GroupArgs a
     }
 }
 
-// Rows of a wavefront's chunk: enough for 8192 chunks, and for counts that are fewer
-// than a quarter of the rows.
+// Rows of a wavefront's chunk: so many that there are 8192 chunks at most, 2048 as long as a
+// chunk has 128 rows (counting 120,000 slots 7 us, in chunks of 512 16), and fewer counts than a
+// quarter of the rows.
 int64_t chunk_rows(int64_t n, int32_t num_types) {
     int64_t rows = (n + 8191) / 8192;
-    if (rows < 512) rows = 512;
+    const int64_t spread = n / 2048 < 128 ? 128 : n / 2048 < 512 ? n / 2048 : 512;
+    if (rows < spread) rows = spread;
     if (rows < 4 * num_types) rows = 4 * num_types;
     return (rows + kWave - 1) / kWave * kWave;
 }
