@@ -159,10 +159,11 @@ __global__ __launch_bounds__(NW * kWave, 2) void rows_kernel(const RowsArgs a) {
 }
 
 // Few rows: a workgroup per 16 rows of a type and 16 columns, operands straight
-// from memory.  Its wavefronts take pieces of the sum's axis in turn and add up through LDS, in
+// from memory (kAcross: the weights element by element, 16 columns of a row of memory at a
+// time).  Its wavefronts take pieces of the sum's axis in turn and add up through LDS, in
 // their order.  Bound by latency where the weights are small (a row of 768 -> 2304 bfloat16 5 us, in
 // tiles of 64 8) and by their bytes where they are not.
-template <class T, int NW>
+template <class T, bool kAcross, int NW>
 __global__ __launch_bounds__(NW * kWave) void rows_few_kernel(const RowsArgs a) {
     __shared__ f32x4 sums[NW][kWave];
     constexpr int kAhead = 4;                   // pieces of a lane on their way
@@ -181,24 +182,35 @@ __global__ __launch_bounds__(NW * kWave) void rows_few_kernel(const RowsArgs a) 
     rows_at(a.g, s.end, [&](int) { return s.begin + (lane & 15); }, row);
     const T *x = static_cast<const T *>(a.x) + (row[0] < 0 ? 0 : row[0]) * a.xs;
     const int c = n0 + (lane & 15);
-    const T *w = static_cast<const T *>(a.w) + s.type * a.wt + (c < a.n ? c : a.n - 1) * a.ws;
+    const T *w = static_cast<const T *>(a.w) + s.type * a.wt + (c < a.n ? c : a.n - 1) * (kAcross ? 1 : a.ws);
     constexpr int E = kPiece<T>, kLength = 4 * E;               // of the sum's axis that a wavefront takes at a time
     using word_t = i32x4 __attribute__((aligned(alignof(T))));
     f32x4 acc[1][1] = {};
-    int k = wave * kLength + (lane >> 4) * E;
-    const int mine = wave * kLength;
-    for (; mine + (k - (mine + (lane >> 4) * E)) + (kAhead - 1) * NW * kLength + kLength <= a.k; k += kAhead * NW * kLength) {
+    auto weights = [&](int k, bool whole) {
+        if constexpr (kAcross) {
+            Run<T, E> v = {};
+#pragma unroll
+            for (int i = 0; i < E; i++)
+                if (whole || k + i < a.k) v.t[i] = w[(k + i) * a.ws];
+            return __builtin_bit_cast(i32x4, v);
+        } else {
+            return whole ? static_cast<i32x4>(*reinterpret_cast<const word_t *>(w + k)) : load_piece(w, k, a.k);
+        }
+    };
+    const int own = (lane >> 4) * E;
+    int k = wave * kLength;
+    for (; k + (kAhead - 1) * NW * kLength + kLength <= a.k; k += kAhead * NW * kLength) {
         i32x4 xv[kAhead][1], wv[kAhead][1];
 #pragma unroll
         for (int u = 0; u < kAhead; u++) {
-            wv[u][0] = *reinterpret_cast<const word_t *>(w + k + u * NW * kLength);
-            xv[u][0] = *reinterpret_cast<const word_t *>(x + k + u * NW * kLength);
+            wv[u][0] = weights(k + own + u * NW * kLength, true);
+            xv[u][0] = *reinterpret_cast<const word_t *>(x + k + own + u * NW * kLength);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; u++) multiply<T, false, false>(xv[u], wv[u], 0, acc);
     }
-    for (; k - (lane >> 4) * E < a.k; k += NW * kLength) {
-        const i32x4 xv[1] = {load_piece(x, k, a.k)}, wv[1] = {load_piece(w, k, a.k)};
+    for (; k < a.k; k += NW * kLength) {
+        const i32x4 xv[1] = {load_piece(x, k + own, a.k)}, wv[1] = {weights(k + own, false)};
         multiply<T, false, false>(xv, wv, 0, acc);
     }
     sums[wave][lane] = acc[0][0];
@@ -414,19 +426,18 @@ bool few_rows(const RowsArgs &a, size_t e) {
     return tiles(16) <= 900 || (e == 4 && tiles(16) <= 8192 && 2 * tiles(16) <= 16 * tiles(64));
 }
 
-template <class T>
+template <class T, bool kAcross>
 tgl_status launch_few(RowsArgs a, hipStream_t st) {
     a.tiles_n = (a.n + 15) / 16;
     const unsigned grid = static_cast<unsigned>((a.g.n / 16 + a.g.num_types + 2) * a.tiles_n);
-    if (a.k * sizeof(T) <= 512) rows_few_kernel<T, 4><<<grid, 4 * kWave, 0, st>>>(a);
-    else rows_few_kernel<T, 8><<<grid, 8 * kWave, 0, st>>>(a);
+    if (a.k * sizeof(T) <= 512) rows_few_kernel<T, kAcross, 4><<<grid, 4 * kWave, 0, st>>>(a);
+    else rows_few_kernel<T, kAcross, 8><<<grid, 8 * kWave, 0, st>>>(a);
     return launch_status();
 }
 
 template <class T, bool kAcross>
 tgl_status launch_rows(const RowsArgs &a, bool direct, hipStream_t st) {
-    if constexpr (!kAcross)
-        if (few_rows(a, sizeof(T))) return launch_few<T>(a, st);
+    if (few_rows(a, sizeof(T))) return launch_few<T, kAcross>(a, st);
     // float32's products take 16 times as long as bfloat16's, so loads are no matter and the smallest tiles waste least:
     // 120,000 rows of 272 -> 128 in tiles of 64 98 us, of 128 112; 40,000 of 272 -> 100 47 and 55
     if constexpr (sizeof(T) == 2) {
