@@ -404,6 +404,9 @@ Groups groups_of(const tgl_row_groups *g) { return Groups{g->order, g->offsets, 
 
 bool wide_rows(const void *p, int64_t stride, size_t e) { return aligned(p, 16) && stride * static_cast<int64_t>(e) % 16 == 0; }
 
+// Types that can have rows.  Tiles of t rows are n / t and one for each of these and for the rows of no type at most.
+int64_t filled_types(const Groups &g) { return g.n < g.num_types ? g.n : g.num_types; }
+
 constexpr int kStepBytes = 128;                         // of the sum's axis
 template <int NW>
 constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - 1) / (NW * kWave);     // of a launch, whose threads are fewer than 2^32
@@ -411,7 +414,7 @@ constexpr int64_t kMostBlocks = ((int64_t(1) << 32) - 1) / (NW * kWave);     // 
 template <class T, bool kAcross, int B, int NW, bool kDirect>
 tgl_status launch_rows(RowsArgs a, hipStream_t st) {
     a.tiles_n = (a.n + B - 1) / B;
-    const int64_t work = (a.g.n / B + a.g.num_types + 1) * a.tiles_n + 8;        // a die rounds up twice
+    const int64_t work = (a.g.n / B + filled_types(a.g) + 1) * a.tiles_n + 8;        // a die rounds up twice
     if (work + 8 > kMostBlocks<NW>) return TGL_EINVAL;
     rows_kernel<T, kAcross, B, B, NW, kStepBytes, kDirect><<<static_cast<unsigned>((work + 7) / 8 * 8), NW * kWave, 0, st>>>(a);
     return launch_status();
@@ -422,14 +425,14 @@ tgl_status launch_rows(RowsArgs a, hipStream_t st) {
 // of 64 / 16: bfloat16 65 x 768 x 1024 of 4 types 7.7 / 5.4, 1801 x 272 x 100 of 3 5.1 / 4.4, 200 x 768 x 1024 of 4 7.9 / 8.4,
 // of 64 17 / 22; float32 19.9 / 8.1, 9.4 / 5.7, 20 / 13.8, 70 / 37, 1000 x 768 x 768 of 3 23 / 39.
 bool few_rows(const RowsArgs &a, size_t e) {
-    auto tiles = [&](int64_t t) { return (a.g.n / t + (a.g.n < a.g.num_types ? a.g.n : a.g.num_types)) * ((a.n + t - 1) / t); };
+    auto tiles = [&](int64_t t) { return (a.g.n / t + filled_types(a.g)) * ((a.n + t - 1) / t); };
     return tiles(16) <= 900 || (e == 4 && tiles(16) <= 8192 && 2 * tiles(16) <= 16 * tiles(64));
 }
 
 template <class T, bool kAcross>
 tgl_status launch_few(RowsArgs a, hipStream_t st) {
     a.tiles_n = (a.n + 15) / 16;
-    const unsigned grid = static_cast<unsigned>((a.g.n / 16 + a.g.num_types + 2) * a.tiles_n);
+    const unsigned grid = static_cast<unsigned>((a.g.n / 16 + filled_types(a.g) + 1) * a.tiles_n);
     if (a.k * sizeof(T) <= 512) rows_few_kernel<T, kAcross, 4><<<grid, 4 * kWave, 0, st>>>(a);
     else rows_few_kernel<T, kAcross, 8><<<grid, 8 * kWave, 0, st>>>(a);
     return launch_status();
