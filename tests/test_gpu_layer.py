@@ -145,7 +145,8 @@ def test_linear_typed(torch, n, k, out, G, dtype):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("n,k,out,G,empty", [(5000, 272, 100, 3, 0.1), (5003, 100, 272, 2, 0.0), (20_000, 64, 72, 40, 0.3), (3001, 520, 776, 2, 0.0),
                                              (9000, 128, 256, 1, 0.0), (4096, 768, 1024, 3, 0.05), (2500, 1023, 515, 2, 0.1), (1500, 1024, 2304, 1, 0.0),
-                                             (70_000, 48, 33, 3, 0.9), (40_000, 200, 264, 200, 0.0), (50_000, 256, 512, 6, 0.02)])
+                                             (70_000, 48, 33, 3, 0.9), (40_000, 200, 264, 200, 0.0), (50_000, 256, 512, 6, 0.02),
+                                             (42_000, 264, 328, 3, 0.1), (33_000, 67, 45, 2, 0.0), (60, 2000, 1030, 3, 0.1)])
 def test_linear_typed_of_many_rows(torch, n, k, out, G, empty, dtype):
     """Sums over rows in several parts, tiles of every size."""
     announce("linear_typed of many %d x %d -> %d, %d types, %s" % (n, k, out, G, dtype))
@@ -544,3 +545,60 @@ def test_captured_step(torch):
             graph.replay()
             for a, c in zip(outs, want):
                 assert torch.equal(a, c)
+
+
+def test_two_calls_at_once(torch):
+    """Two calls at once, on two streams, of the same groups and weights: neither sees the other."""
+    announce("two streams at once")
+    n, k, out, G = 30_000, 128, 96, 5
+    t = torch.randint(-1, G, (n,), device="cuda", dtype=torch.int32)
+    g = P.group_rows(t, G)
+    w = torch.randn(G, out, k, device="cuda").bfloat16()
+    xs = [torch.randn(n, k, device="cuda").bfloat16() for _ in range(2)]
+    ds = [torch.randn(n, out, device="cuda").bfloat16() for _ in range(2)]
+    want = [(P.linear_typed(x, w, g),) + P.linear_typed_backward(d, x, w, g, bias=True) for x, d in zip(xs, ds)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        got = []
+        for s, x, d in zip(streams, xs, ds):
+            got.append((P.linear_typed(x, w, g, stream=s),) + P.linear_typed_backward(d, x, w, g, bias=True, stream=s))
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert all(torch.equal(u, v) for u, v in zip(a, b))
+
+
+def test_gradients_of_gradients_are_refused(torch):
+    announce("gradients of gradients")
+    g = P.group_rows(torch.zeros(8, dtype=torch.int32, device="cuda"), 1)
+    x, w = torch.randn(8, 4, device="cuda", requires_grad=True), torch.randn(1, 4, 4, device="cuda", requires_grad=True)
+    for y in (P.linear_typed(x, w, g), P.layer_norm(x)):
+        d = torch.autograd.grad(y.square().sum(), x, create_graph=True)[0]
+        with pytest.raises(RuntimeError):
+            torch.autograd.grad(d.sum(), x)
+
+
+def test_inputs_changed_since_are_refused_by_backward(torch):
+    announce("inputs changed since")
+    g = P.group_rows(torch.zeros(8, dtype=torch.int32, device="cuda"), 1)
+    x, w = torch.randn(8, 4, device="cuda"), torch.randn(1, 4, 4, device="cuda", requires_grad=True)
+    y = P.linear_typed(x, w, g)
+    x.zero_()
+    with pytest.raises(RuntimeError, match="modified"):
+        torch.autograd.grad(y.sum(), w)
+    y = P.linear_typed(x, w, g)
+    g.order.copy_(g.order.flip(0))
+    with pytest.raises(RuntimeError, match="modified"):
+        torch.autograd.grad(y.sum(), w)
+
+
+def test_group_rows_of_a_copy(torch):
+    """Copies and pickles of groups have their own tensors."""
+    import copy
+    import pickle
+    announce("copies of groups")
+    g = P.group_rows(torch.randint(0, 3, (50,), device="cuda", dtype=torch.int32), 3)
+    x, w = torch.randn(50, 8, device="cuda"), torch.randn(3, 5, 8, device="cuda")
+    for c in (copy.deepcopy(g), pickle.loads(pickle.dumps(g))):
+        assert c.order.data_ptr() != g.order.data_ptr() and c.c_view(50, 0).order == c.order.data_ptr()
+        assert torch.equal(P.linear_typed(x, w, c), P.linear_typed(x, w, g))
