@@ -835,7 +835,9 @@ typedef struct tgl_typed_weights {
  *   outputs may not overlap inputs
  *   workspace  [device] at least the matching *_workspace() bytes, 256-byte
  *              aligned (NULL where that is 0)
- * Never synchronise.  Errors: TGL_EINVAL, TGL_ENOSPACE, TGL_EDEVICE.
+ * Never synchronise.  Errors: TGL_EINVAL (also where tiles of 64 x 64 of the outputs,
+ * or of dw for every type and stretch of rows, would be more than about 2^24),
+ * TGL_ENOSPACE, TGL_EDEVICE.
  */
 tgl_status tgl_linear_typed(const tgl_row_groups *groups, const void *x, int64_t x_stride,
                             const tgl_typed_weights *w, const float *bias, void *y, int64_t y_stride,

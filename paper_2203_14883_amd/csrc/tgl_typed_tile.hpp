@@ -55,7 +55,7 @@ constexpr bool kQuads = sizeof(T) == 4 && kAcross && N % 4 == 0;
 // Each wavefront brings kFetch times 1024 bytes of a side.  kDirect: row starts
 // and strides are multiples of 16 bytes and so is the sum's axis, or the edge's
 // length where it is the one that memory runs along; memory goes straight to LDS.
-// Otherwise it goes through registers: load() a step ahead, store() after.
+// Otherwise it goes through registers: fetch() a step ahead, store() after.
 
 // `along`: rows[f] are the lane's rows of the tile's edge.
 template <class T, int B, int NW, int SB, bool kDirect>
