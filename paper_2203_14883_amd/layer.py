@@ -93,10 +93,12 @@ def _not_captured():
 
 
 def _on(stream, function, *args):
-    """function.apply on that stream (None: the current one)."""
+    """function.apply on that stream (None: the current one), if it is not captured."""
     if stream is None:
+        _not_captured()
         return function.apply(*args)
     with torch.cuda.stream(stream):
+        _not_captured()
         return function.apply(*args)
 
 
@@ -283,7 +285,6 @@ def linear_typed(x: torch.Tensor, w: torch.Tensor, groups: RowGroups, bias: Opti
         if out is not None:
             raise ValueError("out has no gradient: it must be None where gradients are recorded")
         _device(x, "x")
-        _not_captured()
         return _on(stream, _LinearTyped, x, w, bias, groups)
     return _linear(x, w, groups, bias, out, stream)
 
@@ -387,7 +388,6 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     Gradients go to x, residual, weight and bias."""
     if _recorded(x, residual, weight, bias):
         _device(x, "x")
-        _not_captured()
         got = _on(stream, _LayerNorm, x, residual, weight, bias, eps)
         y, stats, h = got if residual is not None else (*got, x)
     else:
