@@ -325,7 +325,8 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const GradArgs a) {
         const bool there = at + sub < a.n;
         const int64_t row = there ? at + sub : a.n - 1;
         const int dim = there ? a.dim : 0;
-        const bool ordinary = fabs(mean) < 0x1p100 && rstd > 0x1p-60 && rstd < 0x1p60;
+        // mean rstd is what normed() gives for the zeros beyond the row, where g is 0: their product has to be a number
+        const bool ordinary = fabs(mean) < 0x1p100 && rstd > 0x1p-60 && rstd < 0x1p60 && fabs(mean) * rstd < 0x1p100;
         const float upper = static_cast<float>(mean), lower = static_cast<float>(mean - upper), scale = static_cast<float>(rstd);
         auto run_of = [&](const auto &held, const void *p, int64_t stride, int h) {
             if constexpr (kHold) return held.v[h];
