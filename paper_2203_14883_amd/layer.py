@@ -18,6 +18,7 @@ for every call of the library.
 from __future__ import annotations
 
 import ctypes as C
+import math
 from dataclasses import dataclass, field
 from typing import Optional
 
@@ -79,6 +80,31 @@ def _output(t: torch.Tensor, name: str, n: int, dim: int, dtype, dev: int) -> in
     if n > 1 and stride < dim:
         raise ValueError("%s's rows overlap" % name)
     return stride
+
+
+def _extent(t: torch.Tensor):
+    """Bytes of t that lie next to each other, the distances between such pieces, and bytes from the first to behind the last."""
+    e = t.element_size()
+    if t.is_contiguous():
+        return t.numel() * e, [], t.numel() * e
+    steps = [stride * e for stride, size in zip(t.stride()[:-1], t.shape) if size > 1]
+    whole = sum((size - 1) * stride for size, stride in zip(t.shape[:-1], t.stride())) + t.shape[-1]
+    return t.shape[-1] * e, steps, whole * e
+
+
+def _separate(out: torch.Tensor, t: Optional[torch.Tensor], name: str):
+    """Refuses an output whose memory workgroups may still read as t.  Pieces that recur at multiples of one distance may lie
+    between each other: columns beside columns, every other row."""
+    if t is None or not t.numel() or not out.numel():
+        return
+    a, b = out.data_ptr(), t.data_ptr()
+    (own, steps, whole), (other, more, all_of) = _extent(out), _extent(t)
+    if b >= a + whole or a >= b + all_of:
+        return
+    pitch = math.gcd(*steps, *more)
+    if pitch and own <= (b - a) % pitch <= pitch - other:
+        return
+    raise ValueError("out shares memory with %s" % name)
 
 
 def _recorded(*tensors) -> bool:
@@ -218,6 +244,8 @@ def _linear(x, w, groups, bias, out, stream):
         ys = wv.out
     else:
         ys = _output(out, "out", n, wv.out, x.dtype, dev)
+        for t, name in ((x, "x"), (w, "w"), (bias, "bias"), (groups.offsets, "the groups"), (groups.order, "the groups")):
+            _separate(out, t, name)
     s = lib().tgl_linear_typed(C.byref(view), x.data_ptr() or None, xs, C.byref(wv), b, out.data_ptr() or None,
                                max(ys, wv.out), dt, _raw_stream(stream, dev))
     if s:
@@ -280,7 +308,8 @@ def linear_typed(x: torch.Tensor, w: torch.Tensor, groups: RowGroups, bias: Opti
 
     ``x [n, in]`` and ``w [types, out, in]`` are float32 or bfloat16, both of one
     type, which the result ``[n, out]`` has too; ``bias`` is float32 ``[types, out]``.
-    Sums are float32.  Gradients go to x, w and bias (not with ``out``)."""
+    Sums are float32.  Gradients go to x, w and bias (not with ``out``, which may share no
+    memory with an input)."""
     if _recorded(x, w, bias, out):
         if out is not None:
             raise ValueError("out has no gradient: it must be None where gradients are recorded")
