@@ -31,18 +31,19 @@ static __device__ const i32x4 kZeros = {0, 0, 0, 0};
 // instruction itself, which has no result in registers: for the builtin the
 // compiler waits, before reads of any buffer that it cannot tell apart, until all loads
 // are done, and with that nothing is on its way any more.  What has to be waited for is in
-// meet().
+// meet().  m0, the place in LDS, is an operand that the compiler fills, so that it knows what is there; an
+// instruction has to lie between.
 __device__ __forceinline__ uint32_t lds_place(const int8_t *to) {
     return __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_t *)to)));
 }
 template <class T>
 __device__ __forceinline__ void to_lds(const T *from, int8_t *to) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(lds_place(to)));
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(lds_place(to)));
 }
 // The same from one place for all lanes and a number of bytes for each.
 template <class T>
 __device__ __forceinline__ void to_lds(const T *from, uint32_t bytes, int8_t *to) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(bytes), "s"(from), "s"(lds_place(to)));
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(bytes), "s"(from), "{m0}"(lds_place(to)));
 }
 
 // Whether a lane's pieces are four columns of one place of the sum's axis
