@@ -827,7 +827,9 @@ typedef struct tgl_typed_weights {
  *   y[i]  = W x[i] + b                             (0 for rows of no type)
  *   dx[i] = W^T dy[i]                              (0 for rows of no type)
  *   dW[g] = sum over the rows i of type g of dy[i] x[i]^T,  db[g] = the sum of dy[i]
- * Rows of no type are not read.
+ * dW is summed in float32 over stretches of a type's rows (their length depends on n,
+ * num_types, out and in), and over those in 64 bits; db in float32 over up to 8 rows, and
+ * over those in 64 bits.  Rows of no type are not read.
  *   x, dx      [device] n rows of w->in elements;  y, dy: of w->out elements
  *   bias       [device] float[num_types][out], contiguous, or NULL
  *   dw         [device] elements [num_types][out][in], contiguous; 0 for types

@@ -28,7 +28,7 @@ struct SumsArgs {               // dW and db
     void *dw;
     float *db;
     float *parts;               // [room][out][in] sums of the stretches of types that are cut into several
-    float *parts_b;             // [room][out]
+    double *parts_b;            // [room][out]
     int64_t dys, xs;
     int32_t out, in;
     int32_t rows;               // of a stretch
@@ -260,7 +260,9 @@ __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
     const int wm = wave / kWaveN, wn = wave % kWaveN;
     f32x4 acc[MT][NT] = {};
     constexpr int kSums = (MT + kWaveN - 1) / kWaveN;
-    float sum[kSums] = {};                      // of dy, tiles wn, wn + kWaveN, ... of the wavefront's rows
+    // Of dy, tiles wn, wn + kWaveN, ... of the wavefront's rows: 4 or 8 places at a time in 32 bits, beyond that in 64.  In 32
+    // alone a lane's sum over 16,384 places of one number is off by 1.5e-4 of it; the time is the same.
+    double sum[kSums] = {};
     const bool want_sum = a.db && ti == 0;
     using D = Gathered<T, BM, NW, SB, kDirect>;
     using X = Gathered<T, BN, NW, SB, kDirect>;
@@ -291,7 +293,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
 #pragma unroll
                 for (int i = 0; i < kGroup<MT>; i++) {
                     if (i % kWaveN != wn) continue;             // first is a multiple of 4, or 0
-                    float &v = sum[(first + i) / kWaveN];
+                    float v = 0.0f;
                     if constexpr (sizeof(T) == 2) {
 #pragma unroll
                         for (int e = 0; e < 4; e++) {
@@ -302,6 +304,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
 #pragma unroll
                         for (int e = 0; e < 4; e++) v += element<T, true>(dv, i, e);
                     }
+                    sum[(first + i) / kWaveN] += v;
                 }
             });
     }
@@ -310,11 +313,11 @@ __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
     for (int i = 0; i < MT; i++) {
         const int o = o0 + wm * MT * 16 + tile_row<T, true, MT>(i);
         if (want_sum && i % kWaveN == wn) {
-            float v = sum[i / kWaveN];
+            double v = sum[i / kWaveN];
             v += __shfl_xor(v, 16, kWave);
             v += __shfl_xor(v, 32, kWave);
             if (lane < 16 && o < a.out) {
-                if (s.count == 1) a.db[static_cast<int64_t>(s.type) * a.out + o] = v;
+                if (s.count == 1) a.db[static_cast<int64_t>(s.type) * a.out + o] = static_cast<float>(v);
                 else a.parts_b[static_cast<int64_t>(s.part) * a.out + o] = v;
             }
         }
@@ -328,7 +331,8 @@ __global__ __launch_bounds__(NW * kWave, 2) void sums_kernel(const SumsArgs a) {
     }
 }
 
-// The stretches of a type together, one after another: four outputs a thread.
+// The stretches of a type together, one after another, in 64 bits (which costs nothing beside their reading, and a hundred
+// of them in 32 lose more than a stretch does): four outputs a thread.
 template <class T>
 __global__ __launch_bounds__(kBlock) void sums_join_kernel(const SumsArgs a, uint32_t blocks) {
     const int type = blockIdx.x / blocks;
@@ -336,27 +340,26 @@ __global__ __launch_bounds__(kBlock) void sums_join_kernel(const SumsArgs a, uin
     const int32_t count = Stretches(a.g, a.rows, 1, 1).of_type(type, first);
     if (count == 1 || first + count > a.room) return;      // offsets that decrease: nothing to read
     const int64_t outs = static_cast<int64_t>(a.out) * a.in;
-    auto join = [&](const float *parts, int64_t n, int64_t i, float (&sum)[4]) {
+    const int64_t own = static_cast<int64_t>(blockIdx.x % blocks) * kBlock + threadIdx.x, step = static_cast<int64_t>(blocks) * kBlock;
+    for (int64_t i = own * 4; i < outs; i += step * 4) {
+        double sum[4] = {};
         // as many loads on their way as there are registers for
 #pragma unroll 8
         for (int32_t c = 0; c < count; c++) {
             float v[4];
-            load_columns<float, 4>(parts + (first + c) * n + i, 0, n - i < 4 ? static_cast<int>(n - i) : 4, v);
+            load_columns<float, 4>(a.parts + (first + c) * outs + i, 0, outs - i < 4 ? static_cast<int>(outs - i) : 4, v);
 #pragma unroll
             for (int e = 0; e < 4; e++) sum[e] += v[e];
         }
-    };
-    const int64_t step = static_cast<int64_t>(blocks) * kBlock * 4;
-    for (int64_t i = (static_cast<int64_t>(blockIdx.x % blocks) * kBlock + threadIdx.x) * 4; i < outs; i += step) {
-        float sum[4] = {};
-        join(a.parts, outs, i, sum);
-        store_columns<T, 4>(static_cast<T *>(a.dw) + type * outs + i, 0, outs - i < 4 ? static_cast<int>(outs - i) : 4, sum);
+        const float joined[4] = {static_cast<float>(sum[0]), static_cast<float>(sum[1]), static_cast<float>(sum[2]), static_cast<float>(sum[3])};
+        store_columns<T, 4>(static_cast<T *>(a.dw) + type * outs + i, 0, outs - i < 4 ? static_cast<int>(outs - i) : 4, joined);
     }
     if (!a.db) return;
-    for (int64_t i = (static_cast<int64_t>(blockIdx.x % blocks) * kBlock + threadIdx.x) * 4; i < a.out; i += step) {
-        float sum[4] = {};
-        join(a.parts_b, a.out, i, sum);
-        store_columns<float, 4>(a.db + static_cast<int64_t>(type) * a.out + i, 0, a.out - i < 4 ? static_cast<int>(a.out - i) : 4, sum);
+    for (int64_t o = own; o < a.out; o += step) {
+        double sum = 0.0;
+#pragma unroll 8
+        for (int32_t c = 0; c < count; c++) sum += a.parts_b[(first + c) * a.out + o];
+        a.db[static_cast<int64_t>(type) * a.out + o] = static_cast<float>(sum);
     }
 }
 
@@ -387,7 +390,7 @@ size_t carve(SumsArgs &a, void *base) {
     Carver c(base);
     if (a.g.n <= a.rows) return 0;              // no type is cut
     a.parts = c.take<float>(static_cast<size_t>(a.room) * a.out * a.in);
-    a.parts_b = c.take<float>(static_cast<size_t>(a.room) * a.out);
+    a.parts_b = c.take<double>(static_cast<size_t>(a.room) * a.out);
     return c.size();
 }
 

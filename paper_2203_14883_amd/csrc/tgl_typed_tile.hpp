@@ -223,11 +223,15 @@ struct Gathered : AcrossLayout<T, B, NW, SB> {
             constexpr int f = decltype(F)::value;
             const int32_t id = places.template row<L::kRows, f * L::kRows>();
             const int c = first + L::column(wave, f);
-            if constexpr (kDirect)
-                to_lds(id < 0 ? reinterpret_cast<const T *>(&kZeros) : base + id * stride + (c < edge ? c : 0),
-                       buf + (wave * kFetch + f) * 1024);
-            else
+            if constexpr (kDirect) {
+                // opaque, or base + column of every load would be kept over the steps, in twice the registers: in tiles of 256
+                // 10 of them were spilled then (16,384 x 4096 x 4096 of 8 types 1.0 ms, 0.65 without)
+                uint32_t column = c < edge ? c : 0;
+                asm volatile("" : "+v"(column));
+                to_lds(id < 0 ? reinterpret_cast<const T *>(&kZeros) : base + id * stride + column, buf + (wave * kFetch + f) * 1024);
+            } else {
                 held[f] = load_piece(id < 0 ? nullptr : base + id * stride, c, edge);
+            }
         });
     }
     __device__ __forceinline__ void store(int wave, int8_t *buf) {
