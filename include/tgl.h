@@ -886,8 +886,10 @@ tgl_status tgl_layer_norm(const void *x, int64_t x_stride, const void *residual,
  *   dweight, dbias  [device] float[dim]; either may be NULL
  *   workspace    [device] at least tgl_layer_norm_grad_workspace(...) bytes,
  *                256-byte aligned; not read where dweight and dbias are NULL
- * Sums are taken in 64 bits.  Never synchronises.  Errors: TGL_EINVAL,
- * TGL_ENOSPACE, TGL_EDEVICE.
+ * A row's two means are sums in float32 over up to 32 of its elements, and over those
+ * in 64 bits (all of it in 64 where float32's range does not do); dweight and dbias are sums
+ * in float32, and within its range, over up to 32 rows, and over those in 64 bits.
+ * Never synchronises.  Errors: TGL_EINVAL, TGL_ENOSPACE, TGL_EDEVICE.
  */
 size_t tgl_layer_norm_grad_workspace(int64_t n, int32_t dim);
 tgl_status tgl_layer_norm_grad(const void *dy, int64_t dy_stride, const void *h, int64_t h_stride,

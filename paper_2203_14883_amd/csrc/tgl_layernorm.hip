@@ -6,11 +6,12 @@
 //   dw = sum dy xh;  db = sum dy
 //
 // A row is read once and stays in the registers of L lanes, so the mean of the
-// squared distances is taken from the distances themselves.  Sums, and
+// squared distances is taken from the distances themselves.  The norm's sums, and
 // distances before they are scaled, are of 64 bits: squares of finite float32
 // numbers leave that type's range, and a mean that is large beside the
 // distances would lose their bits in 32.  The card does 64-bit sums and
-// products at the rate of float32's, and memory bounds these kernels.
+// products at the rate of float32's, and memory bounds these kernels.  What the
+// gradients sum in 32 bits first is said there.
 #include <type_traits>
 
 #include "tgl_typed.hpp"
@@ -231,6 +232,12 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const NormArgs a) {
     }
 }
 
+constexpr float kMost = 3.4028235e38f;      // of float32
+
+// All loads are done.  Said where the next row takes this one's place: left to the compiler, the wait may come where that row is
+// first used, behind the loads of the one after it, and wait for those too (30,000 rows of 2048 bfloat16 131 us, 110 so).
+__device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(0x0f70); }       // vmcnt(0)
+
 // Rows of a lane whose products are summed in 32 bits before they join its 64-bit sums.
 constexpr int kChain = 32;
 
@@ -239,7 +246,8 @@ constexpr int kChain = 32;
 // gradient, where these take 18): distances from the mean are taken from its upper and
 // its lower bits, (h - upper) - lower, which loses nothing that 32 bits could hold, and a row's
 // means and the weights' gradients are sums of 64 bits of a lane's few elements, or kChain rows,
-// in 32.  Rows that leave float32's range on the way are worked in 64.  Rows too
+// in 32.  Rows that leave float32's range on the way (in their mean, 1 / sigma, products or sums)
+// are worked in 64; the weights' sums of kChain rows have float32's range.  Rows too
 // wide for the registers (!kHold) are read again, mostly from L2, once their means are known.
 template <class T, int L, int H, int kThreads, bool kHold, bool kWhole, bool kParams>
 __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const GradArgs a) {
@@ -318,6 +326,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const GradArgs a) {
     };
     int64_t at = static_cast<int64_t>(blockIdx.x) * kRows;
     load(at, dy, x, dh, mean, rstd);
+    arrived();
     int turn = 0, rows = 0;
     bool flushed = false;
     for (; at < a.n; at += stride) {
@@ -335,6 +344,19 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const GradArgs a) {
         auto normed = [&](float v) { return ((v - upper) - lower) * scale; };
         // beyond the row 0, as dy is there: the product need not be a number
         auto normed_wide = [&](float v, int c) { return c < dim ? static_cast<float>((v - mean) * rstd) : 0.0f; };
+        // A run once more from memory, where float32 is left: held in registers for that, rows would take more of them than all
+        // else does.  opaque: addresses are not worked out, and kept, for rows that need none.
+        auto again = [&](int64_t row, int i, int h, run_t<T> &dv, run_t<T> &xv, float(&wv)[E]) {
+            dv = load_run<T, L, kWhole>(a.dy, row * a.dys, i, h, dim);
+            xv = load_run<T, L, kWhole>(a.h, row * a.hs, i, h, dim);
+#pragma unroll
+            for (int k = 0; k < E; k++) wv[k] = 1.0f;
+            if (a.w && (i + h * L) * E < a.dim) load_columns<float, E>(a.w, (i + h * L) * E, a.dim, wv);
+        };
+        auto opaque = [](auto v) {
+            asm volatile("" : "+v"(v));
+            return v;
+        };
         float xh[kHold ? H : 1][E];
         float part[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -362,11 +384,31 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const GradArgs a) {
         }
         if (a.dx) {
             double sums[2] = {part[0], part[1]};
+            // a product of the lane, or a sum, is beyond float32 (once it is, the sum is no finite number again)
+            const bool large = !(fabsf(part[0]) + fabsf(part[1]) <= kMost);
+            if (__builtin_expect(large, false)) {
+                sums[0] = sums[1] = 0.0;
+#pragma unroll 1
+                for (int h = 0; h < H; h++) {
+                    run_t<T> dv, xv;
+                    float wv[E];
+                    const int lane = opaque(i);
+                    again(opaque(row), lane, h, dv, xv, wv);
+#pragma unroll
+                    for (int k = 0; k < E; k++) {
+                        const double g = static_cast<double>(run_at<T>(dv, k)) * wv[k];
+                        sums[0] += g;
+                        sums[1] = __builtin_fma(g, static_cast<double>(normed_wide(run_at<T>(xv, k), (lane + h * L) * E + k)), sums[1]);
+                    }
+                }
+            }
             row_sum<L>(sums, lds[turn]);
             turn ^= 1;
             const double inv = 1.0 / a.dim, c1 = sums[0] * inv, c2 = sums[1] * inv;
             const float c1f = static_cast<float>(c1), c2f = static_cast<float>(c2);
-            if (there) {
+            // then nothing on the way leaves float32: what is subtracted, of |xh| below 2^8, is less than half a unit of its largest number
+            const bool within = ordinary && !large && fmaxf(fabsf(c1f), fabsf(c2f)) < 0x1p90f;
+            if (__builtin_expect(there && within, true)) {
 #pragma unroll
                 for (int h = 0; h < H; h++) {
                     const int c = (i + h * L) * E;
@@ -376,22 +418,31 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const GradArgs a) {
                     if constexpr (!kHold) xv = run_of(x, a.h, a.hs, h);
                     if (a.dh) hv = run_of(dh, a.dh, a.dhs, h);
                     float v[E];
-                    if (ordinary) {
 #pragma unroll
-                        for (int k = 0; k < E; k++) {
-                            const float t = kHold ? xh[kHold ? h : 0][k] : normed(run_at<T>(xv, k));
-                            v[k] = __builtin_fmaf(-c2f, t, run_at<T>(dv, k) * w[h][k] - c1f) * scale;
-                            if (a.dh) v[k] += run_at<T>(hv, k);
-                        }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < E; k++) {
-                            const double t = kHold ? xh[kHold ? h : 0][k] : normed_wide(run_at<T>(xv, k), c + k);
-                            const double d = __builtin_fma(-c2, t, static_cast<double>(run_at<T>(dv, k)) * w[h][k] - c1) * rstd;
-                            v[k] = static_cast<float>(a.dh ? d + run_at<T>(hv, k) : d);
-                        }
+                    for (int k = 0; k < E; k++) {
+                        const float t = kHold ? xh[kHold ? h : 0][k] : normed(run_at<T>(xv, k));
+                        v[k] = __builtin_fmaf(-c2f, t, run_at<T>(dv, k) * w[h][k] - c1f);
+                        v[k] = __builtin_fmaf(v[k], scale, run_at<T>(hv, k));
                     }
                     store_run<T, kWhole>(a.dx, row * a.dxs, c, a.dim, v);
+                }
+            } else if (there) {
+#pragma unroll 1
+                for (int h = 0; h < H; h++) {
+                    const int lane = opaque(i), c = (lane + h * L) * E;
+                    const int64_t own = opaque(row);
+                    if (c >= a.dim) break;
+                    run_t<T> dv, xv, hv = {};
+                    float wv[E], v[E];
+                    again(own, lane, h, dv, xv, wv);
+                    if (a.dh) hv = load_run<T, L, kWhole>(a.dh, own * a.dhs, lane, h, dim);
+#pragma unroll
+                    for (int k = 0; k < E; k++) {
+                        const double t = normed_wide(run_at<T>(xv, k), c + k);
+                        const double d = __builtin_fma(-c2, t, static_cast<double>(run_at<T>(dv, k)) * wv[k] - c1) * rstd;
+                        v[k] = static_cast<float>(d + run_at<T>(hv, k));
+                    }
+                    store_run<T, kWhole>(a.dx, own * a.dxs, c, a.dim, v);
                 }
             }
         }
@@ -402,6 +453,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const GradArgs a) {
                 rows = 0;
             }
         }
+        arrived();
         if constexpr (kHold) {
             dy = next_dy;
             x = next_x;
@@ -443,7 +495,8 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const double *parts, in
 // Workgroups of a call at most: each takes several rows in turn, four where there
 // are enough for every compute unit, and reads the weights and writes the sums of their gradients once.
 constexpr int64_t kBlocks = 2048;
-int64_t grad_blocks(int32_t dim) { return dim <= 1024 ? 1024 : dim <= 4096 ? 512 : 256; }
+// Rows of three runs a lane: two wavefronts a SIMD (132,000 x 768 bfloat16 156 us), not the three that fit (168).
+int64_t grad_blocks(int32_t dim) { return dim <= 512 ? 1024 : dim <= 768 ? 512 : dim <= 1024 ? 1024 : dim <= 4096 ? 512 : 256; }
 
 // f(lanes of a row, runs of a lane, threads of a workgroup, whether a row stays in registers) for a row's width.
 template <class F>
@@ -475,16 +528,32 @@ tgl_status launch_norm(const NormArgs &a, hipStream_t st) {
     return launch_status();
 }
 
+// Workgroups that the card holds at a time: all rows are shared among these, and no few workgroups come after them
+// (for float32 1024, where it holds 768: 132,000 rows of 300 151 us, 126 so; 40,000 of 1024 144 and 130).
+template <class K>
+int resident_blocks(K kernel, int threads) {
+    int each = 0;
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, threads, 0) != hipSuccess || each < 1) {
+        (void)hipGetLastError();
+        each = 1;
+    }
+    return each * 256;
+}
+
 template <class T, bool kParams>
 int64_t launch_grad(const GradArgs &a, hipStream_t st) {
     int64_t count = 0;
     with_shape(a.dim, [&](auto L, auto H, auto N, auto Hold) {
         constexpr int kL = decltype(L)::value, kH = decltype(H)::value, kN = decltype(N)::value;
-        const int64_t most = grad_blocks(a.dim), blocks = (a.n + kN / kL - 1) / (kN / kL);
+        const auto kernel = a.dim % E == 0 ? norm_grad_kernel<T, kL, kH, kN, decltype(Hold)::value, true, kParams>
+                                           : norm_grad_kernel<T, kL, kH, kN, decltype(Hold)::value, false, kParams>;
+        static const int resident[2] = {resident_blocks(norm_grad_kernel<T, kL, kH, kN, decltype(Hold)::value, true, kParams>, kN),
+                                        resident_blocks(norm_grad_kernel<T, kL, kH, kN, decltype(Hold)::value, false, kParams>, kN)};
+        int64_t most = grad_blocks(a.dim);
+        if (most > resident[a.dim % E != 0]) most = resident[a.dim % E != 0];
+        const int64_t blocks = (a.n + kN / kL - 1) / (kN / kL);
         count = blocks < 256 ? blocks : blocks / 4 < 256 ? 256 : blocks / 4 < most ? blocks / 4 : most;
-        const unsigned grid = static_cast<unsigned>(count);
-        if (a.dim % E == 0) norm_grad_kernel<T, kL, kH, kN, decltype(Hold)::value, true, kParams><<<grid, kN, 0, st>>>(a);
-        else norm_grad_kernel<T, kL, kH, kN, decltype(Hold)::value, false, kParams><<<grid, kN, 0, st>>>(a);
+        kernel<<<static_cast<unsigned>(count), kN, 0, st>>>(a);
     });
     return count;
 }
