@@ -219,6 +219,11 @@ def _check(s: int, what: str):
         raise TglError(int(s), what)
 
 
+# Counts memory that a caller gave for results as changed in place: a backward pass that kept it as an input then raises
+# instead of taking the new values.
+_changed = torch.autograd.graph.increment_version
+
+
 def _p(t: Optional[torch.Tensor]):
     return None if t is None else C.c_void_p(t.data_ptr())
 
@@ -639,6 +644,8 @@ def gather(nbr: Optional[torch.Tensor], eid: Optional[torch.Tensor], tables, n: 
     s = lib().tgl_gather(_p(nbr), _p(eid), int(n), _p(count), int(per_count), tabs, len(tables),
                          _stream(stream))
     _check(s, "tgl_gather")
+    if outs is not None:
+        _changed(result)
     return result
 
 
@@ -665,12 +672,15 @@ def time_encode(dt: torch.Tensor, omega: torch.Tensor, phi: torch.Tensor, out_dt
         raise ValueError("count must be a device int64 tensor")
     n = int(dt.shape[0]) if n is None else int(n)
     dim = int(omega.numel())
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty((n, dim), dtype=out_dtype, device=dt.device)
     s = lib().tgl_time_encode(_p(dt), n, _p(count), int(per_count), _p(omega), _p(phi), dim,
                               OUT_F32 if out_dtype == torch.float32 else OUT_BF16,
                               out.data_ptr() if n else None, _stream(stream))
     _check(s, "tgl_time_encode")
+    if given:
+        _changed(out)
     return out
 
 

@@ -26,7 +26,7 @@ import torch
 from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
-from .binding import _check, c_row_groups, c_typed_weights, lib
+from .binding import _changed, _check, c_row_groups, c_typed_weights, lib
 from .layer8 import _apart, _empty, _raw_stream, _rows, _type
 
 MAX_TYPES = 1024
@@ -239,7 +239,8 @@ def _linear(x, w, groups, bias, out, stream):
     n, xs, dt = _matrix(x, "x", wv.in_, dev)
     view = groups.c_view(n, dev)
     b = _floats(bias, (groups.num_types, wv.out), "bias", dev)
-    if out is None:
+    given = out is not None
+    if not given:
         out = _empty(x, (n, wv.out), x.dtype, stream)
         ys = wv.out
     else:
@@ -250,6 +251,8 @@ def _linear(x, w, groups, bias, out, stream):
                                max(ys, wv.out), dt, _raw_stream(stream, dev))
     if s:
         _check(s, "tgl_linear_typed")
+    if given:
+        _changed(out)
     return out
 
 

@@ -21,7 +21,7 @@ from typing import Optional
 import torch
 from torch.autograd import forward_ad
 
-from .binding import OUT_BF16, OUT_F32, _check, c_cache, c_heads, c_seqs, lib
+from .binding import OUT_BF16, OUT_F32, _changed, _check, c_cache, c_heads, c_seqs, lib
 
 _TYPES = {torch.float32: OUT_F32, torch.bfloat16: OUT_BF16}
 MAX_PAGE = 128
@@ -119,10 +119,11 @@ def _quantise(x, weight, residual, normalize, eps, stream, out):
             os = _rows(t, name)[2]
             if n > 1 and os < dim:
                 raise ValueError("out's rows overlap")
+    given = out is not None
     width = _round16(dim)
     store = _empty(x, (n, width), torch.int8, stream)
     scale = _empty(x, (n,), torch.float32, stream)
-    if out is None and residual is not None:
+    if not given and residual is not None:
         out = _empty(x, (n, dim), x.dtype, stream)
         os = dim
     if n:
@@ -131,6 +132,8 @@ def _quantise(x, weight, residual, normalize, eps, stream, out):
                                  None if out is None else out.data_ptr(), os if os > dim else dim, _raw_stream(stream, dev))
         if s:
             _check(s, "tgl_norm_quant")
+    if given:
+        _changed(out)
     return store if width == dim else store[:, :dim], scale, out
 
 
@@ -187,20 +190,23 @@ def linear_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: 
     ws = _vector(w_scale, n, "w_scale", dev)
     b = None if bias is None else _vector(bias, n, "bias", dev)
     ostride = n
-    if out is not None:
+    given = out is not None
+    if given:
         out_dtype = out.dtype
         _also(out, "out", dev)
         om, on, ostride = _rows(out, "out")
         if om != m or on != n or (m > 1 and ostride < n):
             raise ValueError("out must be [%d, %d]" % (m, n))
     ot = _type(out_dtype, "the output")
-    if out is None:
+    if not given:
         out = _empty(x, (m, n), out_dtype, stream)
     if m:
         s = lib().tgl_linear_i8(x.data_ptr(), xstride, xs, m, w.data_ptr(), wstride, ws, b, n, k, out.data_ptr(),
                             ostride if ostride > n else n, ot, _raw_stream(stream, dev))
         if s:
             _check(s, "tgl_linear_i8")
+    if given:
+        _changed(out)
     return out
 
 
@@ -419,6 +425,8 @@ def cache_attend(cache: HistoryCache, q: torch.Tensor, table: torch.Tensor, begi
                            _raw_stream(stream, dev))
     if s:
         _check(s, "tgl_cache_attend")
+    if given:
+        _changed(out)
     return (out, lse) if return_lse else out
 
 
