@@ -1,7 +1,6 @@
 """Training one temporal layer over nodes of several types, on a small graph.
 
-Nodes are of a few kinds, each with weights of its own (as MAG's papers, authors
-and venues are): a batch's slots are sampled (Sec. 3.1 of the TGL paper), their
+Nodes are of a few kinds, each with weights of its own: a batch's slots are sampled (Sec. 3.1 of the TGL paper), their
 rows looked up and given to their kind's projection, averaged per root, added to the
 root's own and normed (Sec. 2.2); the loss asks whether two roots will meet.
 Gradients come from torch's autograd, through the operators' own backward passes.

@@ -829,7 +829,8 @@ typedef struct tgl_typed_weights {
  *   dW[g] = sum over the rows i of type g of dy[i] x[i]^T,  db[g] = the sum of dy[i]
  * dW is summed in float32 over stretches of a type's rows (their length depends on n,
  * num_types, out and in), and over those in 64 bits; db in float32 over up to 8 rows, and
- * over those in 64 bits.  Rows of no type are not read.
+ * over those in 64 bits.  What rows of no type hold changes nothing (a place without a row
+ * may load row 0, which has to be there where n > 0).
  *   x, dx      [device] n rows of w->in elements;  y, dy: of w->out elements
  *   bias       [device] float[num_types][out], contiguous, or NULL
  *   dw         [device] elements [num_types][out][in], contiguous; 0 for types

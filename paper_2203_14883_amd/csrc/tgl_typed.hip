@@ -161,8 +161,8 @@ __global__ __launch_bounds__(NW * kWave, 2) void rows_kernel(const RowsArgs a) {
 // Few rows: a workgroup per 16 rows of a type and 16 columns, operands straight
 // from memory (kAcross: the weights element by element, 16 columns of a row of memory at a
 // time).  Its wavefronts take pieces of the sum's axis in turn and add up through LDS, in
-// their order.  Bound by latency where the weights are small (a row of 768 -> 2304 bfloat16 5 us, in
-// tiles of 64 8) and by their bytes where they are not.
+// their order.  Bound by latency where the weights are small (a row of 768 -> 2304 bfloat16 4.0 us, in
+// tiles of 64 7.9) and by their bytes where they are not.
 template <class T, bool kAcross, int NW>
 __global__ __launch_bounds__(NW * kWave) void rows_few_kernel(const RowsArgs a) {
     __shared__ f32x4 sums[NW][kWave];
@@ -423,10 +423,13 @@ tgl_status launch_rows(RowsArgs a, hipStream_t st) {
     return launch_status();
 }
 
-// Whether a call is too small for tiles of 64, by its tiles of 16: up to 900 of them; in float32, whose products
-// take long, also where they cover half of what tiles of 64 would, as those of many types with few rows.  us of tiles
-// of 64 / 16: bfloat16 65 x 768 x 1024 of 4 types 7.7 / 5.4, 1801 x 272 x 100 of 3 5.1 / 4.4, 200 x 768 x 1024 of 4 7.9 / 8.4,
-// of 64 17 / 22; float32 19.9 / 8.1, 9.4 / 5.7, 20 / 13.8, 70 / 37, 1000 x 768 x 768 of 3 23 / 39.
+// Whether a call is too small for tiles of 64, by its tiles of 16: up to 900 of them (less time at 805 and 896, more at 1024)
+// however long the sum's axis; in float32, whose products take long, also where they cover half of what tiles of 64
+// would, as those of many types with few rows.  us of tiles of 64 / 16: bfloat16 65 x 768 x 1024 of 4 types 7.7 / 5.4, 1801
+// x 272 x 100 of 3 5.1 / 4.4, 200 x 768 x 1024 of 4 7.9 / 8.4, of 64 17 / 22; float32 19.9 / 8.1, 9.4 / 5.7, 20 / 13.8, 70 / 37,
+// 1000 x 768 x 768 of 3 23 / 39.  Long axes, of one type: bfloat16 190 x 16,384 x 1024 148 / 87, 190 x 65,536 x 1024 593 / 337, 3500 x
+// 16,384 x 64 138 / 115; float32 388 / 170, 2048 / 699, 385 / 226.  Weights across the sum's axis, bfloat16: 64 x 16,384 x 1024
+// 162 / 40, 890 x 8192 x 256 81 / 58, but 190 x 768 x 1024 8.5 / 12.3.
 bool few_rows(const RowsArgs &a, size_t e) {
     auto tiles = [&](int64_t t) { return (a.g.n / t + filled_types(a.g)) * ((a.n + t - 1) / t); };
     return tiles(16) <= 900 || (e == 4 && tiles(16) <= 8192 && 2 * tiles(16) <= 16 * tiles(64));

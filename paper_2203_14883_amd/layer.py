@@ -324,7 +324,8 @@ def linear_typed(x: torch.Tensor, w: torch.Tensor, groups: RowGroups, bias: Opti
 def linear_typed_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, groups: RowGroups, bias: bool = False, stream=None):
     """Gradients of ``linear_typed`` for the result's gradient ``dy [n, out]``:
     ``(dx, dw, dbias)`` in x's type, w's type and float32 (None without ``bias``).
-    Rows of no type get zeros, types without rows too."""
+    Rows of no type get zeros, types without rows too.  dw is summed in float32 over
+    stretches of a type's rows and over those in 64 bits, dbias in 64 bits."""
     with torch.no_grad():
         return _linear_backward(dy, x, w, groups, True, True, bias, stream)
 
