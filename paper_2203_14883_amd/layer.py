@@ -92,19 +92,23 @@ def _extent(t: torch.Tensor):
     return t.shape[-1] * e, steps, whole * e
 
 
-def _separate(out: torch.Tensor, t: Optional[torch.Tensor], name: str):
-    """Refuses an output whose memory workgroups may still read as t.  Pieces that recur at multiples of one distance may lie
-    between each other: columns beside columns, every other row."""
-    if t is None or not t.numel() or not out.numel():
-        return
-    a, b = out.data_ptr(), t.data_ptr()
-    (own, steps, whole), (other, more, all_of) = _extent(out), _extent(t)
-    if b >= a + whole or a >= b + all_of:
-        return
-    pitch = math.gcd(*steps, *more)
-    if pitch and own <= (b - a) % pitch <= pitch - other:
-        return
-    raise ValueError("out shares memory with %s" % name)
+def _separate(out: torch.Tensor, *inputs):
+    """Refuses an output whose memory workgroups may still read as one of the inputs (tensor, name).  Pieces that recur at
+    multiples of one distance may lie between each other: columns beside columns, every other row."""
+    own, steps, whole = _extent(out)
+    a = out.data_ptr()
+    for t, name in inputs:
+        if t is None:
+            continue
+        b = t.data_ptr()
+        if b >= a + whole or (t.is_contiguous() and b + t.nbytes <= a):
+            continue
+        other, more, all_of = _extent(t)
+        if b + all_of <= a:
+            continue
+        pitch = math.gcd(*steps, *more)
+        if not pitch or not own <= (b - a) % pitch <= pitch - other:
+            raise ValueError("out shares memory with %s" % name)
 
 
 def _recorded(*tensors) -> bool:
@@ -245,8 +249,7 @@ def _linear(x, w, groups, bias, out, stream):
         ys = wv.out
     else:
         ys = _output(out, "out", n, wv.out, x.dtype, dev)
-        for t, name in ((x, "x"), (w, "w"), (bias, "bias"), (groups.offsets, "the groups"), (groups.order, "the groups")):
-            _separate(out, t, name)
+        _separate(out, (x, "x"), (w, "w"), (bias, "bias"), (groups.offsets, "the groups"), (groups.order, "the groups"))
     s = lib().tgl_linear_typed(C.byref(view), x.data_ptr() or None, xs, C.byref(wv), b, out.data_ptr() or None,
                                max(ys, wv.out), dt, _raw_stream(stream, dev))
     if s:

@@ -86,7 +86,7 @@ def test_shared_memory_is_found_by_counting():
         sets = [{t.storage_offset() + i * step + j for i in range(n) for j in range(k)}
                 for t, n, k, step in ((a, an, ak, astep), (b, bn, bk, bstep))]
         try:
-            layer._separate(a, b, "b")
+            layer._separate(a, (b, "b"))
             ok = True
         except ValueError:
             ok = False
