@@ -358,9 +358,9 @@ constexpr int kGroup = M < 4 ? M : 4;
 //
 // Bound by the matrix units at the clocks that the card's power leaves them: 16384 x 4096 x 4096 in
 // bfloat16, one type, 414 us, its rows' gradient 416 and its weights' 555, where the library's products take
-// 350, 396 and 450.  When it was built, at lower clocks, forward took 493; without its loads 350 to 365, without its reads of LDS 420 to 440.  Three and four buffers of half a
-// step each, wavefronts that take turns at multiplying and loading, and 4 wavefronts of 128 x 128
-// outputs measured the same or up to a fifth more.
+// 350, 396 and 450.  When it was built, at lower clocks, forward took 493; without its loads 350 to 365, without its
+// reads of LDS 420 to 440.  Three and four buffers of half a step each, wavefronts that take turns at multiplying and
+// loading, and 4 wavefronts of 128 x 128 outputs measured the same or up to a fifth more.
 template <class T, bool kAcrossX, bool kAcrossW, bool kApart, int SB, int M, int N, class Buffer, class FetchX, class FetchW, class Store, class ReadX,
           class ReadW, class Used>
 __device__ __forceinline__ void multiply_steps(int steps, const Buffer &buffer, f32x4 (&acc)[M][N], const FetchX &fetch_x,
